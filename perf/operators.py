@@ -1,0 +1,375 @@
+"""Microscaled 4-bit matrices and the expert feed-forward block, as a list of measurable cases.
+
+A case is a dict of plain values; `prepare` makes what a program holds before the call, `run` is one pass through the
+public entry points (`own`) or through the operators' plain form, `exact` the same result in 64-bit arithmetic.
+
+  quantize  rows of activations or weights to 4-bit floats with a scale for each 32 (e2m1 and a power of two), and back
+  gemm      Y = Q(X) Q(W)^T, X quantized in the call; gated: silu(first half of the columns) times the second half
+  route     logits to the k experts of each token, their weights, and the tokens grouped by expert
+  experts   the same product for rows grouped by expert, each group with its expert's matrix
+  combine   the weighted sum of a token's k expert outputs
+
+Distributions are those of the repository's generators: activations N(0, 1) with 1 % of the channels times 20, weights
+N(0, 0.02), quantized once as a stored model holds them (two codes a byte, one scale byte for each 32)."""
+import math
+import zlib
+
+import torch
+
+own = False
+
+TYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+BLOCK = 32
+VALUES = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)   # of the codes 0..7; 8..15 are their negatives
+
+# the largest listed cases, which bound what draw() may give
+MOST_QUANTIZED = 8192 * 8192
+MOST_PRODUCTS = 8192 * 4096 * 28672
+MOST_WEIGHTS = 4096 * 28672
+MOST_EXPERT_WEIGHTS = 32 * 4096 * 4096
+MOST_LOGITS = 8192 * 256
+MOST_COMBINED = 8192 * 8 * 4096
+
+
+def listed():
+    return [
+        # the activation of a few decoded tokens, quantized and read back: what a call costs
+        dict(name="quantize_tokens", kind="quantize", rows=4, K=4096, dtype="bf16"),
+        # the activations of a long prompt (or a square weight matrix) of a 70B-shaped model
+        dict(name="quantize_prompt", kind="quantize", rows=8192, K=8192, dtype="f16"),
+        # one token through the q|k|v projection of an 8B-shaped layer: bound by the weights it streams
+        dict(name="gemm_token", kind="gemm", M=1, N=6144, K=4096, gated=False, dtype="bf16"),
+        # a short prompt, no size a multiple of a tile or of a block, fp32 in and out
+        dict(name="gemm_ragged", kind="gemm", M=77, N=5000, K=11004, gated=False, dtype="f32"),
+        # prefill of 8192 tokens through gate|up of an 8B-shaped layer
+        dict(name="gemm_prompt", kind="gemm", M=8192, N=28672, K=4096, gated=True, dtype="bf16"),
+        # a decoded batch through the router of a layer with 64 experts
+        dict(name="route_batch", kind="route", T=32, E=64, k=6, renorm=True, dtype="bf16"),
+        # a prompt of 8192 tokens over 256 experts, fp32 logits
+        dict(name="route_prompt", kind="route", T=8192, E=256, k=8, renorm=True, dtype="f32"),
+        # four decoded tokens: some experts have a row or two, most have none
+        dict(name="experts_tokens", kind="experts", T=4, E=32, k=4, N=4096, K=4096, gated=True, gather=True, skew=0.0, dtype="bf16"),
+        # down projection of a decoded batch of many requests: each expert has a few rows of its own
+        dict(name="experts_batch", kind="experts", T=128, E=32, k=4, N=4096, K=2048, gated=False, gather=False, skew=0.5, dtype="f16"),
+        # gate|up of a prompt, the load uneven
+        dict(name="experts_prompt", kind="experts", T=4096, E=32, k=4, N=4096, K=4096, gated=True, gather=True, skew=0.5, dtype="bf16"),
+        # back to the tokens: a decoded batch, and a prompt
+        dict(name="combine_batch", kind="combine", T=32, k=4, D=4096, dtype="bf16"),
+        dict(name="combine_prompt", kind="combine", T=8192, k=8, D=4096, dtype="bf16"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _size(rng, lo, hi):
+    """Mostly what models have, one in four any number at all."""
+    n = _log(rng, lo, hi)
+    step = rng.choice([1, 32, 64, 128])
+    return max(lo, n // step * step)
+
+
+def draw(rng):
+    case = _drawn(rng)
+    return {name: 3040 if type(v) is int and v == 3072 else v for name, v in case.items()}   # 3072 is no size of this repository
+
+
+def _drawn(rng):
+    kind = rng.choice(["quantize", "gemm", "gemm", "gemm", "route", "experts", "experts", "experts", "combine"])
+    dtype = rng.choice(["f16", "bf16", "bf16", "f32"])
+    if kind == "quantize":
+        K = _size(rng, 32, 28672)
+        return dict(kind=kind, rows=_log(rng, 1, min(65536, MOST_QUANTIZED // K)), K=K, dtype=dtype)
+    if kind == "gemm":
+        gated = rng.random() < 0.4
+        N, K = _size(rng, 64, 28672), _size(rng, 64, 14336)
+        N = (N + 1) // 2 * 2 if gated else N
+        while N * K > MOST_WEIGHTS:
+            N = max(2, N // 4 * 2)
+        M = rng.choice([1, rng.randint(2, 16), rng.randint(17, 128), _log(rng, 128, 8192)])
+        return dict(kind=kind, M=max(1, min(M, MOST_PRODUCTS // 2 // (N * K))), N=N, K=K, gated=gated, dtype=dtype)
+    if kind == "route":
+        E = rng.randint(4, 384)
+        return dict(kind=kind, T=_log(rng, 1, MOST_LOGITS // E), E=E, k=rng.randint(1, min(8, E)), renorm=rng.random() < 0.5, dtype=dtype)
+    if kind == "combine":
+        D, k = _size(rng, 64, 8192), rng.randint(1, 8)
+        return dict(kind=kind, T=_log(rng, 1, MOST_COMBINED // (D * k * (2 if dtype == "f32" else 1))), k=k, D=D, dtype=dtype)
+    gated, E = rng.random() < 0.5, rng.randint(4, 64)
+    k = rng.randint(1, min(8, E))
+    N, K = _size(rng, 128, 8192), _size(rng, 128, 8192)
+    N = (N + 1) // 2 * 2 if gated else N
+    while E * N * K > MOST_EXPERT_WEIGHTS:
+        N, K = max(2, N // 4 * 2), max(64, K * 3 // 4)
+    T = rng.choice([1, rng.randint(2, 32), _log(rng, 32, 512), _log(rng, 512, 4096)])
+    return dict(kind=kind, T=max(1, min(T, MOST_PRODUCTS // 8 // (k * N * K))), E=E, k=k, N=N, K=K, gated=gated,
+                gather=rng.random() < 0.6, skew=rng.choice([0.0, 0.5, 1.0]), dtype=dtype)
+
+
+# ---- inputs --------------------------------------------------------------------------------------------------------
+
+def _generator(seed, *key):
+    g = torch.Generator(device="cuda")
+    g.manual_seed((int(seed) % (1 << 30) << 32) ^ zlib.crc32(repr(key).encode()))
+    return g
+
+
+def _activations(case, seed, rows, K):
+    g = _generator(seed, "x")
+    x = torch.randn((rows, K), device="cuda", generator=g)
+    x[:, torch.randperm(K, device="cuda", generator=g)[:max(1, round(0.01 * K))]] *= 20.0
+    return x.to(TYPES[case["dtype"]])
+
+
+def _stored_weights(seed, rows, K):
+    """Codes [rows, K up to 32, halved] (two a byte, the even k in the low half) and scale bytes [rows, blocks] of random weights."""
+    g = _generator(seed, "w")
+    codes = torch.empty((rows, (K + BLOCK - 1) // BLOCK * BLOCK // 2), dtype=torch.uint8, device="cuda")
+    scales = torch.empty((rows, (K + BLOCK - 1) // BLOCK), dtype=torch.uint8, device="cuda")
+    step = max(1, (1 << 26) // K)
+    for at in range(0, rows, step):
+        c, e = _to_mx4(torch.randn((min(step, rows - at), K), device="cuda", generator=g).mul_(0.02))
+        c = c.flatten(1).to(torch.uint8)
+        codes[at:at + step] = c[:, 0::2] | (c[:, 1::2] << 4)
+        scales[at:at + step] = (e + 127).squeeze(-1).to(torch.uint8)
+    return codes, scales
+
+
+def _logits(case, seed):
+    g = _generator(seed, "logits")
+    x = torch.randn((case["T"], case["E"]), device="cuda", generator=g)
+    return (x + case.get("skew", 0.0) * torch.randn(case["E"], device="cuda", generator=g)).to(TYPES[case.get("dtype", "f32")])
+
+
+def _bytes(case):
+    return 4 if case["dtype"] == "f32" else 2
+
+
+def prepare(case, seed):
+    s = dict(case=case)
+    kind, dtype = case["kind"], TYPES[case["dtype"]]
+    if kind == "quantize":
+        s["x"] = _activations(case, seed, case["rows"], case["K"])
+    elif kind == "gemm":
+        s["x"] = _activations(case, seed, case["M"], case["K"])
+        s["codes"], s["scales"] = _stored_weights(seed, case["N"], case["K"])
+    elif kind == "route":
+        s["logits"] = _logits(case, seed)
+    elif kind == "experts":
+        T, E, k = case["T"], case["E"], case["k"]
+        ids, _ = _top(_logits(case, seed).float(), k, True)
+        s["offsets"], rows, _ = _group(ids, E)
+        s["rows"] = rows if case["gather"] else None
+        s["most"] = int((s["offsets"][1:] - s["offsets"][:-1]).max())   # of the plain form's padding
+        s["x"] = _activations(case, seed, T if case["gather"] else T * k, case["K"])
+        s["codes"], s["scales"] = _stored_weights(seed, E * case["N"], case["K"])
+    else:
+        T, k, D = case["T"], case["k"], case["D"]
+        g = _generator(seed, "combine")
+        s["y"] = torch.randn((T * k, D), device="cuda", generator=g).to(dtype)
+        s["slots"] = torch.randperm(T * k, device="cuda", generator=g).view(T, k).to(torch.int32)
+        s["weights"] = torch.softmax(torch.randn((T, k), device="cuda", generator=g), -1)
+    if own:
+        _prepare_own(s)
+    return s
+
+
+def _prepare_own(s):
+    from paper_2510_19482_amd import binding as hlq
+
+    case = s["case"]
+    kind, dtype = case["kind"], TYPES[case["dtype"]]
+    if kind in ("gemm", "experts"):
+        s["W"] = hlq.hlq_mx4_pack(s.pop("codes"), s.pop("scales"), case["K"])
+        rows = case["M"] if kind == "gemm" else case["T"] * case["k"]
+        s["out"] = torch.empty((rows, case["N"] // 2 if case["gated"] else case["N"]), dtype=dtype, device="cuda")
+        s["ws"] = hlq.alloc_mx4_workspace(s["W"], s["x"].shape[0], rows, 1 if kind == "gemm" else case["E"])
+    elif kind == "quantize":
+        s["blob"] = hlq.alloc_mx4(case["rows"], case["K"])
+        s["out"] = torch.empty_like(s["x"])
+    elif kind == "route":
+        s["out"] = hlq.alloc_route(case["T"], case["E"], case["k"])
+    else:
+        s["out"] = torch.empty((case["T"], case["D"]), dtype=dtype, device="cuda")
+
+
+# ---- a pass --------------------------------------------------------------------------------------------------------
+
+def run(s):
+    return (_run_own if own else _run_plain)(s)
+
+
+def _run_own(s):
+    from paper_2510_19482_amd import binding as hlq
+
+    case = s["case"]
+    kind = case["kind"]
+    if kind == "quantize":
+        return hlq.hlq_mx4_dequantize(hlq.hlq_mx4_quantize(s["x"], s["blob"]), s["out"])
+    if kind == "gemm":
+        return hlq.hlq_mx4_gemm(s["W"], s["x"], s["out"], gated=case["gated"], ws=s["ws"])
+    if kind == "route":
+        r = hlq.hlq_route(s["logits"], case["k"], renorm=case["renorm"], out=s["out"])
+        return [r.ids, r.weights, r.offsets, r.rows, r.slots]
+    if kind == "experts":
+        return hlq.hlq_expert_gemm(s["W"], s["offsets"], s["x"], s["out"], rows=s["rows"], gated=case["gated"], ws=s["ws"])
+    return hlq.hlq_expert_combine(s["y"], s["slots"], s["weights"], s["out"])
+
+
+def _to_mx4(x):
+    """Codes [rows, blocks, 32] (0..15) and the exponents [rows, blocks, 1] of the scales."""
+    x = torch.nn.functional.pad(x.float(), (0, -x.shape[1] % BLOCK)).unflatten(1, (-1, BLOCK))
+    top = x.abs().amax(-1, keepdim=True)
+    # the largest value gets e2m1's largest exponent, 2: floor(log2(top)) - 2, not below -127
+    e = torch.where(top > 0, torch.frexp(top).exponent - 3, -127).clamp(min=-127)
+    v = torch.ldexp(x, -e)
+    a = v.abs()
+    # to nearest, a tie to the even code; above 5 everything is 6
+    code = (a > 0.25).int() + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0)
+    return code + 8 * torch.signbit(v), e
+
+
+def _values(codes, e):
+    table = torch.tensor(VALUES + tuple(-v for v in VALUES), device=codes.device)
+    return torch.ldexp(table[codes], e).flatten(1)
+
+
+def _decoded(codes, scales):
+    """fp32 [rows, K up to 32] of stored weights."""
+    c = torch.stack((codes & 15, codes >> 4), -1).flatten(1).int()
+    return _values(c.unflatten(1, (-1, BLOCK)), scales.int().unsqueeze(-1) - 127)
+
+
+def _gate(y):
+    g, u = y.chunk(2, -1)
+    return g / (1 + torch.exp(-g)) * u
+
+
+def _top(logits, k, renorm):
+    chosen, ids = (v[:, :k] for v in torch.sort(logits, dim=-1, descending=True, stable=True))
+    top = chosen[:, :1]
+    w = torch.exp(chosen - top)
+    w = w / (w.sum(-1, keepdim=True) if renorm else torch.exp(logits - top).sum(-1, keepdim=True))
+    return ids, w
+
+
+def _group(ids, E):
+    """Offsets of the experts' rows, the token of each row, and each pair's row; in an expert by token."""
+    flat = ids.flatten()
+    order = torch.sort(flat, stable=True).indices
+    counts = (flat[:, None] == torch.arange(E, device=flat.device)).sum(0)
+    offsets = torch.nn.functional.pad(counts.cumsum(0), (1, 0))
+    slots = torch.empty_like(order)
+    slots[order] = torch.arange(len(order), device=flat.device)
+    return offsets.int(), (order // ids.shape[1]).int(), slots.view_as(ids).int()
+
+
+def _run_plain(s):
+    case = s["case"]
+    kind, dtype = case["kind"], TYPES[case["dtype"]]
+    if kind == "quantize":
+        return _values(*_to_mx4(s["x"]))[:, :case["K"]].to(dtype)
+    if kind == "gemm":
+        y = _values(*_to_mx4(s["x"])) @ _decoded(s["codes"], s["scales"]).T
+        return (_gate(y) if case["gated"] else y).to(dtype)
+    if kind == "route":
+        ids, w = _top(s["logits"].float(), case["k"], case["renorm"])
+        return [ids.int(), w, *_group(ids, case["E"])]
+    if kind == "experts":
+        E, R = case["E"], case["T"] * case["k"]
+        x = _values(*_to_mx4(s["x"]))
+        x = x[s["rows"].long()] if case["gather"] else x
+        # the experts' rows side by side, padded to the longest
+        at = torch.arange(R, device="cuda")
+        e = (at[:, None] >= s["offsets"][None, 1:]).sum(1)
+        i = at - s["offsets"][e]
+        padded = torch.zeros((E, s["most"], x.shape[1]), device="cuda")
+        padded[e, i] = x
+        y = torch.bmm(padded, _decoded(s["codes"], s["scales"]).view(E, case["N"], -1).transpose(1, 2))[e, i]
+        return (_gate(y) if case["gated"] else y).to(dtype)
+    return (s["y"][s["slots"].long()].float() * s["weights"].unsqueeze(-1)).sum(1).to(dtype)
+
+
+def work(case):
+    kind, b = case["kind"], _bytes(case)
+    mx4 = 17 / 32   # bytes a value with its share of the scale
+    if kind == "quantize":
+        n = case["rows"] * case["K"]
+        return {"bytes": n * (2 * b + mx4), "flops": 0}
+    if kind == "gemm":
+        M, N, K = case["M"], case["N"], case["K"]
+        return {"bytes": N * K * mx4 + M * K * b + M * N * b / (2 if case["gated"] else 1), "flops": 2 * M * N * K}
+    if kind == "route":
+        T, E, k = case["T"], case["E"], case["k"]
+        return {"bytes": T * E * b + 16 * T * k + 4 * (E + 1), "flops": 0}
+    if kind == "experts":
+        T, E, k, N, K = (case[v] for v in ("T", "E", "k", "N", "K"))
+        used = E * (1 - (1 - k / E) ** T)   # experts that have rows, on average
+        x = (T if case["gather"] else T * k) * K * b
+        return {"bytes": used * N * K * mx4 + x + T * k * N * b / (2 if case["gated"] else 1), "flops": 2 * T * k * N * K}
+    n = case["T"] * case["D"]
+    return {"bytes": (case["k"] + 1) * n * b + 8 * case["T"] * case["k"], "flops": 2 * n * case["k"]}
+
+
+# ---- in 64 bits ----------------------------------------------------------------------------------------------------
+
+def _quantized_64(x):
+    """The values that the 4-bit form of x stands for: a grid whose step doubles at 2 and at 4, rounded half to even."""
+    rows, K = x.shape
+    x = torch.cat((x.double(), torch.zeros((rows, -K % BLOCK), dtype=torch.float64, device=x.device)), 1).reshape(rows, -1, BLOCK)
+    top = x.abs().max(-1, keepdim=True).values
+    unit = torch.exp2(torch.clamp(torch.floor(torch.log2(top)), min=-125) - 2)
+    v = x / unit
+    step = torch.where(v.abs() < 2, 0.5, torch.where(v.abs() < 4, 1.0, 2.0)).double()
+    return ((torch.round(v / step) * step).clamp(-6, 6) * unit).reshape(rows, -1)[:, :K]
+
+
+def _weights_64(codes, scales, K):
+    """sign, two exponent bits, one mantissa bit; scale 2^(byte - 127)."""
+    out = torch.empty((codes.shape[0], codes.shape[1] * 2), dtype=torch.float64, device=codes.device)
+    for half in (0, 1):
+        c = (codes >> (4 * half) & 15).double()
+        sign = 1 - 2 * torch.floor(c / 8)
+        expo, frac = torch.floor(c % 8 / 2), c % 2
+        out[:, half::2] = sign * torch.where(expo > 0, torch.exp2(expo - 1) * (1 + frac / 2), frac / 2)
+    out *= torch.exp2(scales.double() - 127).repeat_interleave(BLOCK, 1)
+    return out[:, :K]
+
+
+def _product_64(x, w, gated):
+    y = x @ w.T
+    if gated:
+        half = y.shape[1] // 2
+        y = y[:, :half] * torch.sigmoid(y[:, :half]) * y[:, half:]
+    return y
+
+
+def exact(case, seed):
+    kind = case["kind"]
+    if kind == "quantize":
+        return _quantized_64(_activations(case, seed, case["rows"], case["K"]))
+    if kind == "gemm":
+        w = _weights_64(*_stored_weights(seed, case["N"], case["K"]), case["K"])
+        return _product_64(_quantized_64(_activations(case, seed, case["M"], case["K"])), w, case["gated"])
+    if kind == "route":
+        p = torch.softmax(_logits(case, seed).double(), -1).sort(-1, descending=True).values[:, :case["k"]]
+        return [None, p / p.sum(-1, keepdim=True) if case["renorm"] else p, None, None, None]
+    if kind == "experts":
+        T, E, k, N, K = (case[v] for v in ("T", "E", "k", "N", "K"))
+        # the grouping is an input here: rows of an expert stand together, by token
+        ids, _ = _top(_logits(case, seed).float(), k, True)
+        x = _quantized_64(_activations(case, seed, T if case["gather"] else T * k, K))
+        codes, scales = _stored_weights(seed, E * N, K)
+        out, at = [], 0
+        for e in range(E):
+            tokens = (ids == e).any(1).nonzero().flatten()
+            rows = tokens if case["gather"] else torch.arange(at, at + len(tokens), device="cuda")
+            at += len(tokens)
+            out.append(_product_64(x[rows], _weights_64(codes[e * N:(e + 1) * N], scales[e * N:(e + 1) * N], K), case["gated"]))
+        return torch.cat(out)
+    s = prepare(dict(case), seed)
+    y = s["y"].double()
+    out = torch.zeros((case["T"], case["D"]), dtype=torch.float64, device="cuda")
+    for i in range(case["k"]):
+        out += s["weights"][:, i:i + 1].double() * y[s["slots"][:, i].long()]
+    return out
