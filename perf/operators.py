@@ -28,7 +28,7 @@ MOST_PRODUCTS = 8192 * 4096 * 28672
 MOST_WEIGHTS = 4096 * 28672
 MOST_EXPERT_WEIGHTS = 32 * 4096 * 4096
 MOST_LOGITS = 8192 * 256
-MOST_COMBINED = 8192 * 8 * 4096
+MOST_COMBINED = 8192 * 9 * 4096   # read and written
 
 
 def listed():
@@ -94,7 +94,7 @@ def _drawn(rng):
         return dict(kind=kind, T=_log(rng, 1, MOST_LOGITS // E), E=E, k=rng.randint(1, min(8, E)), renorm=rng.random() < 0.5, dtype=dtype)
     if kind == "combine":
         D, k = _size(rng, 64, 8192), rng.randint(1, 8)
-        return dict(kind=kind, T=_log(rng, 1, MOST_COMBINED // (D * k * (2 if dtype == "f32" else 1))), k=k, D=D, dtype=dtype)
+        return dict(kind=kind, T=_log(rng, 1, min(65536, MOST_COMBINED * 9 // 10 // (D * (k + 1) * (2 if dtype == "f32" else 1)))), k=k, D=D, dtype=dtype)
     gated, E = rng.random() < 0.5, rng.randint(4, 64)
     k = rng.randint(1, min(8, E))
     N, K = _size(rng, 128, 8192), _size(rng, 128, 8192)
