@@ -27,6 +27,7 @@ MOST_QUANTIZED = 8192 * 8192
 MOST_PRODUCTS = 8192 * 4096 * 28672
 MOST_WEIGHTS = 4096 * 28672
 MOST_EXPERT_WEIGHTS = 32 * 4096 * 4096
+MOST_VALUES = 8192 * (4096 + 14336)   # activations and results of a product
 MOST_LOGITS = 8192 * 256
 MOST_COMBINED = 8192 * 9 * 4096   # read and written
 
@@ -88,7 +89,7 @@ def _drawn(rng):
         while N * K > MOST_WEIGHTS:
             N = max(2, N // 4 * 2)
         M = rng.choice([1, rng.randint(2, 16), rng.randint(17, 128), _log(rng, 128, 8192)])
-        return dict(kind=kind, M=max(1, min(M, MOST_PRODUCTS // 2 // (N * K))), N=N, K=K, gated=gated, dtype=dtype)
+        return dict(kind=kind, M=max(1, min(M, MOST_PRODUCTS // 2 // (N * K), MOST_VALUES * 9 // 10 // (N + K))), N=N, K=K, gated=gated, dtype=dtype)
     if kind == "route":
         E = rng.randint(4, 384)
         return dict(kind=kind, T=_log(rng, 1, MOST_LOGITS // E), E=E, k=rng.randint(1, min(8, E)), renorm=rng.random() < 0.5, dtype=dtype)
@@ -102,7 +103,7 @@ def _drawn(rng):
     while E * N * K > MOST_EXPERT_WEIGHTS:
         N, K = max(2, N // 4 * 2), max(64, K * 3 // 4)
     T = rng.choice([1, rng.randint(2, 32), _log(rng, 32, 512), _log(rng, 512, 4096)])
-    return dict(kind=kind, T=max(1, min(T, MOST_PRODUCTS // 8 // (k * N * K))), E=E, k=k, N=N, K=K, gated=gated,
+    return dict(kind=kind, T=max(1, min(T, MOST_PRODUCTS // 8 // (k * N * K), MOST_VALUES // 2 // (k * (N + K)))), E=E, k=k, N=N, K=K, gated=gated,
                 gather=rng.random() < 0.6, skew=rng.choice([0.0, 0.5, 1.0]), dtype=dtype)
 
 
