@@ -278,6 +278,86 @@ HLQ_API hlq_status hlq_lut_gemm(const hlq_desc *d, const void *packed, const uin
                         int64_t ldx, void *Y, int64_t ldy, hlq_out_dtype out, void *ws,
                         size_t ws_bytes, void *stream);
 
+/* ---- Microscaled 4-bit matrices (MX4), and the expert block built on them -------------------------------------------
+ *
+ * An MX4 matrix [rows, K] holds its rows in blocks of 32 successive k: a value is an e2m1 float (0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * and their negatives) times 2^(scale byte - 127), one byte a block; byte 255 is NaN.  4.25 bits a value; any K (the last block
+ * of a row may be short).  It is the second weight format beside HLQ's bit planes: the one that the matrix cores multiply as it
+ * is, activations in it too.  A matrix lies in one blob of hlq_mx4_bytes() bytes, 16-byte aligned, whose layout is the
+ * library's (rows padded to 256 k): made by hlq_mx4_quantize from floats, or by hlq_mx4_pack from arrays in the exchange form.
+ * The conventions at the top of this file hold: device pointers, asynchronous on `stream`, arguments checked on the host first.
+ * Limits: K <= 2^21, rows <= 2^31 (a product's x_rows and rows below 2^31 - 256), N <= 2^20, 1024 experts, k <= 64. */
+typedef enum {
+    HLQ_F16 = 0,
+    HLQ_F32 = 1,
+    HLQ_BF16 = 2,
+    HLQ_MX4 = 3      /* activations of a product that are an MX4 blob already */
+} hlq_dtype;
+
+typedef enum {
+    HLQ_MX4_PLAIN = 0, /* Y[r, n] = p[r, n]                                                               */
+    HLQ_MX4_GATED = 1  /* Y[r, n] = silu(p[r, n]) * p[r, N / 2 + n], n < N / 2, silu(v) = v / (1 + e^-v), fp32 */
+} hlq_mx4_epilogue;
+
+#define HLQ_MAX_EXPERTS 1024
+#define HLQ_MAX_CHOICES 64
+
+/* Size of the blob of a matrix (host-only).  rows < 0 or K < 1: HLQ_ERR_BAD_DESC. */
+HLQ_API hlq_status hlq_mx4_bytes(int64_t rows, int32_t K, size_t *bytes);
+
+/* Rows x [rows, K] (f16, bf16 or f32, leading dimension ldx >= K in elements, any alignment of the type) to MX4.  Per block:
+ * e = floor(log2(largest magnitude)) - 2, at least -127; a value is the e2m1 float nearest to x 2^-e (ties: the even code; above 6
+ * it is 6); a block of zeros has byte 0.  A block that holds an infinity or a NaN gets byte 255: all of it is NaN. */
+HLQ_API hlq_status hlq_mx4_quantize(int64_t rows, int32_t K, const void *x, hlq_dtype type, int64_t ldx, void *blob,
+                                    size_t blob_bytes, void *stream);
+
+/* The values that a blob stands for, y [rows, K], leading dimension ldy >= K (exact where the type holds them: f32 and bf16 hold
+ * all but those below their smallest subnormal, f16 those in its range). */
+HLQ_API hlq_status hlq_mx4_dequantize(int64_t rows, int32_t K, const void *blob, void *y, hlq_dtype type, int64_t ldy, void *stream);
+
+/* Exchange form, as stored models have it: codes u8 [rows, (K + 1) / 2], two a byte, the even k in the low four bits; scales u8
+ * [rows, (K + 31) / 32]; their leading dimensions ldc and lds may be larger (codes stored up to a whole block, say), what lies past K is
+ * not read as a value.  hlq_mx4_unpack is the inverse, rows without gaps (codes or scales may be NULL to skip them; with K odd the last
+ * code's upper half reads 0). */
+HLQ_API hlq_status hlq_mx4_pack(int64_t rows, int32_t K, const uint8_t *codes, int64_t ldc, const uint8_t *scales, int64_t lds, void *blob,
+                                size_t blob_bytes, void *stream);
+HLQ_API hlq_status hlq_mx4_unpack(int64_t rows, int32_t K, const void *blob, uint8_t *codes, uint8_t *scales, void *stream);
+
+/* Workspace of hlq_mx4_gemm (experts = 1, x_rows = rows = M) and hlq_expert_gemm (host-only): enough for calls of at most these
+ * numbers of x_rows and rows with this K, N and number of experts.  hlq_workspace_init has to have seen it once, as other workspaces. */
+HLQ_API hlq_status hlq_mx4_workspace_bytes(int64_t N, int32_t K, int32_t experts, int64_t x_rows, int64_t rows, size_t *bytes);
+
+/* Y[M, .] = epilogue(Q(X) W^T): W an MX4 blob of N rows (a row per output column) and K; X [M, K] f16, bf16 or f32 with leading
+ * dimension ldx, quantized as hlq_mx4_quantize does (in the kernel or into the workspace), or an MX4 blob (ldx is not used).
+ * Products and the sums over a block are exact, sums over blocks fp32; Y of type ytype is rounded once, leading dimension ldy >= its
+ * columns (N, or N / 2 gated; N even then).  A NaN block of a row makes the row's results NaN, one of W its column's. */
+HLQ_API hlq_status hlq_mx4_gemm(int64_t N, int32_t K, const void *W, int64_t M, const void *X, hlq_dtype xtype, int64_t ldx, void *Y,
+                                hlq_dtype ytype, int64_t ldy, hlq_mx4_epilogue epilogue, void *ws, size_t ws_bytes, void *stream);
+
+/* The router: for each of T tokens the k largest of its E logits [T, ld >= E], largest first, ties to the lowest expert, and the
+ * tokens grouped by expert.
+ *   ids, weights [T, k]   the chosen experts, and their softmax weights in fp32: over the chosen ones (renorm != 0) or over all E
+ *   offsets [E + 1]       rows offsets[e] .. offsets[e + 1] - 1 are expert e's
+ *   rows [T k]            the token of each row; an expert's rows in the tokens' order
+ *   slots [T, k]          the row of each choice
+ * A logit of -inf is masked, and so is a NaN: never chosen.  A token with fewer than k others has -1 for id and slot and weight 0 in
+ * the places left, and `rows` ends in as many -1.  +inf counts as the largest float. */
+HLQ_API hlq_status hlq_route_workspace_bytes(int64_t T, int32_t E, int32_t k, size_t *bytes);
+HLQ_API hlq_status hlq_route(int64_t T, int32_t E, int32_t k, const void *logits, hlq_dtype type, int64_t ld, int renorm, int32_t *ids,
+                             float *weights, int32_t *offsets, int32_t *rows, int32_t *slots, void *ws, size_t ws_bytes, void *stream);
+
+/* Products grouped by expert: W is one MX4 blob of experts * N rows, expert e's matrix in rows e N ..; for row r < R of expert e
+ * (offsets[e] <= r < offsets[e + 1]; offsets int32 [experts + 1] on the device, ascending from 0) Y[r, .] = epilogue(Q(X[rows[r]]) W_e^T), with
+ * rows NULL of X[r].  Rows from offsets[experts] on are not written; offsets past R count as R, an index outside 0 .. x_rows - 1 as the
+ * nearest inside.  Otherwise as hlq_mx4_gemm. */
+HLQ_API hlq_status hlq_expert_gemm(int32_t experts, int64_t N, int32_t K, const void *W, const int32_t *offsets, const int32_t *rows,
+                                   int64_t R, int64_t x_rows, const void *X, hlq_dtype xtype, int64_t ldx, void *Y, hlq_dtype ytype,
+                                   int64_t ldy, hlq_mx4_epilogue epilogue, void *ws, size_t ws_bytes, void *stream);
+
+/* out[t, .] = sum_i weights[t, i] Y[slots[t, i], .] over i ascending in fp32, Y [R, D]; a slot outside 0 .. R - 1 adds nothing. */
+HLQ_API hlq_status hlq_expert_combine(int64_t T, int32_t k, int32_t D, int64_t R, const void *Y, hlq_dtype ytype, int64_t ldy,
+                                      const int32_t *slots, const float *weights, void *out, hlq_dtype otype, int64_t ldo, void *stream);
+
 /* Measurement helper, no part of the method: read `bytes` of device memory once with 128-bit
  * loads, `blocks` workgroups of 256 lanes each taking one contiguous share (0 = 2048), and store
  * one checksum word per workgroup to `sink`.  Benchmarks time it on as many bytes as a GEMV launch

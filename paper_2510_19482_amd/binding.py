@@ -32,6 +32,23 @@ class HlqError(RuntimeError):
         super().__init__(f"{fn}: {status_string(status)} (status {status})")
 
 
+_vp, _sz, _i64, _i32, _int = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64, ctypes.c_int32, ctypes.c_int
+_szp = ctypes.POINTER(ctypes.c_size_t)
+_MX4_ARGS = {
+    "hlq_mx4_bytes": [_i64, _i32, _szp],
+    "hlq_mx4_quantize": [_i64, _i32, _vp, _int, _i64, _vp, _sz, _vp],
+    "hlq_mx4_dequantize": [_i64, _i32, _vp, _vp, _int, _i64, _vp],
+    "hlq_mx4_pack": [_i64, _i32, _vp, _i64, _vp, _i64, _vp, _sz, _vp],
+    "hlq_mx4_unpack": [_i64, _i32, _vp, _vp, _vp, _vp],
+    "hlq_mx4_workspace_bytes": [_i64, _i32, _i32, _i64, _i64, _szp],
+    "hlq_mx4_gemm": [_i64, _i32, _vp, _i64, _vp, _int, _i64, _vp, _int, _i64, _int, _vp, _sz, _vp],
+    "hlq_route_workspace_bytes": [_i64, _i32, _i32, _szp],
+    "hlq_route": [_i64, _i32, _i32, _vp, _int, _i64, _int, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
+    "hlq_expert_gemm": [_i32, _i64, _i32, _vp, _vp, _vp, _i64, _i64, _vp, _int, _i64, _vp, _int, _i64, _int, _vp, _sz, _vp],
+    "hlq_expert_combine": [_i64, _i32, _i32, _i64, _vp, _int, _i64, _vp, _vp, _vp, _int, _i64, _vp],
+}
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -92,6 +109,10 @@ def _load() -> ctypes.CDLL:
     lib.hlq_mfma_probe.argtypes = [ctypes.c_int, vp, sz, ctypes.c_int, ctypes.c_int, vp, sz, ctypes.POINTER(ctypes.c_double), vp]
     lib.hlq_stream_read_shaped.restype = ctypes.c_int
     lib.hlq_stream_read_shaped.argtypes = [vp, sz, ctypes.c_int, ctypes.c_int, ctypes.c_int, vp, sz, vp]
+    for name, args in _MX4_ARGS.items():
+        fn = getattr(lib, name)
+        fn.restype = ctypes.c_int
+        fn.argtypes = args
     lib.hlq_lut_gemm.restype = ctypes.c_int
     lib.hlq_lut_gemm.argtypes = [dp, vp, vp, i64, i64, vp, i64, ctypes.c_int, vp, sz, vp]
     return lib
@@ -338,3 +359,212 @@ def hlq_lut_gemm(desc: HlqDesc, packed, X, Y=None, out_f32: bool = False, ws=Non
                                             HLQ_OUT_F32 if out_f32 else HLQ_OUT_F16, _ptr(ws), ws.numel(),
                                             _stream_ptr(stream)))
     return Y
+
+
+# ---- microscaled 4-bit matrices and the expert block ----------------------------------------------------------------
+HLQ_F16, HLQ_F32, HLQ_BF16, HLQ_MX4 = 0, 1, 2, 3
+_DTYPES = {torch.float16: HLQ_F16, torch.float32: HLQ_F32, torch.bfloat16: HLQ_BF16}
+
+
+def _dtype_of(t) -> int:
+    try:
+        return _DTYPES[t.dtype]
+    except KeyError:
+        raise TypeError(f"expected a float16, bfloat16 or float32 tensor, got {t.dtype}") from None
+
+
+def _row_stride(t, columns: int) -> int:
+    """Leading dimension of a matrix; one row has none of its own."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"expected a matrix whose rows are contiguous, got shape {tuple(t.shape)} with strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), columns)
+
+
+def _expect(t, shape, dtype, name: str) -> None:
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def mx4_bytes(rows: int, K: int) -> int:
+    n = ctypes.c_size_t()
+    _check("hlq_mx4_bytes", lib.hlq_mx4_bytes(rows, K, ctypes.byref(n)))
+    return n.value
+
+
+class Mx4:
+    """A microscaled 4-bit matrix [rows, K]: the blob (u8) in the library's layout."""
+
+    __slots__ = ("blob", "rows", "K", "_ptr", "_bytes")
+
+    def __init__(self, blob, rows: int, K: int):
+        self.blob, self.rows, self.K = blob, int(rows), int(K)
+        self._ptr, self._bytes = blob.data_ptr(), blob.numel()
+        if blob.dtype != torch.uint8 or not blob.is_contiguous() or self._bytes < mx4_bytes(rows, K):
+            raise ValueError(f"a blob of {mx4_bytes(rows, K)} bytes is needed for {rows} x {K}")
+
+
+def alloc_mx4(rows: int, K: int, device="cuda") -> Mx4:
+    return Mx4(torch.empty(mx4_bytes(rows, K), dtype=torch.uint8, device=device), rows, K)
+
+
+def hlq_mx4_quantize(x, out: Mx4 | None = None, stream=None) -> Mx4:
+    """Rows of x [rows, K] (f16, bf16 or f32) in 4-bit floats, a power-of-two scale for each 32 of a row."""
+    rows, K = x.shape
+    if out is None:
+        out = alloc_mx4(rows, K, x.device)
+    elif out.rows != rows or out.K != K:
+        raise ValueError(f"the output is a matrix of {out.rows} x {out.K}, x is {rows} x {K}")
+    status = lib.hlq_mx4_quantize(rows, K, x.data_ptr(), _dtype_of(x), _row_stride(x, K), out._ptr, out._bytes, _stream_ptr(stream))
+    if status != HLQ_OK:
+        raise HlqError("hlq_mx4_quantize", status)
+    return out
+
+
+def hlq_mx4_dequantize(m: Mx4, y=None, dtype=None, stream=None):
+    """The values [rows, K] that a matrix stands for, in y or a new tensor of `dtype` (f32 by default)."""
+    if y is None:
+        y = torch.empty((m.rows, m.K), dtype=dtype or torch.float32, device=m.blob.device)
+    elif tuple(y.shape) != (m.rows, m.K):
+        raise ValueError(f"y has shape {tuple(y.shape)}, the matrix is {m.rows} x {m.K}")
+    status = lib.hlq_mx4_dequantize(m.rows, m.K, m._ptr, y.data_ptr(), _dtype_of(y), _row_stride(y, m.K), _stream_ptr(stream))
+    if status != HLQ_OK:
+        raise HlqError("hlq_mx4_dequantize", status)
+    return y
+
+
+def hlq_mx4_pack(codes, scales, K: int, out: Mx4 | None = None, stream=None) -> Mx4:
+    """codes u8 [rows, (K + 1) // 2 or more] (the even k in the low half of a byte), scales u8 [rows, (K + 31) // 32 or more] -> matrix."""
+    rows = codes.shape[0]
+    for name, t, least in (("codes", codes, (K + 1) // 2), ("scales", scales, (K + 31) // 32)):
+        if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < least:
+            raise ValueError(f"{name}: expected uint8 of shape ({rows}, at least {least}), got {t.dtype} {tuple(t.shape)}")
+    if out is None:
+        out = alloc_mx4(rows, K, codes.device)
+    elif out.rows != rows or out.K != K:
+        raise ValueError(f"the output is a matrix of {out.rows} x {out.K}, not {rows} x {K}")
+    _check("hlq_mx4_pack", lib.hlq_mx4_pack(rows, K, _ptr(codes), _row_stride(codes, K), _ptr(scales), _row_stride(scales, K), out._ptr, out._bytes, _stream_ptr(stream)))
+    return out
+
+
+def hlq_mx4_unpack(m: Mx4, stream=None):
+    codes = torch.empty((m.rows, (m.K + 1) // 2), dtype=torch.uint8, device=m.blob.device)
+    scales = torch.empty((m.rows, (m.K + 31) // 32), dtype=torch.uint8, device=m.blob.device)
+    _check("hlq_mx4_unpack", lib.hlq_mx4_unpack(m.rows, m.K, m._ptr, _ptr(codes), _ptr(scales), _stream_ptr(stream)))
+    return codes, scales
+
+
+def mx4_workspace_bytes(N: int, K: int, experts: int, x_rows: int, rows: int) -> int:
+    n = ctypes.c_size_t()
+    _check("hlq_mx4_workspace_bytes", lib.hlq_mx4_workspace_bytes(N, K, experts, x_rows, rows, ctypes.byref(n)))
+    return n.value
+
+
+def alloc_mx4_workspace(W: Mx4, x_rows: int, rows: int | None = None, experts: int = 1, stream=None):
+    """Workspace for products with W of up to x_rows activation rows and `rows` result rows (the same if not given)."""
+    return _new_workspace(mx4_workspace_bytes(W.rows // experts, W.K, experts, x_rows, x_rows if rows is None else rows),
+                          W.blob.device, stream)
+
+
+def _product_args(W: Mx4, N: int, X, R: int, Y, gated: bool, out_dtype):
+    """(x pointer, type, ld), Y, (y pointer, type, ld), and the checks that a product's tensors need."""
+    if type(X) is Mx4:
+        x_rows, K, x = X.rows, X.K, (X._ptr, HLQ_MX4, 0)
+    else:
+        x_rows, K = X.shape
+        x = (X.data_ptr(), _dtype_of(X), _row_stride(X, K))
+    if K != W.K:
+        raise ValueError(f"X has {K} columns, the weights {W.K}")
+    cols = N // 2 if gated else N
+    if Y is None:
+        if out_dtype is None:
+            out_dtype = torch.float32 if type(X) is Mx4 else X.dtype
+        Y = torch.empty((R, cols), dtype=out_dtype, device=W.blob.device)
+    elif Y.shape[0] != R or Y.shape[1] != cols:
+        raise ValueError(f"Y has shape {tuple(Y.shape)}, the result is {R} x {cols}")
+    return x_rows, x, Y, (Y.data_ptr(), _dtype_of(Y), _row_stride(Y, cols))
+
+
+def hlq_mx4_gemm(W: Mx4, X, Y=None, gated: bool = False, out_dtype=None, ws=None, stream=None):
+    """Y = Q(X) W^T, or with `gated` silu of its first half of columns times the second; X [M, K] f16, bf16 or f32, or Mx4."""
+    M = X.rows if type(X) is Mx4 else X.shape[0]
+    _, x, Y, y = _product_args(W, W.rows, X, M, Y, gated, out_dtype)
+    if ws is None:
+        ws = alloc_mx4_workspace(W, M, stream=stream)
+    status = lib.hlq_mx4_gemm(W.rows, W.K, W._ptr, M, *x, *y, int(gated), ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+    if status != HLQ_OK:
+        raise HlqError("hlq_mx4_gemm", status)
+    return Y
+
+
+class Route:
+    """What hlq_route writes: ids, weights, slots [T, k], offsets [E + 1], rows [T k], and its workspace."""
+
+    __slots__ = ("ids", "weights", "offsets", "rows", "slots", "ws", "T", "E", "k", "_args")
+
+    def __init__(self, T: int, E: int, k: int, device="cuda"):
+        n = ctypes.c_size_t()
+        _check("hlq_route_workspace_bytes", lib.hlq_route_workspace_bytes(T, E, k, ctypes.byref(n)))
+        self.T, self.E, self.k = T, E, k
+        self.ids, self.slots = (torch.empty((T, k), dtype=torch.int32, device=device) for _ in range(2))
+        self.weights = torch.empty((T, k), dtype=torch.float32, device=device)
+        self.offsets = torch.empty(E + 1, dtype=torch.int32, device=device)
+        self.rows = torch.empty(T * k, dtype=torch.int32, device=device)
+        self.ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+        self._args = tuple(_ptr(t) for t in (self.ids, self.weights, self.offsets, self.rows, self.slots, self.ws)) + (n.value,)
+
+
+def alloc_route(T: int, E: int, k: int, device="cuda") -> Route:
+    return Route(T, E, k, device)
+
+
+def hlq_route(logits, k: int, renorm: bool = True, out: Route | None = None, stream=None) -> Route:
+    """The k experts of each token by its logits [T, E], their weights, and the tokens grouped by expert."""
+    T, E = logits.shape
+    if out is None:
+        out = Route(T, E, k, logits.device)
+    elif (out.T, out.E, out.k) != (T, E, k):
+        raise ValueError(f"the output is for {out.T} tokens, {out.E} experts, {out.k} each")
+    status = lib.hlq_route(T, E, k, logits.data_ptr(), _dtype_of(logits), _row_stride(logits, E), int(renorm), *out._args, _stream_ptr(stream))
+    if status != HLQ_OK:
+        raise HlqError("hlq_route", status)
+    return out
+
+
+def hlq_expert_gemm(W: Mx4, offsets, X, Y=None, rows=None, gated: bool = False, out_dtype=None, ws=None, stream=None):
+    """Y[r] = Q(X[rows[r]]) W_e^T for the rows offsets[e] <= r < offsets[e + 1] of each expert e, or of X[r] without `rows`;
+    W holds the experts' matrices one after the other."""
+    E = offsets.numel() - 1
+    if E < 1 or W.rows % E or offsets.dtype != torch.int32 or not offsets.is_contiguous():
+        raise ValueError(f"offsets: int32, one more than experts; {offsets.numel()} of {offsets.dtype} for {W.rows} rows of weights")
+    if rows is None:
+        R, rows_ptr = X.rows if type(X) is Mx4 else X.shape[0], 0
+    else:
+        if rows.dtype != torch.int32 or not rows.is_contiguous():
+            raise ValueError(f"rows: contiguous int32, got {rows.dtype}")
+        R, rows_ptr = rows.numel(), rows.data_ptr()
+    N = W.rows // E
+    x_rows, x, Y, y = _product_args(W, N, X, R, Y, gated, out_dtype)
+    if ws is None:
+        ws = alloc_mx4_workspace(W, x_rows, R, E, stream)
+    status = lib.hlq_expert_gemm(E, N, W.K, W._ptr, offsets.data_ptr(), rows_ptr, R, x_rows, *x, *y, int(gated), ws.data_ptr(), ws.numel(),
+                                 _stream_ptr(stream))
+    if status != HLQ_OK:
+        raise HlqError("hlq_expert_gemm", status)
+    return Y
+
+
+def hlq_expert_combine(Y, slots, weights, out=None, out_dtype=None, stream=None):
+    """out[t] = sum_i weights[t, i] Y[slots[t, i]] (slot -1: nothing)."""
+    T, k = slots.shape
+    R, D = Y.shape
+    _expect(slots, (T, k), torch.int32, "slots")
+    _expect(weights, (T, k), torch.float32, "weights")
+    if out is None:
+        out = torch.empty((T, D), dtype=out_dtype or Y.dtype, device=Y.device)
+    elif tuple(out.shape) != (T, D):
+        raise ValueError(f"out has shape {tuple(out.shape)}, the result is {T} x {D}")
+    status = lib.hlq_expert_combine(T, k, D, R, Y.data_ptr(), _dtype_of(Y), _row_stride(Y, D), slots.data_ptr(), weights.data_ptr(),
+                                    out.data_ptr(), _dtype_of(out), _row_stride(out, D), _stream_ptr(stream))
+    if status != HLQ_OK:
+        raise HlqError("hlq_expert_combine", status)
+    return out

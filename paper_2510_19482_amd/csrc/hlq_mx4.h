@@ -1,0 +1,172 @@
+// Microscaled 4-bit matrices (MX4): values of a row in blocks of 32 along k, a value = e2m1 code x 2^(scale byte - 127).
+//
+// Layout of a matrix [rows, K] in one blob, Kp = K rounded up to 256:
+//
+//   codes   [rows][Kp / 2]       two codes a byte, the even k in the low half; zero past K
+//   scales  [Kp / 256][rows][8]  of the eight blocks of a panel (256 k) byte (b % 2) * 4 + b / 2 is block b's; zero past K
+//
+// A row's share of a panel is one line of 128 bytes.  The matrix cores take 32 successive k of a row from one lane, which
+// also gives the block's scale byte, chosen from a register by the instruction:
+//   32x32x64   lane l: row l % 32, block 2 s + l / 32 of step s = 0..3: its four scale bytes are the dword l / 32 of the panel
+//   16x16x128  lane l: row l % 16, block 4 s + l / 16 of step s = 0, 1: bytes 0 and 2 of dword (l / 16) % 2 moved right by
+//              8 (l / 32) bits
+// so a lane loads one dword a row and panel, and the rows of an operand stand next to each other: whole lines.
+// Scale byte 255 is NaN and makes the results NaN that its block enters; products and the sum over a block are exact, the
+// accumulation is fp32.
+#pragma once
+
+#include "hlq_internal.h"
+
+typedef int mx4_int4 __attribute__((ext_vector_type(4)));
+typedef int mx4_int8 __attribute__((ext_vector_type(8)));
+typedef float mx4_float4 __attribute__((ext_vector_type(4)));
+typedef float mx4_float8 __attribute__((ext_vector_type(8)));
+typedef float mx4_float16 __attribute__((ext_vector_type(16)));
+typedef _Float16 mx4_half2 __attribute__((ext_vector_type(2)));
+typedef _Float16 mx4_half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 mx4_bf2 __attribute__((ext_vector_type(2)));
+typedef __bf16 mx4_bf8 __attribute__((ext_vector_type(8)));
+
+#define MX4_PANEL_K 256
+#define MX4_MAX_ROWS ((int64_t)1 << 31)
+#define MX4_FP4 4   // the instruction's number of the e2m1 format
+
+struct Mx4Dims {
+    int64_t rows;
+    int K, panels;          // panels = Kp / 256
+    size_t code_bytes, total;
+    __host__ __device__ int row_bytes() const { return panels * (MX4_PANEL_K / 2); }
+};
+
+// what the kernels see of a matrix
+struct Mx4View {
+    const uint8_t *codes, *scales;
+    int64_t rows;           // between a row's scales of one panel and of the next: 8 * rows bytes
+};
+
+hlq_status hlq_mx4_check(int64_t rows, int32_t K, Mx4Dims *out);
+static inline Mx4View hlq_mx4_view(const Mx4Dims &d, const void *blob)
+{
+    return Mx4View{(const uint8_t *)blob, (const uint8_t *)blob + d.code_bytes, d.rows};
+}
+hlq_status hlq_mx4_launch_quantize(const Mx4Dims &d, const void *x, hlq_dtype t, int64_t ldx, void *blob, hipStream_t st);
+
+// byte of block b inside the eight bytes of its panel
+__host__ __device__ __forceinline__ int mx4_scale_byte(int b) { return (b & 1) * 4 + ((b & 7) >> 1); }
+
+static inline int hlq_dtype_bytes(hlq_dtype t) { return t == HLQ_F32 ? 4 : 2; }
+static inline bool hlq_is_float(int t) { return t == HLQ_F16 || t == HLQ_F32 || t == HLQ_BF16; }
+
+// storage type of a dtype
+template <int T> struct Mx4Type;
+template <> struct Mx4Type<HLQ_F16> { using type = _Float16; };
+template <> struct Mx4Type<HLQ_BF16> { using type = __bf16; };
+template <> struct Mx4Type<HLQ_F32> { using type = float; };
+
+// Eight successive values of a row, quantized: what one lane holds of a block of 32 that four lanes share.
+// `top` is the largest magnitude as a float's bits (infinities and NaN: exponent 255).
+__device__ __forceinline__ uint32_t mx4_top_bits(const _Float16 (&v)[8])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t b = __builtin_bit_cast(uint16_t, v[i]) & 0x7fffu;
+        m = b > m ? b : m;
+    }
+    return m >= 0x7c00u ? 0x7f800000u : __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)m));
+}
+__device__ __forceinline__ uint32_t mx4_top_bits(const __bf16 (&v)[8])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t b = __builtin_bit_cast(uint16_t, v[i]) & 0x7fffu;
+        m = b > m ? b : m;
+    }
+    return m << 16;
+}
+__device__ __forceinline__ uint32_t mx4_top_bits(const float (&v)[8])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t b = __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu;
+        m = b > m ? b : m;
+    }
+    return m;
+}
+// Scale byte of a block whose largest magnitude has these bits: floor(log2) - 2 and the bias, at least 0.  Zero and
+// subnormal floats have exponent field 0; a block that holds an infinity or a NaN gets 255.
+__device__ __forceinline__ uint32_t mx4_scale_of(uint32_t top)
+{
+    const uint32_t e = top >> 23;
+    return e == 255u ? 255u : e > 2u ? e - 2u : 0u;
+}
+// Codes of eight values under a scale byte, the first in the lowest four bits: to nearest, ties to the even code, above 5 it
+// is 6.  The conversion takes the scale's exponent field, so 2^-127 (byte 0) is given as +0.  (All finite f16 and bf16 values
+// and f32 grids and ties against a 64-bit reference at scale bytes 0..252: no difference.)
+__device__ __forceinline__ uint32_t mx4_codes(const _Float16 (&v)[8], uint32_t byte)
+{
+    const float s = __builtin_bit_cast(float, byte << 23);
+    uint32_t r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(0u, (mx4_half2){v[0], v[1]}, s, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, (mx4_half2){v[2], v[3]}, s, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, (mx4_half2){v[4], v[5]}, s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, (mx4_half2){v[6], v[7]}, s, 3);
+}
+__device__ __forceinline__ uint32_t mx4_codes(const __bf16 (&v)[8], uint32_t byte)
+{
+    const float s = __builtin_bit_cast(float, byte << 23);
+    uint32_t r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, (mx4_bf2){v[0], v[1]}, s, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, (mx4_bf2){v[2], v[3]}, s, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, (mx4_bf2){v[4], v[5]}, s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, (mx4_bf2){v[6], v[7]}, s, 3);
+}
+__device__ __forceinline__ uint32_t mx4_codes(const float (&v)[8], uint32_t byte)
+{
+    const float s = __builtin_bit_cast(float, byte << 23);
+    uint32_t r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0], v[1], s, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[2], v[3], s, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[4], v[5], s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6], v[7], s, 3);
+}
+
+// Eight values at p of a row that ends `left` values on (left <= 0: none); past the end zeros.  ALIGNED: p is 16-byte aligned.
+template <bool ALIGNED, class T>
+__device__ __forceinline__ void mx4_load8(const T *p, int left, T (&v)[8])
+{
+    if (ALIGNED && left >= 8) {
+        struct alignas(16) Eight { T v[8]; };
+        const Eight e = *(const Eight *)p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = e.v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (T)0.0f;
+    }
+}
+
+__device__ __forceinline__ float mx4_gate(float g, float u)
+{
+    // silu(g) u, each step within an ulp or two of fp32; where exp(-g) overflows the reciprocal is 0, as it should be
+    return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
+}
+
+// n <= 4 successive results of a row, rounded to nearest even
+__device__ __forceinline__ void mx4_store(void *y, int type, int64_t at, const float *v, int n, bool whole)
+{
+    if (type == HLQ_F32) {
+        float *p = (float *)y + at;
+        if (whole) *(mx4_float4 *)p = (mx4_float4){v[0], v[1], v[2], v[3]};
+        else
+            for (int i = 0; i < n; ++i) p[i] = v[i];
+    } else {
+        uint16_t b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            b[i] = type == HLQ_F16 ? __builtin_bit_cast(uint16_t, (_Float16)v[i]) : __builtin_bit_cast(uint16_t, (__bf16)v[i]);
+        uint16_t *p = (uint16_t *)y + at;
+        if (whole) *(uint2 *)p = make_uint2(b[0] | (uint32_t)b[1] << 16, b[2] | (uint32_t)b[3] << 16);
+        else
+            for (int i = 0; i < n; ++i) p[i] = b[i];
+    }
+}

@@ -1,0 +1,238 @@
+// MX4 matrices: quantization of rows, the values back, and the exchange form (codes and scale bytes row by row) in and out.
+//
+//   block b of 32 k:  e = max(floor(log2(max |x|)) - 2, -127);  value = e2m1 nearest to x 2^-e (ties to the even code, at most 6)
+//
+// Quantizing reads a value once and writes 4.25 bits: it is bound by memory.  A wavefront takes a row's panel of 256 k at a
+// time per half: a lane has eight successive values (one 16-byte load of 16-bit types, two of fp32), four lanes a block, whose
+// largest magnitudes meet by two quad permutations; codes leave as a dword a lane, 128 contiguous bytes a panel.
+#include "hlq_mx4.h"
+
+namespace {
+
+constexpr int MX4_WAVES = 4;
+
+__device__ __forceinline__ uint32_t quad_max(uint32_t v)
+{
+    uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true);   // lanes 1 0 3 2
+    v = o > v ? o : v;
+    o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true);            // lanes 2 3 0 1
+    return o > v ? o : v;
+}
+
+// One wavefront: two panels of one row at a time, lanes 0..31 the first.
+template <int T, bool ALIGNED>
+__global__ void __launch_bounds__(64 * MX4_WAVES)
+hlq_mx4_quantize_kernel(const typename Mx4Type<T>::type *__restrict__ x, int64_t ldx, int64_t rows, int K, int panels,
+                        uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, int pairs, int64_t items)
+{
+    const int lane = (int)(threadIdx.x & 63u);
+    for (int64_t it = (int64_t)blockIdx.x * MX4_WAVES + (threadIdx.x >> 6); it < items; it += (int64_t)gridDim.x * MX4_WAVES) {
+        const int64_t row = it / pairs;
+        const int panel = 2 * (int)(it - row * pairs) + (lane >> 5);
+        if (panel >= panels) continue;
+        const int k = panel * MX4_PANEL_K + (lane & 31) * 8;
+        typename Mx4Type<T>::type v[8];
+        mx4_load8<ALIGNED>(x + row * ldx + k, K - k, v);
+        const uint32_t byte = mx4_scale_of(quad_max(mx4_top_bits(v)));
+        *(uint32_t *)(codes + row * panels * 128 + panel * 128 + (lane & 31) * 4) = mx4_codes(v, byte);
+        if ((lane & 3) == 0) scales[((int64_t)panel * rows + row) * 8 + mx4_scale_byte((lane & 31) >> 2)] = (uint8_t)byte;
+    }
+}
+
+__device__ __forceinline__ float code_value(uint32_t c)
+{
+    const uint32_t m = c & 7u;   // 0 0.5 1 1.5 2 3 4 6
+    const float a = m < 2u ? 0.5f * (float)m : __builtin_bit_cast(float, (((m >> 1) + 126u) << 23) | ((m & 1u) << 22));
+    return c & 8u ? -a : a;
+}
+
+template <int T>
+__global__ void __launch_bounds__(256)
+hlq_mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t rows, int K, int panels,
+                          typename Mx4Type<T>::type *__restrict__ y, int64_t ldy, int64_t items)
+{
+    const int eights = panels * 32;
+    for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items; it += (int64_t)gridDim.x * 256) {
+        const int64_t row = it / eights;
+        const int j = (int)(it - row * eights), k = j * 8;
+        if (k >= K) continue;
+        const uint32_t c = *(const uint32_t *)(codes + row * panels * 128 + j * 4);
+        const uint32_t byte = scales[((int64_t)(j >> 5) * rows + row) * 8 + mx4_scale_byte((j >> 2) & 7)];
+        typename Mx4Type<T>::type *p = y + row * ldy + k;
+        for (int i = 0; i < 8 && k + i < K; ++i) {
+            const float v = byte == 255u ? __builtin_nanf("") : ldexpf(code_value(c >> (4 * i)), (int)byte - 127);
+            p[i] = (typename Mx4Type<T>::type)v;
+        }
+    }
+}
+
+// exchange form: codes [rows][(K + 1) / 2], scales [rows][(K + 31) / 32]; a thread makes eight codes, every 32nd also a scale's four lanes
+__global__ void __launch_bounds__(256)
+hlq_mx4_pack_kernel(const uint8_t *__restrict__ in, int64_t ldc, const uint8_t *__restrict__ in_scales, int64_t lds, int64_t rows, int K, int panels,
+                    uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, int64_t items)
+{
+    const int eights = panels * 32, bytes = (K + 1) / 2, blocks = (K + 31) / 32;
+    for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items; it += (int64_t)gridDim.x * 256) {
+        const int64_t row = it / eights;
+        const int j = (int)(it - row * eights);
+        uint32_t c = 0;
+        for (int i = 0; i < 4; ++i) {
+            const int at = 4 * j + i;
+            uint32_t b = at < bytes ? in[row * ldc + at] : 0u;
+            if (2 * at + 1 >= K) b &= 15u;
+            c |= b << (8 * i);
+        }
+        *(uint32_t *)(codes + row * panels * 128 + j * 4) = c;
+        if ((j & 3) == 0)
+            scales[((int64_t)(j >> 5) * rows + row) * 8 + mx4_scale_byte((j >> 2) & 7)] = (j >> 2) < blocks ? in_scales[row * lds + (j >> 2)] : (uint8_t)0;
+    }
+}
+
+__global__ void __launch_bounds__(256)
+hlq_mx4_unpack_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t rows, int K, int panels,
+                      uint8_t *__restrict__ out, uint8_t *__restrict__ out_scales, int64_t items)
+{
+    const int eights = panels * 32, bytes = (K + 1) / 2, blocks = (K + 31) / 32;
+    for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items; it += (int64_t)gridDim.x * 256) {
+        const int64_t row = it / eights;
+        const int j = (int)(it - row * eights);
+        if (out) {
+            const uint32_t c = *(const uint32_t *)(codes + row * panels * 128 + j * 4);
+            for (int i = 0; i < 4 && 4 * j + i < bytes; ++i) out[row * bytes + 4 * j + i] = (uint8_t)(c >> (8 * i));
+        }
+        if (out_scales && (j & 3) == 0 && (j >> 2) < blocks)
+            out_scales[row * blocks + (j >> 2)] = scales[((int64_t)(j >> 5) * rows + row) * 8 + mx4_scale_byte((j >> 2) & 7)];
+    }
+}
+
+unsigned grid_of(int64_t items, int64_t a_block)
+{
+    const int64_t g = (items + a_block - 1) / a_block;
+    return (unsigned)(g < 65536 ? g : 65536);
+}
+
+template <int T>
+void launch_quantize(const Mx4Dims &d, const void *x, int64_t ldx, void *blob, hipStream_t st)
+{
+    using V = typename Mx4Type<T>::type;
+    const int pairs = (d.panels + 1) / 2;
+    const int64_t items = d.rows * pairs;
+    uint8_t *codes = (uint8_t *)blob, *scales = codes + d.code_bytes;
+    const bool aligned = ((uintptr_t)x & 15u) == 0 && (d.rows == 1 || (ldx * (int64_t)sizeof(V)) % 16 == 0);
+    const dim3 grid(grid_of(items, MX4_WAVES)), block(64 * MX4_WAVES);
+    if (aligned) hlq_mx4_quantize_kernel<T, true><<<grid, block, 0, st>>>((const V *)x, ldx, d.rows, d.K, d.panels, codes, scales, pairs, items);
+    else hlq_mx4_quantize_kernel<T, false><<<grid, block, 0, st>>>((const V *)x, ldx, d.rows, d.K, d.panels, codes, scales, pairs, items);
+}
+
+template <int T>
+void launch_dequantize(const Mx4Dims &d, const void *blob, void *y, int64_t ldy, hipStream_t st)
+{
+    using V = typename Mx4Type<T>::type;
+    const int64_t items = d.rows * d.panels * 32;
+    hlq_mx4_dequantize_kernel<T><<<grid_of(items, 256), 256, 0, st>>>((const uint8_t *)blob, (const uint8_t *)blob + d.code_bytes, d.rows, d.K, d.panels, (V *)y, ldy, items);
+}
+
+// what the four calls have in common
+hlq_status check_matrix(int64_t rows, int32_t K, Mx4Dims *d, const void *blob, size_t blob_bytes)
+{
+    const hlq_status s = hlq_mx4_check(rows, K, d);
+    if (s != HLQ_OK) return s;
+    if (rows == 0) return HLQ_OK;
+    if (!blob) return HLQ_ERR_NULL;
+    if ((uintptr_t)blob & 15u) return HLQ_ERR_BAD_STRIDE;
+    return blob_bytes < d->total ? HLQ_ERR_BUFFER_TOO_SMALL : HLQ_OK;
+}
+
+}  // namespace
+
+hlq_status hlq_mx4_check(int64_t rows, int32_t K, Mx4Dims *out)
+{
+    if (rows < 0 || K < 1) return HLQ_ERR_BAD_DESC;
+    if (K > HLQ_MAX_K || rows > MX4_MAX_ROWS) return HLQ_ERR_UNSUPPORTED;
+    Mx4Dims d;
+    d.rows = rows;
+    d.K = K;
+    d.panels = (K + MX4_PANEL_K - 1) / MX4_PANEL_K;
+    d.code_bytes = (size_t)rows * (size_t)d.row_bytes();
+    d.total = d.code_bytes + (size_t)rows * (size_t)d.panels * 8u;
+    *out = d;
+    return HLQ_OK;
+}
+
+hlq_status hlq_mx4_launch_quantize(const Mx4Dims &d, const void *x, hlq_dtype t, int64_t ldx, void *blob, hipStream_t st)
+{
+    if (t == HLQ_F16) launch_quantize<HLQ_F16>(d, x, ldx, blob, st);
+    else if (t == HLQ_BF16) launch_quantize<HLQ_BF16>(d, x, ldx, blob, st);
+    else launch_quantize<HLQ_F32>(d, x, ldx, blob, st);
+    return hlq_hip_status(hipGetLastError());
+}
+
+extern "C" {
+
+hlq_status hlq_mx4_bytes(int64_t rows, int32_t K, size_t *bytes)
+{
+    Mx4Dims d;
+    const hlq_status s = hlq_mx4_check(rows, K, &d);
+    if (s != HLQ_OK) return s;
+    if (!bytes) return HLQ_ERR_NULL;
+    *bytes = d.total;
+    return HLQ_OK;
+}
+
+hlq_status hlq_mx4_quantize(int64_t rows, int32_t K, const void *x, hlq_dtype type, int64_t ldx, void *blob, size_t blob_bytes, void *stream)
+{
+    Mx4Dims d;
+    const hlq_status s = check_matrix(rows, K, &d, blob, blob_bytes);
+    if (s != HLQ_OK) return s;
+    if (!hlq_is_float(type)) return HLQ_ERR_UNSUPPORTED;
+    if (rows > 1 && ldx < K) return HLQ_ERR_BAD_STRIDE;
+    if (rows == 0) return HLQ_OK;
+    if (!x) return HLQ_ERR_NULL;
+    if ((uintptr_t)x % (unsigned)hlq_dtype_bytes(type)) return HLQ_ERR_BAD_STRIDE;
+    hlq_clear_stale_error();
+    return hlq_mx4_launch_quantize(d, x, type, ldx, blob, (hipStream_t)stream);
+}
+
+hlq_status hlq_mx4_dequantize(int64_t rows, int32_t K, const void *blob, void *y, hlq_dtype type, int64_t ldy, void *stream)
+{
+    Mx4Dims d;
+    const hlq_status s = check_matrix(rows, K, &d, blob, SIZE_MAX);
+    if (s != HLQ_OK) return s;
+    if (!hlq_is_float(type)) return HLQ_ERR_UNSUPPORTED;
+    if (rows > 1 && ldy < K) return HLQ_ERR_BAD_STRIDE;
+    if (rows == 0) return HLQ_OK;
+    if (!y) return HLQ_ERR_NULL;
+    if ((uintptr_t)y % (unsigned)hlq_dtype_bytes(type)) return HLQ_ERR_BAD_STRIDE;
+    hlq_clear_stale_error();
+    if (type == HLQ_F16) launch_dequantize<HLQ_F16>(d, blob, y, ldy, (hipStream_t)stream);
+    else if (type == HLQ_BF16) launch_dequantize<HLQ_BF16>(d, blob, y, ldy, (hipStream_t)stream);
+    else launch_dequantize<HLQ_F32>(d, blob, y, ldy, (hipStream_t)stream);
+    return hlq_hip_status(hipGetLastError());
+}
+
+hlq_status hlq_mx4_pack(int64_t rows, int32_t K, const uint8_t *codes, int64_t ldc, const uint8_t *scales, int64_t lds, void *blob, size_t blob_bytes, void *stream)
+{
+    Mx4Dims d;
+    const hlq_status s = check_matrix(rows, K, &d, blob, blob_bytes);
+    if (s != HLQ_OK || rows == 0) return s;
+    if (!codes || !scales) return HLQ_ERR_NULL;
+    if (rows > 1 && (ldc < (K + 1) / 2 || lds < (K + 31) / 32)) return HLQ_ERR_BAD_STRIDE;
+    hlq_clear_stale_error();
+    const int64_t items = rows * d.panels * 32;
+    hlq_mx4_pack_kernel<<<grid_of(items, 256), 256, 0, (hipStream_t)stream>>>(codes, ldc, scales, lds, rows, K, d.panels, (uint8_t *)blob, (uint8_t *)blob + d.code_bytes, items);
+    return hlq_hip_status(hipGetLastError());
+}
+
+hlq_status hlq_mx4_unpack(int64_t rows, int32_t K, const void *blob, uint8_t *codes, uint8_t *scales, void *stream)
+{
+    Mx4Dims d;
+    const hlq_status s = check_matrix(rows, K, &d, blob, SIZE_MAX);
+    if (s != HLQ_OK || rows == 0) return s;
+    if (!codes && !scales) return HLQ_OK;
+    hlq_clear_stale_error();
+    const int64_t items = rows * d.panels * 32;
+    hlq_mx4_unpack_kernel<<<grid_of(items, 256), 256, 0, (hipStream_t)stream>>>((const uint8_t *)blob, (const uint8_t *)blob + d.code_bytes, rows, K, d.panels, codes, scales, items);
+    return hlq_hip_status(hipGetLastError());
+}
+
+}  // extern "C"

@@ -1,0 +1,82 @@
+// Products of MX4 matrices: arguments that the kernels share, and which rows a workgroup takes.
+#pragma once
+
+#include "hlq_mx4.h"
+
+struct Mx4Product {
+    Mx4View W;              // [E * N, K]: matrix e in rows e * N ..
+    int N, cols, K, panels; // cols: of the result, N or N / 2 (gated)
+    const int32_t *offsets; // NULL: one matrix, rows 0..R - 1
+    int E;
+    const int32_t *rows;    // row of x for each of the R rows; NULL: the same
+    int R, x_rows;
+    const void *x;          // f16, bf16 or f32 rows that the kernel quantizes; else A
+    int64_t ldx;
+    bool x_aligned;
+    Mx4View A;
+    void *y;
+    int ytype;
+    int64_t ldy;
+    bool y_aligned;         // four successive results start where one store can write them
+};
+
+// Row tile number `tile` of tiles of BM rows that begin anew at each expert.  Every lane of the wavefront takes part and gets
+// the same answer; n = 0: there are fewer tiles.  Offsets are device data: whatever they hold, rows stay within 0..R - 1.
+struct Mx4RowTile {
+    int e, row0, n;
+};
+template <int BM>
+__device__ __forceinline__ Mx4RowTile mx4_row_tile(const Mx4Product &a, int tile)
+{
+    if (!a.offsets) {
+        const int64_t r = (int64_t)tile * BM;
+        if (r >= a.R) return {0, 0, 0};
+        return {0, (int)r, (int)(a.R - r < BM ? a.R - r : BM)};
+    }
+    const int lane = (int)(threadIdx.x & 63u);
+    int before = 0;
+    for (int base = 0; base < a.E; base += 64) {
+        const int e = base + lane;
+        int lo = a.R, hi = a.R;
+        if (e < a.E) {
+            lo = a.offsets[e];
+            hi = a.offsets[e + 1];
+        }
+        lo = lo < 0 ? 0 : lo > a.R ? a.R : lo;
+        hi = hi < lo ? lo : hi > a.R ? a.R : hi;
+        int upto = (hi - lo) / BM + ((hi - lo) % BM != 0);
+        const int mine = upto;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        const int all = __builtin_amdgcn_readlane(upto, 63);
+        if (tile - before < all) {
+            const uint64_t past = __ballot(upto > tile - before);
+            const int f = (int)__builtin_ctzll(past);
+            const int l = __builtin_amdgcn_readlane(lo, f), h = __builtin_amdgcn_readlane(hi, f);
+            const int r = l + (tile - before - (__builtin_amdgcn_readlane(upto, f) - __builtin_amdgcn_readlane(mine, f))) * BM;
+            return {base + f, r, h - r < BM ? h - r : BM};
+        }
+        before += all;
+    }
+    return {0, 0, 0};
+}
+
+// Most row tiles that R rows of E experts make.
+static inline int64_t mx4_row_tiles(int64_t R, int E, int BM)
+{
+    const int64_t full = (R + BM - 1) / BM;
+    return E <= 1 ? full : R / BM + (R < E ? R : E);
+}
+
+// row of x for row r (r < R); an index outside x is taken as its nearest end, so that nothing outside is read
+__device__ __forceinline__ int mx4_x_row(const Mx4Product &a, int r)
+{
+    if (!a.rows) return r;
+    const int i = a.rows[r];
+    return i < 0 ? 0 : i >= a.x_rows ? a.x_rows - 1 : i;
+}
+
+hlq_status hlq_mx4_launch_few(const Mx4Product &a, int xtype, bool gated, hipStream_t st);
