@@ -1,16 +1,14 @@
 // Microscaled 4-bit matrices (MX4): values of a row in blocks of 32 along k, a value = e2m1 code x 2^(scale byte - 127).
 //
-// Layout of a matrix [rows, K] in one blob, Kp = K rounded up to 256:
+// Layout of a matrix [rows, K] in one blob, panels of 128 k:
 //
-//   codes   [rows][Kp / 2]       two codes a byte, the even k in the low half; zero past K
-//   scales  [Kp / 256][rows][8]  of the eight blocks of a panel (256 k) byte (b % 2) * 4 + b / 2 is block b's; zero past K
+//   codes   [panels][rows][64]   two codes a byte, the even k in the low half; zero past K
+//   scales  [panels][rows][4]    byte (b % 2) * 2 + b / 2 is that of block b of the panel's four; zero past K
 //
-// A row's share of a panel is one line of 128 bytes.  The matrix cores take 32 successive k of a row from one lane, which
-// also gives the block's scale byte, chosen from a register by the instruction:
-//   32x32x64   lane l: row l % 32, block 2 s + l / 32 of step s = 0..3: its four scale bytes are the dword l / 32 of the panel
-//   16x16x128  lane l: row l % 16, block 4 s + l / 16 of step s = 0, 1: bytes 0 and 2 of dword (l / 16) % 2 moved right by
-//              8 (l / 32) bits
-// so a lane loads one dword a row and panel, and the rows of an operand stand next to each other: whole lines.
+// so that what a tile of rows needs of a panel is one contiguous piece of memory.  The matrix cores take 32 successive k of a
+// row from one lane, which also gives the block's scale byte, chosen from a register by the instruction:
+//   32x32x64   lane l: row l % 32, block 2 s + l / 32 of step s = 0, 1: its scale bytes are the 16 bits l / 32 of the row's four
+//   16x16x128  lane l: row l % 16, block l / 16
 // Scale byte 255 is NaN and makes the results NaN that its block enters; products and the sum over a block are exact, the
 // accumulation is fp32.
 #pragma once
@@ -27,21 +25,20 @@ typedef _Float16 mx4_half8 __attribute__((ext_vector_type(8)));
 typedef __bf16 mx4_bf2 __attribute__((ext_vector_type(2)));
 typedef __bf16 mx4_bf8 __attribute__((ext_vector_type(8)));
 
-#define MX4_PANEL_K 256
+#define MX4_PANEL_K 128
 #define MX4_MAX_ROWS ((int64_t)1 << 31)
 #define MX4_FP4 4   // the instruction's number of the e2m1 format
 
 struct Mx4Dims {
     int64_t rows;
-    int K, panels;          // panels = Kp / 256
+    int K, panels;
     size_t code_bytes, total;
-    __host__ __device__ int row_bytes() const { return panels * (MX4_PANEL_K / 2); }
 };
 
 // what the kernels see of a matrix
 struct Mx4View {
     const uint8_t *codes, *scales;
-    int64_t rows;           // between a row's scales of one panel and of the next: 8 * rows bytes
+    int64_t rows;           // a row's place in panel p is p * rows + row
 };
 
 hlq_status hlq_mx4_check(int64_t rows, int32_t K, Mx4Dims *out);
@@ -51,8 +48,8 @@ static inline Mx4View hlq_mx4_view(const Mx4Dims &d, const void *blob)
 }
 hlq_status hlq_mx4_launch_quantize(const Mx4Dims &d, const void *x, hlq_dtype t, int64_t ldx, void *blob, hipStream_t st);
 
-// byte of block b inside the eight bytes of its panel
-__host__ __device__ __forceinline__ int mx4_scale_byte(int b) { return (b & 1) * 4 + ((b & 7) >> 1); }
+// place of the scale byte of block b (0..3) of a panel
+__host__ __device__ __forceinline__ int mx4_scale_byte(int b) { return (b & 1) * 2 + (b >> 1); }
 
 static inline int hlq_dtype_bytes(hlq_dtype t) { return t == HLQ_F32 ? 4 : 2; }
 static inline bool hlq_is_float(int t) { return t == HLQ_F16 || t == HLQ_F32 || t == HLQ_BF16; }

@@ -2,9 +2,9 @@
 //
 //   block b of 32 k:  e = max(floor(log2(max |x|)) - 2, -127);  value = e2m1 nearest to x 2^-e (ties to the even code, at most 6)
 //
-// Quantizing reads a value once and writes 4.25 bits: it is bound by memory.  A wavefront takes a row's panel of 256 k at a
-// time per half: a lane has eight successive values (one 16-byte load of 16-bit types, two of fp32), four lanes a block, whose
-// largest magnitudes meet by two quad permutations; codes leave as a dword a lane, 128 contiguous bytes a panel.
+// Quantizing reads a value once and writes 4.25 bits: it is bound by memory.  A wavefront takes a panel of four rows: a lane has
+// eight successive values (one 16-byte load of 16-bit types, two of fp32), four lanes a block, whose largest magnitudes meet by
+// two quad permutations; codes leave as a dword a lane, 256 contiguous bytes.
 #include "hlq_mx4.h"
 
 namespace {
@@ -19,23 +19,22 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v)
     return o > v ? o : v;
 }
 
-// One wavefront: two panels of one row at a time, lanes 0..31 the first.
 template <int T, bool ALIGNED>
 __global__ void __launch_bounds__(64 * MX4_WAVES)
 hlq_mx4_quantize_kernel(const typename Mx4Type<T>::type *__restrict__ x, int64_t ldx, int64_t rows, int K, int panels,
-                        uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, int pairs, int64_t items)
+                        uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, int64_t items)
 {
-    const int lane = (int)(threadIdx.x & 63u);
+    const int lane = (int)(threadIdx.x & 63u), j = lane & 15;
     for (int64_t it = (int64_t)blockIdx.x * MX4_WAVES + (threadIdx.x >> 6); it < items; it += (int64_t)gridDim.x * MX4_WAVES) {
-        const int64_t row = it / pairs;
-        const int panel = 2 * (int)(it - row * pairs) + (lane >> 5);
-        if (panel >= panels) continue;
-        const int k = panel * MX4_PANEL_K + (lane & 31) * 8;
+        const int64_t quad = it / panels, row = quad * 4 + (lane >> 4);
+        const int panel = (int)(it - quad * panels), k = panel * MX4_PANEL_K + j * 8;
+        if (row >= rows) continue;
         typename Mx4Type<T>::type v[8];
         mx4_load8<ALIGNED>(x + row * ldx + k, K - k, v);
         const uint32_t byte = mx4_scale_of(quad_max(mx4_top_bits(v)));
-        *(uint32_t *)(codes + row * panels * 128 + panel * 128 + (lane & 31) * 4) = mx4_codes(v, byte);
-        if ((lane & 3) == 0) scales[((int64_t)panel * rows + row) * 8 + mx4_scale_byte((lane & 31) >> 2)] = (uint8_t)byte;
+        const int64_t at = panel * rows + row;
+        *(uint32_t *)(codes + at * 64 + j * 4) = mx4_codes(v, byte);
+        if ((lane & 3) == 0) scales[at * 4 + mx4_scale_byte(j >> 2)] = (uint8_t)byte;
     }
 }
 
@@ -51,13 +50,13 @@ __global__ void __launch_bounds__(256)
 hlq_mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t rows, int K, int panels,
                           typename Mx4Type<T>::type *__restrict__ y, int64_t ldy, int64_t items)
 {
-    const int eights = panels * 32;
+    const int eights = panels * 16;
     for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items; it += (int64_t)gridDim.x * 256) {
         const int64_t row = it / eights;
         const int j = (int)(it - row * eights), k = j * 8;
         if (k >= K) continue;
-        const uint32_t c = *(const uint32_t *)(codes + row * panels * 128 + j * 4);
-        const uint32_t byte = scales[((int64_t)(j >> 5) * rows + row) * 8 + mx4_scale_byte((j >> 2) & 7)];
+        const uint32_t c = *(const uint32_t *)(codes + ((int64_t)(j >> 4) * rows + row) * 64 + (j & 15) * 4);
+        const uint32_t byte = scales[((int64_t)(j >> 4) * rows + row) * 4 + mx4_scale_byte((j >> 2) & 3)];
         typename Mx4Type<T>::type *p = y + row * ldy + k;
         for (int i = 0; i < 8 && k + i < K; ++i) {
             const float v = byte == 255u ? __builtin_nanf("") : ldexpf(code_value(c >> (4 * i)), (int)byte - 127);
@@ -71,7 +70,7 @@ __global__ void __launch_bounds__(256)
 hlq_mx4_pack_kernel(const uint8_t *__restrict__ in, int64_t ldc, const uint8_t *__restrict__ in_scales, int64_t lds, int64_t rows, int K, int panels,
                     uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, int64_t items)
 {
-    const int eights = panels * 32, bytes = (K + 1) / 2, blocks = (K + 31) / 32;
+    const int eights = panels * 16, bytes = (K + 1) / 2, blocks = (K + 31) / 32;
     for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items; it += (int64_t)gridDim.x * 256) {
         const int64_t row = it / eights;
         const int j = (int)(it - row * eights);
@@ -82,9 +81,9 @@ hlq_mx4_pack_kernel(const uint8_t *__restrict__ in, int64_t ldc, const uint8_t *
             if (2 * at + 1 >= K) b &= 15u;
             c |= b << (8 * i);
         }
-        *(uint32_t *)(codes + row * panels * 128 + j * 4) = c;
+        *(uint32_t *)(codes + ((int64_t)(j >> 4) * rows + row) * 64 + (j & 15) * 4) = c;
         if ((j & 3) == 0)
-            scales[((int64_t)(j >> 5) * rows + row) * 8 + mx4_scale_byte((j >> 2) & 7)] = (j >> 2) < blocks ? in_scales[row * lds + (j >> 2)] : (uint8_t)0;
+            scales[((int64_t)(j >> 4) * rows + row) * 4 + mx4_scale_byte((j >> 2) & 3)] = (j >> 2) < blocks ? in_scales[row * lds + (j >> 2)] : (uint8_t)0;
     }
 }
 
@@ -92,16 +91,16 @@ __global__ void __launch_bounds__(256)
 hlq_mx4_unpack_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t rows, int K, int panels,
                       uint8_t *__restrict__ out, uint8_t *__restrict__ out_scales, int64_t items)
 {
-    const int eights = panels * 32, bytes = (K + 1) / 2, blocks = (K + 31) / 32;
+    const int eights = panels * 16, bytes = (K + 1) / 2, blocks = (K + 31) / 32;
     for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items; it += (int64_t)gridDim.x * 256) {
         const int64_t row = it / eights;
         const int j = (int)(it - row * eights);
         if (out) {
-            const uint32_t c = *(const uint32_t *)(codes + row * panels * 128 + j * 4);
+            const uint32_t c = *(const uint32_t *)(codes + ((int64_t)(j >> 4) * rows + row) * 64 + (j & 15) * 4);
             for (int i = 0; i < 4 && 4 * j + i < bytes; ++i) out[row * bytes + 4 * j + i] = (uint8_t)(c >> (8 * i));
         }
         if (out_scales && (j & 3) == 0 && (j >> 2) < blocks)
-            out_scales[row * blocks + (j >> 2)] = scales[((int64_t)(j >> 5) * rows + row) * 8 + mx4_scale_byte((j >> 2) & 7)];
+            out_scales[row * blocks + (j >> 2)] = scales[((int64_t)(j >> 4) * rows + row) * 4 + mx4_scale_byte((j >> 2) & 3)];
     }
 }
 
@@ -115,20 +114,19 @@ template <int T>
 void launch_quantize(const Mx4Dims &d, const void *x, int64_t ldx, void *blob, hipStream_t st)
 {
     using V = typename Mx4Type<T>::type;
-    const int pairs = (d.panels + 1) / 2;
-    const int64_t items = d.rows * pairs;
+    const int64_t items = (d.rows + 3) / 4 * d.panels;
     uint8_t *codes = (uint8_t *)blob, *scales = codes + d.code_bytes;
     const bool aligned = ((uintptr_t)x & 15u) == 0 && (d.rows == 1 || (ldx * (int64_t)sizeof(V)) % 16 == 0);
     const dim3 grid(grid_of(items, MX4_WAVES)), block(64 * MX4_WAVES);
-    if (aligned) hlq_mx4_quantize_kernel<T, true><<<grid, block, 0, st>>>((const V *)x, ldx, d.rows, d.K, d.panels, codes, scales, pairs, items);
-    else hlq_mx4_quantize_kernel<T, false><<<grid, block, 0, st>>>((const V *)x, ldx, d.rows, d.K, d.panels, codes, scales, pairs, items);
+    if (aligned) hlq_mx4_quantize_kernel<T, true><<<grid, block, 0, st>>>((const V *)x, ldx, d.rows, d.K, d.panels, codes, scales, items);
+    else hlq_mx4_quantize_kernel<T, false><<<grid, block, 0, st>>>((const V *)x, ldx, d.rows, d.K, d.panels, codes, scales, items);
 }
 
 template <int T>
 void launch_dequantize(const Mx4Dims &d, const void *blob, void *y, int64_t ldy, hipStream_t st)
 {
     using V = typename Mx4Type<T>::type;
-    const int64_t items = d.rows * d.panels * 32;
+    const int64_t items = d.rows * d.panels * 16;
     hlq_mx4_dequantize_kernel<T><<<grid_of(items, 256), 256, 0, st>>>((const uint8_t *)blob, (const uint8_t *)blob + d.code_bytes, d.rows, d.K, d.panels, (V *)y, ldy, items);
 }
 
@@ -153,8 +151,8 @@ hlq_status hlq_mx4_check(int64_t rows, int32_t K, Mx4Dims *out)
     d.rows = rows;
     d.K = K;
     d.panels = (K + MX4_PANEL_K - 1) / MX4_PANEL_K;
-    d.code_bytes = (size_t)rows * (size_t)d.row_bytes();
-    d.total = d.code_bytes + (size_t)rows * (size_t)d.panels * 8u;
+    d.code_bytes = (size_t)rows * (size_t)d.panels * 64u;
+    d.total = d.code_bytes + (size_t)rows * (size_t)d.panels * 4u;
     *out = d;
     return HLQ_OK;
 }
@@ -218,7 +216,7 @@ hlq_status hlq_mx4_pack(int64_t rows, int32_t K, const uint8_t *codes, int64_t l
     if (!codes || !scales) return HLQ_ERR_NULL;
     if (rows > 1 && (ldc < (K + 1) / 2 || lds < (K + 31) / 32)) return HLQ_ERR_BAD_STRIDE;
     hlq_clear_stale_error();
-    const int64_t items = rows * d.panels * 32;
+    const int64_t items = rows * d.panels * 16;
     hlq_mx4_pack_kernel<<<grid_of(items, 256), 256, 0, (hipStream_t)stream>>>(codes, ldc, scales, lds, rows, K, d.panels, (uint8_t *)blob, (uint8_t *)blob + d.code_bytes, items);
     return hlq_hip_status(hipGetLastError());
 }
@@ -230,7 +228,7 @@ hlq_status hlq_mx4_unpack(int64_t rows, int32_t K, const void *blob, uint8_t *co
     if (s != HLQ_OK || rows == 0) return s;
     if (!codes && !scales) return HLQ_OK;
     hlq_clear_stale_error();
-    const int64_t items = rows * d.panels * 32;
+    const int64_t items = rows * d.panels * 16;
     hlq_mx4_unpack_kernel<<<grid_of(items, 256), 256, 0, (hipStream_t)stream>>>((const uint8_t *)blob, (const uint8_t *)blob + d.code_bytes, rows, K, d.panels, codes, scales, items);
     return hlq_hip_status(hipGetLastError());
 }

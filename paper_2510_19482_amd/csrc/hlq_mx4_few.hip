@@ -10,44 +10,35 @@
 
 namespace {
 
-template <int XT>
-struct Operand {   // one lane's share of a panel: blocks l / 16 and 4 + l / 16 of row l % 16
-    mx4_int4 code[2];
-    int scale;      // bytes 0 and 2
+struct Operand {   // one lane's share of a panel: block l / 16 of row l % 16
+    mx4_int4 code;
+    int scale;      // byte 0
 
     __device__ __forceinline__ void none()
     {
-        code[0] = code[1] = (mx4_int4){0, 0, 0, 0};
-        scale = 0x7f7f7f7f;
+        code = (mx4_int4){0, 0, 0, 0};
+        scale = 127;
     }
-    __device__ __forceinline__ void load(const uint8_t *codes, const uint8_t *scales, int g)
+    __device__ __forceinline__ void load(const Mx4View &m, int64_t at, int g)
     {
-        code[0] = *(const mx4_int4 *)(codes + g * 16);
-        code[1] = *(const mx4_int4 *)(codes + 64 + g * 16);
-        scale = (int)(*(const uint32_t *)(scales + (g & 1) * 4) >> (8 * (g >> 1)));
+        code = *(const mx4_int4 *)(m.codes + at * 64 + g * 16);
+        scale = m.scales[at * 4 + mx4_scale_byte(g)];
     }
     template <class T>
-    __device__ __forceinline__ void quantize(const T *p, int left, int g, bool aligned)
+    __device__ __forceinline__ void quantize(const T *p, int left, bool aligned)
     {
-        uint32_t bytes = 0;
+        T v[4][8];
+        uint32_t top = 0;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int k = s * 128 + g * 32;
-            T v[4][8];
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (aligned) mx4_load8<true>(p + k + 8 * i, left - k - 8 * i, v[i]);
-                else mx4_load8<false>(p + k + 8 * i, left - k - 8 * i, v[i]);
-                const uint32_t t = mx4_top_bits(v[i]);
-                top = t > top ? t : top;
-            }
-            const uint32_t byte = mx4_scale_of(top);
-            bytes |= byte << (16 * s);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) code[s][i] = (int)mx4_codes(v[i], byte);
+        for (int i = 0; i < 4; ++i) {
+            if (aligned) mx4_load8<true>(p + 8 * i, left - 8 * i, v[i]);
+            else mx4_load8<false>(p + 8 * i, left - 8 * i, v[i]);
+            const uint32_t t = mx4_top_bits(v[i]);
+            top = t > top ? t : top;
         }
-        scale = (int)bytes;
+        scale = (int)mx4_scale_of(top);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) code[i] = (int)mx4_codes(v[i], (uint32_t)scale);
     }
 };
 
@@ -73,21 +64,18 @@ hlq_mx4_few_kernel(const Mx4Product a, int groups, int64_t items)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[t] = (mx4_float4){0.f, 0.f, 0.f, 0.f};
         for (int p = wave; p < a.panels; p += waves) {
-            Operand<XT> w[NT], x;
+            Operand w[NT], x;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) w[t].load(a.W, p * a.W.rows + wr[t], g);
+            if (xr < 0) x.none();
+            else if constexpr (XT == HLQ_MX4) x.load(a.A, p * a.A.rows + xr, g);
+            else {
+                const int k = p * MX4_PANEL_K + g * 32;
+                x.quantize((const typename Mx4Type<XT>::type *)a.x + xr * a.ldx + k, a.K - k, a.x_aligned);
+            }
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-                w[t].load(a.W.codes + (wr[t] * a.panels + p) * 128, a.W.scales + (p * a.W.rows + wr[t]) * 8, g);
-            if (xr < 0) x.none();
-            else if constexpr (XT == HLQ_MX4) x.load(a.A.codes + ((int64_t)xr * a.panels + p) * 128, a.A.scales + (p * a.A.rows + xr) * 8, g);
-            else {
-                using V = typename Mx4Type<XT>::type;
-                x.quantize((const V *)a.x + xr * a.ldx + p * MX4_PANEL_K, a.K - p * MX4_PANEL_K, g, a.x_aligned);
-            }
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(w[t].code[0]), wide(x.code[0]), acc[t], MX4_FP4, MX4_FP4, 0, w[t].scale, 0, x.scale);
-                acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(w[t].code[1]), wide(x.code[1]), acc[t], MX4_FP4, MX4_FP4, 2, w[t].scale, 2, x.scale);
-            }
+                acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(w[t].code), wide(x.code), acc[t], MX4_FP4, MX4_FP4, 0, w[t].scale, 0, x.scale);
         }
         // lane: results of row lane % 16, columns n0 + 4 (lane / 16) ..
 #pragma unroll

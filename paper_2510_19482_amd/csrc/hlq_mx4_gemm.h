@@ -17,7 +17,7 @@ struct Mx4Product {
     void *y;
     int ytype;
     int64_t ldy;
-    bool y_aligned;         // four successive results start where one store can write them
+    bool y_aligned;         // rows of the result start at 16 bytes
 };
 
 // Row tile number `tile` of tiles of BM rows that begin anew at each expert.  Every lane of the wavefront takes part and gets
@@ -80,3 +80,11 @@ __device__ __forceinline__ int mx4_x_row(const Mx4Product &a, int r)
 }
 
 hlq_status hlq_mx4_launch_few(const Mx4Product &a, int xtype, bool gated, hipStream_t st);
+
+// How a launch of the tiled kernel is cut: col_tiles x row_tiles x splits workgroups, a split `share` panels of K.  Partial
+// sums lie behind the counters in the workspace.
+struct Mx4TilePlan {
+    int BM, BN, col_tiles, row_tiles, splits, share;
+    size_t partial_at, partial_bytes;
+};
+hlq_status hlq_mx4_launch_tile(const Mx4Product &a, const Mx4TilePlan &p, bool gated, void *ws, hipStream_t st);

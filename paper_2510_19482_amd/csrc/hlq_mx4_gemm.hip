@@ -5,12 +5,51 @@ namespace {
 
 // rows up to which the kernel for few rows quantizes activations by itself
 constexpr int64_t QUANTIZE_INSIDE = 16;
+// rows of an expert (on average) up to which the kernel for few rows takes the product; only it can quantize inside
+constexpr int FEW_ROWS = 16;
 
-size_t workspace_need(int64_t x_rows, int32_t K)
+size_t up256(size_t n) { return (n + 255u) & ~(size_t)255u; }
+
+// Launch of the tiled kernel for R rows of E experts, `width` rows of W each.
+Mx4TilePlan tile_plan(int64_t width, int panels, int32_t E, int64_t R)
+{
+    Mx4TilePlan p{};
+    const int64_t each = (R + E - 1) / E;   // rows of an expert, on average
+    const int64_t wide = mx4_row_tiles(R, E, 128) * ((width + 255) / 256);
+    p.BM = each > 64 ? 128 : each > 32 ? 64 : 32;
+    p.BN = p.BM == 128 && wide >= 512 ? 256 : 128;
+    p.col_tiles = (int)((width + p.BN - 1) / p.BN);
+    p.row_tiles = (int)mx4_row_tiles(R, E, p.BM);
+    const int64_t tiles = (int64_t)p.col_tiles * p.row_tiles, room = 512;
+    p.splits = 1;
+    p.share = panels;
+    if (tiles > 0 && tiles * 2 <= room) {
+        int splits = (int)(room / tiles);
+        if (splits > panels / 4) splits = panels / 4;
+        if (splits > 16) splits = 16;
+        if (splits > 1) {
+            p.share = (panels + splits - 1) / splits;
+            p.splits = (panels + p.share - 1) / p.share;
+        }
+    }
+    if (p.splits > 1) p.partial_bytes = (size_t)tiles * (size_t)p.splits * (size_t)p.BM * (size_t)p.BN * 4u;
+    return p;
+}
+
+// rows of W that tiles of BN rows go over: gated halves are cut into 32 columns each
+int64_t tiled_width(int64_t N, bool gated) { return gated ? (N / 2 + 31) / 32 * 64 : N; }
+
+// counters, quantized activations, partial sums
+size_t workspace_need(int64_t N, int32_t K, int32_t E, int64_t x_rows, int64_t R)
 {
     Mx4Dims d;
     if (hlq_mx4_check(x_rows, K, &d) != HLQ_OK) return 0;
-    return (HLQ_WS_COUNTER_BYTES + d.total + 255u) & ~(size_t)255u;
+    size_t part = 0;
+    for (int gated = 0; gated < 2; ++gated) {
+        const size_t n = R ? tile_plan(tiled_width(N, gated), d.panels, E, R).partial_bytes : 0;
+        if (n > part) part = n;
+    }
+    return HLQ_WS_COUNTER_BYTES + up256(d.total) + up256(part);
 }
 
 struct Call {
@@ -66,17 +105,18 @@ hlq_status product(const Call &c, int32_t E, const int32_t *offsets, const int32
     a.y = c.Y;
     a.ytype = c.ytype;
     a.ldy = c.ldy;
-    a.y_aligned = (uintptr_t)c.Y % (4u * (unsigned)hlq_dtype_bytes(c.ytype)) == 0 && (R == 1 || c.ldy % 4 == 0);
+    a.y_aligned = ((uintptr_t)c.Y & 15u) == 0 && (R == 1 || c.ldy * hlq_dtype_bytes(c.ytype) % 16 == 0);
     int xtype = c.xtype;
+    const bool few = R <= (int64_t)FEW_ROWS * E;
     hlq_clear_stale_error();
     if (xtype == HLQ_MX4) a.A = hlq_mx4_view(dx, c.X);
-    else if (R <= QUANTIZE_INSIDE) {
+    else if (few && R <= QUANTIZE_INSIDE) {
         a.x = c.X;
         a.ldx = c.ldx;
         a.x_aligned = ((uintptr_t)c.X & 15u) == 0 && (c.x_rows == 1 || c.ldx * hlq_dtype_bytes(c.xtype) % 16 == 0);
     } else {
         if (!c.ws) return HLQ_ERR_NULL;
-        if (c.ws_bytes < workspace_need(c.x_rows, c.K)) return HLQ_ERR_BUFFER_TOO_SMALL;
+        if (c.ws_bytes < workspace_need(c.N, c.K, E, c.x_rows, R)) return HLQ_ERR_BUFFER_TOO_SMALL;
         if ((uintptr_t)c.ws & 15u) return HLQ_ERR_BAD_STRIDE;
         void *blob = (char *)c.ws + HLQ_WS_COUNTER_BYTES;
         s = hlq_mx4_launch_quantize(dx, c.X, c.xtype, c.ldx, blob, c.stream);
@@ -84,7 +124,10 @@ hlq_status product(const Call &c, int32_t E, const int32_t *offsets, const int32
         a.A = hlq_mx4_view(dx, blob);
         xtype = HLQ_MX4;
     }
-    return hlq_mx4_launch_few(a, xtype, gated, c.stream);
+    if (few) return hlq_mx4_launch_few(a, xtype, gated, c.stream);
+    Mx4TilePlan p = tile_plan(tiled_width(c.N, gated), dw.panels, E, R);
+    p.partial_at = HLQ_WS_COUNTER_BYTES + up256(dx.total);
+    return hlq_mx4_launch_tile(a, p, gated, c.ws, c.stream);
 }
 
 }  // namespace
@@ -98,7 +141,7 @@ hlq_status hlq_mx4_workspace_bytes(int64_t N, int32_t K, int32_t experts, int64_
     hlq_status s = hlq_mx4_check(x_rows, K, &d);
     if (s != HLQ_OK) return s;
     if (!bytes) return HLQ_ERR_NULL;
-    *bytes = workspace_need(x_rows, K);
+    *bytes = workspace_need(N, K, experts, x_rows, rows);
     return HLQ_OK;
 }
 

@@ -25,9 +25,9 @@ def test_oracle_values_and_rounding():
 
 
 def test_bytes():
-    # 4.25 bits a value, rows padded to 256
+    # 4.25 bits a value, rows padded to 128
     assert B.mx4_bytes(10, 256) == 10 * (128 + 8)
-    assert B.mx4_bytes(10, 257) == 10 * 2 * (128 + 8)
+    assert B.mx4_bytes(10, 257) == 10 * 3 * (64 + 4)
     assert B.mx4_bytes(4096, 14336) == 4096 * 14336 * 17 // 32
     assert B.mx4_bytes(0, 5) == 0
     n = ctypes.c_size_t()
@@ -48,7 +48,7 @@ def test_quantize_refusals():
     assert q(2, 64, P + 1, 0, 64, P, BIG, None) == STRIDE
     assert q(2, 64, P + 2, 1, 64, P, BIG, None) == STRIDE
     assert q(2, 64, P, 0, 64, P + 8, BIG, None) == STRIDE
-    assert q(2, 64, P, 0, 64, P, 2 * 136 - 1, None) == SMALL
+    assert q(2, 64, P, 0, 64, P, 2 * 68 - 1, None) == SMALL
     assert q(-1, 64, P, 0, 64, P, BIG, None) == DESC
     assert q(0, 64, None, 0, 64, None, 0, None) == OK
     d = B.lib.hlq_mx4_dequantize
@@ -61,7 +61,7 @@ def test_quantize_refusals():
     assert B.lib.hlq_mx4_pack(2, 64, P, 32, None, 2, P, BIG, None) == NULL
     assert B.lib.hlq_mx4_pack(2, 64, P, 31, P, 2, P, BIG, None) == STRIDE
     assert B.lib.hlq_mx4_pack(2, 64, P, 32, P, 1, P, BIG, None) == STRIDE
-    assert B.lib.hlq_mx4_pack(2, 64, P, 32, P, 2, P, 2 * 136 - 1, None) == SMALL
+    assert B.lib.hlq_mx4_pack(2, 64, P, 32, P, 2, P, 2 * 68 - 1, None) == SMALL
     assert B.lib.hlq_mx4_unpack(2, 64, None, P, P, None) == NULL
     assert B.lib.hlq_mx4_unpack(2, 64, P, None, None, None) == OK
 
