@@ -366,23 +366,20 @@ HLQ_F16, HLQ_F32, HLQ_BF16, HLQ_MX4 = 0, 1, 2, 3
 _DTYPES = {torch.float16: HLQ_F16, torch.float32: HLQ_F32, torch.bfloat16: HLQ_BF16}
 
 
-def _dtype_of(t) -> int:
+def _matrix(t):
+    """(rows, columns, pointer, type, leading dimension) of a matrix whose rows are contiguous; one row's leading dimension is its length.
+    Called several times for an operator whose kernel takes a few microseconds: each attribute of a tensor costs a tenth of one."""
     try:
-        return _DTYPES[t.dtype]
+        dtype = _DTYPES[t.dtype]
     except KeyError:
         raise TypeError(f"expected a float16, bfloat16 or float32 tensor, got {t.dtype}") from None
-
-
-def _row_stride(t, columns: int) -> int:
-    """Leading dimension of a matrix; one row has none of its own."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    if t.dim() != 2:
+        raise ValueError(f"expected a matrix, got shape {tuple(t.shape)}")
+    rows, cols = t.shape
+    ld, one = t.stride()
+    if (one != 1 and cols > 1) or (rows > 1 and ld < cols):
         raise ValueError(f"expected a matrix whose rows are contiguous, got shape {tuple(t.shape)} with strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), columns)
-
-
-def _expect(t, shape, dtype, name: str) -> None:
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return rows, cols, t.data_ptr(), dtype, ld if rows > 1 else cols
 
 
 def mx4_bytes(rows: int, K: int) -> int:
@@ -409,12 +406,12 @@ def alloc_mx4(rows: int, K: int, device="cuda") -> Mx4:
 
 def hlq_mx4_quantize(x, out: Mx4 | None = None, stream=None) -> Mx4:
     """Rows of x [rows, K] (f16, bf16 or f32) in 4-bit floats, a power-of-two scale for each 32 of a row."""
-    rows, K = x.shape
+    rows, K, ptr, dtype, ld = _matrix(x)
     if out is None:
         out = alloc_mx4(rows, K, x.device)
     elif out.rows != rows or out.K != K:
         raise ValueError(f"the output is a matrix of {out.rows} x {out.K}, x is {rows} x {K}")
-    status = lib.hlq_mx4_quantize(rows, K, x.data_ptr(), _dtype_of(x), _row_stride(x, K), out._ptr, out._bytes, _stream_ptr(stream))
+    status = lib.hlq_mx4_quantize(rows, K, ptr, dtype, ld, out._ptr, out._bytes, _stream_ptr(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_quantize", status)
     return out
@@ -424,9 +421,10 @@ def hlq_mx4_dequantize(m: Mx4, y=None, dtype=None, stream=None):
     """The values [rows, K] that a matrix stands for, in y or a new tensor of `dtype` (f32 by default)."""
     if y is None:
         y = torch.empty((m.rows, m.K), dtype=dtype or torch.float32, device=m.blob.device)
-    elif tuple(y.shape) != (m.rows, m.K):
+    rows, K, ptr, dtype, ld = _matrix(y)
+    if rows != m.rows or K != m.K:
         raise ValueError(f"y has shape {tuple(y.shape)}, the matrix is {m.rows} x {m.K}")
-    status = lib.hlq_mx4_dequantize(m.rows, m.K, m._ptr, y.data_ptr(), _dtype_of(y), _row_stride(y, m.K), _stream_ptr(stream))
+    status = lib.hlq_mx4_dequantize(rows, K, m._ptr, ptr, dtype, ld, _stream_ptr(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_dequantize", status)
     return y
@@ -436,13 +434,13 @@ def hlq_mx4_pack(codes, scales, K: int, out: Mx4 | None = None, stream=None) -> 
     """codes u8 [rows, (K + 1) // 2 or more] (the even k in the low half of a byte), scales u8 [rows, (K + 31) // 32 or more] -> matrix."""
     rows = codes.shape[0]
     for name, t, least in (("codes", codes, (K + 1) // 2), ("scales", scales, (K + 31) // 32)):
-        if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < least:
-            raise ValueError(f"{name}: expected uint8 of shape ({rows}, at least {least}), got {t.dtype} {tuple(t.shape)}")
+        if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < least or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise ValueError(f"{name}: expected uint8 of shape ({rows}, at least {least}), rows contiguous, got {t.dtype} {tuple(t.shape)}")
     if out is None:
         out = alloc_mx4(rows, K, codes.device)
     elif out.rows != rows or out.K != K:
         raise ValueError(f"the output is a matrix of {out.rows} x {out.K}, not {rows} x {K}")
-    _check("hlq_mx4_pack", lib.hlq_mx4_pack(rows, K, _ptr(codes), _row_stride(codes, K), _ptr(scales), _row_stride(scales, K), out._ptr, out._bytes, _stream_ptr(stream)))
+    _check("hlq_mx4_pack", lib.hlq_mx4_pack(rows, K, _ptr(codes), codes.stride(0), _ptr(scales), scales.stride(0), out._ptr, out._bytes, _stream_ptr(stream)))
     return out
 
 
@@ -465,32 +463,30 @@ def alloc_mx4_workspace(W: Mx4, x_rows: int, rows: int | None = None, experts: i
                           W.blob.device, stream)
 
 
-def _product_args(W: Mx4, N: int, X, R: int, Y, gated: bool, out_dtype):
-    """(x pointer, type, ld), Y, (y pointer, type, ld), and the checks that a product's tensors need."""
-    if type(X) is Mx4:
-        x_rows, K, x = X.rows, X.K, (X._ptr, HLQ_MX4, 0)
-    else:
-        x_rows, K = X.shape
-        x = (X.data_ptr(), _dtype_of(X), _row_stride(X, K))
-    if K != W.K:
-        raise ValueError(f"X has {K} columns, the weights {W.K}")
-    cols = N // 2 if gated else N
-    if Y is None:
-        if out_dtype is None:
-            out_dtype = torch.float32 if type(X) is Mx4 else X.dtype
-        Y = torch.empty((R, cols), dtype=out_dtype, device=W.blob.device)
-    elif Y.shape[0] != R or Y.shape[1] != cols:
-        raise ValueError(f"Y has shape {tuple(Y.shape)}, the result is {R} x {cols}")
-    return x_rows, x, Y, (Y.data_ptr(), _dtype_of(Y), _row_stride(Y, cols))
+def _operand(X):
+    """(rows, columns, pointer, type, leading dimension) of a product's activations."""
+    return (X.rows, X.K, X._ptr, HLQ_MX4, 0) if type(X) is Mx4 else _matrix(X)
+
+
+def _product_out(W: Mx4, X, R: int, cols: int, out_dtype):
+    if out_dtype is None:
+        out_dtype = torch.float32 if type(X) is Mx4 else X.dtype
+    return torch.empty((R, cols), dtype=out_dtype, device=W.blob.device)
 
 
 def hlq_mx4_gemm(W: Mx4, X, Y=None, gated: bool = False, out_dtype=None, ws=None, stream=None):
     """Y = Q(X) W^T, or with `gated` silu of its first half of columns times the second; X [M, K] f16, bf16 or f32, or Mx4."""
-    M = X.rows if type(X) is Mx4 else X.shape[0]
-    _, x, Y, y = _product_args(W, W.rows, X, M, Y, gated, out_dtype)
+    M, K, x, xtype, ldx = _operand(X)
+    N = W.rows
+    cols = N // 2 if gated else N
+    if Y is None:
+        Y = _product_out(W, X, M, cols, out_dtype)
+    y_rows, y_cols, y, ytype, ldy = _matrix(Y)
+    if K != W.K or y_rows != M or y_cols != cols:
+        raise ValueError(f"X is {M} x {K}, W {N} x {W.K}, Y {y_rows} x {y_cols}{' (gated)' if gated else ''}")
     if ws is None:
         ws = alloc_mx4_workspace(W, M, stream=stream)
-    status = lib.hlq_mx4_gemm(W.rows, W.K, W._ptr, M, *x, *y, int(gated), ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+    status = lib.hlq_mx4_gemm(N, K, W._ptr, M, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0, ws.data_ptr(), ws.numel(), _stream_ptr(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_gemm", status)
     return Y
@@ -519,12 +515,12 @@ def alloc_route(T: int, E: int, k: int, device="cuda") -> Route:
 
 def hlq_route(logits, k: int, renorm: bool = True, out: Route | None = None, stream=None) -> Route:
     """The k experts of each token by its logits [T, E], their weights, and the tokens grouped by expert."""
-    T, E = logits.shape
+    T, E, ptr, dtype, ld = _matrix(logits)
     if out is None:
         out = Route(T, E, k, logits.device)
-    elif (out.T, out.E, out.k) != (T, E, k):
+    elif out.T != T or out.E != E or out.k != k:
         raise ValueError(f"the output is for {out.T} tokens, {out.E} experts, {out.k} each")
-    status = lib.hlq_route(T, E, k, logits.data_ptr(), _dtype_of(logits), _row_stride(logits, E), int(renorm), *out._args, _stream_ptr(stream))
+    status = lib.hlq_route(T, E, k, ptr, dtype, ld, 1 if renorm else 0, *out._args, _stream_ptr(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_route", status)
     return out
@@ -536,18 +532,24 @@ def hlq_expert_gemm(W: Mx4, offsets, X, Y=None, rows=None, gated: bool = False, 
     E = offsets.numel() - 1
     if E < 1 or W.rows % E or offsets.dtype != torch.int32 or not offsets.is_contiguous():
         raise ValueError(f"offsets: int32, one more than experts; {offsets.numel()} of {offsets.dtype} for {W.rows} rows of weights")
+    x_rows, K, x, xtype, ldx = _operand(X)
     if rows is None:
-        R, rows_ptr = X.rows if type(X) is Mx4 else X.shape[0], 0
+        R, rows_ptr = x_rows, None
     else:
         if rows.dtype != torch.int32 or not rows.is_contiguous():
             raise ValueError(f"rows: contiguous int32, got {rows.dtype}")
         R, rows_ptr = rows.numel(), rows.data_ptr()
     N = W.rows // E
-    x_rows, x, Y, y = _product_args(W, N, X, R, Y, gated, out_dtype)
+    cols = N // 2 if gated else N
+    if Y is None:
+        Y = _product_out(W, X, R, cols, out_dtype)
+    y_rows, y_cols, y, ytype, ldy = _matrix(Y)
+    if K != W.K or y_rows != R or y_cols != cols:
+        raise ValueError(f"X is {x_rows} x {K}, a matrix of W {N} x {W.K}, Y {y_rows} x {y_cols} for {R} rows{' (gated)' if gated else ''}")
     if ws is None:
         ws = alloc_mx4_workspace(W, x_rows, R, E, stream)
-    status = lib.hlq_expert_gemm(E, N, W.K, W._ptr, offsets.data_ptr(), rows_ptr, R, x_rows, *x, *y, int(gated), ws.data_ptr(), ws.numel(),
-                                 _stream_ptr(stream))
+    status = lib.hlq_expert_gemm(E, N, K, W._ptr, offsets.data_ptr(), rows_ptr, R, x_rows, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0,
+                                 ws.data_ptr(), ws.numel(), _stream_ptr(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_expert_gemm", status)
     return Y
@@ -556,15 +558,15 @@ def hlq_expert_gemm(W: Mx4, offsets, X, Y=None, rows=None, gated: bool = False, 
 def hlq_expert_combine(Y, slots, weights, out=None, out_dtype=None, stream=None):
     """out[t] = sum_i weights[t, i] Y[slots[t, i]] (slot -1: nothing)."""
     T, k = slots.shape
-    R, D = Y.shape
-    _expect(slots, (T, k), torch.int32, "slots")
-    _expect(weights, (T, k), torch.float32, "weights")
+    R, D, y, ytype, ldy = _matrix(Y)
+    if weights.shape != slots.shape or slots.dtype != torch.int32 or weights.dtype != torch.float32 or not (slots.is_contiguous() and weights.is_contiguous()):
+        raise ValueError(f"slots and weights: contiguous int32 and float32 of one shape, got {slots.dtype} {tuple(slots.shape)} and {weights.dtype} {tuple(weights.shape)}")
     if out is None:
         out = torch.empty((T, D), dtype=out_dtype or Y.dtype, device=Y.device)
-    elif tuple(out.shape) != (T, D):
+    o_rows, o_cols, o, otype, ldo = _matrix(out)
+    if o_rows != T or o_cols != D:
         raise ValueError(f"out has shape {tuple(out.shape)}, the result is {T} x {D}")
-    status = lib.hlq_expert_combine(T, k, D, R, Y.data_ptr(), _dtype_of(Y), _row_stride(Y, D), slots.data_ptr(), weights.data_ptr(),
-                                    out.data_ptr(), _dtype_of(out), _row_stride(out, D), _stream_ptr(stream))
+    status = lib.hlq_expert_combine(T, k, D, R, y, ytype, ldy, slots.data_ptr(), weights.data_ptr(), o, otype, ldo, _stream_ptr(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_expert_combine", status)
     return out

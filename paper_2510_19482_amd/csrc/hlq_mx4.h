@@ -99,6 +99,14 @@ __device__ __forceinline__ uint32_t mx4_scale_of(uint32_t top)
     const uint32_t e = top >> 23;
     return e == 255u ? 255u : e > 2u ? e - 2u : 0u;
 }
+// the largest of four neighbouring lanes
+__device__ __forceinline__ uint32_t mx4_quad_max(uint32_t v)
+{
+    uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true);   // lanes 1 0 3 2
+    v = o > v ? o : v;
+    o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true);            // lanes 2 3 0 1
+    return o > v ? o : v;
+}
 // Codes of eight values under a scale byte, the first in the lowest four bits: to nearest, ties to the even code, above 5 it
 // is 6.  The conversion takes the scale's exponent field, so 2^-127 (byte 0) is given as +0.  (All finite f16 and bf16 values
 // and f32 grids and ties against a 64-bit reference at scale bytes 0..252: no difference.)

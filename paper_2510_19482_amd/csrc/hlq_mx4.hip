@@ -11,14 +11,6 @@ namespace {
 
 constexpr int MX4_WAVES = 4;
 
-__device__ __forceinline__ uint32_t quad_max(uint32_t v)
-{
-    uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true);   // lanes 1 0 3 2
-    v = o > v ? o : v;
-    o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true);            // lanes 2 3 0 1
-    return o > v ? o : v;
-}
-
 template <int T, bool ALIGNED>
 __global__ void __launch_bounds__(64 * MX4_WAVES)
 hlq_mx4_quantize_kernel(const typename Mx4Type<T>::type *__restrict__ x, int64_t ldx, int64_t rows, int K, int panels,
@@ -31,7 +23,7 @@ hlq_mx4_quantize_kernel(const typename Mx4Type<T>::type *__restrict__ x, int64_t
         if (row >= rows) continue;
         typename Mx4Type<T>::type v[8];
         mx4_load8<ALIGNED>(x + row * ldx + k, K - k, v);
-        const uint32_t byte = mx4_scale_of(quad_max(mx4_top_bits(v)));
+        const uint32_t byte = mx4_scale_of(mx4_quad_max(mx4_top_bits(v)));
         const int64_t at = panel * rows + row;
         *(uint32_t *)(codes + at * 64 + j * 4) = mx4_codes(v, byte);
         if ((lane & 3) == 0) scales[at * 4 + mx4_scale_byte(j >> 2)] = (uint8_t)byte;

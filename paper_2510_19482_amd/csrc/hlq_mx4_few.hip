@@ -24,109 +24,171 @@ struct Operand {   // one lane's share of a panel: block l / 16 of row l % 16
         code = *(const mx4_int4 *)(m.codes + at * 64 + g * 16);
         scale = m.scales[at * 4 + mx4_scale_byte(g)];
     }
-    template <class T>
-    __device__ __forceinline__ void quantize(const T *p, int left, bool aligned)
-    {
-        T v[4][8];
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (aligned) mx4_load8<true>(p + 8 * i, left - 8 * i, v[i]);
-            else mx4_load8<false>(p + 8 * i, left - 8 * i, v[i]);
-            const uint32_t t = mx4_top_bits(v[i]);
-            top = t > top ? t : top;
-        }
-        scale = (int)mx4_scale_of(top);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) code[i] = (int)mx4_codes(v[i], (uint32_t)scale);
-    }
 };
+
+// Rows of x in the form that the matrix core takes, in LDS: codes [panel][row][64], scales [panel][row][4], for the n rows of a tile.
+template <class T>
+__device__ __forceinline__ void quantize_rows(const Mx4Product &a, const Mx4RowTile &tile, uint8_t *codes, uint8_t *scales)
+{
+    const int eights = a.panels * 16, lane = (int)(threadIdx.x & 63u);
+    for (int i = (int)threadIdx.x; i < tile.n * eights; i += (int)blockDim.x) {
+        const int m = i / eights, j = i - m * eights, k = j * 8, at = (j >> 4) * tile.n + m;
+        const T *p = (const T *)a.x + mx4_x_row(a, tile.row0 + m) * a.ldx + k;
+        T v[8];
+        if (a.x_aligned) mx4_load8<true>(p, a.K - k, v);
+        else mx4_load8<false>(p, a.K - k, v);
+        const uint32_t byte = mx4_scale_of(mx4_quad_max(mx4_top_bits(v)));
+        *(uint32_t *)(codes + at * 64 + (j & 15) * 4) = mx4_codes(v, byte);
+        if ((lane & 3) == 0) scales[at * 4 + mx4_scale_byte((j >> 2) & 3)] = (uint8_t)byte;
+    }
+}
 
 __device__ __forceinline__ mx4_int8 wide(mx4_int4 v) { return (mx4_int8){v.x, v.y, v.z, v.w, 0, 0, 0, 0}; }
 
-template <int XT, bool GATED>
-__global__ void __launch_bounds__(1024)
-hlq_mx4_few_kernel(const Mx4Product a, int groups, int64_t items)
+constexpr int few_ahead(int MT, int CT) { return MT * CT >= 4 ? 2 : 4; }   // panels requested at a time
+constexpr int few_waves(int MT, int CT) { return MT * CT >= 4 ? 8 : 16; }   // of a workgroup, at most
+
+// MT blocks of 16 rows, CT blocks of 16 columns a wavefront.  K is cut over the `share` wavefronts that have the same columns; a
+// workgroup has blockDim / 64 / share such groups.
+template <int XT, bool GATED, int MT, int CT>
+__global__ void __launch_bounds__(64 * few_waves(MT, CT))
+hlq_mx4_few_kernel(const Mx4Product a, int groups, int share)
 {
-    constexpr int NT = GATED ? 2 : 1;
-    extern __shared__ float sums[];   // [wave][NT][4][64]
-    const int lane = (int)(threadIdx.x & 63u), wave = (int)(threadIdx.x >> 6), waves = (int)(blockDim.x >> 6);
-    const int r = lane & 15, g = lane >> 4;
-    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-        const Mx4RowTile tile = mx4_row_tile<16>(a, (int)(it / groups));
-        if (tile.n == 0) break;   // the later ones are no less past the end
-        const int n0 = (int)(it % groups) * 16;
-        const int xr = r < tile.n ? mx4_x_row(a, tile.row0 + r) : -1;
-        int64_t wr[NT];
+    constexpr int NT = GATED ? 2 * CT : CT, AHEAD = few_ahead(MT, CT);   // blocks of W: gated ones in pairs
+    constexpr bool INSIDE = XT != HLQ_MX4;   // x is quantized here
+    static_assert(!INSIDE || MT == 1, "");
+    extern __shared__ __attribute__((aligned(16))) float sums[];   // [wavefront][MT][NT][4][64], then x
+    const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int r = lane & 15, g = lane >> 4, per = (int)(blockDim.x >> 6) / share;
+    const Mx4RowTile tile = mx4_row_tile<16 * MT>(a, (int)blockIdx.x / groups);
+    if (tile.n == 0) return;
+    const int col = ((int)blockIdx.x % groups * per + wave / share) * 16 * CT, part = wave % share;
+    const bool mine = col < a.cols;   // the last workgroup may have more wavefronts than columns
+    int64_t wr[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) wr[t] = (int64_t)tile.e * a.N + t * a.cols + (n0 + r < a.cols ? n0 + r : a.cols - 1);
-        mx4_float4 acc[NT];
+    for (int t = 0; t < NT; ++t) {
+        const int c = col + (GATED ? t >> 1 : t) * 16 + r;
+        wr[t] = (int64_t)tile.e * a.N + (GATED && (t & 1) ? a.cols : 0) + (c < a.cols ? c : a.cols - 1);
+    }
+    Operand w[AHEAD][NT];
+    auto load_w = [&](int p0) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) acc[t] = (mx4_float4){0.f, 0.f, 0.f, 0.f};
-        for (int p = wave; p < a.panels; p += waves) {
-            Operand w[NT], x;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) w[t].load(a.W, p * a.W.rows + wr[t], g);
-            if (xr < 0) x.none();
-            else if constexpr (XT == HLQ_MX4) x.load(a.A, p * a.A.rows + xr, g);
-            else {
-                const int k = p * MX4_PANEL_K + g * 32;
-                x.quantize((const typename Mx4Type<XT>::type *)a.x + xr * a.ldx + k, a.K - k, a.x_aligned);
-            }
+        for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-                acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(w[t].code), wide(x.code), acc[t], MX4_FP4, MX4_FP4, 0, w[t].scale, 0, x.scale);
-        }
-        // lane: results of row lane % 16, columns n0 + 4 (lane / 16) ..
+                if (p0 + u * share < a.panels) w[u][t].load(a.W, (p0 + u * share) * a.W.rows + wr[t], g);
+                else w[u][t].none();
+    };
+    load_w(part);
+    Mx4View X = a.A;
+    if constexpr (INSIDE) {
+        // while the first weights come
+        uint8_t *codes = (uint8_t *)(sums + (share > 1 ? (int)(blockDim.x >> 6) * NT * 256 : 0)), *scales = codes + tile.n * a.panels * 64;
+        quantize_rows<typename Mx4Type<XT>::type>(a, tile, codes, scales);
+        X = Mx4View{codes, scales, tile.n};
+        __syncthreads();
+    }
+    int xr[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) xr[m] = m * 16 + r >= tile.n ? -1 : INSIDE ? r : mx4_x_row(a, tile.row0 + m * 16 + r);
+    mx4_float4 acc[MT][NT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[m][t] = (mx4_float4){0.f, 0.f, 0.f, 0.f};
+    for (int p0 = part; p0 < a.panels; p0 += share * AHEAD) {
+        if (p0 > part) load_w(p0);
+        Operand x[AHEAD][MT];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+                if (p0 + u * share < a.panels && xr[m] >= 0) x[u][m].load(X, (p0 + u * share) * X.rows + xr[m], g);
+                else x[u][m].none();
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    acc[m][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(w[u][t].code), wide(x[u][m].code), acc[m][t], MX4_FP4, MX4_FP4, 0,
+                                                                             w[u][t].scale, 0, x[u][m].scale);
+    }
+    // a lane has results of row lane % 16, columns 4 (lane / 16) .. of each block; the wavefronts of a group add them up block by block
+    auto leave = [&](int m, int ct, const mx4_float4 &p, const mx4_float4 &up) {
+        const int c = col + ct * 16 + 4 * g, left = a.cols - c;
+        if (m * 16 + r >= tile.n || left <= 0) return;
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = GATED ? mx4_gate(p[i], up[i]) : p[i];
+        mx4_store(a.y, a.ytype, (int64_t)(tile.row0 + m * 16 + r) * a.ldy + c, v, left < 4 ? left : 4, left >= 4 && a.y_aligned);
+    };
+    if (share == 1) {
+        if (mine)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) leave(m, c, acc[m][GATED ? 2 * c : c], acc[m][GATED ? 2 * c + 1 : c]);
+        return;
+    }
+    float *const group = sums + (wave - part) * (MT * NT * 256);
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sums[((wave * NT + t) * 4 + i) * 64 + lane] = acc[t][i];
-        __syncthreads();
-        if (wave == 0 && r < tile.n && n0 + 4 * g < a.cols) {
-            float v[4];
+            for (int i = 0; i < 4; ++i) group[((part * MT + m) * NT + t) * 256 + i * 64 + lane] = acc[m][t][i];
+    __syncthreads();
+    if (!mine) return;
+    for (int b = part; b < MT * CT; b += share) {
+        const int m = b / CT, c = b % CT;
+        mx4_float4 s[2];
+#pragma unroll
+        for (int t = 0; t < (GATED ? 2 : 1); ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float s[NT];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    s[t] = 0.f;
-                    for (int o = 0; o < waves; ++o) s[t] += sums[((o * NT + t) * 4 + i) * 64 + lane];
-                }
-                v[i] = GATED ? mx4_gate(s[0], s[NT - 1]) : s[0];
+                float sum = 0.f;
+                for (int o = 0; o < share; ++o) sum += group[((o * MT + m) * NT + (GATED ? 2 * c + t : c)) * 256 + i * 64 + lane];
+                s[t][i] = sum;
             }
-            const int left = a.cols - n0 - 4 * g;
-            mx4_store(a.y, a.ytype, (int64_t)(tile.row0 + r) * a.ldy + n0 + 4 * g, v, left < 4 ? left : 4, left >= 4 && a.y_aligned);
-        }
-        __syncthreads();
+        leave(m, c, s[0], s[GATED ? 1 : 0]);
     }
 }
 
-template <int XT, bool GATED>
-void launch(const Mx4Product &a, hipStream_t st)
+template <int XT, bool GATED, int MT, int CT>
+hlq_status launch(const Mx4Product &a, hipStream_t st)
 {
-    int waves = 1;
-    while (waves < 16 && waves < a.panels) waves *= 2;
-    const int groups = (a.cols + 15) / 16;
-    const int64_t items = mx4_row_tiles(a.R, a.offsets ? a.E : 1, 16) * groups;
-    const unsigned grid = (unsigned)(items < (1 << 20) ? items : (1 << 20));
-    hlq_mx4_few_kernel<XT, GATED><<<grid, 64 * waves, (size_t)waves * (GATED ? 2 : 1) * 1024, st>>>(a, groups, items);
+    const int col_tiles = (a.cols + 16 * CT - 1) / (16 * CT);
+    const int64_t row_tiles = mx4_row_tiles(a.R, a.offsets ? a.E : 1, 16 * MT);
+    constexpr int MOST = few_waves(MT, CT);
+    // wavefronts that share a column tile: about MOST wavefronts a compute unit in all, AHEAD panels or more each
+    int share = 1;
+    while (share < MOST && row_tiles * col_tiles * share < 256 * MOST && share * few_ahead(MT, CT) < a.panels) share *= 2;
+    // x quantized inside: by fewer workgroups of more wavefronts
+    int waves = XT == HLQ_MX4 ? 4 : MOST;
+    if (waves < share) waves = share;
+    const int per = waves / share, groups = (col_tiles + per - 1) / per;
+    if (row_tiles * groups > INT32_MAX / 1024) return HLQ_ERR_UNSUPPORTED;
+    size_t lds = share > 1 ? (size_t)waves * MT * CT * (GATED ? 2 : 1) * 1024 : 0;
+    if (XT != HLQ_MX4) lds += (size_t)(a.R < 16 ? a.R : 16) * a.panels * 68;
+    hlq_mx4_few_kernel<XT, GATED, MT, CT><<<(unsigned)(row_tiles * groups), 64 * waves, lds, st>>>(a, groups, share);
+    return hlq_hip_status(hipGetLastError());
 }
 
-template <int XT>
-void launch(const Mx4Product &a, bool gated, hipStream_t st)
+template <int XT, int MT, int CT>
+hlq_status launch(const Mx4Product &a, bool gated, hipStream_t st)
 {
-    if (gated) launch<XT, true>(a, st);
-    else launch<XT, false>(a, st);
+    return gated ? launch<XT, true, MT, CT>(a, st) : launch<XT, false, MT, CT>(a, st);
 }
 
 }  // namespace
 
-hlq_status hlq_mx4_launch_few(const Mx4Product &a, int xtype, bool gated, hipStream_t st)
+hlq_status hlq_mx4_launch_few(const Mx4Product &a, int xtype, bool gated, int row_blocks, int col_blocks, hipStream_t st)
 {
-    if (xtype == HLQ_F16) launch<HLQ_F16>(a, gated, st);
-    else if (xtype == HLQ_BF16) launch<HLQ_BF16>(a, gated, st);
-    else if (xtype == HLQ_F32) launch<HLQ_F32>(a, gated, st);
-    else launch<HLQ_MX4>(a, gated, st);
-    return hlq_hip_status(hipGetLastError());
+    if (xtype == HLQ_F16) return launch<HLQ_F16, 1, 1>(a, gated, st);
+    if (xtype == HLQ_BF16) return launch<HLQ_BF16, 1, 1>(a, gated, st);
+    if (xtype == HLQ_F32) return launch<HLQ_F32, 1, 1>(a, gated, st);
+    if (row_blocks == 1) return launch<HLQ_MX4, 1, 1>(a, gated, st);
+    if (row_blocks == 4) return launch<HLQ_MX4, 4, 2>(a, gated, st);
+    return col_blocks == 1 ? launch<HLQ_MX4, 2, 1>(a, gated, st) : launch<HLQ_MX4, 2, 2>(a, gated, st);
 }

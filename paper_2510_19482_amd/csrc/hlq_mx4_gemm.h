@@ -79,7 +79,8 @@ __device__ __forceinline__ int mx4_x_row(const Mx4Product &a, int r)
     return i < 0 ? 0 : i >= a.x_rows ? a.x_rows - 1 : i;
 }
 
-hlq_status hlq_mx4_launch_few(const Mx4Product &a, int xtype, bool gated, hipStream_t st);
+// a wavefront has row_blocks x col_blocks blocks of 16 x 16: 1 x 1, 2 x 1, 2 x 2 or 4 x 2 (1 x 1 if x is quantized inside)
+hlq_status hlq_mx4_launch_few(const Mx4Product &a, int xtype, bool gated, int row_blocks, int col_blocks, hipStream_t st);
 
 // How a launch of the tiled kernel is cut: col_tiles x row_tiles x splits workgroups, a split `share` panels of K.  Partial
 // sums lie behind the counters in the workspace.

@@ -3,53 +3,84 @@
 
 namespace {
 
-// rows up to which the kernel for few rows quantizes activations by itself
-constexpr int64_t QUANTIZE_INSIDE = 16;
-// rows of an expert (on average) up to which the kernel for few rows takes the product; only it can quantize inside
-constexpr int FEW_ROWS = 16;
+// The kernel for few rows quantizes activations by itself where that is little work for each of its workgroups: rows of an
+// expert (on average) times K up to QUANTIZE_INSIDE, and what 16 rows take of LDS.
+constexpr int64_t QUANTIZE_INSIDE = 16384, QUANTIZED_BYTES = 65536;
 
 size_t up256(size_t n) { return (n + 255u) & ~(size_t)255u; }
 
-// Launch of the tiled kernel for R rows of E experts, `width` rows of W each.
-Mx4TilePlan tile_plan(int64_t width, int panels, int32_t E, int64_t R)
+// Which kernel takes a product, by an estimate of its time (us) from measurements of its parts; mx4_few: rows and columns a
+// wavefront, mx4_tile: of a workgroup.
+//
+// Few rows: a start of 2.5, then what a compute unit loads of the panels of its workgroups' rows and columns, or the weights as they
+// come from memory.  Tiled: a start of 3.5, then a stage a panel, `alone` where a compute unit has one workgroup, `shared` per
+// workgroup where it has more, or the weights at 5.2 TB/s.  Cutting K adds the hand-over of the partial sums: 2, and 2 for each 32
+// rows a wavefront has and four splits.
+// Measured / estimated, N x K = 4096 x 4096: 32 rows 5.1 / 5.0 (2 x 1), 128 rows 7.3 / 8.4 (4 x 2), 256 rows 9.5 / 9.3 (32 x 128), 1024 rows
+// 15.2 / 13.1 (128 x 128); 28672 x 4096: 64 rows 13.0 / 15.5 (32 x 128); 4096 x 14336: 32 rows 10.3 / 11.1 (2 x 1), 128 rows
+// 15.2 / 15.6 (32 x 128, K in four).
+constexpr int MOST_SPLITS = 8, LEAST_SHARE = 4, MOST_CUT = 512;   // of K, panels of one, workgroups of a product whose K is cut
+
+struct Choice {
+    int row_blocks, col_blocks;   // few rows, if row_blocks > 0
+    Mx4TilePlan tile;
+};
+
+Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
 {
-    Mx4TilePlan p{};
-    const int64_t each = (R + E - 1) / E;   // rows of an expert, on average
-    const int64_t wide = mx4_row_tiles(R, E, 128) * ((width + 255) / 256);
-    p.BM = each > 64 ? 128 : each > 32 ? 64 : 32;
-    p.BN = p.BM == 128 && wide >= 512 ? 256 : 128;
-    p.col_tiles = (int)((width + p.BN - 1) / p.BN);
-    p.row_tiles = (int)mx4_row_tiles(R, E, p.BM);
-    const int64_t tiles = (int64_t)p.col_tiles * p.row_tiles, room = 512;
-    p.splits = 1;
-    p.share = panels;
-    if (tiles > 0 && tiles * 2 <= room) {
-        int splits = (int)(room / tiles);
-        if (splits > panels / 4) splits = panels / 4;
-        if (splits > 16) splits = 16;
-        if (splits > 1) {
-            p.share = (panels + splits - 1) / splits;
-            p.splits = (panels + p.share - 1) / p.share;
+    const int64_t used = E < R ? E : R;                      // experts that have rows, at most
+    const double each = (double)R / (double)used;
+    auto row_tiles = [&](int BM) { return E == 1 ? (double)((R + BM - 1) / BM) : (double)used * (each <= 1.0 ? 1.0 : each / BM + 0.5 > 1.0 ? each / BM + 0.5 : 1.0); };
+    const double weights = (double)used * (double)N * panels * 68.0 * 1e-6;   // MB; 1 TB/s is 1 MB a microsecond
+    Choice best{};
+    double least = 1e30;
+    struct Few {
+        int rows, cols;
+        double load, stream;   // bytes a nanosecond and compute unit, TB/s of weights
+    };
+    static const Few few[] = {{1, 1, 43, 5.5}, {2, 1, 43, 5.0}, {2, 2, 43, 4.6}, {4, 2, 36, 4.2}};
+    for (const auto &k : few) {
+        const int64_t cols = gated ? N / 2 : N, col_tiles = (cols + 16 * k.cols - 1) / (16 * k.cols);
+        const double groups = row_tiles(16 * k.rows) * (double)col_tiles, rounds = groups < 1024 ? (double)(((int64_t)groups + 255) / 256) : groups / 256;
+        const double loads = rounds * panels * 1.1 * (k.rows + k.cols * (gated ? 2 : 1)) / k.load, stream = weights / k.stream;
+        const double t = 2.5 + (loads > stream ? loads : stream);
+        if (t < least) {
+            least = t;
+            best.row_blocks = k.rows;
+            best.col_blocks = k.cols;
         }
     }
-    if (p.splits > 1) p.partial_bytes = (size_t)tiles * (size_t)p.splits * (size_t)p.BM * (size_t)p.BN * 4u;
-    return p;
+    struct Tile {
+        int BM, BN, passes;   // passes: of four splits' partial sums; 0: K is not cut
+        double alone, shared;
+    };
+    static const Tile tiles[] = {{32, 128, 1, 0.18, 0.145}, {64, 128, 2, 0.24, 0.22}, {128, 128, 2, 0.27, 0.30}, {128, 256, 0, 0.45, 0.43}};
+    const int64_t width = gated ? (N / 2 + 31) / 32 * 64 : N;   // gated halves are interleaved 32 columns at a time
+    for (const auto &k : tiles) {
+        const int64_t col_tiles = (width + k.BN - 1) / k.BN;
+        const double count = row_tiles(k.BM) * (double)col_tiles;
+        for (int want = 1; want <= (k.passes ? MOST_SPLITS : 1); want *= 2) {
+            const int share = (panels + want - 1) / want, splits = (panels + share - 1) / share;
+            if (splits < want || (want > 1 && (mx4_row_tiles(R, E, k.BM) * col_tiles * want > MOST_CUT || share < LEAST_SHARE))) break;
+            const double full = count * splits / 256, stage = full <= 1.0 ? k.alone : full * k.shared > k.alone ? full * k.shared : k.alone;
+            double t = 3.5 + (share * stage > weights / 5.2 ? share * stage : weights / 5.2);
+            if (splits > 1) t += 2.0 + 2.0 * k.passes * ((splits + 3) / 4);
+            if (t < least) {
+                least = t;
+                best.row_blocks = 0;
+                best.tile = Mx4TilePlan{k.BM, k.BN, (int)col_tiles, (int)mx4_row_tiles(R, E, k.BM), splits, share, 0, 0};
+            }
+        }
+    }
+    Mx4TilePlan &p = best.tile;
+    if (best.row_blocks == 0 && p.splits > 1) p.partial_bytes = (size_t)p.row_tiles * (size_t)p.col_tiles * (size_t)p.splits * (size_t)p.BM * (size_t)p.BN * 4u;
+    return best;
 }
 
-// rows of W that tiles of BN rows go over: gated halves are cut into 32 columns each
-int64_t tiled_width(int64_t N, bool gated) { return gated ? (N / 2 + 31) / 32 * 64 : N; }
-
 // counters, quantized activations, partial sums
-size_t workspace_need(int64_t N, int32_t K, int32_t E, int64_t x_rows, int64_t R)
+size_t workspace_need(const Mx4Dims &dx, bool quantize, const Choice &c)
 {
-    Mx4Dims d;
-    if (hlq_mx4_check(x_rows, K, &d) != HLQ_OK) return 0;
-    size_t part = 0;
-    for (int gated = 0; gated < 2; ++gated) {
-        const size_t n = R ? tile_plan(tiled_width(N, gated), d.panels, E, R).partial_bytes : 0;
-        if (n > part) part = n;
-    }
-    return HLQ_WS_COUNTER_BYTES + up256(d.total) + up256(part);
+    return HLQ_WS_COUNTER_BYTES + (quantize ? up256(dx.total) : 0u) + up256(c.row_blocks ? 0 : c.tile.partial_bytes);
 }
 
 struct Call {
@@ -107,27 +138,27 @@ hlq_status product(const Call &c, int32_t E, const int32_t *offsets, const int32
     a.ldy = c.ldy;
     a.y_aligned = ((uintptr_t)c.Y & 15u) == 0 && (R == 1 || c.ldy * hlq_dtype_bytes(c.ytype) % 16 == 0);
     int xtype = c.xtype;
-    const bool few = R <= (int64_t)FEW_ROWS * E;
+    Choice how = choose(c.N, gated, a.panels, E, R);
+    const bool quantize = xtype != HLQ_MX4;
+    if (!c.ws) return HLQ_ERR_NULL;
+    if (c.ws_bytes < workspace_need(dx, quantize, how)) return HLQ_ERR_BUFFER_TOO_SMALL;
+    if ((uintptr_t)c.ws & 15u) return HLQ_ERR_BAD_STRIDE;
     hlq_clear_stale_error();
-    if (xtype == HLQ_MX4) a.A = hlq_mx4_view(dx, c.X);
-    else if (few && R <= QUANTIZE_INSIDE) {
+    if (!quantize) a.A = hlq_mx4_view(dx, c.X);
+    else if (how.row_blocks == 1 && (R + E - 1) / E * c.K <= QUANTIZE_INSIDE && (R < 16 ? R : 16) * (int64_t)a.panels * 68 <= QUANTIZED_BYTES) {
         a.x = c.X;
         a.ldx = c.ldx;
         a.x_aligned = ((uintptr_t)c.X & 15u) == 0 && (c.x_rows == 1 || c.ldx * hlq_dtype_bytes(c.xtype) % 16 == 0);
+        return hlq_mx4_launch_few(a, xtype, gated, 1, 1, c.stream);
     } else {
-        if (!c.ws) return HLQ_ERR_NULL;
-        if (c.ws_bytes < workspace_need(c.N, c.K, E, c.x_rows, R)) return HLQ_ERR_BUFFER_TOO_SMALL;
-        if ((uintptr_t)c.ws & 15u) return HLQ_ERR_BAD_STRIDE;
         void *blob = (char *)c.ws + HLQ_WS_COUNTER_BYTES;
         s = hlq_mx4_launch_quantize(dx, c.X, c.xtype, c.ldx, blob, c.stream);
         if (s != HLQ_OK) return s;
         a.A = hlq_mx4_view(dx, blob);
-        xtype = HLQ_MX4;
     }
-    if (few) return hlq_mx4_launch_few(a, xtype, gated, c.stream);
-    Mx4TilePlan p = tile_plan(tiled_width(c.N, gated), dw.panels, E, R);
-    p.partial_at = HLQ_WS_COUNTER_BYTES + up256(dx.total);
-    return hlq_mx4_launch_tile(a, p, gated, c.ws, c.stream);
+    if (how.row_blocks) return hlq_mx4_launch_few(a, HLQ_MX4, gated, how.row_blocks, how.col_blocks, c.stream);
+    how.tile.partial_at = HLQ_WS_COUNTER_BYTES + (quantize ? up256(dx.total) : 0u);
+    return hlq_mx4_launch_tile(a, how.tile, gated, c.ws, c.stream);
 }
 
 }  // namespace
@@ -141,7 +172,15 @@ hlq_status hlq_mx4_workspace_bytes(int64_t N, int32_t K, int32_t experts, int64_
     hlq_status s = hlq_mx4_check(x_rows, K, &d);
     if (s != HLQ_OK) return s;
     if (!bytes) return HLQ_ERR_NULL;
-    *bytes = workspace_need(N, K, experts, x_rows, rows);
+    // partial sums: a bound that grows with the rows, so that fewer rows never need more
+    size_t part = 0;
+    if (d.panels >= 2 * LEAST_SHARE && rows > 0) {
+        const size_t used = (size_t)(rows < experts ? rows : experts);
+        part = ((size_t)rows + used * 128u) * (size_t)(up256((size_t)N) + 256u) * (size_t)MOST_SPLITS * 4u;
+        const size_t most = (size_t)MOST_CUT * 128u * 128u * 4u;
+        if (part > most) part = most;
+    }
+    *bytes = HLQ_WS_COUNTER_BYTES + up256(d.total) + up256(part);
     return HLQ_OK;
 }
 

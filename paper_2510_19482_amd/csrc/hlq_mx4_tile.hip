@@ -29,11 +29,11 @@ __device__ __forceinline__ int xcd_order(int id, int n)
     return x * each + (x < more ? x : more) + id / 8;
 }
 
-// TM x TN blocks of 32 x 32 a wavefront, GM x GN wavefronts, BUFFERS stages of a panel in LDS.
+// TM x TN blocks of 32 x 32 a wavefront, GM x GN wavefronts, BUFFERS stages of a panel in LDS; CUT: K may be cut over workgroups.
 constexpr int up(int n, int a) { return (n + a - 1) / a * a; }
 constexpr int tile_stage(int TM, int TN, int GM, int GN) { return 32 * (TM * GM + TN * GN) * 64 + up(32 * (TM * GM + TN * GN), 64) * 4; }
 
-template <int TM, int TN, int GM, int GN, int BUFFERS, bool GATED>
+template <int TM, int TN, int GM, int GN, int BUFFERS, bool CUT, bool GATED>
 __global__ void __launch_bounds__(64 * GM * GN, 2)
 hlq_mx4_tile_kernel(const Mx4Product a, const Tiles t)
 {
@@ -41,7 +41,7 @@ hlq_mx4_tile_kernel(const Mx4Product a, const Tiles t)
     constexpr int LOADS = (BM + BN) / 16 / WAVES;                          // requests of 16 rows' codes, a wavefront and stage
     constexpr int SCALE_LOADS = (up(BM + BN, 64) / 64 + WAVES - 1) / WAVES;   // of 64 rows' scales; those past the last repeat it
     constexpr int SCALES = (BM + BN) * 64, STAGE = tile_stage(TM, TN, GM, GN);
-    extern __shared__ char lds[];
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int r = lane & 31, g = lane >> 5, wm = wave / GN, wn = wave % GN;
 
@@ -180,16 +180,22 @@ hlq_mx4_tile_kernel(const Mx4Product a, const Tiles t)
     for (; p < count; ++p) buffer = panel(buffer, std::false_type{});
     __syncthreads();
 
-    if (t.splits > 1) {
-        // partial sums past the XCD's own L2; whoever is last of the tile adds them in the order of the splits
-        float *mine = t.partial + ((int64_t)tile_id * t.splits + split) * (BM * BN) + wave * (TM * TN * 16 * 64) + lane;
+    if (CUT && t.splits > 1) {
+        // Partial sums go past the XCD's own L2 (device-scope stores, complete before the arrival is counted); whoever is last of
+        // the tile adds them in the order of the splits, those of four splits on their way at a time.
+        constexpr int64_t TILE = (int64_t)BM * BN / 2;   // in pairs
+        uint64_t *const all = (uint64_t *)t.partial + (int64_t)tile_id * t.splits * TILE + (wave * TM * TN * 8) * 64 + lane;
+        uint64_t *const mine = all + split * TILE;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int c = 0; c < 16; ++c)
-                    __hip_atomic_store(mine + ((i * TN + j) * 16 + c) * 64, acc[i][j][c], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                for (int c = 0; c < 8; ++c) {
+                    const float low = acc[i][j][2 * c], high = acc[i][j][2 * c + 1];
+                    const uint64_t pair = __builtin_bit_cast(uint32_t, low) | (uint64_t)__builtin_bit_cast(uint32_t, high) << 32;
+                    __hip_atomic_store(mine + ((i * TN + j) * 8 + c) * 64, pair, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         int *last = (int *)lds;
@@ -197,18 +203,34 @@ hlq_mx4_tile_kernel(const Mx4Product a, const Tiles t)
         __syncthreads();
         if (!*last) return;
         if (threadIdx.x == 0) __hip_atomic_store(t.arrived + tile_id, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const float *all = t.partial + (int64_t)tile_id * t.splits * (BM * BN) + wave * (TM * TN * 16 * 64) + lane;
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int c = 0; c < 16; ++c) acc[i][j][c] = 0.f;
-                for (int o = 0; o < t.splits; ++o)
+            for (int o = 0; o < t.splits; o += 4) {
+                uint64_t pair[4][TN][8];
 #pragma unroll
-                    for (int c = 0; c < 16; ++c)
-                        acc[i][j][c] += __hip_atomic_load(all + (int64_t)o * (BM * BN) + ((i * TN + j) * 16 + c) * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+                            pair[q][j][c] = __hip_atomic_load(all + (o + q < t.splits ? o + q : o) * TILE + ((i * TN + j) * 8 + c) * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (o + q < t.splits)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j)
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) {
+                                acc[i][j][2 * c] += __builtin_bit_cast(float, (uint32_t)pair[q][j][c]);
+                                acc[i][j][2 * c + 1] += __builtin_bit_cast(float, (uint32_t)(pair[q][j][c] >> 32));
+                            }
             }
+        }
+        __syncthreads();
     }
 
     // Results leave by way of LDS, so that rows are written in whole lines: a lane has row m and of each 32 columns 8 q + 4 g .. + 3.
@@ -256,14 +278,14 @@ hlq_mx4_tile_kernel(const Mx4Product a, const Tiles t)
     else leave((__bf16)0.f);
 }
 
-template <int TM, int TN, int GM, int GN, int BUFFERS>
+template <int TM, int TN, int GM, int GN, int BUFFERS, bool CUT>
 hlq_status launch(const Mx4Product &a, const Mx4TilePlan &p, bool gated, void *ws, hipStream_t st)
 {
     constexpr size_t lds = (size_t)tile_stage(TM, TN, GM, GN) * BUFFERS;
     const Tiles t{p.col_tiles, p.row_tiles, p.splits, p.share, (int *)ws, (float *)((char *)ws + p.partial_at)};
     const int64_t blocks = (int64_t)p.col_tiles * p.row_tiles * p.splits;
     if (blocks > INT32_MAX / 1024) return HLQ_ERR_UNSUPPORTED;
-    auto kernel = gated ? hlq_mx4_tile_kernel<TM, TN, GM, GN, BUFFERS, true> : hlq_mx4_tile_kernel<TM, TN, GM, GN, BUFFERS, false>;
+    auto kernel = gated ? hlq_mx4_tile_kernel<TM, TN, GM, GN, BUFFERS, CUT, true> : hlq_mx4_tile_kernel<TM, TN, GM, GN, BUFFERS, CUT, false>;
     kernel<<<(unsigned)blocks, 64 * GM * GN, lds, st>>>(a, t);
     return hlq_hip_status(hipGetLastError());
 }
@@ -272,8 +294,8 @@ hlq_status launch(const Mx4Product &a, const Mx4TilePlan &p, bool gated, void *w
 
 hlq_status hlq_mx4_launch_tile(const Mx4Product &a, const Mx4TilePlan &p, bool gated, void *ws, hipStream_t st)
 {
-    if (p.BM == 128 && p.BN == 256) return launch<2, 4, 2, 2, 3>(a, p, gated, ws, st);
-    if (p.BM == 128) return launch<2, 2, 2, 2, 4>(a, p, gated, ws, st);
-    if (p.BM == 64) return launch<2, 2, 1, 2, 4>(a, p, gated, ws, st);
-    return launch<1, 2, 1, 2, 4>(a, p, gated, ws, st);
+    if (p.BM == 128 && p.BN == 256) return launch<2, 4, 2, 2, 3, false>(a, p, gated, ws, st);
+    if (p.BM == 128) return launch<2, 2, 2, 2, 4, true>(a, p, gated, ws, st);
+    if (p.BM == 64) return launch<2, 2, 1, 2, 4, true>(a, p, gated, ws, st);
+    return launch<1, 2, 1, 2, 4, true>(a, p, gated, ws, st);
 }
