@@ -30,29 +30,42 @@ hlq_mx4_quantize_kernel(const typename Mx4Type<T>::type *__restrict__ x, int64_t
     }
 }
 
-__device__ __forceinline__ float code_value(uint32_t c)
+// Upper bytes of the f16 that four codes (the low halves of c's bytes) stand for; the lower bytes are 0.
+__device__ __forceinline__ uint32_t code_bytes(uint32_t c)
 {
-    const uint32_t m = c & 7u;   // 0 0.5 1 1.5 2 3 4 6
-    const float a = m < 2u ? 0.5f * (float)m : __builtin_bit_cast(float, (((m >> 1) + 126u) << 23) | ((m & 1u) << 22));
-    return c & 8u ? -a : a;
+    // 0 0.5 1 1.5 2 3 4 6
+    return __builtin_amdgcn_perm(0x46444240u, 0x3e3c3800u, c & 0x07070707u) | (c & 0x08080808u) << 4;
 }
 
-template <int T>
-__global__ void __launch_bounds__(256)
+// As in quantizing: a wavefront takes a panel of four rows, a lane eight successive values.
+template <int T, bool ALIGNED>
+__global__ void __launch_bounds__(64 * MX4_WAVES)
 hlq_mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t rows, int K, int panels,
                           typename Mx4Type<T>::type *__restrict__ y, int64_t ldy, int64_t items)
 {
-    const int eights = panels * 16;
-    for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items; it += (int64_t)gridDim.x * 256) {
-        const int64_t row = it / eights;
-        const int j = (int)(it - row * eights), k = j * 8;
-        if (k >= K) continue;
-        const uint32_t c = *(const uint32_t *)(codes + ((int64_t)(j >> 4) * rows + row) * 64 + (j & 15) * 4);
-        const uint32_t byte = scales[((int64_t)(j >> 4) * rows + row) * 4 + mx4_scale_byte((j >> 2) & 3)];
-        typename Mx4Type<T>::type *p = y + row * ldy + k;
-        for (int i = 0; i < 8 && k + i < K; ++i) {
-            const float v = byte == 255u ? __builtin_nanf("") : ldexpf(code_value(c >> (4 * i)), (int)byte - 127);
-            p[i] = (typename Mx4Type<T>::type)v;
+    using V = typename Mx4Type<T>::type;
+    const int lane = (int)(threadIdx.x & 63u), j = lane & 15;
+    for (int64_t it = (int64_t)blockIdx.x * MX4_WAVES + (threadIdx.x >> 6); it < items; it += (int64_t)gridDim.x * MX4_WAVES) {
+        const int64_t quad = it / panels, row = quad * 4 + (lane >> 4);
+        const int panel = (int)(it - quad * panels), k = panel * MX4_PANEL_K + j * 8;
+        if (row >= rows || k >= K) continue;
+        const int64_t at = panel * rows + row;
+        const uint32_t c = *(const uint32_t *)(codes + at * 64 + j * 4);
+        const int byte = scales[at * 4 + mx4_scale_byte(j >> 2)];
+        const uint32_t even = code_bytes(c), odd = code_bytes(c >> 4);
+        struct alignas(16) Eight { V v[8]; } out;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint16_t half = (uint16_t)((i & 1 ? odd : even) >> (8 * (i >> 1)) << 8);
+            const float v = ldexpf((float)__builtin_bit_cast(_Float16, half), byte - 127);
+            out.v[i] = (V)(byte == 255 ? __builtin_nanf("") : v);
+        }
+        V *p = y + row * ldy + k;
+        if (ALIGNED && k + 8 <= K) *(Eight *)p = out;
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + i < K) p[i] = out.v[i];
         }
     }
 }
@@ -118,8 +131,12 @@ template <int T>
 void launch_dequantize(const Mx4Dims &d, const void *blob, void *y, int64_t ldy, hipStream_t st)
 {
     using V = typename Mx4Type<T>::type;
-    const int64_t items = d.rows * d.panels * 16;
-    hlq_mx4_dequantize_kernel<T><<<grid_of(items, 256), 256, 0, st>>>((const uint8_t *)blob, (const uint8_t *)blob + d.code_bytes, d.rows, d.K, d.panels, (V *)y, ldy, items);
+    const int64_t items = (d.rows + 3) / 4 * d.panels;
+    const uint8_t *codes = (const uint8_t *)blob, *scales = codes + d.code_bytes;
+    const bool aligned = ((uintptr_t)y & 15u) == 0 && (d.rows == 1 || (ldy * (int64_t)sizeof(V)) % 16 == 0);
+    const dim3 grid(grid_of(items, MX4_WAVES)), block(64 * MX4_WAVES);
+    if (aligned) hlq_mx4_dequantize_kernel<T, true><<<grid, block, 0, st>>>(codes, scales, d.rows, d.K, d.panels, (V *)y, ldy, items);
+    else hlq_mx4_dequantize_kernel<T, false><<<grid, block, 0, st>>>(codes, scales, d.rows, d.K, d.panels, (V *)y, ldy, items);
 }
 
 // what the four calls have in common

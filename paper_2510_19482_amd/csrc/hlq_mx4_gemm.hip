@@ -33,6 +33,10 @@ Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
     auto row_tiles = [&](int BM) { return E == 1 ? (double)((R + BM - 1) / BM) : (double)used * (each <= 1.0 ? 1.0 : each / BM + 0.5 > 1.0 ? each / BM + 0.5 : 1.0); };
     const double weights = (double)used * (double)N * panels * 68.0 * 1e-6;   // MB; 1 TB/s is 1 MB a microsecond
     Choice best{};
+    if (R <= 16) {   // whatever else there is reads as much
+        best.row_blocks = best.col_blocks = 1;
+        return best;
+    }
     double least = 1e30;
     struct Few {
         int rows, cols;

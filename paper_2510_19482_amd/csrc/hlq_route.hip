@@ -1,19 +1,19 @@
 // Experts: the router (k largest logits of a token, their softmax weights, tokens grouped by expert) and the weighted sum of the
 // experts' outputs.
 //
-// Router.  Logits become unsigned keys whose order is the numbers' (0: masked, never chosen); a wavefront holds a token's logits,
-// lane l those of experts l, l + 64, ..., and takes the largest k times: a maximum over the lanes, then the lowest expert that
-// has it.  Weights: softmax in fp32, over the chosen ones or over all.
+// Router.  A logit becomes a 42-bit key: its order as a number (0: masked, never chosen), then the expert, the lowest largest, so
+// that keys differ and the largest key is the next choice.  Sixteen lanes hold a token's keys, as the bits of positive doubles,
+// whose maximum is one instruction, and take the largest k times.  Weights: softmax in fp32, over the chosen ones or over all.
 // Grouping is a counting sort, stable and without atomics whose order could matter: a token takes an expert at most once, so
-// for the 64 tokens of a chunk an expert's rows are a 64-bit mask, its count the bits of it, and a row's place among them the
-// bits below its own.  Chunks' counts are summed by whoever needs them (up to 256 chunks) or by a scan in between.
+// for the 32 tokens of a chunk an expert's rows are a 32-bit mask, its count the bits of it, and a row's place among them the
+// bits below its own.  Chunks' counts are added up by each workgroup that places rows (up to 512 chunks) or by a scan in between.
 #include "hlq_mx4.h"
 
 namespace {
 
-constexpr int CHUNK = 64;           // tokens, bits of a mask
-constexpr int DIRECT_CHUNKS = 256;  // up to here each workgroup of the second kernel adds the counts by itself
-constexpr int TOP_WAVES = 16;
+constexpr int CHUNK = 32;           // tokens, bits of a mask; of one workgroup
+constexpr int DIRECT_CHUNKS = 512;  // up to here each workgroup of the second kernel adds the counts by itself, in 16 bits
+constexpr int PLACE_THREADS = 512;
 
 struct Route {
     int64_t T;
@@ -29,23 +29,30 @@ struct Route {
     int chunks;
 };
 
-// largest of 64 unsigned values, in every lane's hands as a scalar
-__device__ __forceinline__ uint32_t wave_max(uint32_t v)
+// of the sixteen lanes of a row, in each of them: the maximum, and the sum
+__device__ __forceinline__ uint64_t max_key(uint64_t a, uint64_t b)
 {
-    auto step = [&](uint32_t o) { v = o > v ? o : v; };
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true));   // from 1, 2, 4, 8 lanes below in a row of 16
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true));
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true));
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true));
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));  // a row's last lane to the next row
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));  // the lower half's last lane to the upper half
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+    uint64_t m;
+    asm("v_max_f64 %0, %1, %2" : "=v"(m) : "v"(a), "v"(b));
+    return m;
 }
-__device__ __forceinline__ float wave_sum(float v)
+template <int CTRL>
+__device__ __forceinline__ uint32_t rotated(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true); }
+template <int CTRL>
+__device__ __forceinline__ uint64_t rotated_key(uint64_t v) { return rotated<CTRL>((uint32_t)v) | (uint64_t)rotated<CTRL>((uint32_t)(v >> 32)) << 32; }
+__device__ __forceinline__ uint64_t row_max(uint64_t v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-    return v;
+    v = max_key(v, rotated_key<0x128>(v));   // from 8, 4, 2, 1 lanes on
+    v = max_key(v, rotated_key<0x124>(v));
+    v = max_key(v, rotated_key<0x122>(v));
+    return max_key(v, rotated_key<0x121>(v));
+}
+__device__ __forceinline__ float row_sum(float v)
+{
+    v += __builtin_bit_cast(float, rotated<0x128>(__builtin_bit_cast(uint32_t, v)));
+    v += __builtin_bit_cast(float, rotated<0x124>(__builtin_bit_cast(uint32_t, v)));
+    v += __builtin_bit_cast(float, rotated<0x122>(__builtin_bit_cast(uint32_t, v)));
+    return v + __builtin_bit_cast(float, rotated<0x121>(__builtin_bit_cast(uint32_t, v)));
 }
 
 __device__ __forceinline__ uint32_t key_of(float v)
@@ -61,19 +68,19 @@ __device__ __forceinline__ float value_of(uint32_t key)
 }
 
 // masks of a chunk's rows by expert from its choices, staged in LDS as [token][k]
-__device__ __forceinline__ void set_masks(const Route &a, const int *picks, unsigned long long *masks, int tokens)
+__device__ __forceinline__ void set_masks(const Route &a, const int *picks, uint32_t *masks, int tokens)
 {
     for (int i = (int)threadIdx.x; i < tokens * a.k; i += (int)blockDim.x)
-        if (picks[i] >= 0) atomicOr(&masks[picks[i]], 1ull << (i / a.k));
+        if (picks[i] >= 0) atomicOr(&masks[picks[i]], 1u << (i / a.k));
 }
 // slots and rows of a chunk; base: first row of each expert's share of it
-__device__ __forceinline__ void place(const Route &a, const int *picks, const unsigned long long *masks, const int *base, int64_t t0, int tokens)
+__device__ __forceinline__ void place(const Route &a, const int *picks, const uint32_t *masks, const int *base, int64_t t0, int tokens)
 {
     for (int i = (int)threadIdx.x; i < tokens * a.k; i += (int)blockDim.x) {
         const int e = picks[i], t = i / a.k;
         int slot = -1;
         if (e >= 0) {
-            slot = base[e] + __popcll(masks[e] & ((1ull << t) - 1ull));
+            slot = base[e] + __popc(masks[e] & ((1u << t) - 1u));
             a.rows[slot] = (int32_t)(t0 + t);
         }
         a.slots[t0 * a.k + i] = slot;
@@ -100,57 +107,62 @@ __device__ __forceinline__ int prefix(const int *count, int *first, int n)
 
 // V: logits a lane holds
 template <int T, int V>
-__global__ void __launch_bounds__(64 * TOP_WAVES)
+__global__ void __launch_bounds__(16 * CHUNK)
 hlq_route_top_kernel(const Route a)
 {
-    extern __shared__ unsigned long long lds[];
-    unsigned long long *masks = lds;                 // [E]
-    int *picks = (int *)(masks + a.E);               // [CHUNK][k]
-    int *count = picks + CHUNK * a.k, *first = count + a.E;   // [E] each
-    const int lane = (int)(threadIdx.x & 63u), wave = (int)(threadIdx.x >> 6);
+    extern __shared__ int lds[];
+    uint32_t *masks = (uint32_t *)lds;               // [E]
+    int *count = lds + a.E, *first = count + a.E;    // [E] each
+    int *picks = first + a.E;                        // [CHUNK][k]
+    float *values = (float *)(picks + CHUNK * a.k);  // [CHUNK][k]
+    const int lane = (int)(threadIdx.x & 63u), wave = (int)(threadIdx.x >> 6), l = lane & 15, t = (int)(threadIdx.x >> 4);
     const int64_t t0 = (int64_t)blockIdx.x * CHUNK;
     const int tokens = (int)(a.T - t0 < CHUNK ? a.T - t0 : CHUNK);
-    for (int e = (int)threadIdx.x; e < a.E; e += (int)blockDim.x) masks[e] = 0ull;
-    for (int t = wave; t < tokens; t += TOP_WAVES) {
+    for (int e = (int)threadIdx.x; e < a.E; e += (int)blockDim.x) masks[e] = 0u;
+    if (t < tokens) {
+        constexpr uint64_t NORMAL = 1ull << 62;      // a key that is not masked is a normal double
         const typename Mx4Type<T>::type *row = (const typename Mx4Type<T>::type *)a.logits + (t0 + t) * a.ld;
-        uint32_t key[V], all[V];
+        uint64_t key[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) key[j] = all[j] = 64 * j + lane < a.E ? key_of((float)row[64 * j + lane]) : 0u;
-        uint32_t mine = 0u;      // lane i: the i-th choice
-        int id = -1;
-        for (int i = 0; i < a.k; ++i) {
-            uint32_t best = key[0];
+        for (int j = 0; j < V; ++j) {
+            const int e = 16 * j + l;
+            const uint32_t k32 = e < a.E ? key_of((float)row[e]) : 0u;
+            key[j] = k32 ? NORMAL | (uint64_t)k32 << 10 | (uint32_t)(HLQ_MAX_EXPERTS - 1 - e) : 0ull;
+        }
+        float top = 0.f, sum = 0.f;
+        int found = 0;
+        for (; found < a.k; ++found) {
+            uint64_t best = key[0];
 #pragma unroll
-            for (int j = 1; j < V; ++j) best = key[j] > best ? key[j] : best;
-            best = wave_max(best);
-            if (best == 0u) break;
-            int e = -1;
+            for (int j = 1; j < V; ++j) best = max_key(best, key[j]);
+            best = row_max(best);
+            if (best == 0ull) break;
+            const float v = value_of((uint32_t)(best >> 10));
+            if (found == 0) {
+                top = v;
+                if (!a.renorm) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const uint64_t has = __ballot(key[j] == best);
-                if (e < 0 && has) {
-                    e = 64 * j + (int)__builtin_ctzll(has);
-                    if (lane == (e & 63)) key[j] = 0u;
+                    for (int j = 0; j < V; ++j) sum += key[j] ? expf(value_of((uint32_t)(key[j] >> 10)) - top) : 0.f;
                 }
             }
-            if (lane == i) {
-                mine = best;
-                id = e;
+            if (l == 0) {
+                picks[t * a.k + found] = HLQ_MAX_EXPERTS - 1 - (int)(best & (HLQ_MAX_EXPERTS - 1));
+                values[t * a.k + found] = v;
             }
-        }
-        const float top = value_of((uint32_t)__builtin_amdgcn_readfirstlane((int)mine));
-        const float p = mine ? expf(value_of(mine) - top) : 0.f;
-        float sum = p;
-        if (!a.renorm) {
-            sum = 0.f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) sum += all[j] ? expf(value_of(all[j]) - top) : 0.f;
+            for (int j = 0; j < V; ++j) key[j] = key[j] == best ? 0ull : key[j];
         }
-        sum = wave_sum(sum);
-        if (lane < a.k) {
-            a.ids[(t0 + t) * a.k + lane] = id;
-            a.weights[(t0 + t) * a.k + lane] = mine ? p / sum : 0.f;
-            picks[t * a.k + lane] = id;
+        // what lane 0 of the row wrote is there for the others: they are of one wavefront, whose LDS accesses keep their order
+        __builtin_amdgcn_wave_barrier();
+        if (a.renorm) {
+            for (int i = l; i < found; i += 16) sum += expf(values[t * a.k + i] - top);
+        }
+        sum = row_sum(sum);
+        for (int i = l; i < a.k; i += 16) {
+            const int id = i < found ? picks[t * a.k + i] : -1;
+            if (i >= found) picks[t * a.k + i] = -1;
+            a.ids[(t0 + t) * a.k + i] = id;
+            a.weights[(t0 + t) * a.k + i] = i < found ? expf(values[t * a.k + i] - top) / sum : 0.f;
         }
     }
     __syncthreads();
@@ -158,10 +170,10 @@ hlq_route_top_kernel(const Route a)
     __syncthreads();
     if (a.chunks > 1) {
         for (int e = (int)threadIdx.x; e < a.pitch; e += (int)blockDim.x)
-            a.counts[(int64_t)blockIdx.x * a.pitch + e] = e < a.E ? (uint8_t)__popcll(masks[e]) : (uint8_t)0;
+            a.counts[(int64_t)blockIdx.x * a.pitch + e] = e < a.E ? (uint8_t)__popc(masks[e]) : (uint8_t)0;
         return;
     }
-    for (int e = (int)threadIdx.x; e < a.E; e += (int)blockDim.x) count[e] = __popcll(masks[e]);
+    for (int e = (int)threadIdx.x; e < a.E; e += (int)blockDim.x) count[e] = __popc(masks[e]);
     __syncthreads();
     if (wave == 0) {
         const int all = prefix(count, first, a.E);
@@ -216,69 +228,74 @@ hlq_route_scan_kernel(const Route a)
     }
 }
 
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(PLACE_THREADS)
 hlq_route_place_kernel(const Route a)
 {
-    extern __shared__ unsigned long long lds[];
-    unsigned long long *masks = lds;
-    int *picks = (int *)(masks + a.E);
-    int *count = picks + CHUNK * a.k, *first = count + a.E, *before = first + a.E;
+    extern __shared__ int lds[];
+    uint32_t *masks = (uint32_t *)lds;                                         // [pitch] each
+    int *count = lds + a.pitch, *first = count + a.pitch, *before = first + a.pitch;
+    int *picks = before + a.pitch;                                             // [CHUNK][k]
     __shared__ int total;
     const int64_t t0 = (int64_t)blockIdx.x * CHUNK;
-    const int tokens = (int)(a.T - t0 < CHUNK ? a.T - t0 : CHUNK), me = (int)blockIdx.x;
-    for (int i = (int)threadIdx.x; i < tokens * a.k; i += 256) picks[i] = a.ids[t0 * a.k + i];
-    for (int e = (int)threadIdx.x; e < a.E; e += 256) {
-        masks[e] = 0ull;
-        if (a.chunks > DIRECT_CHUNKS) {
-            count[e] = a.before[(int64_t)a.chunks * a.E + e];
-            before[e] = a.before[(int64_t)me * a.E + e];
-        }
+    const int tokens = (int)(a.T - t0 < CHUNK ? a.T - t0 : CHUNK), me = (int)blockIdx.x, tid = (int)threadIdx.x;
+    for (int i = tid; i < tokens * a.k; i += PLACE_THREADS) picks[i] = a.ids[t0 * a.k + i];
+    const bool scanned = a.chunks > DIRECT_CHUNKS;
+    for (int e = tid; e < a.pitch; e += PLACE_THREADS) {
+        masks[e] = 0u;
+        count[e] = scanned && e < a.E ? a.before[(int64_t)a.chunks * a.E + e] : 0;
+        before[e] = scanned && e < a.E ? a.before[(int64_t)me * a.E + e] : 0;
     }
-    if (a.chunks <= DIRECT_CHUNKS)
-        for (int e = 4 * (int)threadIdx.x; e < a.pitch; e += 4 * 256) {
-            int all[4] = {0, 0, 0, 0}, less[4] = {0, 0, 0, 0};
-#pragma unroll 8
-            for (int c = 0; c < a.chunks; ++c) {
-                const uint32_t w = *(const uint32_t *)(a.counts + (int64_t)c * a.pitch + e);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int n = (int)(w >> (8 * i) & 255u);
-                    all[i] += n;
-                    less[i] += c < me ? n : 0;
-                }
-            }
-            for (int i = 0; i < 4 && e + i < a.E; ++i) {
-                count[e + i] = all[i];
-                before[e + i] = less[i];
-            }
-        }
     __syncthreads();
     set_masks(a, picks, masks, tokens);
-    if (threadIdx.x < 64) {
+    if (!scanned) {
+        // a thread has four experts over a share of the chunks, their counts in the bytes of a word
+        const int quads = a.pitch / 4, shares = quads < PLACE_THREADS ? PLACE_THREADS / quads : 1;
+        for (int i = tid; i < quads * shares; i += PLACE_THREADS) {
+            const int quad = i % quads, share = i / quads;
+            uint32_t all[2] = {0u, 0u}, less[2] = {0u, 0u};   // experts 0 and 2, 1 and 3, in 16 bits
+#pragma unroll 8
+            for (int c = share; c < a.chunks; c += shares) {
+                const uint32_t w = *(const uint32_t *)(a.counts + (int64_t)c * a.pitch + quad * 4);
+                const uint32_t even = w & 0x00ff00ffu, odd = (w >> 8) & 0x00ff00ffu;
+                all[0] += even;
+                all[1] += odd;
+                less[0] += c < me ? even : 0u;
+                less[1] += c < me ? odd : 0u;
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                atomicAdd(&count[quad * 4 + n], (int)(all[n & 1] >> (16 * (n >> 1)) & 0xffffu));
+                atomicAdd(&before[quad * 4 + n], (int)(less[n & 1] >> (16 * (n >> 1)) & 0xffffu));
+            }
+        }
+    }
+    __syncthreads();
+    if (tid < 64) {
         const int all = prefix(count, first, a.E);
-        if (threadIdx.x == 0) total = all;
+        if (tid == 0) total = all;
     }
     __syncthreads();
     if (me == 0) {
-        for (int e = (int)threadIdx.x; e < a.E; e += 256) a.offsets[e] = first[e];
-        if (threadIdx.x == 0) a.offsets[a.E] = total;
+        for (int e = tid; e < a.E; e += PLACE_THREADS) a.offsets[e] = first[e];
+        if (tid == 0) a.offsets[a.E] = total;
     }
-    for (int e = (int)threadIdx.x; e < a.E; e += 256) before[e] += first[e];
+    for (int e = tid; e < a.E; e += PLACE_THREADS) before[e] += first[e];
     // rows that no token took
-    for (int64_t i = total + (int64_t)me * 256 + threadIdx.x; i < a.T * a.k; i += (int64_t)gridDim.x * 256) a.rows[i] = -1;
+    for (int64_t i = total + (int64_t)me * PLACE_THREADS + tid; i < a.T * a.k; i += (int64_t)gridDim.x * PLACE_THREADS) a.rows[i] = -1;
     __syncthreads();
     place(a, picks, masks, before, t0, tokens);
 }
 
 template <int T>
-void launch_top(const Route &a, size_t lds, hipStream_t st)
+void launch_top(const Route &a, hipStream_t st)
 {
-    const dim3 grid((unsigned)a.chunks), block(64 * TOP_WAVES);
-    if (a.E <= 64) hlq_route_top_kernel<T, 1><<<grid, block, lds, st>>>(a);
-    else if (a.E <= 128) hlq_route_top_kernel<T, 2><<<grid, block, lds, st>>>(a);
-    else if (a.E <= 256) hlq_route_top_kernel<T, 4><<<grid, block, lds, st>>>(a);
-    else if (a.E <= 512) hlq_route_top_kernel<T, 8><<<grid, block, lds, st>>>(a);
-    else hlq_route_top_kernel<T, 16><<<grid, block, lds, st>>>(a);
+    const dim3 grid((unsigned)a.chunks), block(16 * CHUNK);
+    const size_t lds = (size_t)a.E * 12u + (size_t)CHUNK * a.k * 8u;
+    if (a.E <= 64) hlq_route_top_kernel<T, 4><<<grid, block, lds, st>>>(a);
+    else if (a.E <= 128) hlq_route_top_kernel<T, 8><<<grid, block, lds, st>>>(a);
+    else if (a.E <= 256) hlq_route_top_kernel<T, 16><<<grid, block, lds, st>>>(a);
+    else if (a.E <= 512) hlq_route_top_kernel<T, 32><<<grid, block, lds, st>>>(a);
+    else hlq_route_top_kernel<T, 64><<<grid, block, lds, st>>>(a);
 }
 
 struct Combine {
@@ -401,13 +418,12 @@ hlq_status hlq_route(int64_t T, int32_t E, int32_t k, const void *logits, hlq_dt
     a.counts = (uint8_t *)ws;
     a.before = ws ? (int32_t *)((char *)ws + counts_bytes(T, E)) : nullptr;
     const hipStream_t st = (hipStream_t)stream;
-    const size_t lds = (size_t)E * 16u + (size_t)CHUNK * k * 4u;
     hlq_clear_stale_error();
-    if (type == HLQ_F16) launch_top<HLQ_F16>(a, lds, st);
-    else if (type == HLQ_BF16) launch_top<HLQ_BF16>(a, lds, st);
-    else launch_top<HLQ_F32>(a, lds, st);
+    if (type == HLQ_F16) launch_top<HLQ_F16>(a, st);
+    else if (type == HLQ_BF16) launch_top<HLQ_BF16>(a, st);
+    else launch_top<HLQ_F32>(a, st);
     if (a.chunks > DIRECT_CHUNKS) hlq_route_scan_kernel<<<(E + 15) / 16, 1024, 0, st>>>(a);
-    if (a.chunks > 1) hlq_route_place_kernel<<<(unsigned)a.chunks, 256, lds + (size_t)E * 4u, st>>>(a);
+    if (a.chunks > 1) hlq_route_place_kernel<<<(unsigned)a.chunks, PLACE_THREADS, (size_t)a.pitch * 16u + (size_t)CHUNK * k * 4u, st>>>(a);
     return hlq_hip_status(hipGetLastError());
 }
 

@@ -356,8 +356,8 @@ def test_route_ties_masks_and_infinities(T):
 
 
 def test_route_many_chunks_and_strided_logits():
-    # over 256 chunks of 64 tokens the counts are scanned by a kernel of their own
-    T, E, k = 64 * 300 + 5, 10, 3
+    # over 512 chunks of 32 tokens the counts are scanned by a kernel of their own
+    T, E, k = 32 * 600 + 5, 10, 3
     wide = on_gpu(rng("many").normal(size=(T, E + 3)), "bf16")
     t = wide[:, 2:2 + E]
     ids, w, offsets, rows, slots = routed(B.hlq_route(t, k))
