@@ -382,6 +382,20 @@ def _matrix(t):
     return rows, cols, t.data_ptr(), dtype, ld if rows > 1 else cols
 
 
+def _need_gpu(*tensors) -> None:
+    for t in tensors:
+        if not t.is_cuda:
+            raise ValueError(f"expected tensors on the GPU, got one on {t.device}")
+
+
+def _empty(shape, dtype, device, stream):
+    """A new tensor of the stream that the call runs on: memory that another stream still uses is not handed out for it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def mx4_bytes(rows: int, K: int) -> int:
     n = ctypes.c_size_t()
     _check("hlq_mx4_bytes", lib.hlq_mx4_bytes(rows, K, ctypes.byref(n)))
@@ -400,17 +414,23 @@ class Mx4:
             raise ValueError(f"a blob of {mx4_bytes(rows, K)} bytes is needed for {rows} x {K}")
 
 
-def alloc_mx4(rows: int, K: int, device="cuda") -> Mx4:
-    return Mx4(torch.empty(mx4_bytes(rows, K), dtype=torch.uint8, device=device), rows, K)
+def alloc_mx4(rows: int, K: int, device="cuda", stream=None) -> Mx4:
+    return Mx4(_empty(mx4_bytes(rows, K), torch.uint8, device, stream), rows, K)
+
+
+def _mx4_out(out, rows: int, K: int, device, stream) -> Mx4:
+    if out is None:
+        return alloc_mx4(rows, K, device, stream)
+    if out.rows != rows or out.K != K:
+        raise ValueError(f"the output is a matrix of {out.rows} x {out.K}, not {rows} x {K}")
+    return out
 
 
 def hlq_mx4_quantize(x, out: Mx4 | None = None, stream=None) -> Mx4:
     """Rows of x [rows, K] (f16, bf16 or f32) in 4-bit floats, a power-of-two scale for each 32 of a row."""
     rows, K, ptr, dtype, ld = _matrix(x)
-    if out is None:
-        out = alloc_mx4(rows, K, x.device)
-    elif out.rows != rows or out.K != K:
-        raise ValueError(f"the output is a matrix of {out.rows} x {out.K}, x is {rows} x {K}")
+    out = _mx4_out(out, rows, K, x.device, stream)
+    _need_gpu(x, out.blob)
     status = lib.hlq_mx4_quantize(rows, K, ptr, dtype, ld, out._ptr, out._bytes, _stream_ptr(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_quantize", status)
@@ -420,10 +440,11 @@ def hlq_mx4_quantize(x, out: Mx4 | None = None, stream=None) -> Mx4:
 def hlq_mx4_dequantize(m: Mx4, y=None, dtype=None, stream=None):
     """The values [rows, K] that a matrix stands for, in y or a new tensor of `dtype` (f32 by default)."""
     if y is None:
-        y = torch.empty((m.rows, m.K), dtype=dtype or torch.float32, device=m.blob.device)
+        y = _empty((m.rows, m.K), dtype or torch.float32, m.blob.device, stream)
     rows, K, ptr, dtype, ld = _matrix(y)
     if rows != m.rows or K != m.K:
         raise ValueError(f"y has shape {tuple(y.shape)}, the matrix is {m.rows} x {m.K}")
+    _need_gpu(y, m.blob)
     status = lib.hlq_mx4_dequantize(rows, K, m._ptr, ptr, dtype, ld, _stream_ptr(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_dequantize", status)
@@ -436,17 +457,16 @@ def hlq_mx4_pack(codes, scales, K: int, out: Mx4 | None = None, stream=None) -> 
     for name, t, least in (("codes", codes, (K + 1) // 2), ("scales", scales, (K + 31) // 32)):
         if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < least or (t.shape[1] > 1 and t.stride(1) != 1):
             raise ValueError(f"{name}: expected uint8 of shape ({rows}, at least {least}), rows contiguous, got {t.dtype} {tuple(t.shape)}")
-    if out is None:
-        out = alloc_mx4(rows, K, codes.device)
-    elif out.rows != rows or out.K != K:
-        raise ValueError(f"the output is a matrix of {out.rows} x {out.K}, not {rows} x {K}")
+    out = _mx4_out(out, rows, K, codes.device, stream)
+    _need_gpu(codes, scales, out.blob)
     _check("hlq_mx4_pack", lib.hlq_mx4_pack(rows, K, _ptr(codes), codes.stride(0), _ptr(scales), scales.stride(0), out._ptr, out._bytes, _stream_ptr(stream)))
     return out
 
 
 def hlq_mx4_unpack(m: Mx4, stream=None):
-    codes = torch.empty((m.rows, (m.K + 1) // 2), dtype=torch.uint8, device=m.blob.device)
-    scales = torch.empty((m.rows, (m.K + 31) // 32), dtype=torch.uint8, device=m.blob.device)
+    _need_gpu(m.blob)
+    codes = _empty((m.rows, (m.K + 1) // 2), torch.uint8, m.blob.device, stream)
+    scales = _empty((m.rows, (m.K + 31) // 32), torch.uint8, m.blob.device, stream)
     _check("hlq_mx4_unpack", lib.hlq_mx4_unpack(m.rows, m.K, m._ptr, _ptr(codes), _ptr(scales), _stream_ptr(stream)))
     return codes, scales
 
@@ -459,8 +479,9 @@ def mx4_workspace_bytes(N: int, K: int, experts: int, x_rows: int, rows: int) ->
 
 def alloc_mx4_workspace(W: Mx4, x_rows: int, rows: int | None = None, experts: int = 1, stream=None):
     """Workspace for products with W of up to x_rows activation rows and `rows` result rows (the same if not given)."""
-    return _new_workspace(mx4_workspace_bytes(W.rows // experts, W.K, experts, x_rows, x_rows if rows is None else rows),
-                          W.blob.device, stream)
+    ws = _empty(mx4_workspace_bytes(W.rows // experts, W.K, experts, x_rows, x_rows if rows is None else rows), torch.uint8, W.blob.device, stream)
+    _check("hlq_workspace_init", lib.hlq_workspace_init(_ptr(ws), ws.numel(), _stream_ptr(stream)))
+    return ws
 
 
 def _operand(X):
@@ -468,10 +489,10 @@ def _operand(X):
     return (X.rows, X.K, X._ptr, HLQ_MX4, 0) if type(X) is Mx4 else _matrix(X)
 
 
-def _product_out(W: Mx4, X, R: int, cols: int, out_dtype):
+def _product_out(W: Mx4, X, R: int, cols: int, out_dtype, stream):
     if out_dtype is None:
         out_dtype = torch.float32 if type(X) is Mx4 else X.dtype
-    return torch.empty((R, cols), dtype=out_dtype, device=W.blob.device)
+    return _empty((R, cols), out_dtype, W.blob.device, stream)
 
 
 def hlq_mx4_gemm(W: Mx4, X, Y=None, gated: bool = False, out_dtype=None, ws=None, stream=None):
@@ -480,12 +501,13 @@ def hlq_mx4_gemm(W: Mx4, X, Y=None, gated: bool = False, out_dtype=None, ws=None
     N = W.rows
     cols = N // 2 if gated else N
     if Y is None:
-        Y = _product_out(W, X, M, cols, out_dtype)
+        Y = _product_out(W, X, M, cols, out_dtype, stream)
     y_rows, y_cols, y, ytype, ldy = _matrix(Y)
     if K != W.K or y_rows != M or y_cols != cols:
         raise ValueError(f"X is {M} x {K}, W {N} x {W.K}, Y {y_rows} x {y_cols}{' (gated)' if gated else ''}")
     if ws is None:
         ws = alloc_mx4_workspace(W, M, stream=stream)
+    _need_gpu(W.blob, X.blob if type(X) is Mx4 else X, Y, ws)
     status = lib.hlq_mx4_gemm(N, K, W._ptr, M, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0, ws.data_ptr(), ws.numel(), _stream_ptr(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_gemm", status)
@@ -497,29 +519,30 @@ class Route:
 
     __slots__ = ("ids", "weights", "offsets", "rows", "slots", "ws", "T", "E", "k", "_args")
 
-    def __init__(self, T: int, E: int, k: int, device="cuda"):
+    def __init__(self, T: int, E: int, k: int, device="cuda", stream=None):
         n = ctypes.c_size_t()
         _check("hlq_route_workspace_bytes", lib.hlq_route_workspace_bytes(T, E, k, ctypes.byref(n)))
         self.T, self.E, self.k = T, E, k
-        self.ids, self.slots = (torch.empty((T, k), dtype=torch.int32, device=device) for _ in range(2))
-        self.weights = torch.empty((T, k), dtype=torch.float32, device=device)
-        self.offsets = torch.empty(E + 1, dtype=torch.int32, device=device)
-        self.rows = torch.empty(T * k, dtype=torch.int32, device=device)
-        self.ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+        self.ids, self.slots = (_empty((T, k), torch.int32, device, stream) for _ in range(2))
+        self.weights = _empty((T, k), torch.float32, device, stream)
+        self.offsets = _empty(E + 1, torch.int32, device, stream)
+        self.rows = _empty(T * k, torch.int32, device, stream)
+        self.ws = _empty(n.value, torch.uint8, device, stream)
         self._args = tuple(_ptr(t) for t in (self.ids, self.weights, self.offsets, self.rows, self.slots, self.ws)) + (n.value,)
 
 
-def alloc_route(T: int, E: int, k: int, device="cuda") -> Route:
-    return Route(T, E, k, device)
+def alloc_route(T: int, E: int, k: int, device="cuda", stream=None) -> Route:
+    return Route(T, E, k, device, stream)
 
 
 def hlq_route(logits, k: int, renorm: bool = True, out: Route | None = None, stream=None) -> Route:
     """The k experts of each token by its logits [T, E], their weights, and the tokens grouped by expert."""
     T, E, ptr, dtype, ld = _matrix(logits)
     if out is None:
-        out = Route(T, E, k, logits.device)
+        out = Route(T, E, k, logits.device, stream)
     elif out.T != T or out.E != E or out.k != k:
         raise ValueError(f"the output is for {out.T} tokens, {out.E} experts, {out.k} each")
+    _need_gpu(logits, out.offsets)
     status = lib.hlq_route(T, E, k, ptr, dtype, ld, 1 if renorm else 0, *out._args, _stream_ptr(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_route", status)
@@ -542,12 +565,15 @@ def hlq_expert_gemm(W: Mx4, offsets, X, Y=None, rows=None, gated: bool = False, 
     N = W.rows // E
     cols = N // 2 if gated else N
     if Y is None:
-        Y = _product_out(W, X, R, cols, out_dtype)
+        Y = _product_out(W, X, R, cols, out_dtype, stream)
     y_rows, y_cols, y, ytype, ldy = _matrix(Y)
     if K != W.K or y_rows != R or y_cols != cols:
         raise ValueError(f"X is {x_rows} x {K}, a matrix of W {N} x {W.K}, Y {y_rows} x {y_cols} for {R} rows{' (gated)' if gated else ''}")
     if ws is None:
         ws = alloc_mx4_workspace(W, x_rows, R, E, stream)
+    _need_gpu(W.blob, offsets, X.blob if type(X) is Mx4 else X, Y, ws)
+    if rows is not None:
+        _need_gpu(rows)
     status = lib.hlq_expert_gemm(E, N, K, W._ptr, offsets.data_ptr(), rows_ptr, R, x_rows, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0,
                                  ws.data_ptr(), ws.numel(), _stream_ptr(stream))
     if status != HLQ_OK:
@@ -562,10 +588,11 @@ def hlq_expert_combine(Y, slots, weights, out=None, out_dtype=None, stream=None)
     if weights.shape != slots.shape or slots.dtype != torch.int32 or weights.dtype != torch.float32 or not (slots.is_contiguous() and weights.is_contiguous()):
         raise ValueError(f"slots and weights: contiguous int32 and float32 of one shape, got {slots.dtype} {tuple(slots.shape)} and {weights.dtype} {tuple(weights.shape)}")
     if out is None:
-        out = torch.empty((T, D), dtype=out_dtype or Y.dtype, device=Y.device)
+        out = _empty((T, D), out_dtype or Y.dtype, Y.device, stream)
     o_rows, o_cols, o, otype, ldo = _matrix(out)
     if o_rows != T or o_cols != D:
         raise ValueError(f"out has shape {tuple(out.shape)}, the result is {T} x {D}")
+    _need_gpu(Y, slots, weights, out)
     status = lib.hlq_expert_combine(T, k, D, R, y, ytype, ldy, slots.data_ptr(), weights.data_ptr(), o, otype, ldo, _stream_ptr(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_expert_combine", status)

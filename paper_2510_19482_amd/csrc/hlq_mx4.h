@@ -135,6 +135,21 @@ __device__ __forceinline__ uint32_t mx4_codes(const float (&v)[8], uint32_t byte
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6], v[7], s, 3);
 }
 
+// as _Float16 x 8, __bf16 x 8, float x 8; 16 bytes at a time, not to be kept in the caches
+template <class T>
+__device__ __forceinline__ void mx4_stream8(const T *p, T (&v)[8])
+{
+    typedef uint32_t four __attribute__((ext_vector_type(4)));
+    constexpr int N = sizeof(T) / 2;
+    struct alignas(16) Eight { T v[8]; };
+    struct alignas(16) Raw { four r[N]; } raw;
+#pragma unroll
+    for (int i = 0; i < N; ++i) raw.r[i] = __builtin_nontemporal_load((const four *)p + i);
+    const Eight e = __builtin_bit_cast(Eight, raw);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = e.v[i];
+}
+
 // Eight values at p of a row that ends `left` values on (left <= 0: none); past the end zeros.  ALIGNED: p is 16-byte aligned.
 template <bool ALIGNED, class T>
 __device__ __forceinline__ void mx4_load8(const T *p, int left, T (&v)[8])
@@ -173,5 +188,24 @@ __device__ __forceinline__ void mx4_store(void *y, int type, int64_t at, const f
         if (whole) *(uint2 *)p = make_uint2(b[0] | (uint32_t)b[1] << 16, b[2] | (uint32_t)b[3] << 16);
         else
             for (int i = 0; i < n; ++i) p[i] = b[i];
+    }
+}
+
+// eight successive results of a row that has `left` more, in 16-byte stores if whole and aligned, not to be kept in the caches
+__device__ __forceinline__ void mx4_store8(void *y, int type, int64_t at, const float *v, int left, bool aligned)
+{
+    typedef uint32_t four __attribute__((ext_vector_type(4)));
+    if (left < 8 || !aligned) {
+        mx4_store(y, type, at, v, left < 4 ? left : 4, false);
+        if (left > 4) mx4_store(y, type, at + 4, v + 4, left < 8 ? left - 4 : 4, false);
+    } else if (type == HLQ_F32) {
+        typedef float quad __attribute__((ext_vector_type(4)));
+        __builtin_nontemporal_store((quad){v[0], v[1], v[2], v[3]}, (quad *)((float *)y + at));
+        __builtin_nontemporal_store((quad){v[4], v[5], v[6], v[7]}, (quad *)((float *)y + at + 4));
+    } else {
+        uint32_t b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = type == HLQ_F16 ? __builtin_bit_cast(uint16_t, (_Float16)v[i]) : __builtin_bit_cast(uint16_t, (__bf16)v[i]);
+        __builtin_nontemporal_store((four){b[0] | b[1] << 16, b[2] | b[3] << 16, b[4] | b[5] << 16, b[6] | b[7] << 16}, (four *)((uint16_t *)y + at));
     }
 }

@@ -22,7 +22,8 @@ hlq_mx4_quantize_kernel(const typename Mx4Type<T>::type *__restrict__ x, int64_t
         const int panel = (int)(it - quad * panels), k = panel * MX4_PANEL_K + j * 8;
         if (row >= rows) continue;
         typename Mx4Type<T>::type v[8];
-        mx4_load8<ALIGNED>(x + row * ldx + k, K - k, v);
+        if (ALIGNED && k + 8 <= K) mx4_stream8(x + row * ldx + k, v);
+        else mx4_load8<ALIGNED>(x + row * ldx + k, K - k, v);
         const uint32_t byte = mx4_scale_of(mx4_quad_max(mx4_top_bits(v)));
         const int64_t at = panel * rows + row;
         *(uint32_t *)(codes + at * 64 + j * 4) = mx4_codes(v, byte);
@@ -61,7 +62,13 @@ hlq_mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__re
             out.v[i] = (V)(byte == 255 ? __builtin_nanf("") : v);
         }
         V *p = y + row * ldy + k;
-        if (ALIGNED && k + 8 <= K) *(Eight *)p = out;
+        if (ALIGNED && k + 8 <= K) {
+            typedef uint32_t four __attribute__((ext_vector_type(4)));
+            struct alignas(16) Raw { four r[sizeof(V) / 2]; };
+            const Raw raw = __builtin_bit_cast(Raw, out);
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(V) / 2; ++i) __builtin_nontemporal_store(raw.r[i], (four *)p + i);
+        }
         else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)

@@ -168,7 +168,7 @@ hlq_status launch(const Mx4Product &a, hipStream_t st)
     int waves = XT == HLQ_MX4 ? 4 : MOST;
     if (waves < share) waves = share;
     const int per = waves / share, groups = (col_tiles + per - 1) / per;
-    if (row_tiles * groups > INT32_MAX / 1024) return HLQ_ERR_UNSUPPORTED;
+    if (row_tiles * groups > (int64_t)(UINT32_MAX / 1024)) return HLQ_ERR_UNSUPPORTED;   // threads of a launch: below 2^32
     size_t lds = share > 1 ? (size_t)waves * MT * CT * (GATED ? 2 : 1) * 1024 : 0;
     if (XT != HLQ_MX4) lds += (size_t)(a.R < 16 ? a.R : 16) * a.panels * 68;
     hlq_mx4_few_kernel<XT, GATED, MT, CT><<<(unsigned)(row_tiles * groups), 64 * waves, lds, st>>>(a, groups, share);

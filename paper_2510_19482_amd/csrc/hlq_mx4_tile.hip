@@ -284,7 +284,7 @@ hlq_status launch(const Mx4Product &a, const Mx4TilePlan &p, bool gated, void *w
     constexpr size_t lds = (size_t)tile_stage(TM, TN, GM, GN) * BUFFERS;
     const Tiles t{p.col_tiles, p.row_tiles, p.splits, p.share, (int *)ws, (float *)((char *)ws + p.partial_at)};
     const int64_t blocks = (int64_t)p.col_tiles * p.row_tiles * p.splits;
-    if (blocks > INT32_MAX / 1024) return HLQ_ERR_UNSUPPORTED;
+    if (blocks > (int64_t)(UINT32_MAX / 256)) return HLQ_ERR_UNSUPPORTED;   // threads of a launch: below 2^32
     auto kernel = gated ? hlq_mx4_tile_kernel<TM, TN, GM, GN, BUFFERS, CUT, true> : hlq_mx4_tile_kernel<TM, TN, GM, GN, BUFFERS, CUT, false>;
     kernel<<<(unsigned)blocks, 64 * GM * GN, lds, st>>>(a, t);
     return hlq_hip_status(hipGetLastError());

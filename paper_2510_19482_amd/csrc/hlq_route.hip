@@ -334,7 +334,10 @@ hlq_expert_combine_kernel(const Combine a, int64_t items)
                     const int s = a.slots[t * a.k + i + j];
                     has[j] = s >= 0 && s < a.R;
                     w[j] = a.weights[t * a.k + i + j];
-                    if (has[j]) mx4_load8<ALIGNED>((const V *)a.y + s * a.ld + d, a.D - d, v[j]);
+                    if (has[j]) {
+                        if (ALIGNED && d + 8 <= a.D) mx4_stream8((const V *)a.y + s * a.ld + d, v[j]);
+                        else mx4_load8<ALIGNED>((const V *)a.y + s * a.ld + d, a.D - d, v[j]);
+                    }
                 }
             }
 #pragma unroll
@@ -343,9 +346,7 @@ hlq_expert_combine_kernel(const Combine a, int64_t items)
 #pragma unroll
                     for (int c = 0; c < 8; ++c) sum[c] = fmaf(w[j], (float)v[j][c], sum[c]);
         }
-        const int left = a.D - d;
-        mx4_store(a.out, a.otype, t * a.ldo + d, sum, left < 4 ? left : 4, left >= 4 && a.out_aligned);
-        if (left > 4) mx4_store(a.out, a.otype, t * a.ldo + d + 4, sum + 4, left < 8 ? left - 4 : 4, left >= 8 && a.out_aligned);
+        mx4_store8(a.out, a.otype, t * a.ldo + d, sum, a.D - d, a.out_aligned);
     }
 }
 
@@ -438,7 +439,7 @@ hlq_status hlq_expert_combine(int64_t T, int32_t k, int32_t D, int64_t R, const 
     if ((uintptr_t)Y % (unsigned)hlq_dtype_bytes(ytype) || (uintptr_t)out % (unsigned)hlq_dtype_bytes(otype) || (((uintptr_t)slots | (uintptr_t)weights) & 3u))
         return HLQ_ERR_BAD_STRIDE;
     Combine a{T, k, D, (D + 7) / 8, R, Y, ldy, slots, weights, out, otype, ldo, false};
-    a.out_aligned = (uintptr_t)out % (4u * (unsigned)hlq_dtype_bytes(otype)) == 0 && (T == 1 || ldo % 4 == 0);
+    a.out_aligned = ((uintptr_t)out & 15u) == 0 && (T == 1 || ldo * hlq_dtype_bytes(otype) % 16 == 0);
     const bool aligned = ((uintptr_t)Y & 15u) == 0 && (R <= 1 || ldy * hlq_dtype_bytes(ytype) % 16 == 0);
     const hipStream_t st = (hipStream_t)stream;
     hlq_clear_stale_error();

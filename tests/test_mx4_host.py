@@ -144,3 +144,12 @@ def test_binding_refuses_what_it_cannot_hand_over():
         B.hlq_expert_gemm(m, torch.zeros(3, dtype=torch.int64), torch.zeros((2, 64)))
     with pytest.raises(ValueError):
         B.hlq_expert_combine(torch.zeros((4, 8)), torch.zeros((2, 2), dtype=torch.int64), torch.zeros((2, 2)))
+
+
+@pytest.mark.parametrize("part", ["hlq_mx4_quantize_kernel", "hlq_mx4_dequantize_kernel", "hlq_mx4_few_kernel", "hlq_mx4_tile_kernel", "hlq_route_top_kernel",
+                                  "hlq_route_place_kernel", "hlq_expert_combine_kernel"])
+def test_no_scratch_memory(part):
+    from test_kernel_resources import kernels
+    mine = {n: k for n, k in kernels().items() if part in n}
+    assert mine
+    assert {n: k[".private_segment_fixed_size"] for n, k in mine.items() if k[".private_segment_fixed_size"]} == {}
