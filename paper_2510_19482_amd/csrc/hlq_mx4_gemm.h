@@ -25,6 +25,32 @@ struct Mx4Product {
 struct Mx4RowTile {
     int e, row0, n;
 };
+// rows [lo, hi) of expert e, within 0..R - 1; none for e >= E
+__device__ __forceinline__ void mx4_expert_rows(const Mx4Product &a, int e, int &lo, int &hi)
+{
+    lo = hi = a.R;
+    if (e < a.E) {
+        lo = a.offsets[e];
+        hi = a.offsets[e + 1];
+    }
+    lo = lo < 0 ? 0 : lo > a.R ? a.R : lo;
+    hi = hi < lo ? lo : hi > a.R ? a.R : hi;
+}
+// how many there are, in a scalar register
+template <int BM>
+__device__ __forceinline__ int mx4_count_row_tiles(const Mx4Product &a)
+{
+    const int lane = (int)(threadIdx.x & 63u);
+    int n = 0;
+    for (int base = 0; base < a.E; base += 64) {
+        int lo, hi;
+        mx4_expert_rows(a, base + lane, lo, hi);
+        n += (hi - lo) / BM + ((hi - lo) % BM != 0);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
+    return __builtin_amdgcn_readfirstlane(n);
+}
 template <int BM>
 __device__ __forceinline__ Mx4RowTile mx4_row_tile(const Mx4Product &a, int tile)
 {
@@ -36,14 +62,8 @@ __device__ __forceinline__ Mx4RowTile mx4_row_tile(const Mx4Product &a, int tile
     const int lane = (int)(threadIdx.x & 63u);
     int before = 0;
     for (int base = 0; base < a.E; base += 64) {
-        const int e = base + lane;
-        int lo = a.R, hi = a.R;
-        if (e < a.E) {
-            lo = a.offsets[e];
-            hi = a.offsets[e + 1];
-        }
-        lo = lo < 0 ? 0 : lo > a.R ? a.R : lo;
-        hi = hi < lo ? lo : hi > a.R ? a.R : hi;
+        int lo, hi;
+        mx4_expert_rows(a, base + lane, lo, hi);
         int upto = (hi - lo) / BM + ((hi - lo) % BM != 0);
         const int mine = upto;
 #pragma unroll

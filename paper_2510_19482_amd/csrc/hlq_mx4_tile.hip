@@ -45,15 +45,17 @@ hlq_mx4_tile_kernel(const Mx4Product a, const Tiles t)
     const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int r = lane & 31, g = lane >> 5, wm = wave / GN, wn = wave % GN;
 
-    const int tiles = t.col_tiles * t.row_tiles;
+    // the launch is for the most row tiles that the experts' rows can make; those there are, are dealt out to all XCDs
+    const int made = a.offsets ? mx4_count_row_tiles<BM>(a) : t.row_tiles;
+    const int row_tiles = made < t.row_tiles ? made : t.row_tiles, tiles = t.col_tiles * row_tiles;   // never more than there is room for
+    if ((int)blockIdx.x >= tiles * t.splits) return;
     const int id = xcd_order((int)blockIdx.x, tiles * t.splits);
     const int split = id % t.splits, tile_id = id / t.splits;
     // bands of 8 row tiles, columns after columns
-    const int band = tile_id / (8 * t.col_tiles), first = band * 8, high = t.row_tiles - first < 8 ? t.row_tiles - first : 8;
+    const int band = tile_id / (8 * t.col_tiles), first = band * 8, high = row_tiles - first < 8 ? row_tiles - first : 8;
     const int in_band = tile_id - first * t.col_tiles;
     const int nt = in_band / high;
     const Mx4RowTile tile = mx4_row_tile<BM>(a, first + in_band % high);
-    if (tile.n == 0) return;
 
     // row of W for row j of the tile; gated: 32 rows of the first half, then the 32 of the second that go with them
     auto w_row = [&](int j) {

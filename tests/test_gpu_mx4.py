@@ -306,6 +306,22 @@ def test_rows_past_the_experts_are_not_written_and_bad_indexes_stay_inside(R):
     check(out[counts[0]:], a[counts[0]:], w[2 * N:], False, "f32")
 
 
+@pytest.mark.parametrize("R,N,K", [(40, 64, 128), (700, 300, 256), (90, 200, 2000)])
+def test_offsets_that_overlap_write_rows_only(R, N, K):
+    # offsets are the caller's to keep ascending; whatever they hold, only the R rows of the result are written
+    E = 9
+    x = on_gpu(activations(R, K), "bf16")
+    codes, scales = stored(E * N, K)
+    W = matrix(codes, scales, K)
+    out = torch.full((R + 8, N), 3.0, device="cuda")
+    for off in ([0, R, 0, R, 0, R, 0, R, 0, R], [-5, R + 5, -5, 1 << 30, -(1 << 30), R, R, 0, 0, R], [R] * 10, [0] * 9 + [R]):
+        B.hlq_expert_gemm(W, torch.tensor(off, dtype=torch.int32, device="cuda"), x, out[4:4 + R])
+        torch.cuda.synchronize()
+        assert (out[:4] == 3).all() and (out[4 + R:] == 3).all()
+    # the last: everything is the last expert's
+    check(out[4:4 + R], O.rounded(host(x)), O.dequantize(codes, scales, K)[-N:], False, "f32")
+
+
 # ---- router and combination -----------------------------------------------------------------------------------------
 
 def routed(r):
