@@ -105,6 +105,14 @@ __device__ __forceinline__ int prefix(const int *count, int *first, int n)
     return before;
 }
 
+// of N keys, as a tree
+template <int N>
+__device__ __forceinline__ uint64_t max_of(const uint64_t *key)
+{
+    if constexpr (N == 1) return key[0];
+    else return max_key(max_of<N / 2>(key), max_of<N - N / 2>(key + N / 2));
+}
+
 // V: logits a lane holds
 template <int T, int V>
 __global__ void __launch_bounds__(16 * CHUNK)
@@ -132,17 +140,14 @@ hlq_route_top_kernel(const Route a)
         float top = 0.f, sum = 0.f;
         int found = 0;
         for (; found < a.k; ++found) {
-            uint64_t best = key[0];
-#pragma unroll
-            for (int j = 1; j < V; ++j) best = max_key(best, key[j]);
-            best = row_max(best);
-            if (best == 0ull) break;
+            const uint64_t best = row_max(max_of<V>(key));
+            if (best < NORMAL) break;
             const float v = value_of((uint32_t)(best >> 10));
             if (found == 0) {
                 top = v;
                 if (!a.renorm) {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) sum += key[j] ? expf(value_of((uint32_t)(key[j] >> 10)) - top) : 0.f;
+                    for (int j = 0; j < V; ++j) sum += key[j] >= NORMAL ? expf(value_of((uint32_t)(key[j] >> 10)) - top) : 0.f;
                 }
             }
             if (l == 0) {
@@ -150,7 +155,10 @@ hlq_route_top_kernel(const Route a)
                 values[t * a.k + found] = v;
             }
 #pragma unroll
-            for (int j = 0; j < V; ++j) key[j] = key[j] == best ? 0ull : key[j];
+            for (int j = 0; j < V; ++j) {   // the lower words differ, by the expert's number: taken, it is below all that are left
+                const uint32_t low = (uint32_t)key[j];
+                key[j] = low | (uint64_t)(low == (uint32_t)best ? 0u : (uint32_t)(key[j] >> 32)) << 32;
+            }
         }
         // what lane 0 of the row wrote is there for the others: they are of one wavefront, whose LDS accesses keep their order
         __builtin_amdgcn_wave_barrier();
