@@ -164,8 +164,8 @@ hlq_status launch(const Mx4Product &a, hipStream_t st)
     // wavefronts that share a column tile: about MOST wavefronts a compute unit in all, AHEAD panels or more each
     int share = 1;
     while (share < MOST && row_tiles * col_tiles * share < 256 * MOST && share * few_ahead(MT, CT) < a.panels) share *= 2;
-    // x quantized inside: by fewer workgroups of more wavefronts
-    int waves = XT == HLQ_MX4 ? 4 : MOST;
+    // x quantized inside: by wavefronts enough. us with 8 / 16: one row, 4096 x 4096 4.4 / 5.2; four rows, 6144 x 4096 7.1 / 6.2
+    int waves = XT == HLQ_MX4 ? 4 : (int64_t)((a.R + a.E - 1) / a.E) * a.K > 8192 ? 16 : 8;
     if (waves < share) waves = share;
     const int per = waves / share, groups = (col_tiles + per - 1) / per;
     if (row_tiles * groups > (int64_t)(UINT32_MAX / 1024)) return HLQ_ERR_UNSUPPORTED;   // threads of a launch: below 2^32
