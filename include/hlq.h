@@ -286,7 +286,8 @@ HLQ_API hlq_status hlq_lut_gemm(const hlq_desc *d, const void *packed, const uin
  * is, activations in it too.  A matrix lies in one blob of hlq_mx4_bytes() bytes, 16-byte aligned, whose layout is the
  * library's (rows padded to 128 k): made by hlq_mx4_quantize from floats, or by hlq_mx4_pack from arrays in the exchange form.
  * The conventions at the top of this file hold: device pointers, asynchronous on `stream`, arguments checked on the host first.
- * Limits: K <= 2^21, rows <= 2^31 (a product's x_rows and rows below 2^31 - 256), N <= 2^20, 1024 experts, k <= 64. */
+ * Limits: K <= 2^21, rows <= 2^31 (a product's x_rows and rows below 2^31 - 256), N <= 2^20, 1024 experts, k <= 64, 2^27 tokens
+ * to route. */
 typedef enum {
     HLQ_F16 = 0,
     HLQ_F32 = 1,

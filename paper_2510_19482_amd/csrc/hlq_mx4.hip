@@ -4,7 +4,8 @@
 //
 // Quantizing reads a value once and writes 4.25 bits: it is bound by memory.  A wavefront takes a panel of four rows: a lane has
 // eight successive values (one 16-byte load of 16-bit types, two of fp32), four lanes a block, whose largest magnitudes meet by
-// two quad permutations; codes leave as a dword a lane, 256 contiguous bytes.
+// two quad permutations; codes leave as a dword a lane, 256 contiguous bytes.  The values are read, and in dequantizing written, past
+// the caches: 8192 x 8192 f16 35 us (170 MB, 4.9 TB/s; through them 38), back 34 (through them 42).
 #include "hlq_mx4.h"
 
 namespace {

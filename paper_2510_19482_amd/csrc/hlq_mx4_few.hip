@@ -1,11 +1,15 @@
-// Products of MX4 matrices for few rows (an expert's few rows, a decoded batch): up to 16 rows a workgroup.
+// Products of MX4 matrices for few rows (a decoded token or batch, an expert's few rows): up to 64 rows a workgroup, no LDS in the loop.
 //
 //   y[r, n] = sum over blocks b of 2^(a_rb + w_nb - 254) sum_{k in b} A[r, k] W[n, k]        (gated: silu(y[r, n]) y[r, N / 2 + n])
 //
-// Bound by the weights' bytes.  A wavefront holds 16 rows of W (results' columns) and a share of the panels; the wavefronts of a
-// workgroup share the columns and add their sums through LDS, in order.  Weights go straight to registers in the form that the
-// matrix core takes.  Activations that come as f16, bf16 or f32 are quantized by the lane that feeds them to the matrix core:
-// it holds whole blocks of 32 of a row, so no lane needs another's.
+// Bound by the weights' bytes.  A wavefront holds 16 or 32 rows of W (results' columns), 16 to 64 rows of x and a share of the
+// panels; the wavefronts of a workgroup that share the columns add their sums through LDS, in order.  Operands go straight to
+// registers in the form that v_mfma_scale_f32_16x16x128_f8f6f4 takes, panels of several steps requested together.  A few rows
+// that come as f16, bf16 or f32 are quantized by the workgroup into LDS while its first weights come; that saves a launch.
+// us, one bf16 row: 4096 x 4096 4.4, 6144 x 4096 5.3, 28672 x 4096 12.3 (62 MB, 5.1 TB/s), 4096 x 14336 7.2;
+// 16 rows of 32 experts (14 of them used), gated 4096 x 4096: 25 (118 MB, 4.7 TB/s).
+// With more rows what a compute unit loads into registers (43 bytes a nanosecond) takes over: 32 rows 4096 x 14336 10.3, 128 rows 4096 x 4096 7.3.
+// Loads that bypass the caches for the weights: no difference (28672 x 4096 12.2 -> 12.7).
 #include "hlq_mx4_gemm.h"
 
 namespace {

@@ -20,6 +20,7 @@ size_t up256(size_t n) { return (n + 255u) & ~(size_t)255u; }
 // 15.2 / 13.1 (128 x 128); 28672 x 4096: 64 rows 13.0 / 15.5 (32 x 128); 4096 x 14336: 32 rows 10.3 / 11.1 (2 x 1), 128 rows
 // 15.2 / 15.6 (32 x 128, K in four).
 constexpr int MOST_SPLITS = 8, LEAST_SHARE = 4, MOST_CUT = 512;   // of K, panels of one, workgroups of a product whose K is cut
+constexpr int64_t MOST_GROUPS = 1 << 22, MOST_TILES = 1 << 23;    // workgroups, so that a launch stays below 2^32 threads
 
 struct Choice {
     int row_blocks, col_blocks;   // few rows, if row_blocks > 0
@@ -45,6 +46,7 @@ Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
     static const Few few[] = {{1, 1, 43, 5.5}, {2, 1, 43, 5.0}, {2, 2, 43, 4.6}, {4, 2, 36, 4.2}};
     for (const auto &k : few) {
         const int64_t cols = gated ? N / 2 : N, col_tiles = (cols + 16 * k.cols - 1) / (16 * k.cols);
+        if (mx4_row_tiles(R, E, 16 * k.rows) * col_tiles > MOST_GROUPS) continue;
         const double groups = row_tiles(16 * k.rows) * (double)col_tiles, rounds = groups < 1024 ? (double)(((int64_t)groups + 255) / 256) : groups / 256;
         const double loads = rounds * panels * 1.1 * (k.rows + k.cols * (gated ? 2 : 1)) / k.load, stream = weights / k.stream;
         const double t = 2.5 + (loads > stream ? loads : stream);
@@ -62,6 +64,7 @@ Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
     const int64_t width = gated ? (N / 2 + 31) / 32 * 64 : N;   // gated halves are interleaved 32 columns at a time
     for (const auto &k : tiles) {
         const int64_t col_tiles = (width + k.BN - 1) / k.BN;
+        if (mx4_row_tiles(R, E, k.BM) * col_tiles > MOST_TILES && k.BN < 256) continue;
         const double count = row_tiles(k.BM) * (double)col_tiles;
         for (int want = 1; want <= (k.passes ? MOST_SPLITS : 1); want *= 2) {
             const int share = (panels + want - 1) / want, splits = (panels + share - 1) / share;

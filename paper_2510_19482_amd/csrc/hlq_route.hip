@@ -7,6 +7,8 @@
 // Grouping is a counting sort, stable and without atomics whose order could matter: a token takes an expert at most once, so
 // for the 32 tokens of a chunk an expert's rows are a 32-bit mask, its count the bits of it, and a row's place among them the
 // bits below its own.  Chunks' counts are added up by each workgroup that places rows (up to 512 chunks) or by a scan in between.
+// 8192 tokens, 256 experts, k = 8, f32: choices 9.4 us (8 MB; two wavefronts a SIMD in dependent maxima; with 64 lanes a token and
+// ballots 19), places 6.0; 32 tokens, 64 experts: 4.5 in one launch.
 #include "hlq_mx4.h"
 
 namespace {
@@ -14,6 +16,7 @@ namespace {
 constexpr int CHUNK = 32;           // tokens, bits of a mask; of one workgroup
 constexpr int DIRECT_CHUNKS = 512;  // up to here each workgroup of the second kernel adds the counts by itself, in 16 bits
 constexpr int PLACE_THREADS = 512;
+constexpr int64_t MOST_TOKENS = (int64_t)1 << 27;   // a launch stays below 2^32 threads
 
 struct Route {
     int64_t T;
@@ -321,7 +324,8 @@ struct Combine {
 };
 
 // y[t, d] = sum_i weights[t, i] Y[slots[t, i], d], i ascending, fp32: a thread has eight successive d of a token.  Bound by the
-// bytes of Y; the loads of four experts are in flight together.
+// bytes of Y; the loads of four experts are in flight together, and pass the caches by.  8192 tokens, 8 of 4096, bf16: 121 us
+// (605 MB, 5.0 TB/s; through the caches 131).
 template <int T, bool ALIGNED>
 __global__ void __launch_bounds__(256)
 hlq_expert_combine_kernel(const Combine a, int64_t items)
@@ -370,7 +374,7 @@ void launch_combine(const Combine &a, bool aligned, hipStream_t st)
 hlq_status check_route(int64_t T, int32_t E, int32_t k)
 {
     if (T < 0 || E < 1 || k < 1 || k > E) return HLQ_ERR_BAD_DESC;
-    if (E > HLQ_MAX_EXPERTS || k > HLQ_MAX_CHOICES || T > (((int64_t)1 << 31) - 256) / k) return HLQ_ERR_UNSUPPORTED;
+    if (E > HLQ_MAX_EXPERTS || k > HLQ_MAX_CHOICES || T > MOST_TOKENS || T > (((int64_t)1 << 31) - 256) / k) return HLQ_ERR_UNSUPPORTED;
     return HLQ_OK;
 }
 size_t counts_bytes(int64_t T, int32_t E) { return ((size_t)((T + CHUNK - 1) / CHUNK) * (size_t)((E + 3) & ~3) + 15u) & ~(size_t)15u; }
