@@ -135,31 +135,47 @@ __device__ __forceinline__ uint32_t mx4_codes(const float (&v)[8], uint32_t byte
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6], v[7], s, 3);
 }
 
-// as _Float16 x 8, __bf16 x 8, float x 8; 16 bytes at a time, not to be kept in the caches
-template <class T>
-__device__ __forceinline__ void mx4_stream8(const T *p, T (&v)[8])
+// Rows begin at any element, so 16 bytes are read and written at the alignment of one (this target takes global accesses of any
+// alignment).
+typedef uint32_t mx4_u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t mx4_u4 __attribute__((ext_vector_type(4)));
+typedef mx4_u2 mx4_u2_any __attribute__((aligned(2)));
+typedef mx4_u4 mx4_u4_any __attribute__((aligned(2)));
+template <class T> struct Mx4Eight {
+    static constexpr int N = sizeof(T) / 2;              // of 16 bytes
+    struct alignas(16) Raw { mx4_u4 r[N]; };
+    struct alignas(16) Values { T v[8]; };
+};
+// eight values at p; STREAM: not to be kept in the caches
+template <bool STREAM, class T>
+__device__ __forceinline__ void mx4_read8(const T *p, T (&v)[8])
 {
-    typedef uint32_t four __attribute__((ext_vector_type(4)));
-    constexpr int N = sizeof(T) / 2;
-    struct alignas(16) Eight { T v[8]; };
-    struct alignas(16) Raw { four r[N]; } raw;
+    using E = Mx4Eight<T>;
+    typename E::Raw raw;
 #pragma unroll
-    for (int i = 0; i < N; ++i) raw.r[i] = __builtin_nontemporal_load((const four *)p + i);
-    const Eight e = __builtin_bit_cast(Eight, raw);
+    for (int i = 0; i < E::N; ++i) {
+        const mx4_u4_any *q = (const mx4_u4_any *)(p + i * 8 / E::N);
+        if constexpr (STREAM) raw.r[i] = __builtin_nontemporal_load(q);
+        else raw.r[i] = *q;
+    }
+    const typename E::Values e = __builtin_bit_cast(typename E::Values, raw);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = e.v[i];
 }
-
-// Eight values at p of a row that ends `left` values on (left <= 0: none); past the end zeros.  ALIGNED: p is 16-byte aligned.
-template <bool ALIGNED, class T>
+template <class T>
+__device__ __forceinline__ void mx4_stream8(const typename Mx4Eight<T>::Values &e, T *p)
+{
+    using E = Mx4Eight<T>;
+    const typename E::Raw raw = __builtin_bit_cast(typename E::Raw, e);
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) __builtin_nontemporal_store(raw.r[i], (mx4_u4_any *)(p + i * 8 / E::N));
+}
+// Eight values at p of a row that ends `left` values on (left <= 0: none); past the end zeros.
+template <bool STREAM, class T>
 __device__ __forceinline__ void mx4_load8(const T *p, int left, T (&v)[8])
 {
-    if (ALIGNED && left >= 8) {
-        struct alignas(16) Eight { T v[8]; };
-        const Eight e = *(const Eight *)p;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = e.v[i];
-    } else {
+    if (left >= 8) mx4_read8<STREAM>(p, v);
+    else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (T)0.0f;
     }
@@ -171,41 +187,47 @@ __device__ __forceinline__ float mx4_gate(float g, float u)
     return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
 }
 
-// n <= 4 successive results of a row, rounded to nearest even
-__device__ __forceinline__ void mx4_store(void *y, int type, int64_t at, const float *v, int n, bool whole)
+__device__ __forceinline__ uint32_t mx4_bits16(float v, int type)
+{
+    return type == HLQ_F16 ? __builtin_bit_cast(uint16_t, (_Float16)v) : __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+// four successive results of a row that has `left` more, rounded to nearest even
+__device__ __forceinline__ void mx4_store4(void *y, int type, int64_t at, const float *v, int left)
 {
     if (type == HLQ_F32) {
+        typedef mx4_float4 any __attribute__((aligned(4)));
         float *p = (float *)y + at;
-        if (whole) *(mx4_float4 *)p = (mx4_float4){v[0], v[1], v[2], v[3]};
+        if (left >= 4) *(any *)p = (mx4_float4){v[0], v[1], v[2], v[3]};
         else
-            for (int i = 0; i < n; ++i) p[i] = v[i];
+            for (int i = 0; i < left; ++i) p[i] = v[i];
     } else {
-        uint16_t b[4];
+        uint32_t b[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            b[i] = type == HLQ_F16 ? __builtin_bit_cast(uint16_t, (_Float16)v[i]) : __builtin_bit_cast(uint16_t, (__bf16)v[i]);
+        for (int i = 0; i < 4; ++i) b[i] = mx4_bits16(v[i], type);
         uint16_t *p = (uint16_t *)y + at;
-        if (whole) *(uint2 *)p = make_uint2(b[0] | (uint32_t)b[1] << 16, b[2] | (uint32_t)b[3] << 16);
-        else
-            for (int i = 0; i < n; ++i) p[i] = b[i];
+        if (left >= 4) *(mx4_u2_any *)p = (mx4_u2){b[0] | b[1] << 16, b[2] | b[3] << 16};
+        else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < left) p[i] = (uint16_t)b[i];
+        }
     }
 }
-
-// eight successive results of a row that has `left` more, in 16-byte stores if whole and aligned, not to be kept in the caches
-__device__ __forceinline__ void mx4_store8(void *y, int type, int64_t at, const float *v, int left, bool aligned)
+// eight of them, not to be kept in the caches
+__device__ __forceinline__ void mx4_store8(void *y, int type, int64_t at, const float *v, int left)
 {
-    typedef uint32_t four __attribute__((ext_vector_type(4)));
-    if (left < 8 || !aligned) {
-        mx4_store(y, type, at, v, left < 4 ? left : 4, false);
-        if (left > 4) mx4_store(y, type, at + 4, v + 4, left < 8 ? left - 4 : 4, false);
+    if (left < 8) {
+        mx4_store4(y, type, at, v, left);
+        if (left > 4) mx4_store4(y, type, at + 4, v + 4, left - 4);
     } else if (type == HLQ_F32) {
-        typedef float quad __attribute__((ext_vector_type(4)));
-        __builtin_nontemporal_store((quad){v[0], v[1], v[2], v[3]}, (quad *)((float *)y + at));
-        __builtin_nontemporal_store((quad){v[4], v[5], v[6], v[7]}, (quad *)((float *)y + at + 4));
-    } else {
-        uint32_t b[8];
+        Mx4Eight<float>::Values e;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = type == HLQ_F16 ? __builtin_bit_cast(uint16_t, (_Float16)v[i]) : __builtin_bit_cast(uint16_t, (__bf16)v[i]);
-        __builtin_nontemporal_store((four){b[0] | b[1] << 16, b[2] | b[3] << 16, b[4] | b[5] << 16, b[6] | b[7] << 16}, (four *)((uint16_t *)y + at));
+        for (int i = 0; i < 8; ++i) e.v[i] = v[i];
+        mx4_stream8(e, (float *)y + at);
+    } else {
+        Mx4Eight<uint16_t>::Values e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e.v[i] = (uint16_t)mx4_bits16(v[i], type);
+        mx4_stream8(e, (uint16_t *)y + at);
     }
 }

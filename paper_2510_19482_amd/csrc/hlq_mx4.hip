@@ -12,7 +12,7 @@ namespace {
 
 constexpr int MX4_WAVES = 4;
 
-template <int T, bool ALIGNED>
+template <int T>
 __global__ void __launch_bounds__(64 * MX4_WAVES)
 hlq_mx4_quantize_kernel(const typename Mx4Type<T>::type *__restrict__ x, int64_t ldx, int64_t rows, int K, int panels,
                         uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, int64_t items)
@@ -23,8 +23,7 @@ hlq_mx4_quantize_kernel(const typename Mx4Type<T>::type *__restrict__ x, int64_t
         const int panel = (int)(it - quad * panels), k = panel * MX4_PANEL_K + j * 8;
         if (row >= rows) continue;
         typename Mx4Type<T>::type v[8];
-        if (ALIGNED && k + 8 <= K) mx4_stream8(x + row * ldx + k, v);
-        else mx4_load8<ALIGNED>(x + row * ldx + k, K - k, v);
+        mx4_load8<true>(x + row * ldx + k, K - k, v);
         const uint32_t byte = mx4_scale_of(mx4_quad_max(mx4_top_bits(v)));
         const int64_t at = panel * rows + row;
         *(uint32_t *)(codes + at * 64 + j * 4) = mx4_codes(v, byte);
@@ -40,7 +39,7 @@ __device__ __forceinline__ uint32_t code_bytes(uint32_t c)
 }
 
 // As in quantizing: a wavefront takes a panel of four rows, a lane eight successive values.
-template <int T, bool ALIGNED>
+template <int T>
 __global__ void __launch_bounds__(64 * MX4_WAVES)
 hlq_mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t rows, int K, int panels,
                           typename Mx4Type<T>::type *__restrict__ y, int64_t ldy, int64_t items)
@@ -55,7 +54,7 @@ hlq_mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__re
         const uint32_t c = *(const uint32_t *)(codes + at * 64 + j * 4);
         const int byte = scales[at * 4 + mx4_scale_byte(j >> 2)];
         const uint32_t even = code_bytes(c), odd = code_bytes(c >> 4);
-        struct alignas(16) Eight { V v[8]; } out;
+        typename Mx4Eight<V>::Values out;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint16_t half = (uint16_t)((i & 1 ? odd : even) >> (8 * (i >> 1)) << 8);
@@ -63,13 +62,7 @@ hlq_mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__re
             out.v[i] = (V)(byte == 255 ? __builtin_nanf("") : v);
         }
         V *p = y + row * ldy + k;
-        if (ALIGNED && k + 8 <= K) {
-            typedef uint32_t four __attribute__((ext_vector_type(4)));
-            struct alignas(16) Raw { four r[sizeof(V) / 2]; };
-            const Raw raw = __builtin_bit_cast(Raw, out);
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(V) / 2; ++i) __builtin_nontemporal_store(raw.r[i], (four *)p + i);
-        }
+        if (k + 8 <= K) mx4_stream8(out, p);
         else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -129,10 +122,8 @@ void launch_quantize(const Mx4Dims &d, const void *x, int64_t ldx, void *blob, h
     using V = typename Mx4Type<T>::type;
     const int64_t items = (d.rows + 3) / 4 * d.panels;
     uint8_t *codes = (uint8_t *)blob, *scales = codes + d.code_bytes;
-    const bool aligned = ((uintptr_t)x & 15u) == 0 && (d.rows == 1 || (ldx * (int64_t)sizeof(V)) % 16 == 0);
     const dim3 grid(grid_of(items, MX4_WAVES)), block(64 * MX4_WAVES);
-    if (aligned) hlq_mx4_quantize_kernel<T, true><<<grid, block, 0, st>>>((const V *)x, ldx, d.rows, d.K, d.panels, codes, scales, items);
-    else hlq_mx4_quantize_kernel<T, false><<<grid, block, 0, st>>>((const V *)x, ldx, d.rows, d.K, d.panels, codes, scales, items);
+    hlq_mx4_quantize_kernel<T><<<grid, block, 0, st>>>((const V *)x, ldx, d.rows, d.K, d.panels, codes, scales, items);
 }
 
 template <int T>
@@ -141,10 +132,8 @@ void launch_dequantize(const Mx4Dims &d, const void *blob, void *y, int64_t ldy,
     using V = typename Mx4Type<T>::type;
     const int64_t items = (d.rows + 3) / 4 * d.panels;
     const uint8_t *codes = (const uint8_t *)blob, *scales = codes + d.code_bytes;
-    const bool aligned = ((uintptr_t)y & 15u) == 0 && (d.rows == 1 || (ldy * (int64_t)sizeof(V)) % 16 == 0);
     const dim3 grid(grid_of(items, MX4_WAVES)), block(64 * MX4_WAVES);
-    if (aligned) hlq_mx4_dequantize_kernel<T, true><<<grid, block, 0, st>>>(codes, scales, d.rows, d.K, d.panels, (V *)y, ldy, items);
-    else hlq_mx4_dequantize_kernel<T, false><<<grid, block, 0, st>>>(codes, scales, d.rows, d.K, d.panels, (V *)y, ldy, items);
+    hlq_mx4_dequantize_kernel<T><<<grid, block, 0, st>>>(codes, scales, d.rows, d.K, d.panels, (V *)y, ldy, items);
 }
 
 // what the four calls have in common

@@ -39,8 +39,7 @@ __device__ __forceinline__ void quantize_rows(const Mx4Product &a, const Mx4RowT
         const int m = i / eights, j = i - m * eights, k = j * 8, at = (j >> 4) * tile.n + m;
         const T *p = (const T *)a.x + mx4_x_row(a, tile.row0 + m) * a.ldx + k;
         T v[8];
-        if (a.x_aligned) mx4_load8<true>(p, a.K - k, v);
-        else mx4_load8<false>(p, a.K - k, v);
+        mx4_load8<false>(p, a.K - k, v);
         const uint32_t byte = mx4_scale_of(mx4_quad_max(mx4_top_bits(v)));
         *(uint32_t *)(codes + at * 64 + (j & 15) * 4) = mx4_codes(v, byte);
         if ((lane & 3) == 0) scales[at * 4 + mx4_scale_byte((j >> 2) & 3)] = (uint8_t)byte;
@@ -125,7 +124,7 @@ hlq_mx4_few_kernel(const Mx4Product a, int groups, int share)
         float v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = GATED ? mx4_gate(p[i], up[i]) : p[i];
-        mx4_store(a.y, a.ytype, (int64_t)(tile.row0 + m * 16 + r) * a.ldy + c, v, left < 4 ? left : 4, left >= 4 && a.y_aligned);
+        mx4_store4(a.y, a.ytype, (int64_t)(tile.row0 + m * 16 + r) * a.ldy + c, v, left);
     };
     if (share == 1) {
         if (mine)

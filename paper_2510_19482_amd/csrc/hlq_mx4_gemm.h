@@ -12,12 +12,10 @@ struct Mx4Product {
     int R, x_rows;
     const void *x;          // f16, bf16 or f32 rows that the kernel quantizes; else A
     int64_t ldx;
-    bool x_aligned;
     Mx4View A;
     void *y;
     int ytype;
     int64_t ldy;
-    bool y_aligned;         // rows of the result start at 16 bytes
 };
 
 // Row tile number `tile` of tiles of BM rows that begin anew at each expert.  Every lane of the wavefront takes part and gets

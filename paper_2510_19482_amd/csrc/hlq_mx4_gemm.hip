@@ -143,7 +143,6 @@ hlq_status product(const Call &c, int32_t E, const int32_t *offsets, const int32
     a.y = c.Y;
     a.ytype = c.ytype;
     a.ldy = c.ldy;
-    a.y_aligned = ((uintptr_t)c.Y & 15u) == 0 && (R == 1 || c.ldy * hlq_dtype_bytes(c.ytype) % 16 == 0);
     int xtype = c.xtype;
     Choice how = choose(c.N, gated, a.panels, E, R);
     const bool quantize = xtype != HLQ_MX4;
@@ -155,7 +154,6 @@ hlq_status product(const Call &c, int32_t E, const int32_t *offsets, const int32
     else if (how.row_blocks == 1 && (R + E - 1) / E * c.K <= QUANTIZE_INSIDE && (R < 16 ? R : 16) * (int64_t)a.panels * 68 <= QUANTIZED_BYTES) {
         a.x = c.X;
         a.ldx = c.ldx;
-        a.x_aligned = ((uintptr_t)c.X & 15u) == 0 && (c.x_rows == 1 || c.ldx * hlq_dtype_bytes(c.xtype) % 16 == 0);
         return hlq_mx4_launch_few(a, xtype, gated, 1, 1, c.stream);
     } else {
         void *blob = (char *)c.ws + HLQ_WS_COUNTER_BYTES;

@@ -278,14 +278,13 @@ hlq_mx4_tile_kernel(const Mx4Product a, const Tiles t)
             for (int n = (int)threadIdx.x; n < ROWS * EIGHTS; n += 64 * WAVES) {
                 const int row = n / EIGHTS, c = (n % EIGHTS) * 8, m = ((row >> 5) * TM + i) * 32 + (row & 31);
                 if (m >= tile.n || col0 + c >= a.cols) continue;
-                typedef V Eight __attribute__((ext_vector_type(8)));
-                const Eight v = *(const Eight *)(out + row * PITCH + c * (int)sizeof(V));
+                const auto v = *(const typename Mx4Eight<V>::Values *)(out + row * PITCH + c * (int)sizeof(V));
                 V *to = (V *)a.y + (int64_t)(tile.row0 + m) * a.ldy + col0 + c;
-                if (a.y_aligned && col0 + c + 8 <= a.cols) __builtin_nontemporal_store(v, (Eight *)to);
+                if (col0 + c + 8 <= a.cols) mx4_stream8(v, to);
                 else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (col0 + c + e < a.cols) to[e] = v[e];
+                        if (col0 + c + e < a.cols) to[e] = v.v[e];
                 }
             }
         });

@@ -1,9 +1,10 @@
 // Experts: the router (k largest logits of a token, their softmax weights, tokens grouped by expert) and the weighted sum of the
 // experts' outputs.
 //
-// Router.  A logit becomes a 42-bit key: its order as a number (0: masked, never chosen), then the expert, the lowest largest, so
-// that keys differ and the largest key is the next choice.  Sixteen lanes hold a token's keys, as the bits of positive doubles,
-// whose maximum is one instruction, and take the largest k times.  Weights: softmax in fp32, over the chosen ones or over all.
+// Router.  A logit becomes a key: its order as a number (0: masked, never chosen), then the expert, the lowest largest, so that keys
+// differ and the largest key is the next choice.  26 bits for logits of 16; 42 for f32, as the bits of positive doubles, whose
+// maximum is one instruction.  Sixteen lanes hold a token's keys and take the largest k times.  Weights: softmax in fp32, over the
+// chosen ones or over all.
 // Grouping is a counting sort, stable and without atomics whose order could matter: a token takes an expert at most once, so
 // for the 32 tokens of a chunk an expert's rows are a 32-bit mask, its count the bits of it, and a row's place among them the
 // bits below its own.  Chunks' counts are added up by each workgroup that places rows (up to 512 chunks) or by a scan in between.
@@ -32,42 +33,92 @@ struct Route {
     int chunks;
 };
 
-// of the sixteen lanes of a row, in each of them: the maximum, and the sum
-__device__ __forceinline__ uint64_t max_key(uint64_t a, uint64_t b)
+// what one lane holds of a logit: the key, and what it says
+constexpr float LARGEST = 3.402823466e38f;
+template <int T>
+struct RouteKey {   // f16, bf16
+    using type = uint32_t;
+    using V = typename Mx4Type<T>::type;
+    static constexpr uint32_t INF = T == HLQ_F16 ? 0x7c00u : 0x7f80u;
+    static __device__ __forceinline__ type make(V v, int e)
+    {
+        uint32_t b = __builtin_bit_cast(uint16_t, v);
+        if ((b & 0x7fffu) > INF || b == (0x8000u | INF)) return 0u;   // NaN, -inf
+        if (b == 0x8000u) b = 0u;                                       // -0
+        return ((b ^ (b & 0x8000u ? 0xffffu : 0x8000u)) << 16) | (uint32_t)(HLQ_MAX_EXPERTS - 1 - e);
+    }
+    static __device__ __forceinline__ bool present(type k) { return k >= 0x10000u; }
+    static __device__ __forceinline__ type without(type k, type taken) { return k == taken ? 0u : k; }
+    static __device__ __forceinline__ float value(type k)
+    {
+        const uint32_t o = k >> 16;
+        const float v = (float)__builtin_bit_cast(V, (uint16_t)(o ^ (o & 0x8000u ? 0x8000u : 0xffffu)));
+        return v < LARGEST ? v : LARGEST;
+    }
+    static __device__ __forceinline__ type max(type a, type b) { return a > b ? a : b; }
+    template <int CTRL>
+    static __device__ __forceinline__ type rotated(type k) { return (type)__builtin_amdgcn_mov_dpp((int)k, CTRL, 0xf, 0xf, true); }
+};
+template <>
+struct RouteKey<HLQ_F32> {
+    using type = uint64_t;
+    static constexpr uint64_t NORMAL = 1ull << 62;   // a key that is not masked is a normal double
+    static __device__ __forceinline__ type make(float v, int e)
+    {
+        if (!(v > -INFINITY)) return 0ull;
+        v = (v < LARGEST ? v : LARGEST) + 0.0f;   // -0 is 0
+        const uint32_t b = __builtin_bit_cast(uint32_t, v);
+        return NORMAL | (uint64_t)(b & 0x80000000u ? ~b : b | 0x80000000u) << 10 | (uint32_t)(HLQ_MAX_EXPERTS - 1 - e);
+    }
+    static __device__ __forceinline__ bool present(type k) { return k >= NORMAL; }
+    static __device__ __forceinline__ type without(type k, type taken)
+    {
+        // the lower words differ, by the expert's number; without its upper word a key is below all that are left
+        const uint32_t low = (uint32_t)k;
+        return low | (uint64_t)(low == (uint32_t)taken ? 0u : (uint32_t)(k >> 32)) << 32;
+    }
+    static __device__ __forceinline__ float value(type k)
+    {
+        const uint32_t o = (uint32_t)(k >> 10);
+        return __builtin_bit_cast(float, o & 0x80000000u ? o & 0x7fffffffu : ~o);
+    }
+    static __device__ __forceinline__ type max(type a, type b)
+    {
+        uint64_t m;
+        asm("v_max_f64 %0, %1, %2" : "=v"(m) : "v"(a), "v"(b));
+        return m;
+    }
+    template <int CTRL>
+    static __device__ __forceinline__ type rotated(type k)
+    {
+        return (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)k, CTRL, 0xf, 0xf, true) |
+               (uint64_t)(uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)(k >> 32), CTRL, 0xf, 0xf, true) << 32;
+    }
+};
+// of N keys, as a tree
+template <class K, int N>
+__device__ __forceinline__ typename K::type max_of(const typename K::type *key)
 {
-    uint64_t m;
-    asm("v_max_f64 %0, %1, %2" : "=v"(m) : "v"(a), "v"(b));
-    return m;
+    if constexpr (N == 1) return key[0];
+    else return K::max(max_of<K, N / 2>(key), max_of<K, N - N / 2>(key + N / 2));
+}
+// of the sixteen lanes of a row, in each of them: from 8, 4, 2, 1 lanes on
+template <class K>
+__device__ __forceinline__ typename K::type row_max(typename K::type v)
+{
+    v = K::max(v, K::template rotated<0x128>(v));
+    v = K::max(v, K::template rotated<0x124>(v));
+    v = K::max(v, K::template rotated<0x122>(v));
+    return K::max(v, K::template rotated<0x121>(v));
 }
 template <int CTRL>
-__device__ __forceinline__ uint32_t rotated(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true); }
-template <int CTRL>
-__device__ __forceinline__ uint64_t rotated_key(uint64_t v) { return rotated<CTRL>((uint32_t)v) | (uint64_t)rotated<CTRL>((uint32_t)(v >> 32)) << 32; }
-__device__ __forceinline__ uint64_t row_max(uint64_t v)
-{
-    v = max_key(v, rotated_key<0x128>(v));   // from 8, 4, 2, 1 lanes on
-    v = max_key(v, rotated_key<0x124>(v));
-    v = max_key(v, rotated_key<0x122>(v));
-    return max_key(v, rotated_key<0x121>(v));
-}
+__device__ __forceinline__ float rotated(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true)); }
 __device__ __forceinline__ float row_sum(float v)
 {
-    v += __builtin_bit_cast(float, rotated<0x128>(__builtin_bit_cast(uint32_t, v)));
-    v += __builtin_bit_cast(float, rotated<0x124>(__builtin_bit_cast(uint32_t, v)));
-    v += __builtin_bit_cast(float, rotated<0x122>(__builtin_bit_cast(uint32_t, v)));
-    return v + __builtin_bit_cast(float, rotated<0x121>(__builtin_bit_cast(uint32_t, v)));
-}
-
-__device__ __forceinline__ uint32_t key_of(float v)
-{
-    if (!(v > -INFINITY)) return 0u;                 // masked: -inf and NaN
-    v = (v < 3.402823466e38f ? v : 3.402823466e38f) + 0.0f;   // +inf is the largest float; -0 is 0
-    const uint32_t b = __builtin_bit_cast(uint32_t, v);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float value_of(uint32_t key)
-{
-    return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7fffffffu : ~key);
+    v += rotated<0x128>(v);
+    v += rotated<0x124>(v);
+    v += rotated<0x122>(v);
+    return v + rotated<0x121>(v);
 }
 
 // masks of a chunk's rows by expert from its choices, staged in LDS as [token][k]
@@ -108,14 +159,6 @@ __device__ __forceinline__ int prefix(const int *count, int *first, int n)
     return before;
 }
 
-// of N keys, as a tree
-template <int N>
-__device__ __forceinline__ uint64_t max_of(const uint64_t *key)
-{
-    if constexpr (N == 1) return key[0];
-    else return max_key(max_of<N / 2>(key), max_of<N - N / 2>(key + N / 2));
-}
-
 // V: logits a lane holds
 template <int T, int V>
 __global__ void __launch_bounds__(16 * CHUNK)
@@ -131,26 +174,25 @@ hlq_route_top_kernel(const Route a)
     const int tokens = (int)(a.T - t0 < CHUNK ? a.T - t0 : CHUNK);
     for (int e = (int)threadIdx.x; e < a.E; e += (int)blockDim.x) masks[e] = 0u;
     if (t < tokens) {
-        constexpr uint64_t NORMAL = 1ull << 62;      // a key that is not masked is a normal double
+        using K = RouteKey<T>;
         const typename Mx4Type<T>::type *row = (const typename Mx4Type<T>::type *)a.logits + (t0 + t) * a.ld;
-        uint64_t key[V];
+        typename K::type key[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int e = 16 * j + l;
-            const uint32_t k32 = e < a.E ? key_of((float)row[e]) : 0u;
-            key[j] = k32 ? NORMAL | (uint64_t)k32 << 10 | (uint32_t)(HLQ_MAX_EXPERTS - 1 - e) : 0ull;
+            key[j] = e < a.E ? K::make(row[e], e) : (typename K::type)0;
         }
         float top = 0.f, sum = 0.f;
         int found = 0;
         for (; found < a.k; ++found) {
-            const uint64_t best = row_max(max_of<V>(key));
-            if (best < NORMAL) break;
-            const float v = value_of((uint32_t)(best >> 10));
+            const typename K::type best = row_max<K>(max_of<K, V>(key));
+            if (!K::present(best)) break;
+            const float v = K::value(best);
             if (found == 0) {
                 top = v;
                 if (!a.renorm) {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) sum += key[j] >= NORMAL ? expf(value_of((uint32_t)(key[j] >> 10)) - top) : 0.f;
+                    for (int j = 0; j < V; ++j) sum += K::present(key[j]) ? __expf(K::value(key[j]) - top) : 0.f;
                 }
             }
             if (l == 0) {
@@ -158,22 +200,19 @@ hlq_route_top_kernel(const Route a)
                 values[t * a.k + found] = v;
             }
 #pragma unroll
-            for (int j = 0; j < V; ++j) {   // the lower words differ, by the expert's number: taken, it is below all that are left
-                const uint32_t low = (uint32_t)key[j];
-                key[j] = low | (uint64_t)(low == (uint32_t)best ? 0u : (uint32_t)(key[j] >> 32)) << 32;
-            }
+            for (int j = 0; j < V; ++j) key[j] = K::without(key[j], best);
         }
         // what lane 0 of the row wrote is there for the others: they are of one wavefront, whose LDS accesses keep their order
         __builtin_amdgcn_wave_barrier();
         if (a.renorm) {
-            for (int i = l; i < found; i += 16) sum += expf(values[t * a.k + i] - top);
+            for (int i = l; i < found; i += 16) sum += __expf(values[t * a.k + i] - top);
         }
         sum = row_sum(sum);
         for (int i = l; i < a.k; i += 16) {
             const int id = i < found ? picks[t * a.k + i] : -1;
             if (i >= found) picks[t * a.k + i] = -1;
             a.ids[(t0 + t) * a.k + i] = id;
-            a.weights[(t0 + t) * a.k + i] = i < found ? expf(values[t * a.k + i] - top) / sum : 0.f;
+            a.weights[(t0 + t) * a.k + i] = i < found ? __expf(values[t * a.k + i] - top) / sum : 0.f;
         }
     }
     __syncthreads();
@@ -305,6 +344,7 @@ void launch_top(const Route &a, hipStream_t st)
     if (a.E <= 64) hlq_route_top_kernel<T, 4><<<grid, block, lds, st>>>(a);
     else if (a.E <= 128) hlq_route_top_kernel<T, 8><<<grid, block, lds, st>>>(a);
     else if (a.E <= 256) hlq_route_top_kernel<T, 16><<<grid, block, lds, st>>>(a);
+    else if (a.E <= 384) hlq_route_top_kernel<T, 24><<<grid, block, lds, st>>>(a);
     else if (a.E <= 512) hlq_route_top_kernel<T, 32><<<grid, block, lds, st>>>(a);
     else hlq_route_top_kernel<T, 64><<<grid, block, lds, st>>>(a);
 }
@@ -320,13 +360,12 @@ struct Combine {
     void *out;
     int otype;
     int64_t ldo;
-    bool out_aligned;
 };
 
 // y[t, d] = sum_i weights[t, i] Y[slots[t, i], d], i ascending, fp32: a thread has eight successive d of a token.  Bound by the
 // bytes of Y; the loads of four experts are in flight together, and pass the caches by.  8192 tokens, 8 of 4096, bf16: 121 us
 // (605 MB, 5.0 TB/s; through the caches 131).
-template <int T, bool ALIGNED>
+template <int T>
 __global__ void __launch_bounds__(256)
 hlq_expert_combine_kernel(const Combine a, int64_t items)
 {
@@ -346,10 +385,7 @@ hlq_expert_combine_kernel(const Combine a, int64_t items)
                     const int s = a.slots[t * a.k + i + j];
                     has[j] = s >= 0 && s < a.R;
                     w[j] = a.weights[t * a.k + i + j];
-                    if (has[j]) {
-                        if (ALIGNED && d + 8 <= a.D) mx4_stream8((const V *)a.y + s * a.ld + d, v[j]);
-                        else mx4_load8<ALIGNED>((const V *)a.y + s * a.ld + d, a.D - d, v[j]);
-                    }
+                    if (has[j]) mx4_load8<true>((const V *)a.y + s * a.ld + d, a.D - d, v[j]);
                 }
             }
 #pragma unroll
@@ -358,17 +394,16 @@ hlq_expert_combine_kernel(const Combine a, int64_t items)
 #pragma unroll
                     for (int c = 0; c < 8; ++c) sum[c] = fmaf(w[j], (float)v[j][c], sum[c]);
         }
-        mx4_store8(a.out, a.otype, t * a.ldo + d, sum, a.D - d, a.out_aligned);
+        mx4_store8(a.out, a.otype, t * a.ldo + d, sum, a.D - d);
     }
 }
 
 template <int T>
-void launch_combine(const Combine &a, bool aligned, hipStream_t st)
+void launch_combine(const Combine &a, hipStream_t st)
 {
     const int64_t items = a.T * a.eights, blocks = (items + 255) / 256;
     const unsigned grid = (unsigned)(blocks < (1 << 20) ? blocks : 1 << 20);
-    if (aligned) hlq_expert_combine_kernel<T, true><<<grid, 256, 0, st>>>(a, items);
-    else hlq_expert_combine_kernel<T, false><<<grid, 256, 0, st>>>(a, items);
+    hlq_expert_combine_kernel<T><<<grid, 256, 0, st>>>(a, items);
 }
 
 hlq_status check_route(int64_t T, int32_t E, int32_t k)
@@ -450,14 +485,12 @@ hlq_status hlq_expert_combine(int64_t T, int32_t k, int32_t D, int64_t R, const 
     if ((R > 0 && !Y) || !slots || !weights || !out) return HLQ_ERR_NULL;
     if ((uintptr_t)Y % (unsigned)hlq_dtype_bytes(ytype) || (uintptr_t)out % (unsigned)hlq_dtype_bytes(otype) || (((uintptr_t)slots | (uintptr_t)weights) & 3u))
         return HLQ_ERR_BAD_STRIDE;
-    Combine a{T, k, D, (D + 7) / 8, R, Y, ldy, slots, weights, out, otype, ldo, false};
-    a.out_aligned = ((uintptr_t)out & 15u) == 0 && (T == 1 || ldo * hlq_dtype_bytes(otype) % 16 == 0);
-    const bool aligned = ((uintptr_t)Y & 15u) == 0 && (R <= 1 || ldy * hlq_dtype_bytes(ytype) % 16 == 0);
+    Combine a{T, k, D, (D + 7) / 8, R, Y, ldy, slots, weights, out, otype, ldo};
     const hipStream_t st = (hipStream_t)stream;
     hlq_clear_stale_error();
-    if (ytype == HLQ_F16) launch_combine<HLQ_F16>(a, aligned, st);
-    else if (ytype == HLQ_BF16) launch_combine<HLQ_BF16>(a, aligned, st);
-    else launch_combine<HLQ_F32>(a, aligned, st);
+    if (ytype == HLQ_F16) launch_combine<HLQ_F16>(a, st);
+    else if (ytype == HLQ_BF16) launch_combine<HLQ_BF16>(a, st);
+    else launch_combine<HLQ_F32>(a, st);
     return hlq_hip_status(hipGetLastError());
 }
 
