@@ -369,23 +369,26 @@ _DTYPES = {torch.float16: HLQ_F16, torch.float32: HLQ_F32, torch.bfloat16: HLQ_B
 def _matrix(t):
     """(rows, columns, pointer, type, leading dimension) of a matrix whose rows are contiguous; one row's leading dimension is its length.
     Called several times for an operator whose kernel takes a few microseconds: each attribute of a tensor costs a tenth of one."""
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None:
+        raise TypeError(f"expected a float16, bfloat16 or float32 tensor, got {t.dtype}")
     try:
-        dtype = _DTYPES[t.dtype]
-    except KeyError:
-        raise TypeError(f"expected a float16, bfloat16 or float32 tensor, got {t.dtype}") from None
-    if t.dim() != 2:
-        raise ValueError(f"expected a matrix, got shape {tuple(t.shape)}")
-    rows, cols = t.shape
-    ld, one = t.stride()
+        rows, cols = t.shape
+        ld, one = t.stride()
+    except ValueError:
+        raise ValueError(f"expected a matrix, got shape {tuple(t.shape)}") from None
     if (one != 1 and cols > 1) or (rows > 1 and ld < cols):
         raise ValueError(f"expected a matrix whose rows are contiguous, got shape {tuple(t.shape)} with strides {t.stride()}")
     return rows, cols, t.data_ptr(), dtype, ld if rows > 1 else cols
 
 
-def _need_gpu(*tensors) -> None:
-    for t in tensors:
-        if not t.is_cuda:
-            raise ValueError(f"expected tensors on the GPU, got one on {t.device}")
+def _not_on_gpu(*tensors):
+    return ValueError(f"expected tensors on the GPU, got {', '.join(str(t.device) for t in tensors)}")
+
+
+def _stream_of(stream) -> int:
+    """As _stream_ptr, for calls that have seen a tensor on the GPU."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else int(stream.cuda_stream)
 
 
 def _empty(shape, dtype, device, stream):
@@ -405,13 +408,16 @@ def mx4_bytes(rows: int, K: int) -> int:
 class Mx4:
     """A microscaled 4-bit matrix [rows, K]: the blob (u8) in the library's layout."""
 
-    __slots__ = ("blob", "rows", "K", "_ptr", "_bytes")
+    __slots__ = ("blob", "rows", "K", "on_gpu", "_ptr", "_bytes")
 
     def __init__(self, blob, rows: int, K: int):
         self.blob, self.rows, self.K = blob, int(rows), int(K)
-        self._ptr, self._bytes = blob.data_ptr(), blob.numel()
+        self.on_gpu, self._ptr, self._bytes = blob.is_cuda, blob.data_ptr(), blob.numel()
         if blob.dtype != torch.uint8 or not blob.is_contiguous() or self._bytes < mx4_bytes(rows, K):
             raise ValueError(f"a blob of {mx4_bytes(rows, K)} bytes is needed for {rows} x {K}")
+
+    is_cuda = property(lambda self: self.on_gpu)
+    device = property(lambda self: self.blob.device)
 
 
 def alloc_mx4(rows: int, K: int, device="cuda", stream=None) -> Mx4:
@@ -430,8 +436,9 @@ def hlq_mx4_quantize(x, out: Mx4 | None = None, stream=None) -> Mx4:
     """Rows of x [rows, K] (f16, bf16 or f32) in 4-bit floats, a power-of-two scale for each 32 of a row."""
     rows, K, ptr, dtype, ld = _matrix(x)
     out = _mx4_out(out, rows, K, x.device, stream)
-    _need_gpu(x, out.blob)
-    status = lib.hlq_mx4_quantize(rows, K, ptr, dtype, ld, out._ptr, out._bytes, _stream_ptr(stream))
+    if not (x.is_cuda and out.on_gpu):
+        raise _not_on_gpu(x, out.blob)
+    status = lib.hlq_mx4_quantize(rows, K, ptr, dtype, ld, out._ptr, out._bytes, _stream_of(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_quantize", status)
     return out
@@ -444,8 +451,9 @@ def hlq_mx4_dequantize(m: Mx4, y=None, dtype=None, stream=None):
     rows, K, ptr, dtype, ld = _matrix(y)
     if rows != m.rows or K != m.K:
         raise ValueError(f"y has shape {tuple(y.shape)}, the matrix is {m.rows} x {m.K}")
-    _need_gpu(y, m.blob)
-    status = lib.hlq_mx4_dequantize(rows, K, m._ptr, ptr, dtype, ld, _stream_ptr(stream))
+    if not (y.is_cuda and m.on_gpu):
+        raise _not_on_gpu(y, m.blob)
+    status = lib.hlq_mx4_dequantize(rows, K, m._ptr, ptr, dtype, ld, _stream_of(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_dequantize", status)
     return y
@@ -458,13 +466,15 @@ def hlq_mx4_pack(codes, scales, K: int, out: Mx4 | None = None, stream=None) -> 
         if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < least or (t.shape[1] > 1 and t.stride(1) != 1):
             raise ValueError(f"{name}: expected uint8 of shape ({rows}, at least {least}), rows contiguous, got {t.dtype} {tuple(t.shape)}")
     out = _mx4_out(out, rows, K, codes.device, stream)
-    _need_gpu(codes, scales, out.blob)
+    if not (codes.is_cuda and scales.is_cuda and out.on_gpu):
+        raise _not_on_gpu(codes, scales, out.blob)
     _check("hlq_mx4_pack", lib.hlq_mx4_pack(rows, K, _ptr(codes), codes.stride(0), _ptr(scales), scales.stride(0), out._ptr, out._bytes, _stream_ptr(stream)))
     return out
 
 
 def hlq_mx4_unpack(m: Mx4, stream=None):
-    _need_gpu(m.blob)
+    if not m.on_gpu:
+        raise _not_on_gpu(m.blob)
     codes = _empty((m.rows, (m.K + 1) // 2), torch.uint8, m.blob.device, stream)
     scales = _empty((m.rows, (m.K + 31) // 32), torch.uint8, m.blob.device, stream)
     _check("hlq_mx4_unpack", lib.hlq_mx4_unpack(m.rows, m.K, m._ptr, _ptr(codes), _ptr(scales), _stream_ptr(stream)))
@@ -507,8 +517,9 @@ def hlq_mx4_gemm(W: Mx4, X, Y=None, gated: bool = False, out_dtype=None, ws=None
         raise ValueError(f"X is {M} x {K}, W {N} x {W.K}, Y {y_rows} x {y_cols}{' (gated)' if gated else ''}")
     if ws is None:
         ws = alloc_mx4_workspace(W, M, stream=stream)
-    _need_gpu(W.blob, X.blob if type(X) is Mx4 else X, Y, ws)
-    status = lib.hlq_mx4_gemm(N, K, W._ptr, M, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0, ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+    if not (W.on_gpu and X.is_cuda and Y.is_cuda and ws.is_cuda):
+        raise _not_on_gpu(W.blob, X, Y, ws)
+    status = lib.hlq_mx4_gemm(N, K, W._ptr, M, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0, ws.data_ptr(), ws.numel(), _stream_of(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_gemm", status)
     return Y
@@ -517,12 +528,12 @@ def hlq_mx4_gemm(W: Mx4, X, Y=None, gated: bool = False, out_dtype=None, ws=None
 class Route:
     """What hlq_route writes: ids, weights, slots [T, k], offsets [E + 1], rows [T k], and its workspace."""
 
-    __slots__ = ("ids", "weights", "offsets", "rows", "slots", "ws", "T", "E", "k", "_args")
+    __slots__ = ("ids", "weights", "offsets", "rows", "slots", "ws", "T", "E", "k", "on_gpu", "_args")
 
     def __init__(self, T: int, E: int, k: int, device="cuda", stream=None):
         n = ctypes.c_size_t()
         _check("hlq_route_workspace_bytes", lib.hlq_route_workspace_bytes(T, E, k, ctypes.byref(n)))
-        self.T, self.E, self.k = T, E, k
+        self.T, self.E, self.k, self.on_gpu = T, E, k, torch.device(device).type == "cuda"
         self.ids, self.slots = (_empty((T, k), torch.int32, device, stream) for _ in range(2))
         self.weights = _empty((T, k), torch.float32, device, stream)
         self.offsets = _empty(E + 1, torch.int32, device, stream)
@@ -542,8 +553,9 @@ def hlq_route(logits, k: int, renorm: bool = True, out: Route | None = None, str
         out = Route(T, E, k, logits.device, stream)
     elif out.T != T or out.E != E or out.k != k:
         raise ValueError(f"the output is for {out.T} tokens, {out.E} experts, {out.k} each")
-    _need_gpu(logits, out.offsets)
-    status = lib.hlq_route(T, E, k, ptr, dtype, ld, 1 if renorm else 0, *out._args, _stream_ptr(stream))
+    if not (logits.is_cuda and out.on_gpu):
+        raise _not_on_gpu(logits, out.offsets)
+    status = lib.hlq_route(T, E, k, ptr, dtype, ld, 1 if renorm else 0, *out._args, _stream_of(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_route", status)
     return out
@@ -571,11 +583,10 @@ def hlq_expert_gemm(W: Mx4, offsets, X, Y=None, rows=None, gated: bool = False, 
         raise ValueError(f"X is {x_rows} x {K}, a matrix of W {N} x {W.K}, Y {y_rows} x {y_cols} for {R} rows{' (gated)' if gated else ''}")
     if ws is None:
         ws = alloc_mx4_workspace(W, x_rows, R, E, stream)
-    _need_gpu(W.blob, offsets, X.blob if type(X) is Mx4 else X, Y, ws)
-    if rows is not None:
-        _need_gpu(rows)
+    if not (W.on_gpu and offsets.is_cuda and X.is_cuda and Y.is_cuda and ws.is_cuda and (rows is None or rows.is_cuda)):
+        raise _not_on_gpu(W.blob, offsets, X, Y, ws, *([] if rows is None else [rows]))
     status = lib.hlq_expert_gemm(E, N, K, W._ptr, offsets.data_ptr(), rows_ptr, R, x_rows, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0,
-                                 ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+                                 ws.data_ptr(), ws.numel(), _stream_of(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_expert_gemm", status)
     return Y
@@ -585,15 +596,16 @@ def hlq_expert_combine(Y, slots, weights, out=None, out_dtype=None, stream=None)
     """out[t] = sum_i weights[t, i] Y[slots[t, i]] (slot -1: nothing)."""
     T, k = slots.shape
     R, D, y, ytype, ldy = _matrix(Y)
-    if weights.shape != slots.shape or slots.dtype != torch.int32 or weights.dtype != torch.float32 or not (slots.is_contiguous() and weights.is_contiguous()):
+    if slots.dtype != torch.int32 or weights.dtype != torch.float32 or weights.shape != slots.shape or not (slots.is_contiguous() and weights.is_contiguous()):
         raise ValueError(f"slots and weights: contiguous int32 and float32 of one shape, got {slots.dtype} {tuple(slots.shape)} and {weights.dtype} {tuple(weights.shape)}")
     if out is None:
         out = _empty((T, D), out_dtype or Y.dtype, Y.device, stream)
     o_rows, o_cols, o, otype, ldo = _matrix(out)
     if o_rows != T or o_cols != D:
         raise ValueError(f"out has shape {tuple(out.shape)}, the result is {T} x {D}")
-    _need_gpu(Y, slots, weights, out)
-    status = lib.hlq_expert_combine(T, k, D, R, y, ytype, ldy, slots.data_ptr(), weights.data_ptr(), o, otype, ldo, _stream_ptr(stream))
+    if not (Y.is_cuda and slots.is_cuda and weights.is_cuda and out.is_cuda):
+        raise _not_on_gpu(Y, slots, weights, out)
+    status = lib.hlq_expert_combine(T, k, D, R, y, ytype, ldy, slots.data_ptr(), weights.data_ptr(), o, otype, ldo, _stream_of(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_expert_combine", status)
     return out

@@ -65,12 +65,12 @@ hlq_mx4_tile_kernel(const Mx4Product a, const Tiles t)
     const int row_tiles = made < t.row_tiles ? made : t.row_tiles, tiles = t.col_tiles * row_tiles;   // never more than there is room for
     if ((int)blockIdx.x >= tiles * t.splits) return;
     const int id = xcd_order((int)blockIdx.x, tiles * t.splits);
-    const int split = id % t.splits, tile_id = id / t.splits;
+    const int split = CUT ? id % t.splits : 0, tile_id = CUT ? id / t.splits : id;
     // bands of 8 row tiles, columns after columns
     const int band = tile_id / (8 * t.col_tiles), first = band * 8, high = row_tiles - first < 8 ? row_tiles - first : 8;
     const int in_band = tile_id - first * t.col_tiles;
     const int nt = in_band / high;
-    const Mx4RowTile tile = mx4_row_tile<BM>(a, first + in_band % high);
+    const Mx4RowTile tile = mx4_row_tile<BM>(a, first + in_band - nt * high);
 
     // row of W for row j of the tile; gated: 32 rows of the first half, then the 32 of the second that go with them
     auto w_row = [&](int j) {
