@@ -107,3 +107,5 @@ struct Mx4TilePlan {
     size_t partial_at, partial_bytes;
 };
 hlq_status hlq_mx4_launch_tile(const Mx4Product &a, const Mx4TilePlan &p, bool gated, void *ws, hipStream_t st);
+// BM = 256, K not cut; a workgroup takes tile after tile
+hlq_status hlq_mx4_launch_big(const Mx4Product &a, const Mx4TilePlan &p, bool gated, hipStream_t st);

@@ -8,34 +8,21 @@
 // A stage is a panel of 128 k of the tile's rows, requested straight into LDS (codes 16 bytes a lane, scales 4), a ring of three
 // or four stages deep.  Two workgroups share a compute unit: the wavefronts of one multiply while the other waits, starts or
 // writes its results.  128 x 256 with a ring of three is the largest that two of fit.  us, 8192 rows, gated, 28672 x 4096:
-//   256 x 256, 4 wavefronts, two stages of 256 k    605     its requests spread between the matrix instructions       541
+//   two stages of 256 k, 256 x 256                  605     its requests spread between the matrix instructions       541
 //   ... in a ring of four stages of 128 k           495     128 x 256, ring of three, two workgroups a unit           463
-//   (the 256 x 256 tile with 8 wavefronts 482; 128 x 128 529)     ... results in streaming stores                     471 (then 481)
-// What bounds it there (4.1 PFLOP/s): the power of the matrix cores and of what feeds them.  The clock is at 1.6 GHz, where the
-// instruction alone with the same data runs at 1.55; with operands of zeros the same launch takes 325.  For experts' rows (512 each
-// on average, 218): waiting for weights that come from memory once, 2.8 TB/s in all with the clock at 2.1 GHz.
-#include "hlq_mx4_gemm.h"
-#include "hlq_mfma_common.h"
+//   (128 x 128 529)                                         ... results in streaming stores                     471 (then 481)
+// From about one round of the card's units, 256 x 256 with a workgroup that goes from tile to tile is faster (another kernel); this one
+// has what is less or does not fill whole rounds.  For experts' rows (512 each on average, 218): waiting for weights that come
+// from memory once, 2.8 TB/s in all with the clock at 2.1 GHz.
+#include "hlq_mx4_stage.h"
 
 namespace {
-
-// A lane of the matrix core holds 16 bytes of a row.  In LDS a row's panel is four such pieces, piece p at place p ^ key(row):
-// reading one piece of 8 or of 16 successive rows then meets every bank once.
-__device__ __forceinline__ int piece_key(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
-
-__device__ __forceinline__ mx4_int8 wide(mx4_int4 v) { return (mx4_int8){v.x, v.y, v.z, v.w, 0, 0, 0, 0}; }
 
 struct Tiles {
     int col_tiles, row_tiles, splits, share;   // share: panels of a split
     int *arrived;                              // [tile]
     float *partial;                            // [tile][split][wave][register][lane]
 };
-
-// as dma_16B_per_lane, 4 bytes a lane
-__device__ __forceinline__ void dma_4B_per_lane(const void *gptr, uint32_t lds_base)
-{
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(gptr), "s"(lds_base) : "memory", "m0");
-}
 
 // Workgroups go to the eight XCDs in turn: each XCD takes a run of tiles, so that its L2 sees few rows and columns.
 __device__ __forceinline__ int xcd_order(int id, int n)
