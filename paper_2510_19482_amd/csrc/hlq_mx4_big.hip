@@ -9,19 +9,26 @@
 //   one workgroup a tile                                    453 / 786 (then 465 / 846)
 //   a workgroup goes from tile to tile                      438 / 771
 //   results in lines of 128 bytes, not 64                   450 / 809 (8192 x 28672 x 256 plain, all results: 172 -> 110)
-//   a step's operands read 6 products behind the barrier    426 / 777
-// 5 % between devices.  4 wavefronts with 4 x 4 blocks: 4 % less a panel, but 20 us a tile for results that spill.  A wavefront's
-// priority raised for its products: 2 % slower.
+//   a step's operands read 6 products behind the barrier    426 / 777 (devices differ by 5 %)
+// 4 wavefronts with 4 x 4 blocks: 4 % less a panel, but 20 us a tile for results that spill.  A wavefront's priority raised for its
+// products: 2 % slower.
+// Experts' rows, 16384 of 32, gated 4096 x 4096, skewed / 512 each give or take 22, against 193 / 208 of 128 x 256:
+//   every tile multiplied in full                           188 / 230
+//   offsets from LDS, the next tile's rows looked up early, wavefronts without rows do not multiply    177 / 230
+//   low tiles after the high ones                           180 / 207 (8192 rows of 8 89 -> 85, of 64 133)
+//   (a queue that workgroups take tiles from: 182 / 203, but 8192 rows of 8 102: a number's way is 5 us a tile)
+// What bounds them: weights that come from memory once, and rows gathered by index (512 each exactly: 150; rows in order 131).
 #include "hlq_mx4_stage.h"
 
 namespace {
 
 constexpr int TM = 2, TN = 4, GM = 4, GN = 2;       // blocks of 32 x 32 a wavefront, wavefronts
 constexpr int BM = 32 * TM * GM, BN = 32 * TN * GN, WAVES = GM * GN;
+constexpr int BAND = 4;   // row tiles that a run of tiles goes through column after column
 constexpr int BUFFERS = 4, SCALES = (BM + BN) * 64, STAGE = (BM + BN) * 68;
 constexpr int LOADS = (BM + BN) / 16 / WAVES, PER = LOADS + 1, HALF = PER / 2;   // requests of a wavefront and stage: codes, scales
 constexpr int PITCH = 144, STAGING = 16 * PITCH;    // of a wavefront: 16 rows of 128 bytes
-constexpr int LDS = BUFFERS * STAGE + WAVES * STAGING;
+constexpr int STARTS = BUFFERS * STAGE + WAVES * STAGING, LDS = STARTS + 4 * (HLQ_MAX_EXPERTS + 1);   // where the experts' offsets are
 static_assert((BM + BN) == 64 * WAVES && LDS <= 160 * 1024 && TM == 2 && TN == 4 && PER == 5 && HALF == 2, "the schedule of a panel");
 
 struct Place {
@@ -38,23 +45,43 @@ hlq_mx4_big_kernel(const Mx4Product a, int col_tiles, int most_row_tiles)
     const int r = lane & 31, g = lane >> 5, wm = wave / GN, wn = wave % GN;
     const bool of_x = wave >= BN / 64;   // a wavefront requests 64 rows of W or of x
 
-    // Workgroups go to the eight XCDs in turn: each XCD has a run of tiles, in bands of 8 row tiles, columns after columns, so that
+    // Row tiles of experts: the high ones first, then those of an expert's last 128 rows or fewer, in which half of the wavefronts have
+    // nothing to multiply; so that the workgroups end nearly together.
+    const int *const starts = (const int *)(lds + STARTS);
+    const auto start = [&](int e) { return starts[e]; };
+    const auto high = [](int n) { return n / BM + (n % BM > BM / 2); };
+    const auto low = [](int n) { return (int)(n % BM > 0 && n % BM <= BM / 2); };
+    int row_tiles = most_row_tiles, low_row_tiles = 0;
+    if (a.offsets) {
+        for (int e = (int)threadIdx.x; e <= a.E; e += 64 * WAVES) *(int *)(lds + STARTS + 4 * e) = a.offsets[e];
+        __syncthreads();
+        // never more than the host has counted on, whatever the offsets are
+        row_tiles = mx4_count_tiles(a, start, high);
+        low_row_tiles = mx4_count_tiles(a, start, low);
+        row_tiles = row_tiles < 0 || row_tiles > most_row_tiles ? most_row_tiles : row_tiles;
+    }
+    // Workgroups go to the eight XCDs in turn: each XCD has a run of tiles, in bands of four row tiles, columns after columns, so that
     // its L2 sees few rows and columns; its workgroups take them in turn.
-    const int made = a.offsets ? mx4_count_row_tiles<BM>(a) : most_row_tiles;
-    const int row_tiles = made < most_row_tiles ? made : most_row_tiles, tiles = col_tiles * row_tiles;
-    const int xcd = (int)blockIdx.x % 8, each = tiles / 8, more = tiles % 8;
-    const int run = xcd * each + (xcd < more ? xcd : more), end = run + each + (xcd < more);
-    const int step = ((int)gridDim.x - xcd + 7) / 8;   // workgroups of this XCD
+    const int xcd = (int)blockIdx.x % 8, step = ((int)gridDim.x - xcd + 7) / 8;   // workgroups of this XCD
+    auto run = [&](int tiles, int x) { return x * (tiles / 8) + (x < tiles % 8 ? x : tiles % 8); };   // where XCD x begins
+    const int first_high = run(col_tiles * row_tiles, xcd), high_ones = run(col_tiles * row_tiles, xcd + 1) - first_high;
+    const int first_low = run(col_tiles * low_row_tiles, xcd), end = high_ones + run(col_tiles * low_row_tiles, xcd + 1) - first_low;
     auto place = [&](int id) {
-        const int band = id / (8 * col_tiles), first = band * 8, high = row_tiles - first < 8 ? row_tiles - first : 8;
-        const int in_band = id - first * col_tiles, nt = in_band / high;
-        return Place{nt, mx4_row_tile<BM>(a, first + in_band - nt * high)};
+        const bool is_low = id >= high_ones;
+        const int tile = is_low ? first_low + id - high_ones : first_high + id, rows = is_low ? low_row_tiles : row_tiles;
+        const int band = tile / (BAND * col_tiles), first = band * BAND, height = rows - first < BAND ? rows - first : BAND;
+        const int in_band = tile - first * col_tiles, nt = in_band / height, mt = first + in_band - nt * height;
+        if (!a.offsets) return Place{nt, mx4_row_tile<BM>(a, mt)};
+        const Mx4ExpertTile t = is_low ? mx4_find_tile(a, mt, start, low) : mx4_find_tile(a, mt, start, high);
+        const int n = t.hi - t.lo, r = is_low ? n / BM * BM : t.index * BM;
+        return Place{nt, Mx4RowTile{t.e, t.lo + r, n - r < BM ? n - r : BM}};
     };
-    // the row of W or of x that this lane's number of the wavefront's 64 rows is
-    auto row_of = [&](const Place &p) {
+    // the row of W or of x that this lane's number of the wavefront's 64 rows is; of x as it stands, not yet known to be inside
+    auto look = [&](const Place &p) {
         if (of_x) {
             const int j = wave * 64 - BN + lane;
-            return mx4_x_row(a, p.rows.row0 + (j < p.rows.n ? j : 0));
+            const int i = p.rows.row0 + (j < p.rows.n ? j : 0);
+            return a.rows ? a.rows[i] : i;
         }
         const int j = wave * 64 + lane;
         int c = p.nt * BN + j, half = 0;
@@ -66,7 +93,8 @@ hlq_mx4_big_kernel(const Mx4Product a, int col_tiles, int most_row_tiles)
     };
     const int64_t rows64 = (of_x ? a.A.rows : a.W.rows) * 64, rows4 = (of_x ? a.A.rows : a.W.rows) * 4;
     const uint8_t *from[LOADS], *scale_from;
-    auto aim = [&](int row) {
+    auto aim = [&](int found) {
+        const int row = of_x ? mx4_inside_x(a, found) : found;
         const uint8_t *codes = of_x ? a.A.codes : a.W.codes, *scales = of_x ? a.A.scales : a.W.scales;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
@@ -164,6 +192,23 @@ hlq_mx4_big_kernel(const Mx4Product a, int col_tiles, int most_row_tiles)
         return next;
     };
 
+    auto idle = [&](int buffer, auto More) {   // a panel without products
+        if constexpr (decltype(More)::value) {
+#pragma unroll
+            for (int i = HALF; i < PER; ++i) request(buffer == 0 ? BUFFERS - 1 : buffer - 1, i);
+            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((BUFFERS - 2) * PER) : "memory");
+#pragma unroll
+            for (int i = 0; i < HALF; ++i) request(buffer, i);
+        } else
+            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        return buffer == BUFFERS - 1 ? 0 : buffer + 1;
+    };
+    auto request_rest = [&](int buffer) {
+        if (count >= BUFFERS)
+#pragma unroll
+            for (int i = HALF; i < PER; ++i) request(buffer == 0 ? BUFFERS - 1 : buffer - 1, i);
+    };
+
     // Results of one tile: a wavefront turns its blocks round in LDS of its own, 16 rows of 128 bytes at a time, so that rows leave
     // in whole lines.  No barrier: LDS accesses of a wavefront keep their order.
     constexpr int OUT = GATED ? BN / 2 : BN;   // columns of the tile
@@ -219,49 +264,59 @@ hlq_mx4_big_kernel(const Mx4Product a, int col_tiles, int most_row_tiles)
         });
     };
 
-    int id = run + (int)blockIdx.x / 8;
-    if (id >= end) return;
-    Place now = place(id);
-    aim(row_of(now));
-    request_first();
-    for (;;) {
-        // where the next tile is: its rows are looked up while this one is multiplied
+    int id = (int)blockIdx.x / 8;
+    Place now{};
+    if (id < end) {
+        now = place(id);
+        aim(look(now));
+        request_first();
+    }
+    while (id < end) {
+        // loads come in the order of their requests; stores of the tile before, where there are any, only add to the count
+        if (count >= BUFFERS) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((BUFFERS - 2) * PER + HALF) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        // where the next tile is: its rows are looked up while this one is multiplied (nothing here waits for memory: loads come in
+        // order, so that would be waiting for all that is requested)
         const int next_id = id + step;
         const bool more = next_id < end;
         Place next = now;
-        int next_row = 0;
+        int found = 0;
         if (more) {
             next = place(next_id);
-            next_row = row_of(next);
+            found = look(next);
         }
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int c = 0; c < 16; ++c) acc[i][j][c] = 0.f;
-        // loads come in the order of their requests; stores of the tile before, where there are any, only add to the count
-        if (count >= BUFFERS) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((BUFFERS - 2) * PER + HALF) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-        read(0, 0, 0);
-        read_scales(0);
-        turn_scales();
         int buffer = 0, p = 0;
-        for (; p + BUFFERS < count; ++p) buffer = panel(buffer, std::true_type{});
-        if (count >= BUFFERS)
+        // every wavefront has passed the last panel's barrier, behind which nothing of this tile is read: the next one is requested, and
+        // comes while this one's results leave
+        auto turn = [&]() {
+            if (more) {
+                aim(found);
+                request_first();
+            }
+        };
+        if (wm * 32 * TM < now.rows.n) {
 #pragma unroll
-            for (int i = HALF; i < PER; ++i) request(buffer == 0 ? BUFFERS - 1 : buffer - 1, i);
-        for (; p < count; ++p) buffer = panel(buffer, std::false_type{});
-        // every wavefront has passed the barrier behind which nothing of this tile is read: the next one is requested, and comes while
-        // this one's results leave
-        if (more) {
-            aim(next_row);
-            request_first();
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) acc[i][j][c] = 0.f;
+            read(0, 0, 0);
+            read_scales(0);
+            turn_scales();
+            for (; p + BUFFERS < count; ++p) buffer = panel(buffer, std::true_type{});
+            request_rest(buffer);
+            for (; p < count; ++p) buffer = panel(buffer, std::false_type{});
+            turn();
+            if (a.ytype == HLQ_F32) leave(now, float{});
+            else if (a.ytype == HLQ_F16) leave(now, (_Float16)0.f);
+            else leave(now, (__bf16)0.f);
+        } else {   // none of this wavefront's rows is there: it only requests
+            for (; p + BUFFERS < count; ++p) buffer = idle(buffer, std::true_type{});
+            request_rest(buffer);
+            for (; p < count; ++p) buffer = idle(buffer, std::false_type{});
+            turn();
         }
-        if (a.ytype == HLQ_F32) leave(now, float{});
-        else if (a.ytype == HLQ_F16) leave(now, (_Float16)0.f);
-        else leave(now, (__bf16)0.f);
-        if (!more) break;
         id = next_id;
         now = next;
     }
@@ -273,8 +328,7 @@ hlq_status hlq_mx4_launch_big(const Mx4Product &a, const Mx4TilePlan &p, bool ga
 {
     const int64_t tiles = (int64_t)p.col_tiles * p.row_tiles;
     if (tiles > INT32_MAX / 2) return HLQ_ERR_UNSUPPORTED;
-    const unsigned grid = (unsigned)(tiles < 256 ? tiles : 256);   // as many as there are compute units
     auto kernel = gated ? hlq_mx4_big_kernel<true> : hlq_mx4_big_kernel<false>;
-    kernel<<<grid, 64 * WAVES, LDS, st>>>(a, p.col_tiles, p.row_tiles);
+    kernel<<<256, 64 * WAVES, LDS, st>>>(a, p.col_tiles, p.row_tiles);
     return hlq_hip_status(hipGetLastError());
 }

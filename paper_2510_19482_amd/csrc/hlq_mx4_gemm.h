@@ -23,46 +23,46 @@ struct Mx4Product {
 struct Mx4RowTile {
     int e, row0, n;
 };
-// rows [lo, hi) of expert e, within 0..R - 1; none for e >= E
-__device__ __forceinline__ void mx4_expert_rows(const Mx4Product &a, int e, int &lo, int &hi)
+// rows [lo, hi) of expert e, within 0..R - 1; none for e >= E.  start(e): offset e
+template <class Start>
+__device__ __forceinline__ void mx4_expert_rows(const Mx4Product &a, int e, int &lo, int &hi, Start start)
 {
     lo = hi = a.R;
     if (e < a.E) {
-        lo = a.offsets[e];
-        hi = a.offsets[e + 1];
+        lo = start(e);
+        hi = start(e + 1);
     }
     lo = lo < 0 ? 0 : lo > a.R ? a.R : lo;
     hi = hi < lo ? lo : hi > a.R ? a.R : hi;
 }
-// how many there are, in a scalar register
-template <int BM>
-__device__ __forceinline__ int mx4_count_row_tiles(const Mx4Product &a)
+// the sum of tiles(n) over the experts, n the rows of one, in a scalar register
+template <class Start, class Tiles>
+__device__ __forceinline__ int mx4_count_tiles(const Mx4Product &a, Start start, Tiles tiles)
 {
     const int lane = (int)(threadIdx.x & 63u);
     int n = 0;
     for (int base = 0; base < a.E; base += 64) {
         int lo, hi;
-        mx4_expert_rows(a, base + lane, lo, hi);
-        n += (hi - lo) / BM + ((hi - lo) % BM != 0);
+        mx4_expert_rows(a, base + lane, lo, hi, start);
+        n += tiles(hi - lo);
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
     return __builtin_amdgcn_readfirstlane(n);
 }
-template <int BM>
-__device__ __forceinline__ Mx4RowTile mx4_row_tile(const Mx4Product &a, int tile)
+// which expert has tile number `tile` of those, the how manieth of its own it is, and the expert's rows; rows 0..-1: there are fewer tiles
+struct Mx4ExpertTile {
+    int e, index, lo, hi;
+};
+template <class Start, class Tiles>
+__device__ __forceinline__ Mx4ExpertTile mx4_find_tile(const Mx4Product &a, int tile, Start start, Tiles tiles)
 {
-    if (!a.offsets) {
-        const int64_t r = (int64_t)tile * BM;
-        if (r >= a.R) return {0, 0, 0};
-        return {0, (int)r, (int)(a.R - r < BM ? a.R - r : BM)};
-    }
     const int lane = (int)(threadIdx.x & 63u);
     int before = 0;
     for (int base = 0; base < a.E; base += 64) {
         int lo, hi;
-        mx4_expert_rows(a, base + lane, lo, hi);
-        int upto = (hi - lo) / BM + ((hi - lo) % BM != 0);
+        mx4_expert_rows(a, base + lane, lo, hi, start);
+        int upto = tiles(hi - lo);
         const int mine = upto;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -73,13 +73,29 @@ __device__ __forceinline__ Mx4RowTile mx4_row_tile(const Mx4Product &a, int tile
         if (tile - before < all) {
             const uint64_t past = __ballot(upto > tile - before);
             const int f = (int)__builtin_ctzll(past);
-            const int l = __builtin_amdgcn_readlane(lo, f), h = __builtin_amdgcn_readlane(hi, f);
-            const int r = l + (tile - before - (__builtin_amdgcn_readlane(upto, f) - __builtin_amdgcn_readlane(mine, f))) * BM;
-            return {base + f, r, h - r < BM ? h - r : BM};
+            return {base + f, tile - before - (__builtin_amdgcn_readlane(upto, f) - __builtin_amdgcn_readlane(mine, f)), __builtin_amdgcn_readlane(lo, f),
+                    __builtin_amdgcn_readlane(hi, f)};
         }
         before += all;
     }
-    return {0, 0, 0};
+    return {0, 0, 0, 0};
+}
+template <int BM>
+__device__ __forceinline__ int mx4_count_row_tiles(const Mx4Product &a)
+{
+    return mx4_count_tiles(a, [&](int e) { return a.offsets[e]; }, [](int n) { return n / BM + (n % BM != 0); });
+}
+template <int BM>
+__device__ __forceinline__ Mx4RowTile mx4_row_tile(const Mx4Product &a, int tile)
+{
+    if (!a.offsets) {
+        const int64_t r = (int64_t)tile * BM;
+        if (r >= a.R) return {0, 0, 0};
+        return {0, (int)r, (int)(a.R - r < BM ? a.R - r : BM)};
+    }
+    const Mx4ExpertTile t = mx4_find_tile(a, tile, [&](int e) { return a.offsets[e]; }, [](int n) { return n / BM + (n % BM != 0); });
+    const int r = t.lo + t.index * BM;
+    return {t.e, r, t.hi - r < BM ? t.hi - r : BM};
 }
 
 // Most row tiles that R rows of E experts make.
@@ -90,12 +106,8 @@ static inline int64_t mx4_row_tiles(int64_t R, int E, int BM)
 }
 
 // row of x for row r (r < R); an index outside x is taken as its nearest end, so that nothing outside is read
-__device__ __forceinline__ int mx4_x_row(const Mx4Product &a, int r)
-{
-    if (!a.rows) return r;
-    const int i = a.rows[r];
-    return i < 0 ? 0 : i >= a.x_rows ? a.x_rows - 1 : i;
-}
+__device__ __forceinline__ int mx4_inside_x(const Mx4Product &a, int i) { return i < 0 ? 0 : i >= a.x_rows ? a.x_rows - 1 : i; }
+__device__ __forceinline__ int mx4_x_row(const Mx4Product &a, int r) { return a.rows ? mx4_inside_x(a, a.rows[r]) : r; }
 
 // a wavefront has row_blocks x col_blocks blocks of 16 x 16: 1 x 1, 2 x 1, 2 x 2 or 4 x 2 (1 x 1 if x is quantized inside)
 hlq_status hlq_mx4_launch_few(const Mx4Product &a, int xtype, bool gated, int row_blocks, int col_blocks, hipStream_t st);

@@ -18,9 +18,10 @@ size_t up256(size_t n) { return (n + 255u) & ~(size_t)255u; }
 // rows a wavefront has and four splits.
 // Measured / estimated, N x K = 4096 x 4096: 32 rows 5.1 / 5.0 (2 x 1), 128 rows 7.3 / 8.4 (4 x 2), 256 rows 9.5 / 9.3 (32 x 128), 1024 rows
 // 15.2 / 13.1 (128 x 128); 28672 x 4096: 64 rows 13.0 / 15.5 (32 x 128); 4096 x 14336: 32 rows 10.3 / 11.1 (2 x 1), 128 rows
-// 15.2 / 15.6 (32 x 128, K in four).  256 x 256 against 128 x 256, measured, rows x N x K: 4096 x 4096 x 14336 107 / 116 (one round),
-// 8192 x 8192 x 4096 at 71 / 73 (two), 8192 x 28672 x 4096 gated 440 / 485 (14); taken by the estimate for 128 x 256: 2048 x 4096 x 4096
-// (half a round) 22.7 / 27, 16384 rows of 32 experts 191 / 188, of 4 experts 147 / 135.
+// 15.2 / 15.6 (32 x 128, K in four).
+// 256 x 256 against 128 x 256, measured, rows x N x K: 4096 x 4096 x 14336 107 / 116 (one round of the card), 8192 x 4096 x 4096 65 / 73
+// (two), 8192 x 28672 x 4096 gated 440 / 485 (14), but half a round, 2048 x 4096 x 4096, 24 / 22.  Experts' rows, gated 4096 x 4096: 16384
+// of 32 experts 180 / 193, 8192 of 8 85 / 92, 8192 of 64 133 / 169 (weights: 4.3 TB/s); against 32 x 128, 4096 of 64 117 / 181.
 constexpr int MOST_SPLITS = 8, LEAST_SHARE = 4, MOST_CUT = 512;   // of K, panels of one, workgroups of a product whose K is cut
 constexpr int64_t MOST_GROUPS = 1 << 22, MOST_TILES = 1 << 23;    // workgroups, so that a launch stays below 2^32 threads
 
@@ -63,7 +64,7 @@ Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
         double alone, shared;
     };
     static const Tile tiles[] = {{32, 128, 1, 0.18, 0.145}, {64, 128, 2, 0.24, 0.22}, {128, 128, 2, 0.27, 0.30}, {128, 256, 0, 0.45, 0.43},
-                                 {256, 256, 0, 0.79, 0.79}};
+                                 {256, 256, 0, 0.765, 0.765}};
     const int64_t width = gated ? (N / 2 + 31) / 32 * 64 : N;   // gated halves are interleaved 32 columns at a time
     for (const auto &k : tiles) {
         const int64_t col_tiles = (width + k.BN - 1) / k.BN;
@@ -72,11 +73,16 @@ Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
         for (int want = 1; want <= (k.passes ? MOST_SPLITS : 1); want *= 2) {
             const int share = (panels + want - 1) / want, splits = (panels + share - 1) / share;
             if (splits < want || (want > 1 && (mx4_row_tiles(R, E, k.BM) * col_tiles * want > MOST_CUT || share < LEAST_SHARE))) break;
-            const double full = k.BM == 256 ? (double)(((int64_t)count + 255) / 256) : count * splits / 256;   // 256 x 256: whole rounds
+            // 256 x 256: whole rounds of tiles that are alike; experts' last tiles, up to half of them not even half filled, cost a third
+            const double full = k.BM < 256 ? count * splits / 256
+                                : E == 1   ? (double)(((int64_t)count + 255) / 256)
+                                           : (double)used * (each / 256 + 0.3) * (double)col_tiles / 256;
             const double stage = full <= 1.0 ? k.alone : full * k.shared > k.alone ? full * k.shared : k.alone;
-            double t = 3.5 + (share * stage > weights / 5.2 ? share * stage : weights / 5.2);
+            // an expert's weights come from memory again, in part, for a second row tile
+            const double stream = weights / 5.2 * (E == 1 ? 1.0 : 0.7 + 0.3 * row_tiles(k.BM) / (double)used);
+            double t = 3.5 + (share * stage > stream ? share * stage : stream);
             if (splits > 1) t += 2.0 + 2.0 * k.passes * ((splits + 3) / 4);
-            if (t < least) {
+            if (t < least || (t == least && k.BM == 256)) {   // as near where weights bound both: 256 x 256 streams them faster
                 least = t;
                 best.row_blocks = 0;
                 best.tile = Mx4TilePlan{k.BM, k.BN, (int)col_tiles, (int)mx4_row_tiles(R, E, k.BM), splits, share, 0, 0};

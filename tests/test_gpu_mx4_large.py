@@ -108,3 +108,23 @@ def test_offsets_that_overlap_write_rows_only():
         torch.cuda.synchronize()
         assert bool((out[:4] == 3).all()) and bool((out[4 + R:] == 3).all())
     check(out[4:4 + R], x, w[-N:], False)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_many_experts_of_few_rows(gated):
+    # weights enough that their way from memory decides
+    E, N, K, T = 64, 2048, 1024, 500
+    g = torch.Generator("cuda").manual_seed(9)
+    counts = torch.randint(0, 200, (E,), device="cuda", generator=g)
+    counts[:6] = torch.tensor([0, 1, 64, 65, 128, 129])
+    off = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), counts.cumsum(0)]).int()
+    R = int(off[-1])
+    rows = torch.randint(0, T, (R,), dtype=torch.int32, device="cuda", generator=g)
+    W, w = mx4(E * N, K, 3, K**-0.5)
+    X, x = mx4(T, K, 4)
+    y = B.hlq_expert_gemm(W, off, X, rows=rows, gated=gated, out_dtype=torch.bfloat16)
+    at = 0
+    for e, n in enumerate(counts.tolist()):
+        if n:
+            check(y[at:at + n], x[rows[at:at + n].long()], w[e * N:(e + 1) * N], gated)
+        at += n
