@@ -82,7 +82,9 @@ Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
             const double stream = weights / 5.2 * (E == 1 ? 1.0 : 0.7 + 0.3 * row_tiles(k.BM) / (double)used);
             double t = 3.5 + (share * stage > stream ? share * stage : stream);
             if (splits > 1) t += 2.0 + 2.0 * k.passes * ((splits + 3) / 4);
-            if (t < least || (t == least && k.BM == 256)) {   // as near where weights bound both: 256 x 256 streams them faster
+            // as near where weights bound both: 256 x 256 streams them faster (gated 4096 x 4096, 24 rows each of 32 experts 51 / 54, of 64
+            // not gated 105 / 115) but for the fewest rows (16 each, not gated 4096 x 2048 30 / 27)
+            if (t < least || (t == least && k.BM == 256 && each > 16)) {
                 least = t;
                 best.row_blocks = 0;
                 best.tile = Mx4TilePlan{k.BM, k.BN, (int)col_tiles, (int)mx4_row_tiles(R, E, k.BM), splits, share, 0, 0};

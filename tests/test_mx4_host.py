@@ -153,3 +153,9 @@ def test_no_scratch_memory(part):
     mine = {n: k for n, k in kernels().items() if part in n}
     assert mine
     assert {n: k[".private_segment_fixed_size"] for n, k in mine.items() if k[".private_segment_fixed_size"]} == {}
+
+
+def test_no_scratch_memory_in_large_products():
+    from test_kernel_resources import kernels
+    mine = {n: k for n, k in kernels().items() if "hlq_mx4_big_kernel" in n}
+    assert len(mine) == 2 and all(k[".private_segment_fixed_size"] == 0 for k in mine.values())
