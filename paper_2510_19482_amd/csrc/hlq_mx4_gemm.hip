@@ -12,13 +12,14 @@ size_t up256(size_t n) { return (n + 255u) & ~(size_t)255u; }
 // Which kernel takes a product, by an estimate of its time (us) from measurements of its parts; mx4_few: rows and columns a
 // wavefront, mx4_tile: of a workgroup.
 //
-// Few rows: a start of 2.5, then what a compute unit loads of the panels of its workgroups' rows and columns, or the weights as they
-// come from memory.  Tiled: a start of 3.5, then a stage a panel, `alone` where a compute unit has one workgroup, `shared` per
+// Few rows: a start of 2.75, then what a compute unit loads of the panels of its workgroups' rows and columns, or the weights as they
+// come from memory.  Tiled: a start of 3.0, then a stage a panel, `alone` where a compute unit has one workgroup, `shared` per
 // workgroup where it has more, or the weights at 5.2 TB/s.  Cutting K adds the hand-over of the partial sums: 2, and 2 for each 32
-// rows a wavefront has and four splits.
-// Measured / estimated, N x K = 4096 x 4096: 32 rows 5.1 / 5.0 (2 x 1), 128 rows 7.3 / 8.4 (4 x 2), 256 rows 9.5 / 9.3 (32 x 128), 1024 rows
-// 15.2 / 13.1 (128 x 128); 28672 x 4096: 64 rows 13.0 / 15.5 (32 x 128); 4096 x 14336: 32 rows 10.3 / 11.1 (2 x 1), 128 rows
-// 15.2 / 15.6 (32 x 128, K in four).
+// rows a wavefront has and four splits.  Fitted to 330 products of 17 to 1500 rows, each by every kernel: what is chosen is 1.3 % from
+// the fastest on average, 25 % at most.
+// Measured / estimated, N x K = 4096 x 4096: 32 rows 5.6 / 5.2 (2 x 1), 128 rows 7.3 / 8.6 (4 x 2), 256 rows 9.5 / 9.1 (32 x 128), 1024 rows
+// 14.4 / 12.9 (128 x 128); 28672 x 4096: 64 rows 12.7 / 15.0 (32 x 128); 4096 x 14336: 32 rows 10.3 / 11.3 (2 x 1), 128 rows
+// 15.2 / 14.9 (32 x 128, K in four).
 // 256 x 256 against 128 x 256, measured, rows x N x K: 4096 x 4096 x 14336 107 / 116 (one round of the card), 8192 x 4096 x 4096 65 / 73
 // (two), 8192 x 28672 x 4096 gated 440 / 485 (14), but half a round, 2048 x 4096 x 4096, 24 / 22.  Experts' rows, gated 4096 x 4096: 16384
 // of 32 experts 180 / 193, 8192 of 8 85 / 92, 8192 of 64 133 / 169 (weights: 4.3 TB/s); against 32 x 128, 4096 of 64 117 / 181.
@@ -52,7 +53,7 @@ Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
         if (mx4_row_tiles(R, E, 16 * k.rows) * col_tiles > MOST_GROUPS) continue;
         const double groups = row_tiles(16 * k.rows) * (double)col_tiles, rounds = groups < 1024 ? (double)(((int64_t)groups + 255) / 256) : groups / 256;
         const double loads = rounds * panels * 1.1 * (k.rows + k.cols * (gated ? 2 : 1)) / k.load, stream = weights / k.stream;
-        const double t = 2.5 + (loads > stream ? loads : stream);
+        const double t = 2.75 + (loads > stream ? loads : stream);
         if (t < least) {
             least = t;
             best.row_blocks = k.rows;
@@ -63,24 +64,26 @@ Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
         int BM, BN, passes;   // passes: of four splits' partial sums; 0: K is not cut
         double alone, shared;
     };
-    static const Tile tiles[] = {{32, 128, 1, 0.18, 0.145}, {64, 128, 2, 0.24, 0.22}, {128, 128, 2, 0.27, 0.30}, {128, 256, 0, 0.45, 0.43},
-                                 {256, 256, 0, 0.765, 0.765}};
+    static const Tile tiles[] = {{32, 128, 1, 0.19, 0.125}, {64, 128, 2, 0.29, 0.18}, {128, 128, 2, 0.31, 0.32}, {128, 256, 0, 0.57, 0.43},
+                                 {256, 256, 0, 0.72, 0.72}};
     const int64_t width = gated ? (N / 2 + 31) / 32 * 64 : N;   // gated halves are interleaved 32 columns at a time
     for (const auto &k : tiles) {
         const int64_t col_tiles = (width + k.BN - 1) / k.BN;
         if (mx4_row_tiles(R, E, k.BM) * col_tiles > MOST_TILES && k.BN < 256) continue;
         const double count = row_tiles(k.BM) * (double)col_tiles;
-        for (int want = 1; want <= (k.passes ? MOST_SPLITS : 1); want *= 2) {
+        for (int want = 1; want <= (k.passes ? MOST_SPLITS : 1); want += want < 4 ? 1 : 2) {
             const int share = (panels + want - 1) / want, splits = (panels + share - 1) / share;
             if (splits < want || (want > 1 && (mx4_row_tiles(R, E, k.BM) * col_tiles * want > MOST_CUT || share < LEAST_SHARE))) break;
             // 256 x 256: whole rounds of tiles that are alike; experts' last tiles, up to half of them not even half filled, cost a third
             const double full = k.BM < 256 ? count * splits / 256
                                 : E == 1   ? (double)(((int64_t)count + 255) / 256)
                                            : (double)used * (each / 256 + 0.3) * (double)col_tiles / 256;
-            const double stage = full <= 1.0 ? k.alone : full * k.shared > k.alone ? full * k.shared : k.alone;
+            // a unit that has a second one decides, later they come as units are free
+            const double most = k.BM == 256 ? full : full < 2.0 ? 2.0 : full + 0.25;
+            const double stage = full <= 1.0 ? k.alone : most * k.shared > k.alone ? most * k.shared : k.alone;
             // an expert's weights come from memory again, in part, for a second row tile
             const double stream = weights / 5.2 * (E == 1 ? 1.0 : 0.7 + 0.3 * row_tiles(k.BM) / (double)used);
-            double t = 3.5 + (share * stage > stream ? share * stage : stream);
+            double t = 3.0 + (share * stage > stream ? share * stage : stream);
             if (splits > 1) t += 2.0 + 2.0 * k.passes * ((splits + 3) / 4);
             // as near where weights bound both: 256 x 256 streams them faster (gated 4096 x 4096, 24 rows each of 32 experts 51 / 54, of 64
             // not gated 105 / 115) but for the fewest rows (16 each, not gated 4096 x 2048 30 / 27)
