@@ -10,19 +10,21 @@ constexpr int64_t QUANTIZE_INSIDE = 16384, QUANTIZED_BYTES = 65536;
 size_t up256(size_t n) { return (n + 255u) & ~(size_t)255u; }
 
 // Which kernel takes a product, by an estimate of its time (us) from measurements of its parts; mx4_few: rows and columns a
-// wavefront, mx4_tile: of a workgroup.
+// wavefront, mx4_tile and mx4_big: of a workgroup.
 //
-// Few rows: a start of 2.75, then what a compute unit loads of the panels of its workgroups' rows and columns, or the weights as they
-// come from memory.  Tiled: a start of 3.0, then a stage a panel, `alone` where a compute unit has one workgroup, `shared` per
-// workgroup where it has more, or the weights at 5.2 TB/s.  Cutting K adds the hand-over of the partial sums: 2, and 2 for each 32
-// rows a wavefront has and four splits.  Fitted to 330 products of 17 to 1500 rows, each by every kernel: what is chosen is 1.3 % from
-// the fastest on average, 25 % at most.
-// Measured / estimated, N x K = 4096 x 4096: 32 rows 5.6 / 5.2 (2 x 1), 128 rows 7.3 / 8.6 (4 x 2), 256 rows 9.5 / 9.1 (32 x 128), 1024 rows
-// 14.4 / 12.9 (128 x 128); 28672 x 4096: 64 rows 12.7 / 15.0 (32 x 128); 4096 x 14336: 32 rows 10.3 / 11.3 (2 x 1), 128 rows
-// 15.2 / 14.9 (32 x 128, K in four).
+// A start (2.9, tiled 3.1), then the longer of two.  First, what the busiest compute unit does.  Few rows: it loads the panels of its
+// workgroups' rows and columns.  Tiled: a workgroup takes `alone` a panel where it has the unit for itself, `shared` where there are
+// more, and `own` for its start and results (`search` more for experts, whose rows it looks up).  Second, memory: weights at 4.6 TB/s
+// (experts' 5.1), tiled 5.3, an expert's again in part for a second row tile; results, taken as 16 bits, at 4.2.  Cutting K adds the hand-over of
+// the partial sums: 1, and 3 for each 32 rows a wavefront has and four splits.
+//
+// Fitted to products that were each timed on every kernel (experts' rows 2 to 800 each, even and skewed; 17 to 16384 rows of one
+// matrix).  On 840 others what is chosen is from the fastest on average: 1.5 % up to 1500 rows, 0.8 % above, 4 % for experts; at most 56 %,
+// two rows each of 68 experts with K = 273.
 // 256 x 256 against 128 x 256, measured, rows x N x K: 4096 x 4096 x 14336 107 / 116 (one round of the card), 8192 x 4096 x 4096 65 / 73
 // (two), 8192 x 28672 x 4096 gated 440 / 485 (14), but half a round, 2048 x 4096 x 4096, 24 / 22.  Experts' rows, gated 4096 x 4096: 16384
-// of 32 experts 180 / 193, 8192 of 8 85 / 92, 8192 of 64 133 / 169 (weights: 4.3 TB/s); against 32 x 128, 4096 of 64 117 / 181.
+// of 32 experts 180 / 193, 8192 of 8 85 / 92, 8192 of 64 133 / 169 (weights: 4.3 TB/s); against 32 x 128, 4096 of 64 117 / 181; 7686 of 126,
+// 796 x 303 not gated, 22 / 12.
 constexpr int MOST_SPLITS = 8, LEAST_SHARE = 4, MOST_CUT = 512;   // of K, panels of one, workgroups of a product whose K is cut
 constexpr int64_t MOST_GROUPS = 1 << 22, MOST_TILES = 1 << 23;    // workgroups, so that a launch stays below 2^32 threads
 
@@ -43,17 +45,18 @@ Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
         return best;
     }
     double least = 1e30;
+    const double results = (double)R * (double)(gated ? N / 2 : N) * 2e-6 / 4.2;
     struct Few {
         int rows, cols;
-        double load, stream;   // bytes a nanosecond and compute unit, TB/s of weights
+        double load;   // bytes a nanosecond and compute unit
     };
-    static const Few few[] = {{1, 1, 43, 5.5}, {2, 1, 43, 5.0}, {2, 2, 43, 4.6}, {4, 2, 36, 4.2}};
+    static const Few few[] = {{1, 1, 43}, {2, 1, 43}, {2, 2, 43}, {4, 2, 34}};
     for (const auto &k : few) {
         const int64_t cols = gated ? N / 2 : N, col_tiles = (cols + 16 * k.cols - 1) / (16 * k.cols);
-        if (mx4_row_tiles(R, E, 16 * k.rows) * col_tiles > MOST_GROUPS) continue;
+        if (each > (E == 1 ? 600 : 64) || mx4_row_tiles(R, E, 16 * k.rows) * col_tiles > MOST_GROUPS) continue;   // above, no faster anywhere
         const double groups = row_tiles(16 * k.rows) * (double)col_tiles, rounds = groups < 1024 ? (double)(((int64_t)groups + 255) / 256) : groups / 256;
-        const double loads = rounds * panels * 1.1 * (k.rows + k.cols * (gated ? 2 : 1)) / k.load, stream = weights / k.stream;
-        const double t = 2.75 + (loads > stream ? loads : stream);
+        const double loads = rounds * panels * 1.1 * (k.rows + k.cols * (gated ? 2 : 1)) / k.load, stream = weights / (E == 1 ? 4.6 : 5.1) + results;
+        const double t = 2.9 + (loads > stream ? loads : stream);
         if (t < least) {
             least = t;
             best.row_blocks = k.rows;
@@ -62,32 +65,37 @@ Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
     }
     struct Tile {
         int BM, BN, passes;   // passes: of four splits' partial sums; 0: K is not cut
-        double alone, shared;
+        double alone, shared, own, search;
     };
-    static const Tile tiles[] = {{32, 128, 1, 0.19, 0.125}, {64, 128, 2, 0.29, 0.18}, {128, 128, 2, 0.31, 0.32}, {128, 256, 0, 0.57, 0.43},
-                                 {256, 256, 0, 0.72, 0.72}};
+    static const Tile tiles[] = {{32, 128, 1, 0.19, 0.12, 0.28, 0.55}, {64, 128, 2, 0.39, 0.204, 0.35, 1.0}, {128, 128, 2, 0.216, 0.211, 1.02, 1.7},
+                                 {128, 256, 0, 0.57, 0.42, 1.41, 1.0}, {256, 256, 0, 0.70, 0.70, 4.0, 2.0}};
     const int64_t width = gated ? (N / 2 + 31) / 32 * 64 : N;   // gated halves are interleaved 32 columns at a time
     for (const auto &k : tiles) {
         const int64_t col_tiles = (width + k.BN - 1) / k.BN;
         if (mx4_row_tiles(R, E, k.BM) * col_tiles > MOST_TILES && k.BN < 256) continue;
-        const double count = row_tiles(k.BM) * (double)col_tiles;
+        const double count = row_tiles(k.BM) * (double)col_tiles, own = k.own + (E > 1 ? k.search : 0.0);
+        const double stream = weights / 5.3 * (E == 1 ? 1.0 : 0.52 + 0.48 * row_tiles(k.BM) / (double)used) + results;
         for (int want = 1; want <= (k.passes ? MOST_SPLITS : 1); want += want < 4 ? 1 : 2) {
             const int share = (panels + want - 1) / want, splits = (panels + share - 1) / share;
             if (splits < want || (want > 1 && (mx4_row_tiles(R, E, k.BM) * col_tiles * want > MOST_CUT || share < LEAST_SHARE))) break;
-            // 256 x 256: whole rounds of tiles that are alike; experts' last tiles, up to half of them not even half filled, cost a third
-            const double full = k.BM < 256 ? count * splits / 256
-                                : E == 1   ? (double)(((int64_t)count + 255) / 256)
-                                           : (double)used * (each / 256 + 0.3) * (double)col_tiles / 256;
-            // a unit that has a second one decides, later they come as units are free
-            const double most = k.BM == 256 ? full : full < 2.0 ? 2.0 : full + 0.25;
-            const double stage = full <= 1.0 ? k.alone : most * k.shared > k.alone ? most * k.shared : k.alone;
-            // an expert's weights come from memory again, in part, for a second row tile
-            const double stream = weights / 5.2 * (E == 1 ? 1.0 : 0.7 + 0.3 * row_tiles(k.BM) / (double)used);
-            double t = 3.0 + (share * stage > stream ? share * stage : stream);
-            if (splits > 1) t += 2.0 + 2.0 * k.passes * ((splits + 3) / 4);
-            // as near where weights bound both: 256 x 256 streams them faster (gated 4096 x 4096, 24 rows each of 32 experts 51 / 54, of 64
-            // not gated 105 / 115) but for the fewest rows (16 each, not gated 4096 x 2048 30 / 27)
-            if (t < least || (t == least && k.BM == 256 && each > 16)) {
+            // workgroups, or tiles of 256 x 256, of a compute unit: whole rounds of the latter that are alike (an expert's last one, up to
+            // half of them not even half filled, counts 0.58); of the former two where some units have two, later as units are free
+            double full, most;
+            if (k.BM == 256) {
+                full = E == 1 ? (double)(((int64_t)count + 255) / 256) : (double)used * (each / 256 + 0.58) * (double)col_tiles / 256;
+                most = full;
+            } else {
+                full = count * splits / 256;
+                most = full < 2.0 ? 2.0 : full + 0.33;
+            }
+            double work = share * k.alone + own;
+            if (full > 1.0 && most * (share * k.shared + own) > work) work = most * (share * k.shared + own);
+            double t = 3.1 + (work > stream ? work : stream);
+            if (splits > 1) t += 1.0 + 3.0 * k.passes * ((splits + 3) / 4);
+            // as near where memory bounds both: larger tiles (gated 4096 x 4096, 24 rows each of 32 experts 51 / 54, of 64 not gated
+            // 105 / 115), but for experts' fewest rows (16 each, not gated 4096 x 2048 30 / 27) and rows that do not fill them (64,
+            // 28672 x 4096 13.7 / 12.7)
+            if (t < least || (t == least && (E == 1 ? R >= k.BM : each > 16))) {
                 least = t;
                 best.row_blocks = 0;
                 best.tile = Mx4TilePlan{k.BM, k.BN, (int)col_tiles, (int)mx4_row_tiles(R, E, k.BM), splits, share, 0, 0};
