@@ -128,3 +128,56 @@ def test_many_experts_of_few_rows(gated):
         if n:
             check(y[at:at + n], x[rows[at:at + n].long()], w[e * N:(e + 1) * N], gated)
         at += n
+
+
+# the same where K is long enough for the largest tiles by its own
+@pytest.mark.parametrize("dtype", list(HALF_ULP), ids=str)
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("at,room", [(0, 0), (3, 5), (64, 64)])
+def test_strides_of_longer_rows(at, room, gated, dtype):
+    M, N, K = 4010, 4032, 1500
+    cols = N // 2 if gated else N
+    W, w = mx4(N, K, 5, K**-0.5)
+    X, x = mx4(M, K, 6)
+    out = torch.full((M + 2, at + cols + room), 5.0, dtype=dtype, device="cuda")
+    y = out[1:1 + M, at:at + cols]
+    B.hlq_mx4_gemm(W, X, y, gated=gated)
+    check(y, x, w, gated)
+    y[:] = 5.0
+    assert bool((out == 5).all())
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("counts", [[7300], [1, 7299], [2000, 0, 3000, 2400], [7300, 100, 0, 0], [1850, 1850, 1850, 1850]], ids=str)
+def test_expert_product_of_longer_rows(counts, gated):
+    E, R, N, K, T = len(counts), sum(counts), 4096, 1500, 3000
+    g = torch.Generator("cuda").manual_seed(R + E)
+    rows = torch.randint(0, T, (R,), dtype=torch.int32, device="cuda", generator=g)
+    W, w = mx4(E * N, K, 3, K**-0.5)
+    X, x = mx4(T, K, 4)
+    off = torch.tensor([0] + counts, dtype=torch.int32, device="cuda").cumsum(0).int()
+    y = B.hlq_expert_gemm(W, off, X, rows=rows, gated=gated, out_dtype=torch.bfloat16)
+    at = 0
+    for e, n in enumerate(counts):
+        if n:
+            check(y[at:at + n], x[rows[at:at + n].long()], w[e * N:(e + 1) * N], gated)
+        at += n
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_more_experts_of_few_longer_rows(gated):
+    E, N, K, T = 24, 4096, 2048, 500
+    g = torch.Generator("cuda").manual_seed(10)
+    counts = torch.randint(0, 200, (E,), device="cuda", generator=g)
+    counts[:8] = torch.tensor([0, 1, 64, 65, 128, 129, 256, 257])
+    off = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), counts.cumsum(0)]).int()
+    R = int(off[-1])
+    rows = torch.randint(0, T, (R,), dtype=torch.int32, device="cuda", generator=g)
+    W, w = mx4(E * N, K, 3, K**-0.5)
+    X, x = mx4(T, K, 4)
+    y = B.hlq_expert_gemm(W, off, X, rows=rows, gated=gated, out_dtype=torch.float32)
+    at = 0
+    for e, n in enumerate(counts.tolist()):
+        if n:
+            check(y[at:at + n], x[rows[at:at + n].long()], w[e * N:(e + 1) * N], gated)
+        at += n
