@@ -6,6 +6,7 @@ the library has not been built, importing this module raises."""
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -406,18 +407,33 @@ def mx4_bytes(rows: int, K: int) -> int:
 
 
 class Mx4:
-    """A microscaled 4-bit matrix [rows, K]: the blob (u8) in the library's layout."""
+    """A microscaled 4-bit matrix [rows, K]: the blob (u8) in the library's layout.  Another blob may be put in its place."""
 
-    __slots__ = ("blob", "rows", "K", "on_gpu", "_ptr", "_bytes")
+    __slots__ = ("blob", "rows", "K", "_need")
 
     def __init__(self, blob, rows: int, K: int):
-        self.blob, self.rows, self.K = blob, int(rows), int(K)
-        self.on_gpu, self._ptr, self._bytes = blob.is_cuda, blob.data_ptr(), blob.numel()
-        if blob.dtype != torch.uint8 or not blob.is_contiguous() or self._bytes < mx4_bytes(rows, K):
-            raise ValueError(f"a blob of {mx4_bytes(rows, K)} bytes is needed for {rows} x {K}")
+        for name, value in (("rows", int(rows)), ("K", int(K)), ("_need", mx4_bytes(rows, K))):
+            object.__setattr__(self, name, value)
+        self.blob = blob
 
-    is_cuda = property(lambda self: self.on_gpu)
+    def __setattr__(self, name, value):
+        if name != "blob":
+            raise AttributeError(f"{name} of a matrix stays as it was made")
+        if value.dtype != torch.uint8 or not value.is_contiguous() or value.numel() < self._need:
+            raise ValueError(f"a blob of {self._need} bytes is needed for {self.rows} x {self.K}")
+        object.__setattr__(self, name, value)
+
+    is_cuda = property(lambda self: self.blob.is_cuda)
     device = property(lambda self: self.blob.device)
+
+
+def _blob(m: Mx4):
+    """Address and size of a matrix's blob as it is now: its data may have been replaced since the last call."""
+    blob = m.blob
+    size = blob.numel()
+    if size < m._need or not blob.is_contiguous():
+        raise ValueError(f"a blob of {m._need} bytes is needed for {m.rows} x {m.K}")
+    return blob.data_ptr(), size
 
 
 def alloc_mx4(rows: int, K: int, device="cuda", stream=None) -> Mx4:
@@ -436,9 +452,10 @@ def hlq_mx4_quantize(x, out: Mx4 | None = None, stream=None) -> Mx4:
     """Rows of x [rows, K] (f16, bf16 or f32) in 4-bit floats, a power-of-two scale for each 32 of a row."""
     rows, K, ptr, dtype, ld = _matrix(x)
     out = _mx4_out(out, rows, K, x.device, stream)
-    if not (x.is_cuda and out.on_gpu):
+    blob, size = _blob(out)
+    if not (x.is_cuda and out.blob.is_cuda):
         raise _not_on_gpu(x, out.blob)
-    status = lib.hlq_mx4_quantize(rows, K, ptr, dtype, ld, out._ptr, out._bytes, _stream_of(stream))
+    status = lib.hlq_mx4_quantize(rows, K, ptr, dtype, ld, blob, size, _stream_of(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_quantize", status)
     return out
@@ -451,9 +468,10 @@ def hlq_mx4_dequantize(m: Mx4, y=None, dtype=None, stream=None):
     rows, K, ptr, dtype, ld = _matrix(y)
     if rows != m.rows or K != m.K:
         raise ValueError(f"y has shape {tuple(y.shape)}, the matrix is {m.rows} x {m.K}")
-    if not (y.is_cuda and m.on_gpu):
+    blob, _ = _blob(m)
+    if not (y.is_cuda and m.blob.is_cuda):
         raise _not_on_gpu(y, m.blob)
-    status = lib.hlq_mx4_dequantize(rows, K, m._ptr, ptr, dtype, ld, _stream_of(stream))
+    status = lib.hlq_mx4_dequantize(rows, K, blob, ptr, dtype, ld, _stream_of(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_dequantize", status)
     return y
@@ -466,18 +484,20 @@ def hlq_mx4_pack(codes, scales, K: int, out: Mx4 | None = None, stream=None) -> 
         if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < least or (t.shape[1] > 1 and t.stride(1) != 1):
             raise ValueError(f"{name}: expected uint8 of shape ({rows}, at least {least}), rows contiguous, got {t.dtype} {tuple(t.shape)}")
     out = _mx4_out(out, rows, K, codes.device, stream)
-    if not (codes.is_cuda and scales.is_cuda and out.on_gpu):
+    blob, size = _blob(out)
+    if not (codes.is_cuda and scales.is_cuda and out.blob.is_cuda):
         raise _not_on_gpu(codes, scales, out.blob)
-    _check("hlq_mx4_pack", lib.hlq_mx4_pack(rows, K, _ptr(codes), codes.stride(0), _ptr(scales), scales.stride(0), out._ptr, out._bytes, _stream_ptr(stream)))
+    _check("hlq_mx4_pack", lib.hlq_mx4_pack(rows, K, _ptr(codes), codes.stride(0), _ptr(scales), scales.stride(0), blob, size, _stream_ptr(stream)))
     return out
 
 
 def hlq_mx4_unpack(m: Mx4, stream=None):
-    if not m.on_gpu:
+    blob, _ = _blob(m)
+    if not m.blob.is_cuda:
         raise _not_on_gpu(m.blob)
     codes = _empty((m.rows, (m.K + 1) // 2), torch.uint8, m.blob.device, stream)
     scales = _empty((m.rows, (m.K + 31) // 32), torch.uint8, m.blob.device, stream)
-    _check("hlq_mx4_unpack", lib.hlq_mx4_unpack(m.rows, m.K, m._ptr, _ptr(codes), _ptr(scales), _stream_ptr(stream)))
+    _check("hlq_mx4_unpack", lib.hlq_mx4_unpack(m.rows, m.K, blob, _ptr(codes), _ptr(scales), _stream_ptr(stream)))
     return codes, scales
 
 
@@ -496,7 +516,7 @@ def alloc_mx4_workspace(W: Mx4, x_rows: int, rows: int | None = None, experts: i
 
 def _operand(X):
     """(rows, columns, pointer, type, leading dimension) of a product's activations."""
-    return (X.rows, X.K, X._ptr, HLQ_MX4, 0) if type(X) is Mx4 else _matrix(X)
+    return (X.rows, X.K, _blob(X)[0], HLQ_MX4, 0) if type(X) is Mx4 else _matrix(X)
 
 
 def _product_out(W: Mx4, X, R: int, cols: int, out_dtype, stream):
@@ -508,7 +528,7 @@ def _product_out(W: Mx4, X, R: int, cols: int, out_dtype, stream):
 def hlq_mx4_gemm(W: Mx4, X, Y=None, gated: bool = False, out_dtype=None, ws=None, stream=None):
     """Y = Q(X) W^T, or with `gated` silu of its first half of columns times the second; X [M, K] f16, bf16 or f32, or Mx4."""
     M, K, x, xtype, ldx = _operand(X)
-    N = W.rows
+    N, (blob, _) = W.rows, _blob(W)
     cols = N // 2 if gated else N
     if Y is None:
         Y = _product_out(W, X, M, cols, out_dtype, stream)
@@ -517,29 +537,37 @@ def hlq_mx4_gemm(W: Mx4, X, Y=None, gated: bool = False, out_dtype=None, ws=None
         raise ValueError(f"X is {M} x {K}, W {N} x {W.K}, Y {y_rows} x {y_cols}{' (gated)' if gated else ''}")
     if ws is None:
         ws = alloc_mx4_workspace(W, M, stream=stream)
-    if not (W.on_gpu and X.is_cuda and Y.is_cuda and ws.is_cuda):
+    if not (W.blob.is_cuda and X.is_cuda and Y.is_cuda and ws.is_cuda):
         raise _not_on_gpu(W.blob, X, Y, ws)
-    status = lib.hlq_mx4_gemm(N, K, W._ptr, M, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0, ws.data_ptr(), ws.numel(), _stream_of(stream))
+    status = lib.hlq_mx4_gemm(N, K, blob, M, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0, ws.data_ptr(), ws.numel(), _stream_of(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_gemm", status)
     return Y
 
 
 class Route:
-    """What hlq_route writes: ids, weights, slots [T, k], offsets [E + 1], rows [T k], and its workspace."""
+    """What hlq_route writes: ids, weights, slots [T, k], offsets [E + 1], rows [T k], and its workspace; views of memory that lives as long
+    as this does."""
 
-    __slots__ = ("ids", "weights", "offsets", "rows", "slots", "ws", "T", "E", "k", "on_gpu", "_args")
+    __slots__ = ("ids", "weights", "offsets", "rows", "slots", "ws", "T", "E", "k", "on_gpu", "_memory", "_args")
 
     def __init__(self, T: int, E: int, k: int, device="cuda", stream=None):
         n = ctypes.c_size_t()
         _check("hlq_route_workspace_bytes", lib.hlq_route_workspace_bytes(T, E, k, ctypes.byref(n)))
-        self.T, self.E, self.k, self.on_gpu = T, E, k, torch.device(device).type == "cuda"
-        self.ids, self.slots = (_empty((T, k), torch.int32, device, stream) for _ in range(2))
-        self.weights = _empty((T, k), torch.float32, device, stream)
-        self.offsets = _empty(E + 1, torch.int32, device, stream)
-        self.rows = _empty(T * k, torch.int32, device, stream)
-        self.ws = _empty(n.value, torch.uint8, device, stream)
-        self._args = tuple(_ptr(t) for t in (self.ids, self.weights, self.offsets, self.rows, self.slots, self.ws)) + (n.value,)
+        parts = (("ids", torch.int32, (T, k)), ("weights", torch.float32, (T, k)), ("offsets", torch.int32, (E + 1,)), ("rows", torch.int32, (T * k,)),
+                 ("slots", torch.int32, (T, k)), ("ws", torch.uint8, (n.value,)))
+        sizes = [math.prod(shape) * dtype.itemsize for _, dtype, shape in parts]
+        starts = [0]
+        for size in sizes:
+            starts.append((starts[-1] + size + 15) // 16 * 16)
+        memory = _empty(starts[-1], torch.uint8, device, stream)
+        mine = {name: memory[at:at + size].view(dtype).view(shape) for (name, dtype, shape), at, size in zip(parts, starts, sizes)}
+        base = memory.data_ptr()
+        for name, value in dict(mine, T=T, E=E, k=k, on_gpu=memory.is_cuda, _memory=memory, _args=(*(base + at for at in starts[:-1]), n.value)).items():
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name} of a route stays as it was made")
 
 
 def alloc_route(T: int, E: int, k: int, device="cuda", stream=None) -> Route:
@@ -574,7 +602,7 @@ def hlq_expert_gemm(W: Mx4, offsets, X, Y=None, rows=None, gated: bool = False, 
         if rows.dtype != torch.int32 or not rows.is_contiguous():
             raise ValueError(f"rows: contiguous int32, got {rows.dtype}")
         R, rows_ptr = rows.numel(), rows.data_ptr()
-    N = W.rows // E
+    N, (blob, _) = W.rows // E, _blob(W)
     cols = N // 2 if gated else N
     if Y is None:
         Y = _product_out(W, X, R, cols, out_dtype, stream)
@@ -583,9 +611,9 @@ def hlq_expert_gemm(W: Mx4, offsets, X, Y=None, rows=None, gated: bool = False, 
         raise ValueError(f"X is {x_rows} x {K}, a matrix of W {N} x {W.K}, Y {y_rows} x {y_cols} for {R} rows{' (gated)' if gated else ''}")
     if ws is None:
         ws = alloc_mx4_workspace(W, x_rows, R, E, stream)
-    if not (W.on_gpu and offsets.is_cuda and X.is_cuda and Y.is_cuda and ws.is_cuda and (rows is None or rows.is_cuda)):
+    if not (W.blob.is_cuda and offsets.is_cuda and X.is_cuda and Y.is_cuda and ws.is_cuda and (rows is None or rows.is_cuda)):
         raise _not_on_gpu(W.blob, offsets, X, Y, ws, *([] if rows is None else [rows]))
-    status = lib.hlq_expert_gemm(E, N, K, W._ptr, offsets.data_ptr(), rows_ptr, R, x_rows, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0,
+    status = lib.hlq_expert_gemm(E, N, K, blob, offsets.data_ptr(), rows_ptr, R, x_rows, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0,
                                  ws.data_ptr(), ws.numel(), _stream_of(stream))
     if status != HLQ_OK:
         raise HlqError("hlq_expert_gemm", status)
