@@ -384,12 +384,22 @@ def _matrix(t):
 
 
 def _not_on_gpu(*tensors):
-    return ValueError(f"expected tensors on the GPU, got {', '.join(str(t.device) for t in tensors)}")
+    return ValueError(f"expected tensors on the GPU, all on one GPU, got {', '.join(str(t.device) for t in tensors)}")
 
 
-def _stream_of(stream) -> int:
-    """As _stream_ptr, for calls that have seen a tensor on the GPU."""
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else int(stream.cuda_stream)
+def _stream_of(stream, device: int) -> int:
+    """Handle of the stream that a call on this device runs on."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    if stream.device_index != device:
+        raise ValueError(f"the tensors are on cuda:{device}, the stream is of cuda:{stream.device_index}")
+    return int(stream.cuda_stream)
+
+
+def _there(device: int, call, *args):
+    """The call with its operands' device as the current one, which the library launches on."""
+    with torch.cuda.device(device):
+        return call(*args)
 
 
 def _empty(shape, dtype, device, stream):
@@ -426,6 +436,9 @@ class Mx4:
     is_cuda = property(lambda self: self.blob.is_cuda)
     device = property(lambda self: self.blob.device)
 
+    def get_device(self) -> int:
+        return self.blob.get_device()
+
 
 def _blob(m: Mx4):
     """Address and size of a matrix's blob as it is now: its data may have been replaced since the last call."""
@@ -453,9 +466,12 @@ def hlq_mx4_quantize(x, out: Mx4 | None = None, stream=None) -> Mx4:
     rows, K, ptr, dtype, ld = _matrix(x)
     out = _mx4_out(out, rows, K, x.device, stream)
     blob, size = _blob(out)
-    if not (x.is_cuda and out.blob.is_cuda):
+    device = x.get_device()
+    if device < 0 or out.blob.get_device() != device:
         raise _not_on_gpu(x, out.blob)
-    status = lib.hlq_mx4_quantize(rows, K, ptr, dtype, ld, blob, size, _stream_of(stream))
+    if device != torch._C._cuda_getDevice():
+        return _there(device, hlq_mx4_quantize, x, out, stream)
+    status = lib.hlq_mx4_quantize(rows, K, ptr, dtype, ld, blob, size, _stream_of(stream, device))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_quantize", status)
     return out
@@ -469,9 +485,12 @@ def hlq_mx4_dequantize(m: Mx4, y=None, dtype=None, stream=None):
     if rows != m.rows or K != m.K:
         raise ValueError(f"y has shape {tuple(y.shape)}, the matrix is {m.rows} x {m.K}")
     blob, _ = _blob(m)
-    if not (y.is_cuda and m.blob.is_cuda):
+    device = y.get_device()
+    if device < 0 or m.blob.get_device() != device:
         raise _not_on_gpu(y, m.blob)
-    status = lib.hlq_mx4_dequantize(rows, K, blob, ptr, dtype, ld, _stream_of(stream))
+    if device != torch._C._cuda_getDevice():
+        return _there(device, hlq_mx4_dequantize, m, y, None, stream)
+    status = lib.hlq_mx4_dequantize(rows, K, blob, ptr, dtype, ld, _stream_of(stream, device))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_dequantize", status)
     return y
@@ -485,19 +504,25 @@ def hlq_mx4_pack(codes, scales, K: int, out: Mx4 | None = None, stream=None) -> 
             raise ValueError(f"{name}: expected uint8 of shape ({rows}, at least {least}), rows contiguous, got {t.dtype} {tuple(t.shape)}")
     out = _mx4_out(out, rows, K, codes.device, stream)
     blob, size = _blob(out)
-    if not (codes.is_cuda and scales.is_cuda and out.blob.is_cuda):
+    device = codes.get_device()
+    if device < 0 or scales.get_device() != device or out.blob.get_device() != device:
         raise _not_on_gpu(codes, scales, out.blob)
-    _check("hlq_mx4_pack", lib.hlq_mx4_pack(rows, K, _ptr(codes), codes.stride(0), _ptr(scales), scales.stride(0), blob, size, _stream_ptr(stream)))
+    if device != torch._C._cuda_getDevice():
+        return _there(device, hlq_mx4_pack, codes, scales, K, out, stream)
+    _check("hlq_mx4_pack", lib.hlq_mx4_pack(rows, K, _ptr(codes), codes.stride(0), _ptr(scales), scales.stride(0), blob, size, _stream_of(stream, device)))
     return out
 
 
 def hlq_mx4_unpack(m: Mx4, stream=None):
     blob, _ = _blob(m)
-    if not m.blob.is_cuda:
+    device = m.blob.get_device()
+    if device < 0:
         raise _not_on_gpu(m.blob)
+    if device != torch._C._cuda_getDevice():
+        return _there(device, hlq_mx4_unpack, m, stream)
     codes = _empty((m.rows, (m.K + 1) // 2), torch.uint8, m.blob.device, stream)
     scales = _empty((m.rows, (m.K + 31) // 32), torch.uint8, m.blob.device, stream)
-    _check("hlq_mx4_unpack", lib.hlq_mx4_unpack(m.rows, m.K, blob, _ptr(codes), _ptr(scales), _stream_ptr(stream)))
+    _check("hlq_mx4_unpack", lib.hlq_mx4_unpack(m.rows, m.K, blob, _ptr(codes), _ptr(scales), _stream_of(stream, device)))
     return codes, scales
 
 
@@ -509,8 +534,13 @@ def mx4_workspace_bytes(N: int, K: int, experts: int, x_rows: int, rows: int) ->
 
 def alloc_mx4_workspace(W: Mx4, x_rows: int, rows: int | None = None, experts: int = 1, stream=None):
     """Workspace for products with W of up to x_rows activation rows and `rows` result rows (the same if not given)."""
+    device = W.blob.get_device()
+    if device < 0:
+        raise _not_on_gpu(W.blob)
+    if device != torch._C._cuda_getDevice():
+        return _there(device, alloc_mx4_workspace, W, x_rows, rows, experts, stream)
     ws = _empty(mx4_workspace_bytes(W.rows // experts, W.K, experts, x_rows, x_rows if rows is None else rows), torch.uint8, W.blob.device, stream)
-    _check("hlq_workspace_init", lib.hlq_workspace_init(_ptr(ws), ws.numel(), _stream_ptr(stream)))
+    _check("hlq_workspace_init", lib.hlq_workspace_init(_ptr(ws), ws.numel(), _stream_of(stream, device)))
     return ws
 
 
@@ -537,9 +567,12 @@ def hlq_mx4_gemm(W: Mx4, X, Y=None, gated: bool = False, out_dtype=None, ws=None
         raise ValueError(f"X is {M} x {K}, W {N} x {W.K}, Y {y_rows} x {y_cols}{' (gated)' if gated else ''}")
     if ws is None:
         ws = alloc_mx4_workspace(W, M, stream=stream)
-    if not (W.blob.is_cuda and X.is_cuda and Y.is_cuda and ws.is_cuda):
+    device = W.blob.get_device()
+    if device < 0 or X.get_device() != device or Y.get_device() != device or ws.get_device() != device:
         raise _not_on_gpu(W.blob, X, Y, ws)
-    status = lib.hlq_mx4_gemm(N, K, blob, M, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0, ws.data_ptr(), ws.numel(), _stream_of(stream))
+    if device != torch._C._cuda_getDevice():
+        return _there(device, hlq_mx4_gemm, W, X, Y, gated, None, ws, stream)
+    status = lib.hlq_mx4_gemm(N, K, blob, M, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0, ws.data_ptr(), ws.numel(), _stream_of(stream, device))
     if status != HLQ_OK:
         raise HlqError("hlq_mx4_gemm", status)
     return Y
@@ -549,7 +582,7 @@ class Route:
     """What hlq_route writes: ids, weights, slots [T, k], offsets [E + 1], rows [T k], and its workspace; views of memory that lives as long
     as this does."""
 
-    __slots__ = ("ids", "weights", "offsets", "rows", "slots", "ws", "T", "E", "k", "on_gpu", "_memory", "_args")
+    __slots__ = ("ids", "weights", "offsets", "rows", "slots", "ws", "T", "E", "k", "_device", "_memory", "_args")
 
     def __init__(self, T: int, E: int, k: int, device="cuda", stream=None):
         n = ctypes.c_size_t()
@@ -563,7 +596,7 @@ class Route:
         memory = _empty(starts[-1], torch.uint8, device, stream)
         mine = {name: memory[at:at + size].view(dtype).view(shape) for (name, dtype, shape), at, size in zip(parts, starts, sizes)}
         base = memory.data_ptr()
-        for name, value in dict(mine, T=T, E=E, k=k, on_gpu=memory.is_cuda, _memory=memory, _args=(*(base + at for at in starts[:-1]), n.value)).items():
+        for name, value in dict(mine, T=T, E=E, k=k, _device=memory.get_device(), _memory=memory, _args=(*(base + at for at in starts[:-1]), n.value)).items():
             object.__setattr__(self, name, value)
 
     def __setattr__(self, name, value):
@@ -581,9 +614,12 @@ def hlq_route(logits, k: int, renorm: bool = True, out: Route | None = None, str
         out = Route(T, E, k, logits.device, stream)
     elif out.T != T or out.E != E or out.k != k:
         raise ValueError(f"the output is for {out.T} tokens, {out.E} experts, {out.k} each")
-    if not (logits.is_cuda and out.on_gpu):
-        raise _not_on_gpu(logits, out.offsets)
-    status = lib.hlq_route(T, E, k, ptr, dtype, ld, 1 if renorm else 0, *out._args, _stream_of(stream))
+    device = logits.get_device()
+    if device < 0 or out._device != device:
+        raise _not_on_gpu(logits, out._memory)
+    if device != torch._C._cuda_getDevice():
+        return _there(device, hlq_route, logits, k, renorm, out, stream)
+    status = lib.hlq_route(T, E, k, ptr, dtype, ld, 1 if renorm else 0, *out._args, _stream_of(stream, device))
     if status != HLQ_OK:
         raise HlqError("hlq_route", status)
     return out
@@ -611,10 +647,14 @@ def hlq_expert_gemm(W: Mx4, offsets, X, Y=None, rows=None, gated: bool = False, 
         raise ValueError(f"X is {x_rows} x {K}, a matrix of W {N} x {W.K}, Y {y_rows} x {y_cols} for {R} rows{' (gated)' if gated else ''}")
     if ws is None:
         ws = alloc_mx4_workspace(W, x_rows, R, E, stream)
-    if not (W.blob.is_cuda and offsets.is_cuda and X.is_cuda and Y.is_cuda and ws.is_cuda and (rows is None or rows.is_cuda)):
+    device = W.blob.get_device()
+    if (device < 0 or offsets.get_device() != device or X.get_device() != device or Y.get_device() != device or ws.get_device() != device
+            or (rows is not None and rows.get_device() != device)):
         raise _not_on_gpu(W.blob, offsets, X, Y, ws, *([] if rows is None else [rows]))
+    if device != torch._C._cuda_getDevice():
+        return _there(device, hlq_expert_gemm, W, offsets, X, Y, rows, gated, None, ws, stream)
     status = lib.hlq_expert_gemm(E, N, K, blob, offsets.data_ptr(), rows_ptr, R, x_rows, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0,
-                                 ws.data_ptr(), ws.numel(), _stream_of(stream))
+                                 ws.data_ptr(), ws.numel(), _stream_of(stream, device))
     if status != HLQ_OK:
         raise HlqError("hlq_expert_gemm", status)
     return Y
@@ -631,9 +671,12 @@ def hlq_expert_combine(Y, slots, weights, out=None, out_dtype=None, stream=None)
     o_rows, o_cols, o, otype, ldo = _matrix(out)
     if o_rows != T or o_cols != D:
         raise ValueError(f"out has shape {tuple(out.shape)}, the result is {T} x {D}")
-    if not (Y.is_cuda and slots.is_cuda and weights.is_cuda and out.is_cuda):
+    device = Y.get_device()
+    if device < 0 or slots.get_device() != device or weights.get_device() != device or out.get_device() != device:
         raise _not_on_gpu(Y, slots, weights, out)
-    status = lib.hlq_expert_combine(T, k, D, R, y, ytype, ldy, slots.data_ptr(), weights.data_ptr(), o, otype, ldo, _stream_of(stream))
+    if device != torch._C._cuda_getDevice():
+        return _there(device, hlq_expert_combine, Y, slots, weights, out, None, stream)
+    status = lib.hlq_expert_combine(T, k, D, R, y, ytype, ldy, slots.data_ptr(), weights.data_ptr(), o, otype, ldo, _stream_of(stream, device))
     if status != HLQ_OK:
         raise HlqError("hlq_expert_combine", status)
     return out
