@@ -387,10 +387,14 @@ def _not_on_gpu(*tensors):
     return ValueError(f"expected tensors on the GPU, all on one GPU, got {', '.join(str(t.device) for t in tensors)}")
 
 
+_current_device = torch._C._cuda_getDevice
+_current_stream = torch._C._cuda_getCurrentRawStream   # of a device, its handle
+
+
 def _stream_of(stream, device: int) -> int:
     """Handle of the stream that a call on this device runs on."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device)
+        return _current_stream(device)
     if stream.device_index != device:
         raise ValueError(f"the tensors are on cuda:{device}, the stream is of cuda:{stream.device_index}")
     return int(stream.cuda_stream)
@@ -419,7 +423,7 @@ def mx4_bytes(rows: int, K: int) -> int:
 class Mx4:
     """A microscaled 4-bit matrix [rows, K]: the blob (u8) in the library's layout.  Another blob may be put in its place."""
 
-    __slots__ = ("blob", "rows", "K", "_need")
+    __slots__ = ("blob", "rows", "K", "_need", "_kept", "_ptr", "_size", "_device")
 
     def __init__(self, blob, rows: int, K: int):
         for name, value in (("rows", int(rows)), ("K", int(K)), ("_need", mx4_bytes(rows, K))):
@@ -429,9 +433,14 @@ class Mx4:
     def __setattr__(self, name, value):
         if name != "blob":
             raise AttributeError(f"{name} of a matrix stays as it was made")
-        if value.dtype != torch.uint8 or not value.is_contiguous() or value.numel() < self._need:
-            raise ValueError(f"a blob of {self._need} bytes is needed for {self.rows} x {self.K}")
+        self._take(value)
         object.__setattr__(self, name, value)
+
+    def _take(self, blob) -> None:
+        if blob.dtype != torch.uint8 or not blob.is_contiguous() or min(blob.numel(), blob.untyped_storage().nbytes() - blob.storage_offset()) < self._need:
+            raise ValueError(f"a blob of {self._need} bytes is needed for {self.rows} x {self.K}")
+        for name, value in (("_kept", blob.detach()), ("_ptr", blob.data_ptr()), ("_size", blob.numel()), ("_device", blob.get_device())):
+            object.__setattr__(self, name, value)
 
     is_cuda = property(lambda self: self.blob.is_cuda)
     device = property(lambda self: self.blob.device)
@@ -441,12 +450,11 @@ class Mx4:
 
 
 def _blob(m: Mx4):
-    """Address and size of a matrix's blob as it is now: its data may have been replaced since the last call."""
-    blob = m.blob
-    size = blob.numel()
-    if size < m._need or not blob.is_contiguous():
-        raise ValueError(f"a blob of {m._need} bytes is needed for {m.rows} x {m.K}")
-    return blob.data_ptr(), size
+    """Address, size and device of a matrix's blob as it is now.  Its data may have been replaced since the last call; at the address that was
+    taken then it has not been, since that memory is kept and nothing else can be there."""
+    if m.blob.data_ptr() != m._ptr:
+        m._take(m.blob)
+    return m._ptr, m._size, m._device
 
 
 def alloc_mx4(rows: int, K: int, device="cuda", stream=None) -> Mx4:
@@ -465,11 +473,11 @@ def hlq_mx4_quantize(x, out: Mx4 | None = None, stream=None) -> Mx4:
     """Rows of x [rows, K] (f16, bf16 or f32) in 4-bit floats, a power-of-two scale for each 32 of a row."""
     rows, K, ptr, dtype, ld = _matrix(x)
     out = _mx4_out(out, rows, K, x.device, stream)
-    blob, size = _blob(out)
+    blob, size, at = _blob(out)
     device = x.get_device()
-    if device < 0 or out.blob.get_device() != device:
+    if device < 0 or at != device:
         raise _not_on_gpu(x, out.blob)
-    if device != torch._C._cuda_getDevice():
+    if device != _current_device():
         return _there(device, hlq_mx4_quantize, x, out, stream)
     status = lib.hlq_mx4_quantize(rows, K, ptr, dtype, ld, blob, size, _stream_of(stream, device))
     if status != HLQ_OK:
@@ -484,11 +492,10 @@ def hlq_mx4_dequantize(m: Mx4, y=None, dtype=None, stream=None):
     rows, K, ptr, dtype, ld = _matrix(y)
     if rows != m.rows or K != m.K:
         raise ValueError(f"y has shape {tuple(y.shape)}, the matrix is {m.rows} x {m.K}")
-    blob, _ = _blob(m)
-    device = y.get_device()
-    if device < 0 or m.blob.get_device() != device:
+    blob, _, device = _blob(m)
+    if device < 0 or y.get_device() != device:
         raise _not_on_gpu(y, m.blob)
-    if device != torch._C._cuda_getDevice():
+    if device != _current_device():
         return _there(device, hlq_mx4_dequantize, m, y, None, stream)
     status = lib.hlq_mx4_dequantize(rows, K, blob, ptr, dtype, ld, _stream_of(stream, device))
     if status != HLQ_OK:
@@ -503,22 +510,20 @@ def hlq_mx4_pack(codes, scales, K: int, out: Mx4 | None = None, stream=None) -> 
         if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < least or (t.shape[1] > 1 and t.stride(1) != 1):
             raise ValueError(f"{name}: expected uint8 of shape ({rows}, at least {least}), rows contiguous, got {t.dtype} {tuple(t.shape)}")
     out = _mx4_out(out, rows, K, codes.device, stream)
-    blob, size = _blob(out)
-    device = codes.get_device()
-    if device < 0 or scales.get_device() != device or out.blob.get_device() != device:
+    blob, size, device = _blob(out)
+    if device < 0 or codes.get_device() != device or scales.get_device() != device:
         raise _not_on_gpu(codes, scales, out.blob)
-    if device != torch._C._cuda_getDevice():
+    if device != _current_device():
         return _there(device, hlq_mx4_pack, codes, scales, K, out, stream)
     _check("hlq_mx4_pack", lib.hlq_mx4_pack(rows, K, _ptr(codes), codes.stride(0), _ptr(scales), scales.stride(0), blob, size, _stream_of(stream, device)))
     return out
 
 
 def hlq_mx4_unpack(m: Mx4, stream=None):
-    blob, _ = _blob(m)
-    device = m.blob.get_device()
+    blob, _, device = _blob(m)
     if device < 0:
         raise _not_on_gpu(m.blob)
-    if device != torch._C._cuda_getDevice():
+    if device != _current_device():
         return _there(device, hlq_mx4_unpack, m, stream)
     codes = _empty((m.rows, (m.K + 1) // 2), torch.uint8, m.blob.device, stream)
     scales = _empty((m.rows, (m.K + 31) // 32), torch.uint8, m.blob.device, stream)
@@ -537,16 +542,16 @@ def alloc_mx4_workspace(W: Mx4, x_rows: int, rows: int | None = None, experts: i
     device = W.blob.get_device()
     if device < 0:
         raise _not_on_gpu(W.blob)
-    if device != torch._C._cuda_getDevice():
+    if device != _current_device():
         return _there(device, alloc_mx4_workspace, W, x_rows, rows, experts, stream)
     ws = _empty(mx4_workspace_bytes(W.rows // experts, W.K, experts, x_rows, x_rows if rows is None else rows), torch.uint8, W.blob.device, stream)
     _check("hlq_workspace_init", lib.hlq_workspace_init(_ptr(ws), ws.numel(), _stream_of(stream, device)))
     return ws
 
 
-def _operand(X):
-    """(rows, columns, pointer, type, leading dimension) of a product's activations."""
-    return (X.rows, X.K, _blob(X)[0], HLQ_MX4, 0) if type(X) is Mx4 else _matrix(X)
+def _operand(X: Mx4):
+    """As _matrix, of activations that are quantized already."""
+    return X.rows, X.K, _blob(X)[0], HLQ_MX4, 0
 
 
 def _product_out(W: Mx4, X, R: int, cols: int, out_dtype, stream):
@@ -557,8 +562,9 @@ def _product_out(W: Mx4, X, R: int, cols: int, out_dtype, stream):
 
 def hlq_mx4_gemm(W: Mx4, X, Y=None, gated: bool = False, out_dtype=None, ws=None, stream=None):
     """Y = Q(X) W^T, or with `gated` silu of its first half of columns times the second; X [M, K] f16, bf16 or f32, or Mx4."""
-    M, K, x, xtype, ldx = _operand(X)
-    N, (blob, _) = W.rows, _blob(W)
+    M, K, x, xtype, ldx = _operand(X) if type(X) is Mx4 else _matrix(X)
+    blob, _, device = _blob(W)
+    N = W.rows
     cols = N // 2 if gated else N
     if Y is None:
         Y = _product_out(W, X, M, cols, out_dtype, stream)
@@ -567,10 +573,9 @@ def hlq_mx4_gemm(W: Mx4, X, Y=None, gated: bool = False, out_dtype=None, ws=None
         raise ValueError(f"X is {M} x {K}, W {N} x {W.K}, Y {y_rows} x {y_cols}{' (gated)' if gated else ''}")
     if ws is None:
         ws = alloc_mx4_workspace(W, M, stream=stream)
-    device = W.blob.get_device()
     if device < 0 or X.get_device() != device or Y.get_device() != device or ws.get_device() != device:
         raise _not_on_gpu(W.blob, X, Y, ws)
-    if device != torch._C._cuda_getDevice():
+    if device != _current_device():
         return _there(device, hlq_mx4_gemm, W, X, Y, gated, None, ws, stream)
     status = lib.hlq_mx4_gemm(N, K, blob, M, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0, ws.data_ptr(), ws.numel(), _stream_of(stream, device))
     if status != HLQ_OK:
@@ -617,7 +622,7 @@ def hlq_route(logits, k: int, renorm: bool = True, out: Route | None = None, str
     device = logits.get_device()
     if device < 0 or out._device != device:
         raise _not_on_gpu(logits, out._memory)
-    if device != torch._C._cuda_getDevice():
+    if device != _current_device():
         return _there(device, hlq_route, logits, k, renorm, out, stream)
     status = lib.hlq_route(T, E, k, ptr, dtype, ld, 1 if renorm else 0, *out._args, _stream_of(stream, device))
     if status != HLQ_OK:
@@ -631,14 +636,15 @@ def hlq_expert_gemm(W: Mx4, offsets, X, Y=None, rows=None, gated: bool = False, 
     E = offsets.numel() - 1
     if E < 1 or W.rows % E or offsets.dtype != torch.int32 or not offsets.is_contiguous():
         raise ValueError(f"offsets: int32, one more than experts; {offsets.numel()} of {offsets.dtype} for {W.rows} rows of weights")
-    x_rows, K, x, xtype, ldx = _operand(X)
+    x_rows, K, x, xtype, ldx = _operand(X) if type(X) is Mx4 else _matrix(X)
     if rows is None:
         R, rows_ptr = x_rows, None
     else:
         if rows.dtype != torch.int32 or not rows.is_contiguous():
             raise ValueError(f"rows: contiguous int32, got {rows.dtype}")
         R, rows_ptr = rows.numel(), rows.data_ptr()
-    N, (blob, _) = W.rows // E, _blob(W)
+    blob, _, device = _blob(W)
+    N = W.rows // E
     cols = N // 2 if gated else N
     if Y is None:
         Y = _product_out(W, X, R, cols, out_dtype, stream)
@@ -647,11 +653,10 @@ def hlq_expert_gemm(W: Mx4, offsets, X, Y=None, rows=None, gated: bool = False, 
         raise ValueError(f"X is {x_rows} x {K}, a matrix of W {N} x {W.K}, Y {y_rows} x {y_cols} for {R} rows{' (gated)' if gated else ''}")
     if ws is None:
         ws = alloc_mx4_workspace(W, x_rows, R, E, stream)
-    device = W.blob.get_device()
     if (device < 0 or offsets.get_device() != device or X.get_device() != device or Y.get_device() != device or ws.get_device() != device
             or (rows is not None and rows.get_device() != device)):
         raise _not_on_gpu(W.blob, offsets, X, Y, ws, *([] if rows is None else [rows]))
-    if device != torch._C._cuda_getDevice():
+    if device != _current_device():
         return _there(device, hlq_expert_gemm, W, offsets, X, Y, rows, gated, None, ws, stream)
     status = lib.hlq_expert_gemm(E, N, K, blob, offsets.data_ptr(), rows_ptr, R, x_rows, x, xtype, ldx, y, ytype, ldy, 1 if gated else 0,
                                  ws.data_ptr(), ws.numel(), _stream_of(stream, device))
@@ -674,7 +679,7 @@ def hlq_expert_combine(Y, slots, weights, out=None, out_dtype=None, stream=None)
     device = Y.get_device()
     if device < 0 or slots.get_device() != device or weights.get_device() != device or out.get_device() != device:
         raise _not_on_gpu(Y, slots, weights, out)
-    if device != torch._C._cuda_getDevice():
+    if device != _current_device():
         return _there(device, hlq_expert_combine, Y, slots, weights, out, None, stream)
     status = lib.hlq_expert_combine(T, k, D, R, y, ytype, ldy, slots.data_ptr(), weights.data_ptr(), o, otype, ldo, _stream_of(stream, device))
     if status != HLQ_OK:

@@ -1,6 +1,7 @@
 """Operands on several devices are refused, and a call runs on the device that its operands are on, whichever is current.  Without a GPU:
 stand-ins for tensors of devices that are not here, and for the library, which note what a call does."""
 import contextlib
+import types
 
 import pytest
 import torch
@@ -33,6 +34,15 @@ class Tensor:
     def data_ptr(self):
         return 0x1000
 
+    def detach(self):
+        return self
+
+    def untyped_storage(self):
+        return types.SimpleNamespace(nbytes=self.numel)
+
+    def storage_offset(self):
+        return 0
+
 
 class Stream:
     def __init__(self, device):
@@ -63,9 +73,8 @@ def machine(monkeypatch):
         setattr(library, name, getattr(sizes, name))
     monkeypatch.setattr(B, "lib", library)
     monkeypatch.setattr(torch.cuda, "device", on)
-    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
-    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0], raising=False)
-    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 100 + device, raising=False)
+    monkeypatch.setattr(B, "_current_device", lambda: current[0])
+    monkeypatch.setattr(B, "_current_stream", lambda device: 100 + device)
     return launched
 
 

@@ -14,11 +14,23 @@ def test_a_matrix_is_where_its_blob_is():
     m = matrix()
     other = torch.ones_like(m.blob)
     m.blob = other
-    assert B._blob(m) == (other.data_ptr(), other.numel())
+    assert B._blob(m) == (other.data_ptr(), other.numel(), -1)
     third = torch.ones_like(other)
     m.blob.data = third
-    assert B._blob(m) == (third.data_ptr(), third.numel())
+    assert B._blob(m) == (third.data_ptr(), third.numel(), -1)
     assert not m.is_cuda and m.device == third.device
+
+
+def test_memory_that_a_call_was_handed_is_not_anothers():
+    # while the matrix still has the address of its last call, nothing else can lie there
+    m = matrix()
+    at = m.blob.data_ptr()
+    m.blob.data = torch.zeros_like(m.blob)
+    assert all(torch.zeros(m._need, dtype=torch.uint8).data_ptr() != at for _ in range(100))
+    assert B._blob(m)[0] == m.blob.data_ptr() != at
+    m.blob.untyped_storage().resize_(0)
+    with pytest.raises(ValueError):
+        B._blob(m)
 
 
 def test_a_blob_that_does_not_hold_the_matrix_is_refused():
