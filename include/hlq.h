@@ -328,6 +328,18 @@ HLQ_API hlq_status hlq_mx4_unpack(int64_t rows, int32_t K, const void *blob, uin
  * numbers of x_rows and rows with this K, N and number of experts.  hlq_workspace_init has to have seen it once, as other workspaces. */
 HLQ_API hlq_status hlq_mx4_workspace_bytes(int64_t N, int32_t K, int32_t experts, int64_t x_rows, int64_t rows, size_t *bytes);
 
+/* Host-only: the kernel that such a call goes to (rows > 0); nothing is launched and no GPU is needed.  For tests and tools. */
+typedef struct {
+    int32_t kernel;              /* 1 = few rows, no LDS in the loop; 2 = tiles through LDS; 3 = the largest tiles, workgroups go from one to the next */
+    int32_t tile_rows, tile_cols; /* rows of the result and of W that a wavefront (kernel 1; twice tile_cols of W gated) or a workgroup has */
+    int32_t k_parts;             /* K is cut over as many wavefronts of a workgroup (kernel 1) or workgroups (kernel 2) */
+    int32_t quantizes;           /* 1: the kernel quantizes the activations; 0: a launch before it does, or they are MX4 */
+    int32_t reserved;
+    int64_t workspace_bytes;     /* that this call needs, at most hlq_mx4_workspace_bytes() */
+} hlq_mx4_plan_info;
+HLQ_API hlq_status hlq_mx4_plan_query(int64_t N, int32_t K, int32_t experts, int64_t x_rows, int64_t rows, hlq_dtype xtype, hlq_mx4_epilogue epilogue,
+                                      hlq_mx4_plan_info *out);
+
 /* Y[M, .] = epilogue(Q(X) W^T): W an MX4 blob of N rows (a row per output column) and K; X [M, K] f16, bf16 or f32 with leading
  * dimension ldx, quantized as hlq_mx4_quantize does (in the kernel or into the workspace), or an MX4 blob (ldx is not used).
  * Products and the sums over a block are exact, sums over blocks fp32; Y of type ytype is rounded once, leading dimension ldy >= its

@@ -27,6 +27,10 @@ class GemvPlanInfo(ctypes.Structure):
                                               "slices", "tile_groups", "first_block", "blocks")]
 
 
+class Mx4PlanInfo(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("kernel", "tile_rows", "tile_cols", "k_parts", "quantizes", "reserved")] + [("workspace_bytes", ctypes.c_int64)]
+
+
 class HlqError(RuntimeError):
     def __init__(self, fn: str, status: int):
         self.status = status
@@ -42,6 +46,7 @@ _MX4_ARGS = {
     "hlq_mx4_pack": [_i64, _i32, _vp, _i64, _vp, _i64, _vp, _sz, _vp],
     "hlq_mx4_unpack": [_i64, _i32, _vp, _vp, _vp, _vp],
     "hlq_mx4_workspace_bytes": [_i64, _i32, _i32, _i64, _i64, _szp],
+    "hlq_mx4_plan_query": [_i64, _i32, _i32, _i64, _i64, _int, _int, ctypes.POINTER(Mx4PlanInfo)],
     "hlq_mx4_gemm": [_i64, _i32, _vp, _i64, _vp, _int, _i64, _vp, _int, _i64, _int, _vp, _sz, _vp],
     "hlq_route_workspace_bytes": [_i64, _i32, _i32, _szp],
     "hlq_route": [_i64, _i32, _i32, _vp, _int, _i64, _int, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
@@ -535,6 +540,13 @@ def mx4_workspace_bytes(N: int, K: int, experts: int, x_rows: int, rows: int) ->
     n = ctypes.c_size_t()
     _check("hlq_mx4_workspace_bytes", lib.hlq_mx4_workspace_bytes(N, K, experts, x_rows, rows, ctypes.byref(n)))
     return n.value
+
+
+def mx4_plan_query(N: int, K: int, rows: int, experts: int = 1, x_rows: int | None = None, xtype: int = HLQ_MX4, gated: bool = False) -> Mx4PlanInfo:
+    """The kernel that a product goes to (host arithmetic, no GPU needed)."""
+    out = Mx4PlanInfo()
+    _check("hlq_mx4_plan_query", lib.hlq_mx4_plan_query(N, K, experts, rows if x_rows is None else x_rows, rows, xtype, 1 if gated else 0, ctypes.byref(out)))
+    return out
 
 
 def alloc_mx4_workspace(W: Mx4, x_rows: int, rows: int | None = None, experts: int = 1, stream=None):

@@ -161,20 +161,11 @@ hlq_mx4_few_kernel(const Mx4Product a, int groups, int share)
 template <int XT, bool GATED, int MT, int CT>
 hlq_status launch(const Mx4Product &a, hipStream_t st)
 {
-    const int col_tiles = (a.cols + 16 * CT - 1) / (16 * CT);
-    const int64_t row_tiles = mx4_row_tiles(a.R, a.offsets ? a.E : 1, 16 * MT);
-    constexpr int MOST = few_waves(MT, CT);
-    // wavefronts that share a column tile: about MOST wavefronts a compute unit in all, AHEAD panels or more each
-    int share = 1;
-    while (share < MOST && row_tiles * col_tiles * share < 256 * MOST && share * few_ahead(MT, CT) < a.panels) share *= 2;
-    // x quantized inside: by wavefronts enough. us with 8 / 16: one row, 4096 x 4096 4.4 / 5.2; four rows, 6144 x 4096 7.1 / 6.2
-    int waves = XT == HLQ_MX4 ? 4 : (int64_t)((a.R + a.E - 1) / a.E) * a.K > 8192 ? 16 : 8;
-    if (waves < share) waves = share;
-    const int per = waves / share, groups = (col_tiles + per - 1) / per;
-    if (row_tiles * groups > (int64_t)(UINT32_MAX / 1024)) return HLQ_ERR_UNSUPPORTED;   // threads of a launch: below 2^32
-    size_t lds = share > 1 ? (size_t)waves * MT * CT * (GATED ? 2 : 1) * 1024 : 0;
+    const Mx4FewShape f = hlq_mx4_few_shape(a.cols, a.K, a.panels, a.offsets ? a.E : 1, a.R, XT, MT, CT);
+    if (f.row_tiles * f.groups > (int64_t)(UINT32_MAX / 1024)) return HLQ_ERR_UNSUPPORTED;   // threads of a launch: below 2^32
+    size_t lds = f.share > 1 ? (size_t)f.waves * MT * CT * (GATED ? 2 : 1) * 1024 : 0;
     if (XT != HLQ_MX4) lds += (size_t)(a.R < 16 ? a.R : 16) * a.panels * 68;
-    hlq_mx4_few_kernel<XT, GATED, MT, CT><<<(unsigned)(row_tiles * groups), 64 * waves, lds, st>>>(a, groups, share);
+    hlq_mx4_few_kernel<XT, GATED, MT, CT><<<(unsigned)(f.row_tiles * f.groups), 64 * f.waves, lds, st>>>(a, f.groups, f.share);
     return hlq_hip_status(hipGetLastError());
 }
 
@@ -185,6 +176,22 @@ hlq_status launch(const Mx4Product &a, bool gated, hipStream_t st)
 }
 
 }  // namespace
+
+Mx4FewShape hlq_mx4_few_shape(int cols, int K, int panels, int E, int64_t R, int xtype, int row_blocks, int col_blocks)
+{
+    const int col_tiles = (cols + 16 * col_blocks - 1) / (16 * col_blocks), most = few_waves(row_blocks, col_blocks);
+    Mx4FewShape f;
+    f.row_tiles = mx4_row_tiles(R, E, 16 * row_blocks);
+    // wavefronts that share a column tile: about `most` wavefronts a compute unit in all, AHEAD panels or more each
+    f.share = 1;
+    while (f.share < most && f.row_tiles * col_tiles * f.share < 256 * most && f.share * few_ahead(row_blocks, col_blocks) < panels) f.share *= 2;
+    // x quantized inside: by wavefronts enough. us with 8 / 16: one row, 4096 x 4096 4.4 / 5.2; four rows, 6144 x 4096 7.1 / 6.2
+    f.waves = xtype == HLQ_MX4 ? 4 : (R + E - 1) / E * K > 8192 ? 16 : 8;
+    if (f.waves < f.share) f.waves = f.share;
+    const int per = f.waves / f.share;
+    f.groups = (col_tiles + per - 1) / per;
+    return f;
+}
 
 hlq_status hlq_mx4_launch_few(const Mx4Product &a, int xtype, bool gated, int row_blocks, int col_blocks, hipStream_t st)
 {

@@ -109,7 +109,13 @@ static inline int64_t mx4_row_tiles(int64_t R, int E, int BM)
 __device__ __forceinline__ int mx4_inside_x(const Mx4Product &a, int i) { return i < 0 ? 0 : i >= a.x_rows ? a.x_rows - 1 : i; }
 __device__ __forceinline__ int mx4_x_row(const Mx4Product &a, int r) { return a.rows ? mx4_inside_x(a, a.rows[r]) : r; }
 
-// a wavefront has row_blocks x col_blocks blocks of 16 x 16: 1 x 1, 2 x 1, 2 x 2 or 4 x 2 (1 x 1 if x is quantized inside)
+// How a launch for few rows is cut: row_tiles x groups workgroups of `waves` wavefronts, `share` of them for the same columns.
+struct Mx4FewShape {
+    int share, waves, groups;
+    int64_t row_tiles;
+};
+// a wavefront has row_blocks x col_blocks blocks of 16 x 16: 1 x 1, 2 x 1, 2 x 2 or 4 x 2 (1 x 1 if x is quantized inside: xtype is not HLQ_MX4)
+Mx4FewShape hlq_mx4_few_shape(int cols, int K, int panels, int E, int64_t R, int xtype, int row_blocks, int col_blocks);
 hlq_status hlq_mx4_launch_few(const Mx4Product &a, int xtype, bool gated, int row_blocks, int col_blocks, hipStream_t st);
 
 // How a launch of the tiled kernel is cut: col_tiles x row_tiles x splits workgroups, a split `share` panels of K.  Partial

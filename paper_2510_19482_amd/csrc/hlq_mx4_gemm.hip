@@ -107,10 +107,20 @@ Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
     return best;
 }
 
-// counters, quantized activations, partial sums
-size_t workspace_need(const Mx4Dims &dx, bool quantize, const Choice &c)
+struct Plan {
+    Choice how;
+    bool inside;     // the kernel quantizes the activations
+    size_t need;     // of workspace: counters, quantized activations, partial sums
+};
+Plan plan_of(int64_t N, int32_t K, bool gated, int32_t E, int64_t R, const Mx4Dims &dx, int xtype)
 {
-    return HLQ_WS_COUNTER_BYTES + (quantize ? up256(dx.total) : 0u) + up256(c.row_blocks ? 0 : c.tile.partial_bytes);
+    Plan p;
+    p.how = choose(N, gated, dx.panels, E, R);
+    const bool quantize = xtype != HLQ_MX4;
+    p.inside = quantize && p.how.row_blocks == 1 && (R + E - 1) / E * K <= QUANTIZE_INSIDE && (R < 16 ? R : 16) * (int64_t)dx.panels * 68 <= QUANTIZED_BYTES;
+    p.how.tile.partial_at = HLQ_WS_COUNTER_BYTES + (quantize ? up256(dx.total) : 0u);
+    p.need = p.how.tile.partial_at + up256(p.how.row_blocks ? 0 : p.how.tile.partial_bytes);
+    return p;
 }
 
 struct Call {
@@ -166,18 +176,17 @@ hlq_status product(const Call &c, int32_t E, const int32_t *offsets, const int32
     a.y = c.Y;
     a.ytype = c.ytype;
     a.ldy = c.ldy;
-    int xtype = c.xtype;
-    Choice how = choose(c.N, gated, a.panels, E, R);
-    const bool quantize = xtype != HLQ_MX4;
+    const Plan p = plan_of(c.N, c.K, gated, E, R, dx, c.xtype);
+    const Choice &how = p.how;
     if (!c.ws) return HLQ_ERR_NULL;
-    if (c.ws_bytes < workspace_need(dx, quantize, how)) return HLQ_ERR_BUFFER_TOO_SMALL;
+    if (c.ws_bytes < p.need) return HLQ_ERR_BUFFER_TOO_SMALL;
     if ((uintptr_t)c.ws & 15u) return HLQ_ERR_BAD_STRIDE;
     hlq_clear_stale_error();
-    if (!quantize) a.A = hlq_mx4_view(dx, c.X);
-    else if (how.row_blocks == 1 && (R + E - 1) / E * c.K <= QUANTIZE_INSIDE && (R < 16 ? R : 16) * (int64_t)a.panels * 68 <= QUANTIZED_BYTES) {
+    if (c.xtype == HLQ_MX4) a.A = hlq_mx4_view(dx, c.X);
+    else if (p.inside) {
         a.x = c.X;
         a.ldx = c.ldx;
-        return hlq_mx4_launch_few(a, xtype, gated, 1, 1, c.stream);
+        return hlq_mx4_launch_few(a, c.xtype, gated, 1, 1, c.stream);
     } else {
         void *blob = (char *)c.ws + HLQ_WS_COUNTER_BYTES;
         s = hlq_mx4_launch_quantize(dx, c.X, c.xtype, c.ldx, blob, c.stream);
@@ -185,7 +194,6 @@ hlq_status product(const Call &c, int32_t E, const int32_t *offsets, const int32
         a.A = hlq_mx4_view(dx, blob);
     }
     if (how.row_blocks) return hlq_mx4_launch_few(a, HLQ_MX4, gated, how.row_blocks, how.col_blocks, c.stream);
-    how.tile.partial_at = HLQ_WS_COUNTER_BYTES + (quantize ? up256(dx.total) : 0u);
     if (how.tile.BM == 256) return hlq_mx4_launch_big(a, how.tile, gated, c.stream);
     return hlq_mx4_launch_tile(a, how.tile, gated, c.ws, c.stream);
 }
@@ -210,6 +218,37 @@ hlq_status hlq_mx4_workspace_bytes(int64_t N, int32_t K, int32_t experts, int64_
         if (part > most) part = most;
     }
     *bytes = HLQ_WS_COUNTER_BYTES + up256(d.total) + up256(part);
+    return HLQ_OK;
+}
+
+hlq_status hlq_mx4_plan_query(int64_t N, int32_t K, int32_t experts, int64_t x_rows, int64_t rows, hlq_dtype xtype, hlq_mx4_epilogue epilogue, hlq_mx4_plan_info *out)
+{
+    const bool gated = epilogue == HLQ_MX4_GATED;
+    if (N < 1 || experts < 1 || rows < 1 || (gated && N % 2)) return HLQ_ERR_BAD_DESC;
+    if ((epilogue != HLQ_MX4_PLAIN && !gated) || experts > HLQ_MAX_EXPERTS || N > HLQ_MAX_N || rows >= ((int64_t)1 << 31) - 256 ||
+        (!hlq_is_float(xtype) && xtype != HLQ_MX4))
+        return HLQ_ERR_UNSUPPORTED;
+    Mx4Dims d;
+    const hlq_status s = hlq_mx4_check(x_rows, K, &d);
+    if (s != HLQ_OK) return s;
+    if (!out) return HLQ_ERR_NULL;
+    const Plan p = plan_of(N, K, gated, experts, rows, d, xtype);
+    *out = hlq_mx4_plan_info{};
+    out->workspace_bytes = (int64_t)p.need;
+    out->quantizes = p.inside;
+    if (p.how.row_blocks) {
+        const Mx4FewShape f = hlq_mx4_few_shape((int)(gated ? N / 2 : N), K, d.panels, experts, rows, p.inside ? xtype : HLQ_MX4, p.how.row_blocks, p.how.col_blocks);
+        out->kernel = 1;
+        out->tile_rows = 16 * p.how.row_blocks;
+        out->tile_cols = 16 * p.how.col_blocks;
+        out->k_parts = f.share;
+        return HLQ_OK;
+    }
+    const Mx4TilePlan &t = p.how.tile;
+    out->kernel = t.BM == 256 ? 3 : 2;
+    out->tile_rows = t.BM;
+    out->tile_cols = t.BN;
+    out->k_parts = t.splits;
     return HLQ_OK;
 }
 
