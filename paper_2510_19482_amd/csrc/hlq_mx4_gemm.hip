@@ -26,6 +26,8 @@ size_t up256(size_t n) { return (n + 255u) & ~(size_t)255u; }
 // of 32 experts 180 / 193, 8192 of 8 85 / 92, 8192 of 64 133 / 169 (weights: 4.3 TB/s); against 32 x 128, 4096 of 64 117 / 181; 7686 of 126,
 // 796 x 303 not gated, 22 / 12.
 constexpr int MOST_SPLITS = 8, LEAST_SHARE = 4, MOST_CUT = 512;   // of K, panels of one, workgroups of a product whose K is cut
+constexpr int share_of(int panels, int parts) { return (panels + parts - 1) / parts; }
+constexpr bool may_cut(int panels) { return share_of(panels, 2) >= LEAST_SHARE; }   // where the workspace has to have room for partial sums
 constexpr int64_t MOST_GROUPS = 1 << 22, MOST_TILES = 1 << 23;    // workgroups, so that a launch stays below 2^32 threads
 
 struct Choice {
@@ -76,8 +78,8 @@ Choice choose(int64_t N, bool gated, int panels, int32_t E, int64_t R)
         const double count = row_tiles(k.BM) * (double)col_tiles, own = k.own + (E > 1 ? k.search : 0.0);
         const double stream = weights / 5.3 * (E == 1 ? 1.0 : 0.52 + 0.48 * row_tiles(k.BM) / (double)used) + results;
         for (int want = 1; want <= (k.passes ? MOST_SPLITS : 1); want += want < 4 ? 1 : 2) {
-            const int share = (panels + want - 1) / want, splits = (panels + share - 1) / share;
-            if (splits < want || (want > 1 && (mx4_row_tiles(R, E, k.BM) * col_tiles * want > MOST_CUT || share < LEAST_SHARE))) break;
+            const int share = share_of(panels, want), splits = (panels + share - 1) / share;
+            if (splits < want || (want > 1 && (!may_cut(panels) || mx4_row_tiles(R, E, k.BM) * col_tiles * want > MOST_CUT || share < LEAST_SHARE))) break;
             // workgroups, or tiles of 256 x 256, of a compute unit: whole rounds of the latter that are alike (an expert's last one, up to
             // half of them not even half filled, counts 0.58); of the former two where some units have two, later as units are free
             double full, most;
@@ -211,7 +213,7 @@ hlq_status hlq_mx4_workspace_bytes(int64_t N, int32_t K, int32_t experts, int64_
     if (!bytes) return HLQ_ERR_NULL;
     // partial sums: a bound that grows with the rows, so that fewer rows never need more
     size_t part = 0;
-    if (d.panels >= 2 * LEAST_SHARE && rows > 0) {
+    if (may_cut(d.panels) && rows > 0) {
         const size_t used = (size_t)(rows < experts ? rows : experts);
         part = ((size_t)rows + used * 128u) * (size_t)(up256((size_t)N) + 256u) * (size_t)MOST_SPLITS * 4u;
         const size_t most = (size_t)MOST_CUT * 128u * 128u * 4u;

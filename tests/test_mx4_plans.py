@@ -74,6 +74,16 @@ def test_a_call_fits_the_workspace_that_is_asked_for():
             assert B.mx4_plan_query(N, K, rows, E, min(x_rows, rows), F32, gated).workspace_bytes <= room
 
 
+@pytest.mark.parametrize("R,N", [(17, 100), (128, 128), (300, 700)])
+def test_room_for_partial_sums_wherever_k_may_be_cut(R, N):
+    # a share of K has four panels of 128 at least, the first of two of seven panels has four; whether the estimate takes it or not
+    def partial(panels):
+        return B.mx4_workspace_bytes(N, 128 * panels, 1, R, R) - 131072 - (R * panels * 68 + 255) // 256 * 256
+    assert partial(6) == 0
+    for panels in (7, 8, 9, 100):
+        assert partial(panels) >= 2 * 4 * R * N
+
+
 def test_refusals():
     out = B.Mx4PlanInfo()
     q = B.lib.hlq_mx4_plan_query
