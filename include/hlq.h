@@ -297,7 +297,8 @@ typedef enum {
 
 typedef enum {
     HLQ_MX4_PLAIN = 0, /* Y[r, n] = p[r, n]                                                               */
-    HLQ_MX4_GATED = 1  /* Y[r, n] = silu(p[r, n]) * p[r, N / 2 + n], n < N / 2, silu(v) = v / (1 + e^-v), fp32 */
+    HLQ_MX4_GATED = 1  /* Y[r, n] = silu(p[r, n]) * p[r, N / 2 + n], n < N / 2, silu(v) = v / (1 + e^-v): in fp32, f32 results to 5 units in the
+                          last place, 16-bit ones to 2^-16 of themselves before they are rounded; silu below 2^-126 may be 0 */
 } hlq_mx4_epilogue;
 
 #define HLQ_MAX_EXPERTS 1024

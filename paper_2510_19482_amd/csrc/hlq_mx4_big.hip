@@ -231,7 +231,7 @@ hlq_mx4_big_kernel(const Mx4Product a, int col_tiles, int most_row_tiles)
                 for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                     for (int n = 0; n < 16; ++n)
-                        four[b][n / 4].v[n % 4] = (V)(GATED ? mx4_gate(acc[i][GATED ? j0 + 2 * b : 0][n], acc[i][GATED ? j0 + 2 * b + 1 : 0][n]) : acc[i][j0 + (GATED ? 0 : b)][n]);
+                        four[b][n / 4].v[n % 4] = (V)(GATED ? mx4_gate<sizeof(V) == 4>(acc[i][GATED ? j0 + 2 * b : 0][n], acc[i][GATED ? j0 + 2 * b + 1 : 0][n]) : acc[i][j0 + (GATED ? 0 : b)][n]);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if ((r >> 4) == h)

@@ -123,7 +123,7 @@ hlq_mx4_few_kernel(const Mx4Product a, int groups, int share)
         if (m * 16 + r >= tile.n || left <= 0) return;
         float v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = GATED ? mx4_gate(p[i], up[i]) : p[i];
+        for (int i = 0; i < 4; ++i) v[i] = GATED ? mx4_gate<true>(p[i], up[i]) : p[i];
         mx4_store4(a.y, a.ytype, (int64_t)(tile.row0 + m * 16 + r) * a.ldy + c, v, left);
     };
     if (share == 1) {

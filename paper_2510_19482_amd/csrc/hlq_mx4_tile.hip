@@ -257,7 +257,7 @@ hlq_mx4_tile_kernel(const Mx4Product a, const Tiles t)
                     struct alignas(4 * sizeof(V)) Four { V v[4]; } four;
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        four.v[e] = (V)(GATED ? mx4_gate(acc[i][j][4 * q + e], acc[i][j + (GATED ? 1 : 0)][4 * q + e]) : acc[i][j][4 * q + e]);
+                        four.v[e] = (V)(GATED ? mx4_gate<sizeof(V) == 4>(acc[i][j][4 * q + e], acc[i][j + (GATED ? 1 : 0)][4 * q + e]) : acc[i][j][4 * q + e]);
                     *(Four *)(out + (wm * 32 + r) * PITCH + (c0 + 8 * q + 4 * g) * (int)sizeof(V)) = four;
                 }
             }
