@@ -192,7 +192,7 @@ hlq_route_top_kernel(const Route a)
                 top = v;
                 if (!a.renorm) {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) sum += K::present(key[j]) ? __expf(K::value(key[j]) - top) : 0.f;
+                    for (int j = 0; j < V; ++j) sum += K::present(key[j]) ? expf(K::value(key[j]) - top) : 0.f;
                 }
             }
             if (l == 0) {
@@ -205,14 +205,14 @@ hlq_route_top_kernel(const Route a)
         // what lane 0 of the row wrote is there for the others: they are of one wavefront, whose LDS accesses keep their order
         __builtin_amdgcn_wave_barrier();
         if (a.renorm) {
-            for (int i = l; i < found; i += 16) sum += __expf(values[t * a.k + i] - top);
+            for (int i = l; i < found; i += 16) sum += expf(values[t * a.k + i] - top);
         }
         sum = row_sum(sum);
         for (int i = l; i < a.k; i += 16) {
             const int id = i < found ? picks[t * a.k + i] : -1;
             if (i >= found) picks[t * a.k + i] = -1;
             a.ids[(t0 + t) * a.k + i] = id;
-            a.weights[(t0 + t) * a.k + i] = i < found ? __expf(values[t * a.k + i] - top) / sum : 0.f;
+            a.weights[(t0 + t) * a.k + i] = i < found ? expf(values[t * a.k + i] - top) / sum : 0.f;
         }
     }
     __syncthreads();
