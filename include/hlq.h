@@ -313,8 +313,9 @@ HLQ_API hlq_status hlq_mx4_bytes(int64_t rows, int32_t K, size_t *bytes);
 HLQ_API hlq_status hlq_mx4_quantize(int64_t rows, int32_t K, const void *x, hlq_dtype type, int64_t ldx, void *blob,
                                     size_t blob_bytes, void *stream);
 
-/* The values that a blob stands for, y [rows, K], leading dimension ldy >= K (exact where the type holds them: f32 and bf16 hold
- * all but those below their smallest subnormal, f16 those in its range). */
+/* The values that a blob stands for, y [rows, K], leading dimension ldy >= K (exact where the type holds them, else rounded
+ * once: f32 and bf16 hold all that hlq_mx4_quantize makes; of packed matrices, values of 2^128 and above, which scale bytes 253 and 254 have, are
+ * infinite). */
 HLQ_API hlq_status hlq_mx4_dequantize(int64_t rows, int32_t K, const void *blob, void *y, hlq_dtype type, int64_t ldy, void *stream);
 
 /* Exchange form, as stored models have it: codes u8 [rows, (K + 1) / 2], two a byte, the even k in the low four bits; scales u8

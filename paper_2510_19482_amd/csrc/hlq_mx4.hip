@@ -71,7 +71,7 @@ hlq_mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__re
     }
 }
 
-// exchange form: codes [rows][(K + 1) / 2], scales [rows][(K + 31) / 32]; a thread makes eight codes, every 32nd also a scale's four lanes
+// exchange form: codes [rows][(K + 1) / 2], scales [rows][(K + 31) / 32]; a thread makes eight codes, every fourth one scale byte too
 __global__ void __launch_bounds__(256)
 hlq_mx4_pack_kernel(const uint8_t *__restrict__ in, int64_t ldc, const uint8_t *__restrict__ in_scales, int64_t lds, int64_t rows, int K, int panels,
                     uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, int64_t items)
