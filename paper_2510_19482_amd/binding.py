@@ -6,7 +6,6 @@ the library has not been built, importing this module raises."""
 from __future__ import annotations
 
 import ctypes
-import math
 import os
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -431,8 +430,10 @@ class Mx4:
     __slots__ = ("blob", "rows", "K", "_need", "_kept", "_ptr", "_size", "_device")
 
     def __init__(self, blob, rows: int, K: int):
-        for name, value in (("rows", int(rows)), ("K", int(K)), ("_need", mx4_bytes(rows, K))):
-            object.__setattr__(self, name, value)
+        put = object.__setattr__
+        put(self, "rows", int(rows))
+        put(self, "K", int(K))
+        put(self, "_need", mx4_bytes(rows, K))
         self.blob = blob
 
     def __setattr__(self, name, value):
@@ -442,10 +443,13 @@ class Mx4:
         object.__setattr__(self, name, value)
 
     def _take(self, blob) -> None:
-        if blob.dtype != torch.uint8 or not blob.is_contiguous() or min(blob.numel(), blob.untyped_storage().nbytes() - blob.storage_offset()) < self._need:
+        size, ptr, put = blob.numel(), blob.data_ptr(), object.__setattr__
+        if blob.dtype != torch.uint8 or size < self._need or not blob.is_contiguous() or (ptr == 0 and self._need):
             raise ValueError(f"a blob of {self._need} bytes is needed for {self.rows} x {self.K}")
-        for name, value in (("_kept", blob.detach()), ("_ptr", blob.data_ptr()), ("_size", blob.numel()), ("_device", blob.get_device())):
-            object.__setattr__(self, name, value)
+        put(self, "_kept", blob.detach())
+        put(self, "_ptr", ptr)
+        put(self, "_size", size)
+        put(self, "_device", blob.get_device())
 
     is_cuda = property(lambda self: self.blob.is_cuda)
     device = property(lambda self: self.blob.device)
@@ -604,16 +608,15 @@ class Route:
     def __init__(self, T: int, E: int, k: int, device="cuda", stream=None):
         n = ctypes.c_size_t()
         _check("hlq_route_workspace_bytes", lib.hlq_route_workspace_bytes(T, E, k, ctypes.byref(n)))
-        parts = (("ids", torch.int32, (T, k)), ("weights", torch.float32, (T, k)), ("offsets", torch.int32, (E + 1,)), ("rows", torch.int32, (T * k,)),
-                 ("slots", torch.int32, (T, k)), ("ws", torch.uint8, (n.value,)))
-        sizes = [math.prod(shape) * dtype.itemsize for _, dtype, shape in parts]
-        starts = [0]
-        for size in sizes:
-            starts.append((starts[-1] + size + 15) // 16 * 16)
-        memory = _empty(starts[-1], torch.uint8, device, stream)
-        mine = {name: memory[at:at + size].view(dtype).view(shape) for (name, dtype, shape), at, size in zip(parts, starts, sizes)}
-        base = memory.data_ptr()
-        for name, value in dict(mine, T=T, E=E, k=k, _device=memory.get_device(), _memory=memory, _args=(*(base + at for at in starts[:-1]), n.value)).items():
+        pairs, room = T * k, (T * k + 3) // 4 * 4                # in words; parts begin at multiples of 16 bytes
+        offsets, ws = 4 * room, 4 * room + (E + 4) // 4 * 4
+        memory = _empty(ws + (n.value + 3) // 4, torch.int32, device, stream)
+        base, bytes_ = memory.data_ptr(), memory.view(torch.uint8)
+        for name, value in (("T", T), ("E", E), ("k", k), ("_memory", bytes_), ("_device", memory.get_device()),
+                            ("ids", memory.as_strided((T, k), (k, 1), 0)), ("slots", memory.as_strided((T, k), (k, 1), room)), ("rows", memory.as_strided((pairs,), (1,), 2 * room)),
+                            ("weights", memory.view(torch.float32).as_strided((T, k), (k, 1), 3 * room)), ("offsets", memory.as_strided((E + 1,), (1,), offsets)),
+                            ("ws", bytes_.as_strided((n.value,), (1,), 4 * ws)),
+                            ("_args", (base, base + 12 * room, base + 4 * offsets, base + 8 * room, base + 4 * room, base + 4 * ws, n.value))):
             object.__setattr__(self, name, value)
 
     def __setattr__(self, name, value):

@@ -1,7 +1,6 @@
 """Operands on several devices are refused, and a call runs on the device that its operands are on, whichever is current.  Without a GPU:
 stand-ins for tensors of devices that are not here, and for the library, which note what a call does."""
 import contextlib
-import types
 
 import pytest
 import torch
@@ -36,12 +35,6 @@ class Tensor:
 
     def detach(self):
         return self
-
-    def untyped_storage(self):
-        return types.SimpleNamespace(nbytes=self.numel)
-
-    def storage_offset(self):
-        return 0
 
 
 class Stream:
