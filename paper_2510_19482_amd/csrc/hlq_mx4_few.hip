@@ -46,8 +46,6 @@ __device__ __forceinline__ void quantize_rows(const Mx4Product &a, const Mx4RowT
     }
 }
 
-__device__ __forceinline__ mx4_int8 wide(mx4_int4 v) { return (mx4_int8){v.x, v.y, v.z, v.w, 0, 0, 0, 0}; }
-
 constexpr int few_ahead(int MT, int CT) { return MT * CT >= 4 ? 2 : 4; }   // panels requested at a time
 constexpr int few_waves(int MT, int CT) { return MT * CT >= 4 ? 8 : 16; }   // of a workgroup, at most
 

@@ -3,6 +3,9 @@
 
 #include "hlq_mx4.h"
 
+// an operand of 4-bit values as the matrix instruction takes it
+__device__ __forceinline__ mx4_int8 wide(mx4_int4 v) { return (mx4_int8){v.x, v.y, v.z, v.w, 0, 0, 0, 0}; }
+
 struct Mx4Product {
     Mx4View W;              // [E * N, K]: matrix e in rows e * N ..
     int N, cols, K, panels; // cols: of the result, N or N / 2 (gated)

@@ -8,8 +8,6 @@
 // reading one piece of 8 or of 16 successive rows then meets every bank once.
 __device__ __forceinline__ int piece_key(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
 
-__device__ __forceinline__ mx4_int8 wide(mx4_int4 v) { return (mx4_int8){v.x, v.y, v.z, v.w, 0, 0, 0, 0}; }
-
 // as dma_16B_per_lane, 4 bytes a lane
 __device__ __forceinline__ void dma_4B_per_lane(const void *gptr, uint32_t lds_base)
 {
