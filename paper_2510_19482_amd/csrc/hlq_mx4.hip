@@ -5,7 +5,7 @@
 // Quantizing reads a value once and writes 4.25 bits: it is bound by memory.  A wavefront takes a panel of four rows: a lane has
 // eight successive values (one 16-byte load of 16-bit types, two of fp32), four lanes a block, whose largest magnitudes meet by
 // two quad permutations; codes leave as a dword a lane, 256 contiguous bytes.  The values are read, and in dequantizing written, past
-// the caches: 8192 x 8192 f16 35 us (170 MB, 4.9 TB/s; through them 38), back 34 (through them 42).
+// the caches: 8192 x 8192 f16 37 us (170 MB, 4.6 TB/s; through them 38), back 35 (through them 42); one after the other, both in 60.
 #include "hlq_mx4.h"
 
 namespace {
@@ -71,7 +71,8 @@ hlq_mx4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__re
     }
 }
 
-// exchange form: codes [rows][(K + 1) / 2], scales [rows][(K + 31) / 32]; a thread makes eight codes, every fourth one scale byte too
+// exchange form: codes [rows][(K + 1) / 2], scales [rows][(K + 31) / 32]; a thread makes eight codes, every fourth one scale byte too.
+// Once for weights that are loaded: 8192 x 8192 52 us (71 MB; bound by its byte loads), back 38
 __global__ void __launch_bounds__(256)
 hlq_mx4_pack_kernel(const uint8_t *__restrict__ in, int64_t ldc, const uint8_t *__restrict__ in_scales, int64_t lds, int64_t rows, int K, int panels,
                     uint8_t *__restrict__ codes, uint8_t *__restrict__ scales, int64_t items)

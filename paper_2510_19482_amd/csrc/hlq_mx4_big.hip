@@ -1,21 +1,23 @@
 // Products of MX4 matrices, large launches: tiles of 256 rows x 256 rows of W, one workgroup a compute unit, which goes from tile to
 // tile.  The mathematics and the staging are those of the smaller tiles.
 //
-// Large products are bound by the power of the matrix cores and of what feeds them (the clock is at 1.6 GHz), so what helps is to
-// feed them less: of LDS a wavefront with 2 x 4 blocks reads 6 pieces for 8 products (2 x 2 blocks: 8), of memory and L2 a tile
-// loads 256 + 256 rows where two of 128 x 256 load 768.  A unit holds one such workgroup (four stages, 136 KB), so nothing hides a
-// tile's first loads and its results but the kernel itself: the next tile's first stages are requested before the results leave.
+// What bounds large products: the clock, which power holds at 1.74 to 1.81 GHz (the matrix cores alone, busy all the time: 1.6 on random codes, 2.3 on
+// zeros; with zeros for operands 454 us become 331), and the cycles in which nothing multiplies, 42 % of them: 5 us a tile are its
+// results, over K the panels run at 5.2 PFLOP/s.  It helps to feed the cores less: of LDS a wavefront with 2 x 4 blocks reads 6 pieces
+// for 8 products (2 x 2 blocks: 8), of memory and L2 a tile loads 256 + 256 rows where two of 128 x 256 load 768.  A unit holds one
+// such workgroup (four stages, 136 KB), so nothing hides a tile's first loads and its results but the kernel itself: the next tile's
+// first stages are requested before the results leave.
 // us, 8192 rows, 28672 x 4096 gated / 8192 x 28672 plain, against 485 / 874 of 128 x 256 in the same minute:
 //   one workgroup a tile                                    453 / 786 (then 465 / 846)
 //   a workgroup goes from tile to tile                      438 / 771
 //   results in lines of 128 bytes, not 64                   450 / 809 (8192 x 28672 x 256 plain, all results: 172 -> 110)
-//   a step's operands read 6 products behind the barrier    426 / 777 (devices differ by 5 %)
+//   a step's operands read 6 products behind the barrier    426 / 777 (devices differ by 5 %: 454 / 771 and 445 / 771 on two others)
 // 4 wavefronts with 4 x 4 blocks: 4 % less a panel, but 20 us a tile for results that spill.  A wavefront's priority raised for its
 // products: 2 % slower.
 // Experts' rows, 16384 of 32, gated 4096 x 4096, skewed / 512 each give or take 22, against 193 / 208 of 128 x 256:
 //   every tile multiplied in full                           188 / 230
 //   offsets from LDS, the next tile's rows looked up early, wavefronts without rows do not multiply    177 / 230
-//   low tiles after the high ones                           180 / 207 (8192 rows of 8 89 -> 85, of 64 133)
+//   low tiles after the high ones                           180 / 207 (8192 rows of 8 89 -> 85, of 64 133; with weights that take turns 194)
 //   (a queue that workgroups take tiles from: 182 / 203, but 8192 rows of 8 102: a number's way is 5 us a tile)
 // What bounds them: weights that come from memory once, and rows gathered by index (512 each exactly: 150; rows in order 131).
 #include "hlq_mx4_stage.h"

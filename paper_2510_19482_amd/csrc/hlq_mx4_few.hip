@@ -6,10 +6,10 @@
 // panels; the wavefronts of a workgroup that share the columns add their sums through LDS, in order.  Operands go straight to
 // registers in the form that v_mfma_scale_f32_16x16x128_f8f6f4 takes, panels of several steps requested together.  A few rows
 // that come as f16, bf16 or f32 are quantized by the workgroup into LDS while its first weights come; that saves a launch.
-// us, one bf16 row: 4096 x 4096 4.4, 6144 x 4096 5.3, 28672 x 4096 12.3 (62 MB, 5.1 TB/s), 4096 x 14336 7.2;
-// 16 rows of 32 experts (14 of them used), gated 4096 x 4096: 25 (118 MB, 4.7 TB/s).
-// With more rows what a compute unit loads into registers (43 bytes a nanosecond) takes over: 32 rows 4096 x 14336 10.3, 128 rows 4096 x 4096 7.3.
-// Loads that bypass the caches for the weights: no difference (28672 x 4096 12.2 -> 12.7).
+// us, weights from memory, one bf16 row: 4096 x 4096 5.4, 6144 x 4096 6.5, 28672 x 4096 15.0 (62 MB, 4.2 TB/s), 4096 x 14336 9.8 (with the weights in
+// the memory-side cache 4.4, 5.3, 12.3, 7.2); 16 rows of 32 experts (14 of them used), gated 4096 x 4096: 25.5 (118 MB, 4.6 TB/s; a plain read reaches 7.1).
+// With more rows what a compute unit loads into registers (43 bytes a nanosecond) takes over: 32 rows 4096 x 14336 12.6, 128 rows 4096 x 4096 8.4.
+// Loads that bypass the caches for the weights: no difference (28672 x 4096, from the memory-side cache, 12.2 -> 12.7).
 #include "hlq_mx4_gemm.h"
 
 namespace {
@@ -183,7 +183,7 @@ Mx4FewShape hlq_mx4_few_shape(int cols, int K, int panels, int E, int64_t R, int
     // wavefronts that share a column tile: about `most` wavefronts a compute unit in all, AHEAD panels or more each
     f.share = 1;
     while (f.share < most && f.row_tiles * col_tiles * f.share < 256 * most && f.share * few_ahead(row_blocks, col_blocks) < panels) f.share *= 2;
-    // x quantized inside: by wavefronts enough. us with 8 / 16: one row, 4096 x 4096 4.4 / 5.2; four rows, 6144 x 4096 7.1 / 6.2
+    // x quantized inside: by wavefronts enough. us with 8 / 16, weights in the memory-side cache: one row, 4096 x 4096 4.4 / 5.2; four rows, 6144 x 4096 7.1 / 6.2
     f.waves = xtype == HLQ_MX4 ? 4 : (R + E - 1) / E * K > 8192 ? 16 : 8;
     if (f.waves < f.share) f.waves = f.share;
     const int per = f.waves / f.share;

@@ -19,8 +19,8 @@ size_t up256(size_t n) { return (n + 255u) & ~(size_t)255u; }
 // the partial sums: 1, and 3 for each 32 rows a wavefront has and four splits.
 //
 // Fitted to products that were each timed on every kernel (experts' rows 2 to 800 each, even and skewed; 17 to 16384 rows of one
-// matrix).  On 840 others what is chosen is from the fastest on average: 1.5 % up to 1500 rows, 0.8 % above, 4 % for experts; at most 56 %,
-// two rows each of 68 experts with K = 273.
+// matrix).  On 420 others (profiles/mx4_plan_choice.txt) what is chosen is from the fastest on average: 2.7 % up to 1500 rows, 1.4 % above, 4.4 %
+// for experts; at most 54 %, two rows each of 68 experts with K = 273.
 // 256 x 256 against 128 x 256, measured, rows x N x K: 4096 x 4096 x 14336 107 / 116 (one round of the card), 8192 x 4096 x 4096 65 / 73
 // (two), 8192 x 28672 x 4096 gated 440 / 485 (14), but half a round, 2048 x 4096 x 4096, 24 / 22.  Experts' rows, gated 4096 x 4096: 16384
 // of 32 experts 180 / 193, 8192 of 8 85 / 92, 8192 of 64 133 / 169 (weights: 4.3 TB/s); against 32 x 128, 4096 of 64 117 / 181; 7686 of 126,

@@ -13,7 +13,7 @@
 //   (128 x 128 529)                                         ... results in streaming stores                     471 (then 481)
 // From about one round of the card's units, 256 x 256 with a workgroup that goes from tile to tile is faster (another kernel); this one
 // has what is less or does not fill whole rounds.  For experts' rows (512 each on average, 218): waiting for weights that come
-// from memory once, 2.8 TB/s in all with the clock at 2.1 GHz.
+// from memory once.
 #include "hlq_mx4_stage.h"
 
 namespace {

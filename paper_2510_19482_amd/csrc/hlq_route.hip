@@ -8,8 +8,9 @@
 // Grouping is a counting sort, stable and without atomics whose order could matter: a token takes an expert at most once, so
 // for the 32 tokens of a chunk an expert's rows are a 32-bit mask, its count the bits of it, and a row's place among them the
 // bits below its own.  Chunks' counts are added up by each workgroup that places rows (up to 512 chunks) or by a scan in between.
+// Exponentials are fp32's own: of an argument rounded once they put a weight 60 half units off; for f32 and all experts' sum 5 % of the time.
 // 8192 tokens, 256 experts, k = 8, f32: choices 9.4 us (8 MB; two wavefronts a SIMD in dependent maxima; with 64 lanes a token and
-// ballots 19), places 6.0; 32 tokens, 64 experts: 4.5 in one launch.
+// ballots 19), places 6.7; 32 tokens, 64 experts: 4.3 in one launch; 131072 tokens, 128 experts, bf16: 30.6, the scan 13.2, places 15.9.
 #include "hlq_mx4.h"
 
 namespace {
@@ -363,8 +364,8 @@ struct Combine {
 };
 
 // y[t, d] = sum_i weights[t, i] Y[slots[t, i], d], i ascending, fp32: a thread has eight successive d of a token.  Bound by the
-// bytes of Y; the loads of four experts are in flight together, and pass the caches by.  8192 tokens, 8 of 4096, bf16: 121 us
-// (605 MB, 5.0 TB/s; through the caches 131).
+// bytes of Y; the loads of four experts are in flight together, and pass the caches by.  8192 tokens, 8 of 4096, bf16: 119 us
+// (605 MB, 5.1 TB/s; through the caches 131).
 template <int T>
 __global__ void __launch_bounds__(256)
 hlq_expert_combine_kernel(const Combine a, int64_t items)
