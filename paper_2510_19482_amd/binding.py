@@ -391,8 +391,8 @@ def _not_on_gpu(*tensors):
     return ValueError(f"expected tensors on the GPU, all on one GPU, got {', '.join(str(t.device) for t in tensors)}")
 
 
-_current_device = torch._C._cuda_getDevice
-_current_stream = torch._C._cuda_getCurrentRawStream   # of a device, its handle
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # of a device, its handle
 
 
 def _stream_of(stream, device: int) -> int:
@@ -456,6 +456,9 @@ class Mx4:
 
     def get_device(self) -> int:
         return self.blob.get_device()
+
+    def __reduce__(self):
+        return Mx4, (self.blob, self.rows, self.K)
 
 
 def _blob(m: Mx4):
@@ -621,6 +624,15 @@ class Route:
 
     def __setattr__(self, name, value):
         raise AttributeError(f"{name} of a route stays as it was made")
+
+    def __reduce__(self):
+        return _route_of, (self.T, self.E, self.k, self._memory)
+
+
+def _route_of(T: int, E: int, k: int, memory) -> Route:
+    route = Route(T, E, k, memory.device)
+    route._memory.copy_(memory)
+    return route
 
 
 def alloc_route(T: int, E: int, k: int, device="cuda", stream=None) -> Route:

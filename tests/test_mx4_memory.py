@@ -1,5 +1,8 @@
 """Whose memory a call is handed: a matrix's is what stands in its blob at the time of the call, a route's is its own for as long as it lives.
 Without a GPU: the library's entry points are replaced by ones that note their arguments."""
+import copy
+import pickle
+
 import pytest
 import torch
 
@@ -75,3 +78,17 @@ def test_a_route_keeps_the_memory_that_it_writes():
     r.ids.data = torch.zeros((T, k), dtype=torch.int32)      # the caller's tensor is another now; what is written is still there
     del parts
     assert r._memory.data_ptr() == lo and r._args[0] >= lo and r._args[0] + 4 * T * k <= hi
+
+
+def test_copies_have_memory_of_their_own():
+    m = matrix()
+    m.blob.random_(0, 255)
+    r = B.alloc_route(300, 10, 3, device="cpu")
+    r.ids.random_(0, 9)
+    for again in (copy.deepcopy, lambda v: pickle.loads(pickle.dumps(v))):
+        c = again(m)
+        assert (c.rows, c.K) == (m.rows, m.K) and torch.equal(c.blob, m.blob)
+        assert B._blob(c)[0] == c.blob.data_ptr() != m.blob.data_ptr()
+        c = again(r)
+        assert (c.T, c.E, c.k) == (r.T, r.E, r.k) and torch.equal(c.ids, r.ids)
+        assert c._args[0] == c.ids.data_ptr() != r.ids.data_ptr() and c._args[5] == c.ws.data_ptr()
