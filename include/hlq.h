@@ -292,7 +292,8 @@ typedef enum {
     HLQ_F16 = 0,
     HLQ_F32 = 1,
     HLQ_BF16 = 2,
-    HLQ_MX4 = 3      /* activations of a product that are an MX4 blob already */
+    HLQ_MX4 = 3,     /* activations of a product that are an MX4 blob already; of a cache: e2m1 values */
+    HLQ_MX8 = 4      /* of a cache: e4m3 values, a power-of-two scale for 32 of them */
 } hlq_dtype;
 
 typedef enum {
@@ -372,6 +373,87 @@ HLQ_API hlq_status hlq_expert_gemm(int32_t experts, int64_t N, int32_t K, const 
 /* out[t, .] = sum_i weights[t, i] Y[slots[t, i], .] over i ascending in fp32, Y [R, D]; a slot outside 0 .. R - 1 adds nothing. */
 HLQ_API hlq_status hlq_expert_combine(int64_t T, int32_t k, int32_t D, int64_t R, const void *Y, hlq_dtype ytype, int64_t ldy,
                                       const int32_t *slots, const float *weights, void *out, hlq_dtype otype, int64_t ldo, void *stream);
+
+/* ---- Attention: rotary positions, the paged cache of keys and values, one token over it, a prompt ----------------------
+ *
+ * Rows of heads: an array [T, heads, dim] whose last axis is contiguous; the other two have strides in elements, `ts` (from token to
+ * token) and `hs` (from head to head), so that q, k and v may be parts of one projection's rows, or stand head by head.  Strides are 0 or
+ * more, any alignment of the type; an output's rows may not overlap each other.  Types f16, bf16 and f32 (attention: f16 and bf16).
+ * Limits: dim a multiple of 8 up to 256, heads <= 1024, T < 2^31.  The conventions at the top of this file hold. */
+
+/* Rotary positions: of each head's first `dims` values (even, at most dim) pairs are turned by position * frequency,
+ *     (a, b) -> magnitude * (a cos - b sin, b cos + a sin),
+ * pair i being values i and i + dims / 2, or (interleaved != 0) 2 i and 2 i + 1.  The other values stay as they are.
+ * `turns` (device, dims / 2 numbers, 8-byte aligned) are the pairs' frequencies as hlq_rotary_turns (host-only) makes them of radians a position:
+ * the part of a turn that a position adds, times 2^64, so that an angle is exact to 2^-33 turns wherever in int32 the position is.  Turned in
+ * 64 bits and rounded once (16-bit types: by way of f32).  Any scheme of stretched positions is a choice of frequencies and magnitude.
+ * A frequency that is not finite or of 2^32 and more: HLQ_ERR_BAD_DESC. */
+typedef struct {
+    int32_t dims, interleaved;
+    float magnitude;
+    const uint64_t *turns;
+} hlq_rotary_desc;
+HLQ_API hlq_status hlq_rotary_turns(int32_t pairs, const double *frequencies, uint64_t *turns);
+
+/* y = x turned by positions [T] (int32); y = x, with the same strides, is allowed. */
+HLQ_API hlq_status hlq_rotary(const hlq_rotary_desc *r, int64_t T, int32_t heads, int32_t dim, hlq_dtype type, const int32_t *positions, const void *x,
+                              int64_t x_ts, int64_t x_hs, void *y, int64_t y_ts, int64_t y_hs, void *stream);
+
+/* A cache of keys and values: `pages` pages of `page_tokens` tokens (16, 32, ... 1024) for each of `heads` heads of `dim` values.
+ * A token's slot is page * page_tokens + its place in the page.  In memory, 16-byte aligned:
+ *   f16, bf16   [pages][2: keys, values][heads][page_tokens][dim]
+ *   MX8, MX4    codes of that shape (e4m3 a byte; e2m1 two a byte, the even one low), then scale bytes [pages][2][heads][dim / 32][page_tokens]:
+ *               a value is its code's times 2^(byte - 127); byte 255 is NaN.  dim is a multiple of 32.
+ * What no call has written is never read as a number: a cache needs no initialisation. */
+typedef struct {
+    int64_t pages;
+    int32_t page_tokens, heads, dim;
+    hlq_dtype type;
+} hlq_kv_desc;
+HLQ_API hlq_status hlq_kv_bytes(const hlq_kv_desc *c, size_t *bytes);   /* host-only */
+
+/* Writes rows k and v [T, heads, dim] of `type` into slots [T] (int64) of the cache.  16-bit caches: rounded to nearest; MX8 and MX4: per 32 values
+ * e = floor(log2(largest magnitude)) - 8 (MX4: - 2), at least -127, a value the code nearest to x 2^-e (ties to the even code, above
+ * 448, or 6, that); with an infinity or a NaN all 32 are NaN.  A slot outside the cache is skipped, so that -1 marks rows of padding.  Slots of
+ * a call are distinct: where two are not, each code and scale byte there is one or the other row's.
+ * With r (positions [T]) k is turned as by hlq_rotary, rounded to its type, and then written; k_out (or NULL, or k itself with its strides) takes the turned
+ * keys, and q_heads > 0 heads q are turned into q_out (or q itself) in the same launch.  Without r: q_heads = 0, k_out NULL. */
+HLQ_API hlq_status hlq_kv_write(const hlq_kv_desc *c, void *cache, size_t cache_bytes, int64_t T, hlq_dtype type, const void *k, int64_t k_ts, int64_t k_hs,
+                                const void *v, int64_t v_ts, int64_t v_hs, const int64_t *slots, const hlq_rotary_desc *r, const int32_t *positions,
+                                void *k_out, int64_t ko_ts, int64_t ko_hs, int32_t q_heads, const void *q, int64_t q_ts, int64_t q_hs, void *q_out,
+                                int64_t qo_ts, int64_t qo_hs, void *stream);
+
+/* Rows k and v [T, heads, dim] of `type` from slots [T] of the cache, exact where the type holds them, else rounded once; k or v may be NULL.
+ * Rows whose slot is outside the cache stay as they were. */
+HLQ_API hlq_status hlq_kv_read(const hlq_kv_desc *c, const void *cache, size_t cache_bytes, int64_t T, const int64_t *slots, hlq_dtype type, void *k,
+                               int64_t k_ts, int64_t k_hs, void *v, int64_t v_ts, int64_t v_hs, void *stream);
+
+/* One new token of each of B sequences over what the cache holds of it: for query head h, with kv head h / (q_heads / heads),
+ *     out[b, h] = sum_j p_j v_j,   p = softmax over j of scale * q[b, h] . k_j,   j < lengths[b], and j >= lengths[b] - window if window > 0;
+ * the newest token's key and value are in the cache already.  table [B, >= pages of a sequence] (int32, leading dimension ld_table): the page of
+ * tokens i * page_tokens ..; lengths [B] int32.  A length counts as at most table_width * page_tokens and as at least 0, a page as the
+ * nearest one inside the cache.  Length 0, or no score above -infinity: 0.  q_heads is a multiple of heads.  q has the type of a 16-bit cache, f16 or
+ * bf16 with MX8 and MX4; out f16, bf16 or f32.  Products are exact, sums fp32; p is held to 2^-16 of itself (f16: 2^-22, absolutely 2^-25).  Results do not
+ * depend on the order in which workgroups end.
+ * ws: of hlq_attn_decode_workspace_bytes() (host-only; enough for smaller B and table_width too), seen by hlq_workspace_init once; calls that may run at
+ * the same time need one each. */
+HLQ_API hlq_status hlq_attn_decode_workspace_bytes(const hlq_kv_desc *c, int32_t q_heads, int64_t B, int32_t table_width, size_t *bytes);
+HLQ_API hlq_status hlq_attn_decode(const hlq_kv_desc *c, const void *cache, size_t cache_bytes, int32_t q_heads, int64_t B, hlq_dtype type, const void *q,
+                                   int64_t q_ts, int64_t q_hs, const int32_t *table, int64_t ld_table, int32_t table_width, const int32_t *lengths,
+                                   int32_t window, float scale, void *out, hlq_dtype otype, int64_t o_ts, int64_t o_hs, void *ws, size_t ws_bytes, void *stream);
+
+/* Prompts: B sequences packed one after the other, sequence b's queries in rows q_offsets[b] .. q_offsets[b + 1] - 1 of q [Tq, q_heads, dim], its keys and
+ * values in rows k_offsets[b] .. of k and v [Tk, heads, dim] (offsets int32 [B + 1], ascending).  The last query and the last key are the same token: query
+ * i of n_q stands at place n_k - n_q + i, and sees key j if
+ *     j < n_k,   j <= its place if causal,   j > its place - window if window > 0;
+ * a query that sees no key (or none whose score is above -infinity) has 0.  out [Tq, q_heads, dim]; rows of no sequence stay as they were.  Offsets count
+ * as the nearest number in 0 .. Tq, or Tk; a sequence that ends before it begins is empty.  Products are exact, sums fp32, p is rounded to the inputs' type (f16, bf16), which is out's too.
+ * ws: as for hlq_attn_decode. */
+HLQ_API hlq_status hlq_attn_prompt_workspace_bytes(int64_t Tq, int64_t Tk, int32_t B, int32_t q_heads, int32_t heads, int32_t dim, size_t *bytes);
+HLQ_API hlq_status hlq_attn_prompt(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, hlq_dtype type, int64_t Tq, const void *q, int64_t q_ts, int64_t q_hs,
+                                   int64_t Tk, const void *k, int64_t k_ts, int64_t k_hs, const void *v, int64_t v_ts, int64_t v_hs, const int32_t *q_offsets,
+                                   const int32_t *k_offsets, int32_t causal, int32_t window, float scale, void *out, int64_t o_ts, int64_t o_hs, void *ws,
+                                   size_t ws_bytes, void *stream);
 
 /* Measurement helper, no part of the method: read `bytes` of device memory once with 128-bit
  * loads, `blocks` workgroups of 256 lanes each taking one contiguous share (0 = 2048), and store

@@ -30,6 +30,14 @@ class Mx4PlanInfo(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("kernel", "tile_rows", "tile_cols", "k_parts", "quantizes", "reserved")] + [("workspace_bytes", ctypes.c_int64)]
 
 
+class HlqKvDesc(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("page_tokens", ctypes.c_int32), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("type", ctypes.c_int)]
+
+
+class HlqRotaryDesc(ctypes.Structure):
+    _fields_ = [("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float), ("turns", ctypes.c_void_p)]
+
+
 class HlqError(RuntimeError):
     def __init__(self, fn: str, status: int):
         self.status = status
@@ -51,6 +59,19 @@ _MX4_ARGS = {
     "hlq_route": [_i64, _i32, _i32, _vp, _int, _i64, _int, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
     "hlq_expert_gemm": [_i32, _i64, _i32, _vp, _vp, _vp, _i64, _i64, _vp, _int, _i64, _vp, _int, _i64, _int, _vp, _sz, _vp],
     "hlq_expert_combine": [_i64, _i32, _i32, _i64, _vp, _int, _i64, _vp, _vp, _vp, _int, _i64, _vp],
+}
+_kvp, _rotp = ctypes.POINTER(HlqKvDesc), ctypes.POINTER(HlqRotaryDesc)
+_ROWS = [_vp, _i64, _i64]   # an array [T, heads, dim]: address, strides from token to token and from head to head
+_ATTN_ARGS = {
+    "hlq_rotary_turns": [_i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_uint64)],
+    "hlq_rotary": [_rotp, _i64, _i32, _i32, _int, _vp, *_ROWS, *_ROWS, _vp],
+    "hlq_kv_bytes": [_kvp, _szp],
+    "hlq_kv_write": [_kvp, _vp, _sz, _i64, _int, *_ROWS, *_ROWS, _vp, _rotp, _vp, *_ROWS, _i32, *_ROWS, *_ROWS, _vp],
+    "hlq_kv_read": [_kvp, _vp, _sz, _i64, _vp, _int, *_ROWS, *_ROWS, _vp],
+    "hlq_attn_decode_workspace_bytes": [_kvp, _i32, _i64, _i32, _szp],
+    "hlq_attn_decode": [_kvp, _vp, _sz, _i32, _i64, _int, *_ROWS, _vp, _i64, _i32, _vp, _i32, ctypes.c_float, _vp, _int, _i64, _i64, _vp, _sz, _vp],
+    "hlq_attn_prompt_workspace_bytes": [_i64, _i64, _i32, _i32, _i32, _i32, _szp],
+    "hlq_attn_prompt": [_i32, _i32, _i32, _i32, _int, _i64, *_ROWS, _i64, *_ROWS, *_ROWS, _vp, _vp, _i32, _i32, ctypes.c_float, *_ROWS, _vp, _sz, _vp],
 }
 
 
@@ -114,7 +135,7 @@ def _load() -> ctypes.CDLL:
     lib.hlq_mfma_probe.argtypes = [ctypes.c_int, vp, sz, ctypes.c_int, ctypes.c_int, vp, sz, ctypes.POINTER(ctypes.c_double), vp]
     lib.hlq_stream_read_shaped.restype = ctypes.c_int
     lib.hlq_stream_read_shaped.argtypes = [vp, sz, ctypes.c_int, ctypes.c_int, ctypes.c_int, vp, sz, vp]
-    for name, args in _MX4_ARGS.items():
+    for name, args in (*_MX4_ARGS.items(), *_ATTN_ARGS.items()):
         fn = getattr(lib, name)
         fn.restype = ctypes.c_int
         fn.argtypes = args
@@ -711,4 +732,308 @@ def hlq_expert_combine(Y, slots, weights, out=None, out_dtype=None, stream=None)
     status = lib.hlq_expert_combine(T, k, D, R, y, ytype, ldy, slots.data_ptr(), weights.data_ptr(), o, otype, ldo, _stream_of(stream, device))
     if status != HLQ_OK:
         raise HlqError("hlq_expert_combine", status)
+    return out
+
+
+# ---- attention: rotary positions, the paged cache, one token over it, prompts ---------------------------------------
+HLQ_MX8 = 4
+
+
+def _heads(t):
+    """(T, heads, dim, pointer, type, token stride, head stride) of rows of heads whose last axis is contiguous."""
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None:
+        raise TypeError(f"expected a float16, bfloat16 or float32 tensor, got {t.dtype}")
+    try:
+        T, H, D = t.shape
+        ts, hs, one = t.stride()
+    except ValueError:
+        raise ValueError(f"expected [tokens, heads, dim], got shape {tuple(t.shape)}") from None
+    if one != 1 and D > 1:
+        raise ValueError(f"expected a contiguous last axis, got shape {tuple(t.shape)} with strides {t.stride()}")
+    return T, H, D, t.data_ptr(), dtype, ts, hs
+
+
+def _numbers(name: str, t, dtype, n: int) -> int:
+    """Address of a vector of n numbers of this type."""
+    if t.dtype != dtype or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {n} contiguous numbers of {dtype}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def rotary_frequencies(dims: int, base: float = 10000.0, factor: float = 1.0, trained: int | None = None, keep=(1.0, 4.0)) -> list:
+    """Radians a position of the dims / 2 pairs: base^(-2 i / dims).  With a factor, positions are stretched: all frequencies divided by it, or, where the
+    model was trained on `trained` positions, those of at most keep[0] turns over them, from keep[1] turns on none, and a ramp between."""
+    if dims < 2 or dims % 2 or not base > 0 or not factor > 0 or not keep[0] < keep[1]:
+        raise ValueError(f"dims {dims} (even), base {base}, factor {factor}, keep {keep}")
+    out = [base ** (-2 * i / dims) for i in range(dims // 2)]
+    if trained is None:
+        return [f / factor for f in out]
+    as_is = [min(1.0, max(0.0, (trained * f / 6.283185307179586 - keep[0]) / (keep[1] - keep[0]))) for f in out]
+    return [f * (r + (1 - r) / factor) for f, r in zip(out, as_is)]
+
+
+class Rotary:
+    """Rotary positions: frequencies (radians a position) of the pairs among each head's first 2 * len(frequencies) values, halves or (interleaved)
+    neighbours; `magnitude` multiplies what is turned.  On one device."""
+
+    __slots__ = ("frequencies", "interleaved", "magnitude", "turns", "_desc", "_device")
+
+    def __init__(self, frequencies, interleaved: bool = False, magnitude: float = 1.0, device="cuda"):
+        f = [float(v) for v in frequencies]
+        host, turns = (ctypes.c_double * len(f))(*f), (ctypes.c_uint64 * len(f))()
+        _check("hlq_rotary_turns", lib.hlq_rotary_turns(len(f), host, turns))
+        tensor = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64).to(device)
+        for name, value in (("frequencies", tuple(f)), ("interleaved", bool(interleaved)), ("magnitude", float(magnitude)), ("turns", tensor), ("_device", tensor.get_device()),
+                            ("_desc", HlqRotaryDesc(2 * len(f), int(bool(interleaved)), float(magnitude), tensor.data_ptr()))):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name} of a rotation stays as it was made")
+
+    device = property(lambda self: self.turns.device)
+
+    def __reduce__(self):
+        return Rotary, (self.frequencies, self.interleaved, self.magnitude, str(self.turns.device))
+
+
+def hlq_rotary(x, positions, rotary: Rotary, out=None, stream=None):
+    """x [T, heads, dim] turned by positions [T] (int32), in `out` (which may be x) or a new tensor."""
+    T, H, D, xp, dtype, xt, xh = _heads(x)
+    if out is None:
+        out = _empty((T, H, D), x.dtype, x.device, stream)
+    oT, oH, oD, op, odtype, ot, oh = _heads(out)
+    if (oT, oH, oD, odtype) != (T, H, D, dtype):
+        raise ValueError(f"x is {x.dtype} {tuple(x.shape)}, out {out.dtype} {tuple(out.shape)}")
+    at = _numbers("positions", positions, torch.int32, T)
+    device = x.get_device()
+    if device < 0 or out.get_device() != device or positions.get_device() != device or rotary._device != device:
+        raise _not_on_gpu(x, out, positions, rotary)
+    if device != _current_device():
+        return _there(device, hlq_rotary, x, positions, rotary, out, stream)
+    status = lib.hlq_rotary(rotary._desc, T, H, D, dtype, at, xp, xt, xh, op, ot, oh, _stream_of(stream, device))
+    if status != HLQ_OK:
+        raise HlqError("hlq_rotary", status)
+    return out
+
+
+def _kv_type(dtype) -> int:
+    return dtype if type(dtype) is int else _DTYPES.get(dtype, -1)
+
+
+class KvCache:
+    """A paged cache of keys and values in the library's layout: `pages` pages of `page` tokens for each of `heads` heads of `dim` values, as torch.float16,
+    torch.bfloat16, HLQ_MX8 or HLQ_MX4.  A token's slot is page number * page + its place in the page."""
+
+    __slots__ = ("blob", "pages", "page", "heads", "dim", "type", "_desc", "_need", "_device")
+
+    def __init__(self, blob, pages: int, page: int, heads: int, dim: int, dtype=None):
+        desc = HlqKvDesc(int(pages), int(page), int(heads), int(dim), _kv_type(torch.float16 if dtype is None else dtype))
+        need = _kv_bytes(desc)
+        if blob.dtype != torch.uint8 or blob.numel() < need or not blob.is_contiguous():
+            raise ValueError(f"a contiguous blob of {need} bytes is needed, got {blob.dtype} {tuple(blob.shape)}")
+        for name, value in (("blob", blob), ("pages", desc.pages), ("page", desc.page_tokens), ("heads", desc.heads), ("dim", desc.dim), ("type", desc.type),
+                            ("_desc", desc), ("_need", need), ("_device", blob.get_device())):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name} of a cache stays as it was made")
+
+    device = property(lambda self: self.blob.device)
+
+    @property
+    def rows(self):
+        """A 16-bit cache as an array [pages, 2 (keys, values), heads, tokens of a page, dim] over the same memory."""
+        if self.type not in (HLQ_F16, HLQ_BF16):
+            raise ValueError("the values of an 8- or 4-bit cache are read by hlq_kv_read")
+        kept = self.blob.reshape(-1)[:self._need].view(torch.float16 if self.type == HLQ_F16 else torch.bfloat16)
+        return kept.view(self.pages, 2, self.heads, self.page, self.dim)
+
+    def __reduce__(self):
+        return _kv_cache_of, (self.blob, self.pages, self.page, self.heads, self.dim, self.type)
+
+
+def _kv_cache_of(blob, pages: int, page: int, heads: int, dim: int, kept: int) -> KvCache:
+    return KvCache(blob, pages, page, heads, dim, kept)
+
+
+def _kv_bytes(desc: HlqKvDesc) -> int:
+    n = ctypes.c_size_t()
+    _check("hlq_kv_bytes", lib.hlq_kv_bytes(desc, ctypes.byref(n)))
+    return n.value
+
+
+def kv_bytes(pages: int, page: int, heads: int, dim: int, dtype) -> int:
+    return _kv_bytes(HlqKvDesc(pages, page, heads, dim, _kv_type(dtype)))
+
+
+def alloc_kv_cache(pages: int, page: int, heads: int, dim: int, dtype=None, device="cuda", stream=None) -> KvCache:
+    dtype = torch.float16 if dtype is None else dtype
+    return KvCache(_empty(kv_bytes(pages, page, heads, dim, dtype), torch.uint8, device, stream), pages, page, heads, dim, dtype)
+
+
+def hlq_kv_write(cache: KvCache, k, v, slots, rotary: Rotary | None = None, positions=None, q=None, q_out=None, k_out=None, stream=None):
+    """Rows k and v [T, heads, dim] into slots [T] (int64; outside the cache, as -1: skipped).  With a rotary, k is turned by positions [T] first, also into
+    k_out if given (which may be k), and q [T, heads of q, dim] into q_out (which may be q; a new tensor if not given), which is returned."""
+    T, H, D, kp, dtype, kt, kh = _heads(k)
+    vT, vH, vD, vp, vtype, vt, vh = _heads(v)
+    if (T, H, D, dtype) != (vT, vH, vD, vtype) or H != cache.heads or D != cache.dim:
+        raise ValueError(f"k is {k.dtype} {tuple(k.shape)}, v {v.dtype} {tuple(v.shape)}, the cache has {cache.heads} heads of {cache.dim}")
+    at = _numbers("slots", slots, torch.int64, T)
+    if rotary is None and (q is not None or k_out is not None):
+        raise ValueError("without a rotary there is nothing to turn: q and k_out are for it")
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    Hq, qp, qt, qh, qop, qot, qoh = 0, None, 0, 0, None, 0, 0
+    if q is not None:
+        if q_out is None:
+            q_out = _empty(tuple(q.shape), q.dtype, q.device, stream)
+        qT, Hq, qD, qp, qtype, qt, qh = _heads(q)
+        oT, oH, oD, qop, otype, qot, qoh = _heads(q_out)
+        if (qT, qD, qtype) != (T, D, dtype) or (oT, oH, oD, otype) != (T, Hq, D, dtype):
+            raise ValueError(f"k is {k.dtype} {tuple(k.shape)}, q {q.dtype} {tuple(q.shape)}, q_out {q_out.dtype} {tuple(q_out.shape)}")
+    kop, kot, koh = None, 0, 0
+    if k_out is not None:
+        oT, oH, oD, kop, otype, kot, koh = _heads(k_out)
+        if (oT, oH, oD, otype) != (T, H, D, dtype):
+            raise ValueError(f"k is {k.dtype} {tuple(k.shape)}, k_out {k_out.dtype} {tuple(k_out.shape)}")
+    desc = places = None
+    device = cache._device
+    there = device >= 0 and k.get_device() == device and v.get_device() == device and slots.get_device() == device
+    if rotary is not None:
+        if positions is None:
+            raise ValueError("a rotary needs positions")
+        desc, places = rotary._desc, _numbers("positions", positions, torch.int32, T)
+        there = there and rotary._device == device and positions.get_device() == device
+    if not there or (q is not None and not (q.get_device() == device and q_out.get_device() == device)) or (k_out is not None and k_out.get_device() != device):
+        raise _not_on_gpu(*(t for t in (cache, k, v, slots, rotary, positions, q, q_out, k_out) if t is not None))
+    if device != _current_device():
+        return _there(device, hlq_kv_write, cache, k, v, slots, rotary, positions, q, q_out, k_out, stream)
+    blob = cache.blob
+    status = lib.hlq_kv_write(cache._desc, blob.data_ptr(), blob.numel(), T, dtype, kp, kt, kh, vp, vt, vh, at, desc, places, kop, kot, koh, Hq, qp, qt, qh, qop, qot, qoh,
+                              _stream_of(stream, device))
+    if status != HLQ_OK:
+        raise HlqError("hlq_kv_write", status)
+    return q_out
+
+
+def hlq_kv_read(cache: KvCache, slots, k=None, v=None, dtype=None, stream=None):
+    """(k, v) [T, heads, dim] from slots [T] (int64) of the cache, in the tensors given or new ones of `dtype` (f32 by default); a row whose slot is outside the
+    cache stays as it was."""
+    T = slots.numel()
+    at = _numbers("slots", slots, torch.int64, T)
+    shape = (T, cache.heads, cache.dim)
+    if dtype is None:
+        dtype = k.dtype if k is not None else v.dtype if v is not None else torch.float32
+    if k is None:
+        k = _empty(shape, dtype, cache.blob.device, stream)
+    if v is None:
+        v = _empty(shape, dtype, cache.blob.device, stream)
+    kT, kH, kD, kp, ktype, kt, kh = _heads(k)
+    vT, vH, vD, vp, vtype, vt, vh = _heads(v)
+    if (kT, kH, kD) != shape or (vT, vH, vD) != shape or ktype != vtype:
+        raise ValueError(f"k is {k.dtype} {tuple(k.shape)}, v {v.dtype} {tuple(v.shape)}, the rows are {shape}")
+    device = cache._device
+    if device < 0 or slots.get_device() != device or k.get_device() != device or v.get_device() != device:
+        raise _not_on_gpu(cache, slots, k, v)
+    if device != _current_device():
+        return _there(device, hlq_kv_read, cache, slots, k, v, None, stream)
+    blob = cache.blob
+    status = lib.hlq_kv_read(cache._desc, blob.data_ptr(), blob.numel(), T, at, ktype, kp, kt, kh, vp, vt, vh, _stream_of(stream, device))
+    if status != HLQ_OK:
+        raise HlqError("hlq_kv_read", status)
+    return k, v
+
+
+def decode_workspace_bytes(cache: KvCache, q_heads: int, batch: int, table_width: int) -> int:
+    n = ctypes.c_size_t()
+    _check("hlq_attn_decode_workspace_bytes", lib.hlq_attn_decode_workspace_bytes(cache._desc, q_heads, batch, table_width, ctypes.byref(n)))
+    return n.value
+
+
+def prompt_workspace_bytes(q_rows: int, k_rows: int, batch: int, q_heads: int, heads: int, dim: int) -> int:
+    n = ctypes.c_size_t()
+    _check("hlq_attn_prompt_workspace_bytes", lib.hlq_attn_prompt_workspace_bytes(q_rows, k_rows, batch, q_heads, heads, dim, ctypes.byref(n)))
+    return n.value
+
+
+def _workspace_on(device: int, nbytes: int, stream):
+    if device != _current_device():
+        return _there(device, _workspace_on, device, nbytes, stream)
+    ws = _empty(nbytes, torch.uint8, torch.device("cuda", device), stream)
+    _check("hlq_workspace_init", lib.hlq_workspace_init(_ptr(ws), ws.numel(), _stream_of(stream, device)))
+    return ws
+
+
+def alloc_decode_workspace(cache: KvCache, q_heads: int, batch: int, table_width: int, stream=None):
+    """Workspace of hlq_attn_decode for up to `batch` sequences of up to `table_width` pages."""
+    if cache._device < 0:
+        raise _not_on_gpu(cache)
+    return _workspace_on(cache._device, decode_workspace_bytes(cache, q_heads, batch, table_width), stream)
+
+
+def alloc_prompt_workspace(q_rows: int, k_rows: int, batch: int, q_heads: int, heads: int, dim: int, device="cuda", stream=None):
+    """Workspace of hlq_attn_prompt for up to these numbers of rows and sequences."""
+    device = torch.device(device)
+    return _workspace_on(_current_device() if device.index is None else device.index, prompt_workspace_bytes(q_rows, k_rows, batch, q_heads, heads, dim), stream)
+
+
+def hlq_attn_decode(cache: KvCache, q, table, lengths, out=None, scale: float | None = None, window: int = 0, out_dtype=None, ws=None, stream=None):
+    """One new token of each sequence over its cached tokens: q [B, heads of q, dim], table int32 [B, pages of a sequence or more], lengths int32 [B], which count the new
+    token; scale 1 / sqrt(dim) if not given, window > 0: the newest so many tokens only."""
+    B, Hq, D, qp, qtype, qt, qh = _heads(q)
+    if out is None:
+        out = _empty((B, Hq, D), out_dtype or q.dtype, q.device, stream)
+    oB, oH, oD, op, otype, ot, oh = _heads(out)
+    if D != cache.dim or (oB, oH, oD) != (B, Hq, D):
+        raise ValueError(f"q is {tuple(q.shape)}, out {tuple(out.shape)}, the cache has heads of {cache.dim}")
+    if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != B or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError(f"table: expected int32 [{B}, pages], rows contiguous, got {table.dtype} {tuple(table.shape)}")
+    width = table.shape[1]
+    counts = _numbers("lengths", lengths, torch.int32, B)
+    device = cache._device
+    if ws is None:
+        ws = alloc_decode_workspace(cache, Hq, B, width, stream)
+    if (device < 0 or q.get_device() != device or out.get_device() != device or table.get_device() != device or lengths.get_device() != device
+            or ws.get_device() != device):
+        raise _not_on_gpu(cache, q, out, table, lengths, ws)
+    if device != _current_device():
+        return _there(device, hlq_attn_decode, cache, q, table, lengths, out, scale, window, None, ws, stream)
+    blob = cache.blob
+    status = lib.hlq_attn_decode(cache._desc, blob.data_ptr(), blob.numel(), Hq, B, qtype, qp, qt, qh, table.data_ptr(), table.stride(0) if B > 1 else width, width, counts,
+                                 window, D ** -0.5 if scale is None else scale, op, otype, ot, oh, ws.data_ptr(), ws.numel(), _stream_of(stream, device))
+    if status != HLQ_OK:
+        raise HlqError("hlq_attn_decode", status)
+    return out
+
+
+def hlq_attn_prompt(q, k, v, q_offsets, k_offsets=None, out=None, causal: bool = True, window: int = 0, scale: float | None = None, ws=None, stream=None):
+    """Attention of packed sequences: q [Tq, heads of q, dim], k and v [Tk, heads, dim]; sequence b has rows q_offsets[b] .. q_offsets[b + 1] of q (int32) and
+    k_offsets[b] .. of k and v (the same if not given).  A sequence's last query and last key are one token's."""
+    Tq, Hq, D, qp, dtype, qt, qh = _heads(q)
+    Tk, H, kD, kp, ktype, kt, kh = _heads(k)
+    vT, vH, vD, vp, vtype, vt, vh = _heads(v)
+    if out is None:
+        out = _empty((Tq, Hq, D), q.dtype, q.device, stream)
+    oT, oH, oD, op, otype, ot, oh = _heads(out)
+    if (Tk, H, kD, ktype) != (vT, vH, vD, vtype) or kD != D or ktype != dtype or (oT, oH, oD, otype) != (Tq, Hq, D, dtype):
+        raise ValueError(f"q is {q.dtype} {tuple(q.shape)}, k {k.dtype} {tuple(k.shape)}, v {v.dtype} {tuple(v.shape)}, out {out.dtype} {tuple(out.shape)}")
+    if k_offsets is None:
+        k_offsets = q_offsets
+    n = q_offsets.numel()
+    if n < 1:
+        raise ValueError("q_offsets: one more than sequences")
+    q_at, k_at = _numbers("q_offsets", q_offsets, torch.int32, n), _numbers("k_offsets", k_offsets, torch.int32, n)
+    device = q.get_device()
+    if ws is None and device >= 0:
+        ws = _workspace_on(device, prompt_workspace_bytes(Tq, Tk, n - 1, Hq, H, D), stream)
+    if (device < 0 or k.get_device() != device or v.get_device() != device or q_offsets.get_device() != device or k_offsets.get_device() != device
+            or out.get_device() != device or ws.get_device() != device):
+        raise _not_on_gpu(*(t for t in (q, k, v, q_offsets, k_offsets, out, ws) if t is not None))
+    if device != _current_device():
+        return _there(device, hlq_attn_prompt, q, k, v, q_offsets, k_offsets, out, causal, window, scale, ws, stream)
+    status = lib.hlq_attn_prompt(n - 1, Hq, H, D, dtype, Tq, qp, qt, qh, Tk, kp, kt, kh, vp, vt, vh, q_at, k_at, 1 if causal else 0, window,
+                                 D ** -0.5 if scale is None else scale, op, ot, oh, ws.data_ptr(), ws.numel(), _stream_of(stream, device))
+    if status != HLQ_OK:
+        raise HlqError("hlq_attn_prompt", status)
     return out

@@ -1,0 +1,625 @@
+// Attention of one new token over the paged cache:  out = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q . k_j - m),  m the largest score.
+//
+// One pass over keys and values with the running maximum and sum (Milakov and Gimelshein's online softmax).  A wavefront has the query heads of one
+// kv head (16 of them at most) and goes through tiles of 32 tokens, all in registers:
+//   scores    two products 16 tokens x 16 heads, keys the first operand.  A lane has tokens 4 g .. 4 g + 3 of each for one head (g = lane / 16).
+//   weights   are then where the second product wants them: its sum over tokens may take them in any order, so place 8 g + e of the sum is
+//             token 4 g + e for e < 4 and 16 + 4 g + e - 4 behind.  No weight changes lanes.
+//   values    a lane loads dim / 16 successive values of its eight tokens, rows whole, and turns the block in registers (a byte permutation
+//             makes two tokens' values of one column): dim / 16 products whose row r is column (dim / 16) r + j.
+// The four wavefronts of a workgroup take tiles in turn and meet in LDS.  A sequence is cut over up to `cuts` workgroups by its length; the last one to
+// end adds their sums in order (hand-over by device-scope stores and a counter), so results do not depend on which is last.
+// Weights are two terms of 16 bits (the second product runs twice: it waits for memory anyway), so that p is not rounded to 8 bits.  8- and 4-bit
+// values become bf16, which holds them and their scale exactly; f16 queries are two bf16 terms then.
+// Pages' pieces are read through buffer descriptors that end with the sequence's last token: what lies behind, and columns past dim, is 0 without a
+// comparison.
+#include "hlq_kv.h"
+
+namespace {
+
+constexpr int WAVES = 4, TILE = 32;
+constexpr float NONE = -__builtin_inff();
+
+typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
+typedef _Float16 half8v __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+
+struct Decode {
+    KvView kv;
+    int D, group, blocks, cuts;   // blocks of 16 query heads of a kv head
+    KvRows q;
+    const int32_t *table;
+    int64_t ld_table;
+    int width;
+    const int32_t *lengths;
+    int window;
+    float scale;                  // times log2(e)
+    KvRows out;
+    int otype;
+    int *arrived;
+    float *partial;
+    int rows;                     // of a partial result: min(16, group)
+};
+
+template <int C> struct Fragment { using type = bf8v; using scalar = __bf16; };
+template <> struct Fragment<HLQ_F16> { using type = half8v; using scalar = _Float16; };
+
+__device__ __forceinline__ float4v multiply(bf8v a, bf8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ float4v multiply(half8v a, half8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// over the four lanes of a head
+__device__ __forceinline__ float over_lanes_max(float v)
+{
+    auto s = __builtin_amdgcn_permlane32_swap(as_bits(v), as_bits(v), false, false);
+    v = fmaxf(as_float(s[0]), as_float(s[1]));
+    s = __builtin_amdgcn_permlane16_swap(as_bits(v), as_bits(v), false, false);
+    return fmaxf(as_float(s[0]), as_float(s[1]));
+}
+__device__ __forceinline__ float over_lanes_sum(float v)
+{
+    auto s = __builtin_amdgcn_permlane32_swap(as_bits(v), as_bits(v), false, false);
+    v = as_float(s[0]) + as_float(s[1]);
+    s = __builtin_amdgcn_permlane16_swap(as_bits(v), as_bits(v), false, false);
+    return as_float(s[0]) + as_float(s[1]);
+}
+// what a maximum is subtracted as: where nothing was seen, or only -infinity, 0, so that no difference is NaN
+__device__ __forceinline__ float base_of(float m) { return m == NONE ? 0.f : m; }
+
+constexpr int OUTSIDE = 0x7fffffff;   // an offset that every descriptor ends before
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const void *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00020000); }
+
+// N dwords (or 2 bytes: N = 0) through a descriptor.  (No scalar offset: only what is added in the lane counts in the comparison with the end.)
+template <int N>
+__device__ __forceinline__ void fetch(uint32_t *to, __amdgpu_buffer_rsrc_t r, int offset)
+{
+    if constexpr (N == 0) to[0] = __builtin_amdgcn_raw_buffer_load_b16(r, offset, 0, 0);
+    else if constexpr (N == 1) to[0] = __builtin_amdgcn_raw_buffer_load_b32(r, offset, 0, 0);
+    else if constexpr (N == 2) {
+        const mx4_u2 v = __builtin_bit_cast(mx4_u2, __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, 0));
+        to[0] = v.x, to[1] = v.y;
+    } else {
+        static_assert(N == 4, "");
+        const mx4_u4 v = __builtin_bit_cast(mx4_u4, __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, 0));
+        to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w;
+    }
+}
+
+// two values of 8 or 4 bits as bf16, times their scale; i: which two of the four or eight in c
+template <int C, int I>
+__device__ __forceinline__ uint32_t widen(uint32_t c, float scale)
+{
+    if constexpr (C == HLQ_MX4) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, I));
+    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, I));
+}
+
+// C: the cache's type, T: the queries', DP: dim up to 64, 128 or 256
+template <int C, int T, int DP>
+__global__ void __launch_bounds__(64 * WAVES)
+hlq_attn_decode_kernel(const Decode a)
+{
+    using F = typename Fragment<C>::type;
+    using S = typename Fragment<C>::scalar;
+    constexpr bool MX = C == HLQ_MX8 || C == HLQ_MX4;
+    constexpr int PER = C == HLQ_MX4 ? 8 : C == HLQ_MX8 ? 4 : 2;   // values of a dword
+    constexpr int KS = DP / 32, E = DP / 16;                       // products over dim; columns of a lane
+    constexpr int TERMS = MX && T == HLQ_F16 ? 2 : 1;              // of the queries
+    constexpr int PITCH = DP + 4;                                  // of a row in LDS
+    __shared__ __attribute__((aligned(16))) float sums[WAVES * 16 * PITCH];
+    __shared__ float tops[WAVES][16], totals[WAVES][16];
+
+    const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int col = lane & 15, g = lane >> 4;
+    int id = (int)blockIdx.x;
+    const int h = id % a.kv.H;
+    id /= a.kv.H;
+    const int block = id % a.blocks;
+    id /= a.blocks;
+    const int cut = id % a.cuts, b = id / a.cuts;
+
+    const int log_page = a.kv.log_page;
+    int64_t room = (int64_t)a.width << log_page;
+    int n = a.lengths[b];
+    n = n < 0 ? 0 : n > room ? (int)room : n;
+    const int start = a.window > 0 && n > a.window ? n - a.window : 0, first = start & ~(TILE - 1);
+    const int tiles = (n - first + TILE - 1) / TILE;
+    // workgroups that have a share, at least one, which writes the zeros of an empty sequence
+    int share = (tiles + a.cuts - 1) / a.cuts;
+    share = (share + WAVES - 1) / WAVES * WAVES;
+    const int active = tiles > 0 ? (tiles + share - 1) / share : 1;
+    if (cut >= active) return;
+    const int tile_end = (cut + 1) * share < tiles ? (cut + 1) * share : tiles;
+
+    const int head0 = block * 16, heads = a.group - head0 < 16 ? a.group - head0 : 16;   // of this workgroup
+    const int first_head = h * a.group + head0;
+    // queries, the second operand: lane (head, g) has what the keys' lanes have of place g of a product
+    F query[TERMS][KS];
+    {
+        using V = typename Mx4Type<T>::type;
+        const V *q = (const V *)a.q.p + b * a.q.ts + (int64_t)(first_head + (col < heads ? col : 0)) * a.q.hs;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const int d = MX ? KS * 8 * g + 8 * s : 32 * s + 8 * g;
+            V v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (V)0.f;
+            if (col < heads && d < a.D) mx4_read8<false>(q + d, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const S hi = (S)(float)v[i];
+                query[0][s][i] = hi;
+                if constexpr (TERMS == 2) query[1][s][i] = (S)((float)v[i] - (float)hi);
+            }
+        }
+    }
+
+    // offsets of this lane: of a key's pieces in its row, of a value's
+    constexpr int KEY_DWORDS = KS * 8 / PER, KEY_PIECE = KEY_DWORDS < 4 ? KEY_DWORDS : 4, KEY_PIECES = KEY_DWORDS / KEY_PIECE;
+    constexpr int VALUE_DWORDS = E / PER, VALUE_PIECE = VALUE_DWORDS < 4 ? VALUE_DWORDS : 4;   // 0: two bytes
+    constexpr int VALUE_PIECES = VALUE_DWORDS ? VALUE_DWORDS / VALUE_PIECE : 1;
+    const int row_bytes = a.kv.row_bytes;
+    int key_at[KEY_PIECES], value_at[4][VALUE_PIECES];
+#pragma unroll
+    for (int i = 0; i < KEY_PIECES; ++i) {
+        const int d = MX ? KS * 8 * g + i * KEY_PIECE * PER : 32 * i + 8 * g;
+        key_at[i] = d < a.D ? col * row_bytes + d * 4 / PER : OUTSIDE;
+    }
+#pragma unroll
+    for (int i = 0; i < VALUE_PIECES; ++i) {
+        const int d = E * col + i * VALUE_PIECE * PER;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) value_at[e][i] = d < a.D ? (4 * g + e) * row_bytes + d * 4 / PER : OUTSIDE;
+    }
+    constexpr int KEY_SCALES = KS == 8 ? 2 : 1;
+    int key_scale_at[KEY_SCALES], value_scale_at = 0;
+    if constexpr (MX) {
+#pragma unroll
+        for (int i = 0; i < KEY_SCALES; ++i) {
+            const int blk = KS * 8 * g / 32 + i;
+            key_scale_at[i] = blk < a.kv.blocks ? (blk << log_page) + col : OUTSIDE;
+        }
+        const int blk = E * col / 32;
+        value_scale_at = blk < a.kv.blocks ? (blk << log_page) + 4 * g : OUTSIDE;
+    }
+
+    // what is loaded of a tile: its two halves of 16 tokens lie in a page each
+    struct Keys { uint32_t v[2][KEY_DWORDS], scale[2][KEY_SCALES]; };
+    struct Values { uint32_t v[8][VALUE_DWORDS ? VALUE_DWORDS : 1], scale[2]; };
+    const int32_t *const table = a.table + b * a.ld_table;
+    auto page_of = [&](int tile, int half) {
+        int tok = first + tile * TILE + 16 * half;
+        tok = tok < n ? tok : n - 1;
+        int64_t page = table[tok >> log_page];
+        page = page < 0 ? 0 : page >= a.kv.pages ? a.kv.pages - 1 : page;
+        return __builtin_amdgcn_readfirstlane((int)page);
+    };
+    // tokens of the half up to the sequence's end, and where the half begins in its page
+    auto inside = [&](int tile, int half) {
+        const int left = n - (first + tile * TILE + 16 * half);
+        return left <= 0 ? 0 : left < 16 ? left : 16;
+    };
+    auto begins = [&](int tile, int half) { return (first + tile * TILE + 16 * half) & ((1 << log_page) - 1); };
+    auto load_keys = [&](Keys &k, int tile, const int (&pages)[2]) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int at = begins(tile, half);
+            const auto r = descriptor(a.kv.rows(pages[half], 0, h) + at * row_bytes, inside(tile, half) * row_bytes);
+#pragma unroll
+            for (int i = 0; i < KEY_PIECES; ++i) fetch<KEY_PIECE>(k.v[half] + i * KEY_PIECE, r, key_at[i]);
+            if constexpr (MX) {
+                const auto rs = descriptor(a.kv.bytes(pages[half], 0, h) + at, (a.kv.blocks << log_page) - at);
+#pragma unroll
+                for (int i = 0; i < KEY_SCALES; ++i) k.scale[half][i] = __builtin_amdgcn_raw_buffer_load_b8(rs, key_scale_at[i], 0, 0);
+            }
+        }
+    };
+    auto load_values = [&](Values &v, int tile, const int (&pages)[2]) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int at = begins(tile, half);
+            const auto r = descriptor(a.kv.rows(pages[half], 1, h) + at * row_bytes, inside(tile, half) * row_bytes);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < VALUE_PIECES; ++i) fetch<VALUE_PIECE>(v.v[4 * half + e] + i * VALUE_PIECE, r, value_at[e][i]);
+            if constexpr (MX) {
+                const auto rs = descriptor(a.kv.bytes(pages[half], 1, h) + at, (a.kv.blocks << log_page) - at);
+                v.scale[half] = __builtin_amdgcn_raw_buffer_load_b32(rs, value_scale_at, 0, 0);
+            }
+        }
+    };
+
+    float4v acc[E];
+    float top = NONE, total = 0.f;
+    // lane (head, g) has columns E (4 g + i) .. of row 4 g + i
+    auto own_sums = [&](int i, int j) { return (float4v *)(sums + (wave * 16 + col) * PITCH + E * (4 * g + i) + j); };
+    auto pass = [&](bool two) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) acc[j] = (float4v){0.f, 0.f, 0.f, 0.f};
+        top = NONE, total = 0.f;
+        int tile = cut * share + wave;
+        if (tile < tile_end) {
+            Keys keys;
+            Values values;
+            int pages[2] = {page_of(tile, 0), page_of(tile, 1)};
+            load_keys(keys, tile, pages);
+            load_values(values, tile, pages);
+            for (;;) {
+                const int next = tile + WAVES;
+                const bool more = next < tile_end;
+                if (more) {
+                    pages[0] = page_of(next, 0);
+                    pages[1] = page_of(next, 1);
+                }
+                const int tok0 = first + tile * TILE;
+                const bool part = tok0 < start || tok0 + TILE > n;   // some tokens are not to be seen
+
+                // scores
+                float x[8];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float4v s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) {
+                        mx4_u4 w;
+                        if constexpr (C == HLQ_MX4) {
+                            const float scale = as_float(keys.scale[half][i * KEY_SCALES / KS] << 23);
+                            const uint32_t c = keys.v[half][i];
+                            w = (mx4_u4){widen<C, 0>(c, scale), widen<C, 1>(c, scale), widen<C, 2>(c, scale), widen<C, 3>(c, scale)};
+                        } else if constexpr (C == HLQ_MX8) {
+                            const float scale = as_float(keys.scale[half][i * KEY_SCALES / KS] << 23);
+                            const uint32_t c = keys.v[half][2 * i], d = keys.v[half][2 * i + 1];
+                            w = (mx4_u4){widen<C, 0>(c, scale), widen<C, 1>(c, scale), widen<C, 0>(d, scale), widen<C, 1>(d, scale)};
+                        } else
+                            w = (mx4_u4){keys.v[half][4 * i], keys.v[half][4 * i + 1], keys.v[half][4 * i + 2], keys.v[half][4 * i + 3]};
+                        const F k = __builtin_bit_cast(F, w);
+#pragma unroll
+                        for (int t = 0; t < TERMS; ++t) s = multiply(k, query[t][i], s);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[4 * half + e] = s[e] * a.scale;
+                }
+                if (more) load_keys(keys, next, pages);
+                if (part) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int tok = tok0 + (e < 4 ? 4 * g + e : 12 + 4 * g + e);
+                        if (tok < start || tok >= n) x[e] = NONE;
+                    }
+                }
+                float m = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+                m = fmaxf(top, over_lanes_max(m));
+                const float base = base_of(m);
+                if (__any(m > top)) {
+                    const float keep = __builtin_amdgcn_exp2f(top - base);
+                    total *= keep;
+#pragma unroll
+                    for (int j = 0; j < E; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[j][i] *= keep;
+                    top = m;
+                }
+                F p, rest;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float w = __builtin_amdgcn_exp2f(x[e] - base);
+                    total += w;
+                    p[e] = (S)w;
+                    rest[e] = (S)(w - (float)p[e]);
+                }
+
+                // values, two tokens' of one column in a register
+                uint32_t rows[8][E / 2];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (MX) {
+                        // the conversion takes the eight bits of the exponent only
+                        const uint32_t four = values.scale[e >> 2];
+                        const float scale = as_float((e & 3) == 3 ? four >> 1 : four << (23 - 8 * (e & 3)));
+#pragma unroll
+                        for (int i = 0; i < E / 2; ++i) {
+                            const uint32_t c = values.v[e][i * 2 / PER];
+                            if constexpr (C == HLQ_MX4) rows[e][i] = i % 4 == 0 ? widen<C, 0>(c, scale) : i % 4 == 1 ? widen<C, 1>(c, scale) : i % 4 == 2 ? widen<C, 2>(c, scale) : widen<C, 3>(c, scale);
+                            else rows[e][i] = i % 2 == 0 ? widen<C, 0>(c, scale) : widen<C, 1>(c, scale);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < E / 2; ++i) rows[e][i] = values.v[e][i];
+                    }
+                }
+                if (part) {
+                    // of tokens that are not to be seen nothing enters, whatever stands there
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int tok = tok0 + (e < 4 ? 4 * g + e : 12 + 4 * g + e);
+                        if (tok < start || tok >= n) {
+                            p[e] = (S)0.f;
+                            rest[e] = (S)0.f;
+#pragma unroll
+                            for (int i = 0; i < E / 2; ++i) rows[e][i] = 0u;
+                        }
+                    }
+                }
+                F turned[E];
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    const uint32_t pick = j & 1 ? 0x07060302u : 0x05040100u;
+                    const mx4_u4 w = {__builtin_amdgcn_perm(rows[1][j >> 1], rows[0][j >> 1], pick), __builtin_amdgcn_perm(rows[3][j >> 1], rows[2][j >> 1], pick),
+                                      __builtin_amdgcn_perm(rows[5][j >> 1], rows[4][j >> 1], pick), __builtin_amdgcn_perm(rows[7][j >> 1], rows[6][j >> 1], pick)};
+                    turned[j] = __builtin_bit_cast(F, w);
+                }
+                if (more) load_values(values, next, pages);
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    acc[j] = multiply(turned[j], p, acc[j]);
+                    if (two) acc[j] = multiply(turned[j], rest, acc[j]);
+                }
+                if (!more) break;
+                tile = next;
+            }
+        }
+    };
+    pass(true);
+    // An infinite value times a second term, which may be 0 or below it, is NaN: where a sum is NaN, the first terms alone are its result.
+    bool nan = false;
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) nan = nan || acc[j][i] != acc[j][i];
+    const bool again = __any(nan);
+    if (again) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < E; j += 4) *own_sums(i, j) = (float4v){acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]};
+        pass(false);
+    }
+    total = over_lanes_sum(total);
+
+    // the wavefronts' sums meet in LDS
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < E; j += 4) {
+            float4v v = {acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]};
+            if (again) {
+                const float4v before = *own_sums(i, j);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] = before[c] == before[c] ? before[c] : v[c];
+            }
+            *own_sums(i, j) = v;
+        }
+    if (g == 0) {
+        tops[wave][col] = top;
+        totals[wave][col] = total;
+    }
+    __syncthreads();
+    const int64_t who = ((int64_t)b * a.blocks + block) * a.kv.H + h;
+    const int64_t size = (int64_t)a.rows * (DP + 2);              // of a partial result: sums, then maximum and total of each head
+    float *const partial = active > 1 ? a.partial + who * a.cuts * size : nullptr;
+    const bool alone = active == 1;
+    auto put = [&](int head, int d, float4v v) {
+        const int64_t at = b * a.out.ts + (int64_t)(first_head + head) * a.out.hs + d;
+        mx4_store4(a.out.p, a.otype, at, (const float *)&v, 4);
+    };
+    for (int it = (int)threadIdx.x; it < heads * (DP / 4); it += 64 * WAVES) {
+        const int head = it / (DP / 4), d = it % (DP / 4) * 4;
+        float m = NONE;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, tops[w][head]);
+        const float base = base_of(m);
+        float4v sum = {0.f, 0.f, 0.f, 0.f};
+        float all = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float weight = __builtin_amdgcn_exp2f(tops[w][head] - base);
+            const float4v v = *(const float4v *)(sums + (w * 16 + head) * PITCH + d);
+            all = fmaf(weight, totals[w][head], all);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = fmaf(weight, v[i], sum[i]);
+        }
+        if (alone) {
+            const float by = all == 0.f ? 0.f : 1.f / all;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] *= by;
+            if (d < a.D) put(head, d, sum);
+        } else {
+            uint64_t *to = (uint64_t *)(partial + cut * size + head * DP + d);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                __hip_atomic_store(to + i, as_bits(sum[2 * i]) | (uint64_t)as_bits(sum[2 * i + 1]) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (d == 0)
+                __hip_atomic_store((uint64_t *)(partial + cut * size + a.rows * DP) + head, as_bits(m) | (uint64_t)as_bits(all) << 32,
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    if (alone) return;
+
+    // Device-scope stores are complete before the arrival is counted; whoever is last adds the cuts in their order.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    int *const last = (int *)&tops[0][0];
+    if (threadIdx.x == 0) *last = __hip_atomic_fetch_add(a.arrived + who, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == active - 1;
+    __syncthreads();
+    if (!*last) return;
+    if (threadIdx.x == 0) __hip_atomic_store(a.arrived + who, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    float *const weights = sums, *const shares = sums + 16 * 128;   // [head][cut], then 1 / total of each head
+    for (int head = wave; head < heads; head += WAVES) {
+        float m[2], all[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int c = lane + 64 * i;
+            m[i] = NONE, all[i] = 0.f;
+            if (c < active) {
+                const uint64_t pair = __hip_atomic_load((const uint64_t *)(partial + c * size + a.rows * DP) + head, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                m[i] = as_float((uint32_t)pair);
+                all[i] = as_float((uint32_t)(pair >> 32));
+            }
+        }
+        float most = fmaxf(m[0], m[1]), sum = 0.f;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o));
+        const float base = base_of(most);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float w = __builtin_amdgcn_exp2f(m[i] - base);
+            sum = fmaf(w, all[i], sum);
+            weights[head * 128 + lane + 64 * i] = w;
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+        if (lane == 0) shares[head] = sum == 0.f ? 0.f : 1.f / sum;
+    }
+    __syncthreads();
+    for (int it = (int)threadIdx.x; it < heads * (DP / 4); it += 64 * WAVES) {
+        const int head = it / (DP / 4), d = it % (DP / 4) * 4;
+        const uint64_t *from = (const uint64_t *)(partial + head * DP + d);
+        float4v sum = {0.f, 0.f, 0.f, 0.f};
+        for (int c0 = 0; c0 < active; c0 += 8) {
+            uint64_t pair[8][2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = c0 + i < active ? c0 + i : c0;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) pair[i][e] = __hip_atomic_load(from + c * (size / 2) + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c0 + i < active) {
+                    const float w = weights[head * 128 + c0 + i];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        sum[2 * e] = fmaf(w, as_float((uint32_t)pair[i][e]), sum[2 * e]);
+                        sum[2 * e + 1] = fmaf(w, as_float((uint32_t)(pair[i][e] >> 32)), sum[2 * e + 1]);
+                    }
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] *= shares[head];
+        if (d < a.D) put(head, d, sum);
+    }
+}
+
+// How a launch is cut.  Workgroups of up to 1024 tokens each, so that long sequences do not end alone, where that is not more than 16384 workgroups;
+// and 2048 of them if there are tokens for that, 128 each at least; 128 cuts at most, and none where the counters do not suffice.
+constexpr int64_t WANTED = 2048, MOST_WORKGROUPS = 16384, MOST_TOKENS = 1024, LEAST_TOKENS = 128, MOST_CUTS = 128;
+struct Cuts {
+    int cuts;
+    size_t room;   // partial results in the workspace, enough for fewer sequences and narrower tables too
+};
+Cuts cuts_of(int64_t workgroups, int64_t tokens)
+{
+    if (workgroups < 1 || workgroups > HLQ_WS_ARRIVAL_COUNTERS || tokens <= LEAST_TOKENS) return {1, 0};
+    const auto up = [](int64_t n, int64_t by) { return (n + by - 1) / by; };
+    const auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
+    const auto most = [](int64_t a, int64_t b) { return a < b ? b : a; };
+    const int64_t cuts = least(most(up(WANTED, workgroups), least(up(tokens, MOST_TOKENS), MOST_WORKGROUPS / workgroups)), least(up(tokens, LEAST_TOKENS), MOST_CUTS));
+    const int64_t room = least(most(WANTED + workgroups, least(workgroups * up(tokens, MOST_TOKENS), MOST_WORKGROUPS + workgroups)),
+                               workgroups * least(up(tokens, LEAST_TOKENS), MOST_CUTS));
+    return {(int)cuts, (size_t)room};
+}
+int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+
+struct Shape {
+    KvDims d;
+    int group, blocks, cuts;
+    int64_t workgroups;
+    size_t bytes;
+};
+hlq_status shape_of(const hlq_kv_desc *c, int32_t q_heads, int64_t B, int32_t width, Shape *out)
+{
+    Shape s{};
+    const hlq_status st = hlq_kv_check(c, &s.d);
+    if (st != HLQ_OK) return st;
+    if (q_heads < 1 || q_heads % s.d.H || B < 0 || width < 0) return HLQ_ERR_BAD_DESC;
+    if (q_heads > KV_MOST_HEADS) return HLQ_ERR_UNSUPPORTED;
+    s.group = q_heads / s.d.H;
+    s.blocks = (s.group + 15) / 16;
+    const int64_t tokens = (int64_t)width << s.d.log_page;
+    if (B > ((int64_t)1 << 24) / (s.d.H * s.blocks) || tokens > 0x7fffffe0) return HLQ_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 lanes
+    s.workgroups = B * s.d.H * s.blocks;
+    const Cuts k = cuts_of(s.workgroups, tokens);
+    s.cuts = k.cuts;
+    s.bytes = HLQ_WS_COUNTER_BYTES + k.room * (size_t)((s.group < 16 ? s.group : 16) * (padded(s.d.D) + 2)) * sizeof(float);
+    s.bytes = (s.bytes + 255u) & ~(size_t)255u;
+    *out = s;
+    return HLQ_OK;
+}
+
+template <int C, int T>
+void launch(const Decode &a, int64_t grid, hipStream_t st)
+{
+    const dim3 g((unsigned)grid), block(64 * WAVES);
+    switch (padded(a.D)) {
+    case 64: hlq_attn_decode_kernel<C, T, 64><<<g, block, 0, st>>>(a); break;
+    case 128: hlq_attn_decode_kernel<C, T, 128><<<g, block, 0, st>>>(a); break;
+    default: hlq_attn_decode_kernel<C, T, 256><<<g, block, 0, st>>>(a); break;
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+hlq_status hlq_attn_decode_workspace_bytes(const hlq_kv_desc *c, int32_t q_heads, int64_t B, int32_t table_width, size_t *bytes)
+{
+    Shape s;
+    const hlq_status st = shape_of(c, q_heads, B, table_width, &s);
+    if (st != HLQ_OK) return st;
+    if (!bytes) return HLQ_ERR_NULL;
+    *bytes = s.bytes;
+    return HLQ_OK;
+}
+
+hlq_status hlq_attn_decode(const hlq_kv_desc *c, const void *cache, size_t cache_bytes, int32_t q_heads, int64_t B, hlq_dtype type, const void *q,
+                           int64_t q_ts, int64_t q_hs, const int32_t *table, int64_t ld_table, int32_t table_width, const int32_t *lengths, int32_t window,
+                           float scale, void *out, hlq_dtype otype, int64_t o_ts, int64_t o_hs, void *ws, size_t ws_bytes, void *stream)
+{
+    Shape s;
+    hlq_status st = shape_of(c, q_heads, B, table_width, &s);
+    if (st != HLQ_OK) return st;
+    const bool mx = s.d.type == HLQ_MX8 || s.d.type == HLQ_MX4;
+    if ((type != HLQ_F16 && type != HLQ_BF16) || (!mx && (int)type != s.d.type) || !hlq_is_float(otype)) return HLQ_ERR_UNSUPPORTED;
+    if (window < 0) return HLQ_ERR_BAD_DESC;
+    if (B == 0) return HLQ_OK;
+    if (!cache || !lengths || (!table && table_width > 0)) return HLQ_ERR_NULL;
+    if ((uintptr_t)cache & 15u || (uintptr_t)table & 3u || (uintptr_t)lengths & 3u || ld_table < 0 || ld_table > (int64_t)1 << 40 || (B > 1 && ld_table < table_width))
+        return HLQ_ERR_BAD_STRIDE;
+    if (cache_bytes < s.d.total) return HLQ_ERR_BUFFER_TOO_SMALL;
+    if ((st = hlq_check_rows(q, B, q_heads, s.d.D, q_ts, q_hs, type, false)) != HLQ_OK) return st;
+    if ((st = hlq_check_rows(out, B, q_heads, s.d.D, o_ts, o_hs, otype, true)) != HLQ_OK) return st;
+    if (s.cuts > 1) {
+        if (!ws) return HLQ_ERR_NULL;
+        if ((uintptr_t)ws & 15u) return HLQ_ERR_BAD_STRIDE;
+        if (ws_bytes < s.bytes) return HLQ_ERR_BUFFER_TOO_SMALL;
+    }
+    Decode a{};
+    a.kv = hlq_kv_view(s.d, cache);
+    a.D = s.d.D;
+    a.group = s.group;
+    a.blocks = s.blocks;
+    a.cuts = s.cuts;
+    a.q = KvRows{const_cast<void *>(q), q_ts, q_hs};
+    a.table = table;
+    a.ld_table = ld_table;
+    a.width = table_width;
+    a.lengths = lengths;
+    a.window = window;
+    a.scale = scale * 1.44269504f;
+    a.out = KvRows{out, o_ts, o_hs};
+    a.otype = otype;
+    a.arrived = (int *)ws;
+    a.partial = ws ? (float *)((char *)ws + HLQ_WS_COUNTER_BYTES) : nullptr;
+    a.rows = s.group < 16 ? s.group : 16;
+    const int64_t grid = s.workgroups * s.cuts;
+    if (grid > ((int64_t)1 << 24) - 1) return HLQ_ERR_UNSUPPORTED;
+    const hipStream_t stm = (hipStream_t)stream;
+    hlq_clear_stale_error();
+    if (s.d.type == HLQ_F16) launch<HLQ_F16, HLQ_F16>(a, grid, stm);
+    else if (s.d.type == HLQ_BF16) launch<HLQ_BF16, HLQ_BF16>(a, grid, stm);
+    else if (s.d.type == HLQ_MX8) type == HLQ_F16 ? launch<HLQ_MX8, HLQ_F16>(a, grid, stm) : launch<HLQ_MX8, HLQ_BF16>(a, grid, stm);
+    else type == HLQ_F16 ? launch<HLQ_MX4, HLQ_F16>(a, grid, stm) : launch<HLQ_MX4, HLQ_BF16>(a, grid, stm);
+    return hlq_hip_status(hipGetLastError());
+}
+
+}  // extern "C"

@@ -1,0 +1,59 @@
+// The paged cache of keys and values as the kernels see it; its layout stands in hlq.h.
+#pragma once
+
+#include "hlq_mx4.h"
+
+constexpr int KV_MOST_DIM = 256, KV_MOST_HEADS = 1024, KV_BLOCK = 32;
+
+struct KvDims {
+    int64_t pages;
+    int H, D, type;
+    int log_page;            // of the tokens of a page
+    int row_bytes, blocks;   // of a token and head: bytes of codes, scale bytes (0: 16-bit values)
+    size_t code_bytes, total;
+};
+hlq_status hlq_kv_check(const hlq_kv_desc *c, KvDims *out);
+
+struct KvView {
+    uint8_t *codes, *scales;
+    int64_t pages;
+    int H, log_page, row_bytes, blocks;
+
+    // where the page's keys (what = 0) or values (1) of a head are
+    __device__ __forceinline__ int64_t piece(int64_t page, int what, int h) const { return (page * 2 + what) * H + h; }
+    __device__ __forceinline__ uint8_t *rows(int64_t page, int what, int h) const { return codes + (piece(page, what, h) << log_page) * row_bytes; }
+    __device__ __forceinline__ uint8_t *bytes(int64_t page, int what, int h) const { return scales + (piece(page, what, h) << log_page) * blocks; }
+};
+static inline KvView hlq_kv_view(const KvDims &d, const void *cache)
+{
+    uint8_t *p = (uint8_t *)const_cast<void *>(cache);
+    return KvView{p, p + d.code_bytes, d.pages, d.H, d.log_page, d.row_bytes, d.blocks};
+}
+
+// rows of heads: strides in elements
+struct KvRows {
+    void *p;
+    int64_t ts, hs;
+};
+// What an array [T, heads, dim] may be.  An output's rows have to stand apart: token by token or head by head.
+static inline hlq_status hlq_check_rows(const void *p, int64_t T, int heads, int dim, int64_t ts, int64_t hs, hlq_dtype type, bool output)
+{
+    constexpr int64_t MOST = (int64_t)1 << 40;
+    if (ts < 0 || hs < 0 || ts > MOST || hs > MOST) return HLQ_ERR_BAD_STRIDE;
+    if (output && (T > 1 || heads > 1)) {
+        const bool by_token = (heads == 1 || hs >= dim) && (T == 1 || ts >= (heads - 1) * hs + dim);
+        const bool by_head = (T == 1 || ts >= dim) && (heads == 1 || hs >= (T - 1) * (__int128)ts + dim);
+        if (!by_token && !by_head) return HLQ_ERR_BAD_STRIDE;
+    }
+    if (!p) return HLQ_ERR_NULL;
+    return (uintptr_t)p % (unsigned)hlq_dtype_bytes(type) ? HLQ_ERR_BAD_STRIDE : HLQ_OK;
+}
+
+// By value: a bit cast of a vector's element reads the vector's first.
+__device__ __forceinline__ float as_float(uint32_t v) { return __builtin_bit_cast(float, v); }
+__device__ __forceinline__ uint32_t as_bits(float v) { return __builtin_bit_cast(uint32_t, v); }
+
+// storage type of a cache's values
+template <int T> struct KvType { using type = uint8_t; };
+template <> struct KvType<HLQ_F16> { using type = _Float16; };
+template <> struct KvType<HLQ_BF16> { using type = __bf16; };

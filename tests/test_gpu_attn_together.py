@@ -1,0 +1,242 @@
+"""The operators of attention together, as a program uses them: prompts into the cache, token after token over it, a prompt in pieces; captured into graphs, on
+other streams, on a workspace that calls share.
+
+A token over a 16-bit cache and the same token's row of the whole prompt come from the same numbers: they differ by both bounds of attn_util at most."""
+import numpy as np
+import pytest
+import torch
+
+from attn_util import HALF_STEP, KINDS, TYPES, bound, host, rng, rounded
+from oracle import attn_oracle as O
+from paper_2510_19482_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+HQ, H, D, PAGE = 8, 2, 64, 16
+
+
+class Layer:
+    """Rows of a projection for sequences that grow, and a cache that they go into."""
+
+    def __init__(self, prompts, steps, kind, dtype, key=()):
+        r = rng("layer", prompts, steps, kind, dtype, *key)
+        self.prompts, self.steps, self.dtype, self.kind = prompts, steps, dtype, kind
+        self.total = [n + steps for n in prompts]
+        need = [-(-n // PAGE) for n in self.total]
+        order = r.permutation(sum(need) + 2)
+        self.table = np.full((len(prompts), max(need)), -1, np.int32)
+        at = 0
+        for b, n in enumerate(need):
+            self.table[b, :n] = order[at:at + n]
+            at += n
+        self.kv = B.alloc_kv_cache(len(order), PAGE, H, D, KINDS[kind])
+        self.kv.blob.fill_(255)
+        self.rows = [rounded(r.normal(size=(n, HQ + 2 * H, D)) * 1.5, dtype)[0].cuda() for n in self.total]
+        self.rotary = B.Rotary(B.rotary_frequencies(D))
+        self.table_gpu = torch.from_numpy(self.table).cuda()
+
+    def slots(self, b, positions):
+        return self.table[b, positions // PAGE].astype(np.int64) * PAGE + positions % PAGE
+
+    def split(self, rows):
+        return rows.split([HQ, H, H], 1)
+
+    def write_prompts(self):
+        """All prompts packed: turned queries and keys, values, offsets."""
+        rows = torch.cat([x[:n] for x, n in zip(self.rows, self.prompts)])
+        positions = np.concatenate([np.arange(n) for n in self.prompts]).astype(np.int32)
+        slots = np.concatenate([self.slots(b, np.arange(n)) for b, n in enumerate(self.prompts)])
+        q, k, v = self.split(rows)
+        turned = torch.empty(k.shape, dtype=k.dtype, device="cuda")
+        q = B.hlq_kv_write(self.kv, k, v, torch.from_numpy(slots).cuda(), self.rotary, torch.from_numpy(positions).cuda(), q=q, k_out=turned)
+        return q, turned, v, torch.tensor(np.concatenate([[0], np.cumsum(self.prompts)]), dtype=torch.int32, device="cuda")
+
+    def step(self, s):
+        """The inputs of step s: rows, slots, positions, lengths."""
+        at = np.array([n + s for n in self.prompts])
+        rows = torch.stack([x[i] for x, i in zip(self.rows, at)])
+        slots = np.array([self.slots(b, np.array([i]))[0] for b, i in enumerate(at)])
+        return rows, torch.from_numpy(slots).cuda(), torch.from_numpy(at.astype(np.int32)).cuda(), torch.from_numpy((at + 1).astype(np.int32)).cuda()
+
+
+@pytest.mark.parametrize("kind,dtype", [("bf16", "bf16"), ("f16", "f16"), ("mx8", "bf16"), ("mx4", "f16")])
+def test_prompts_then_token_after_token(kind, dtype):
+    layer = Layer([37, 1, 130, 16], 20, kind, dtype)
+    q, k, v, at = layer.write_prompts()
+    B.hlq_attn_prompt(q, k, v, at)
+    ws = B.alloc_decode_workspace(layer.kv, HQ, 4, layer.table.shape[1])
+    outs = []
+    for s in range(layer.steps):
+        rows, slots, positions, lengths = layer.step(s)
+        q, k, v = layer.split(rows)
+        q = B.hlq_kv_write(layer.kv, k, v, slots, layer.rotary, positions, q=q)
+        outs.append(B.hlq_attn_decode(layer.kv, q, layer.table_gpu, lengths, ws=ws))
+    # the same from the oracle: keys turned and rounded to their type, then to the cache's values
+    compute = HALF_STEP["f16"] if kind == "f16" else HALF_STEP["bf16"]
+    for b, n in enumerate(layer.prompts):
+        x = layer.rows[b].double().cpu().numpy()
+        places = torch.arange(layer.total[b], dtype=torch.int32, device="cuda")
+        turned = B.hlq_rotary(layer.rows[b][:, :HQ + H], places, layer.rotary)
+        want = O.turned(x[:, :HQ + H], np.arange(layer.total[b]), layer.rotary.frequencies)
+        assert np.abs(host(turned) - want).max() <= (HALF_STEP[dtype] + 2.0**-20) * np.abs(want).max()
+        turned = host(turned)
+        keys, values = turned[:, HQ:], x[:, HQ + H:]
+        if kind.startswith("mx"):
+            keys, values = (O.mx_values(*O.mx_quantize(y, kind), kind) for y in (keys, values))
+        for s in range(layer.steps):
+            i = n + s
+            for h in range(HQ):
+                y, size, products = O.attend(turned[i, h][None], keys[:i + 1, h // 4], values[:i + 1, h // 4], np.ones((1, i + 1), bool), np.float32(D**-0.5))
+                e = bound(size[0], products[0], i + 1, D, np.abs(values).max(), compute**2, dtype, y[0])
+                assert (np.abs(host(outs[s][b, h]) - y[0]) <= e).all(), (b, s, h)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_tokens_one_by_one_are_the_prompts_rows(dtype):
+    layer = Layer([200, 3], 40, dtype, dtype)
+    layer.write_prompts()
+    outs = []
+    for s in range(layer.steps):
+        rows, slots, positions, lengths = layer.step(s)
+        q, k, v = layer.split(rows)
+        q = B.hlq_kv_write(layer.kv, k, v, slots, layer.rotary, positions, q=q)
+        outs.append(B.hlq_attn_decode(layer.kv, q, layer.table_gpu, lengths))
+    for b, n in enumerate(layer.prompts):
+        q, k, v = layer.split(layer.rows[b])
+        places = torch.arange(layer.total[b], dtype=torch.int32, device="cuda")
+        q, k = B.hlq_rotary(q, places, layer.rotary), B.hlq_rotary(k, places, layer.rotary)
+        whole = B.hlq_attn_prompt(q, k, v, torch.tensor([0, layer.total[b]], dtype=torch.int32, device="cuda"))
+        got = torch.stack([o[b] for o in outs])
+        for h in range(HQ):
+            s = np.tril(np.ones((layer.total[b],) * 2, bool))[n:]
+            y, size, products = O.attend(host(q[n:, h]), host(k[:, h // 4]), host(v[:, h // 4]), s, np.float32(D**-0.5))
+            e = bound(size, products[:, None], layer.total[b], D, 6.0, HALF_STEP[dtype], dtype, y)
+            assert (np.abs(host(whole[n:, h]) - host(got[:, h])) <= 2 * e).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "mx8", "mx4"])
+def test_a_prompt_in_pieces_over_what_is_read_back(kind):
+    # each piece attends to the cache's earlier tokens, read back, and its own; with a 16-bit cache that is the whole prompt's result bit for bit where the tiles are alike
+    n, piece = 300, 100
+    layer = Layer([n], 0, kind, "bf16")
+    q, k, v, at = layer.write_prompts()
+    outs = []
+    for start in range(0, n, piece):
+        end = start + piece
+        slots = torch.from_numpy(layer.slots(0, np.arange(end))).cuda()
+        keys, values = B.hlq_kv_read(layer.kv, slots, dtype=torch.bfloat16)
+        q_at, k_at = (torch.tensor([0, m], dtype=torch.int32, device="cuda") for m in (piece, end))
+        outs.append(B.hlq_attn_prompt(q[start:end], keys, values, q_at, k_at))
+    got = host(torch.cat(outs))
+    keys, values = (host(x) for x in B.hlq_kv_read(layer.kv, torch.from_numpy(layer.slots(0, np.arange(n))).cuda()))
+    for h in range(HQ):
+        y, size, products = O.attend(host(q[:, h]), keys[:, h // 4], values[:, h // 4], np.tril(np.ones((n, n), bool)), np.float32(D**-0.5))
+        assert (np.abs(got[:, h] - y) <= bound(size, products[:, None], n, D, 8.0, HALF_STEP["bf16"], "bf16", y)).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "mx4"])
+def test_a_step_in_a_graph(kind):
+    layer = Layer([500, 30, 2000], 12, kind, "bf16", key=("graph",))
+    layer.write_prompts()
+    eager = Layer([500, 30, 2000], 12, kind, "bf16", key=("graph",))
+    eager.write_prompts()
+    rows, slots, positions, lengths = (x.clone() for x in layer.step(0))
+    width = layer.table.shape[1]
+    ws = B.alloc_decode_workspace(layer.kv, HQ, 3, width)
+    q_out, out = torch.empty((3, HQ, D), dtype=torch.bfloat16, device="cuda"), torch.empty((3, HQ, D), dtype=torch.bfloat16, device="cuda")
+    q, k, v = layer.split(rows)
+
+    def step():
+        B.hlq_kv_write(layer.kv, k, v, slots, layer.rotary, positions, q=q, q_out=q_out)
+        B.hlq_attn_decode(layer.kv, q_out, layer.table_gpu, lengths, out=out, ws=ws)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for s in range(layer.steps):
+        new = layer.step(s)
+        for to, x in zip((rows, slots, positions, lengths), new):
+            to.copy_(x)
+        out.fill_(7)
+        graph.replay()
+        e_rows, e_slots, e_positions, e_lengths = eager.step(s)
+        eq, ek, ev = eager.split(e_rows)
+        want = B.hlq_attn_decode(eager.kv, B.hlq_kv_write(eager.kv, ek, ev, e_slots, eager.rotary, e_positions, q=eq), eager.table_gpu, e_lengths)
+        if s % 3 == 0:
+            torch.cuda.synchronize()
+        assert torch.equal(out, want), s
+    assert torch.equal(layer.kv.blob, eager.kv.blob)
+
+
+def test_a_prompt_in_a_graph_and_two_graphs_on_one_workspace():
+    r = rng("two graphs")
+    Tq, n = 300, 5000
+    q = rounded(r.normal(size=(Tq, HQ, D)), "bf16")[0].cuda()
+    k, v = (rounded(r.normal(size=(n, H, D)), "bf16")[0].cuda() for _ in range(2))
+    cuts = [([0, 100, 300], [0, 2000, 5000]), ([0, 299, 300], [0, 4000, 4001]), ([0, 1, 9], [0, 4990, 5000])]
+    at = [[torch.tensor(x, dtype=torch.int32, device="cuda") for x in c] for c in cuts]
+    want = [B.hlq_attn_prompt(q, k, v, *a) for a in at]
+    ws = B.alloc_prompt_workspace(Tq, n, 2, HQ, H, D)
+    q_at, k_at = (x.clone() for x in at[0])
+    outs = [torch.empty_like(q) for _ in range(2)]
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    B.hlq_attn_prompt(q, k, v, q_at, k_at, out=outs[0], ws=ws)
+    torch.cuda.synchronize()
+    for g, o in zip(graphs, outs):
+        with torch.cuda.graph(g):
+            B.hlq_attn_prompt(q, k, v, q_at, k_at, out=o, ws=ws)
+    for i in (0, 1, 2, 1, 0, 2):
+        q_at.copy_(at[i][0])
+        k_at.copy_(at[i][1])
+        for o in outs:
+            o.fill_(3)
+        for g in graphs:
+            g.replay()
+        end = cuts[i][0][-1]
+        for o in outs:
+            assert torch.equal(o[:end], want[i][:end]) and (o[end:] == 3).all()
+
+
+def test_on_another_stream():
+    layer = Layer([900, 40], 1, "bf16", "bf16", key=("stream",))
+    layer.write_prompts()
+    rows, slots, positions, lengths = layer.step(0)
+    q, k, v = layer.split(rows)
+    want_q = B.hlq_kv_write(layer.kv, k, v, slots, layer.rotary, positions, q=q)
+    want = B.hlq_attn_decode(layer.kv, want_q, layer.table_gpu, lengths)
+    at = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    want_prompt = B.hlq_attn_prompt(want_q, k, v, at)
+    want_read = B.hlq_kv_read(layer.kv, slots)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        got_q = B.hlq_kv_write(layer.kv, k, v, slots, layer.rotary, positions, q=q, stream=side)
+        turned = B.hlq_rotary(q, positions, layer.rotary, stream=side)
+        got = B.hlq_attn_decode(layer.kv, got_q, layer.table_gpu, lengths, stream=side)
+        got_prompt = B.hlq_attn_prompt(got_q, k, v, at, stream=side)
+        got_read = B.hlq_kv_read(layer.kv, slots, stream=side)
+        side.synchronize()
+        for a, b in ((got_q, want_q), (turned, want_q), (got, want), (got_prompt, want_prompt), *zip(got_read, want_read)):
+            assert torch.equal(a, b)
+
+
+def test_two_streams_with_a_workspace_each():
+    batches = []
+    for i in range(2):
+        layer = Layer([6000 + 500 * i, 3000], 1, "bf16", "bf16", key=("two", i))
+        layer.write_prompts()
+        rows, slots, positions, lengths = layer.step(0)
+        q, k, v = layer.split(rows)
+        q = B.hlq_kv_write(layer.kv, k, v, slots, layer.rotary, positions, q=q)
+        want = B.hlq_attn_decode(layer.kv, q, layer.table_gpu, lengths)
+        batches.append((layer, q, lengths, want, torch.cuda.Stream(), B.alloc_decode_workspace(layer.kv, HQ, 2, layer.table.shape[1]), [torch.empty_like(want) for _ in range(20)]))
+    torch.cuda.synchronize()
+    for i in range(20):
+        for layer, q, lengths, want, stream, ws, outs in batches:
+            B.hlq_attn_decode(layer.kv, q, layer.table_gpu, lengths, out=outs[i], ws=ws, stream=stream)
+    torch.cuda.synchronize()
+    for _, _, _, want, _, _, outs in batches:
+        for o in outs:
+            assert torch.equal(o, want)
