@@ -1,32 +1,37 @@
 // Attention of packed prompts:  out_i = sum_j p_ij v_j / sum_j p_ij over the keys j that query i sees,  p_ij = exp(scale q_i . k_j - m_i).
 //
-// One pass over the keys with the running maximum and sum of each query.  A workgroup has 128 queries of one head of one sequence, a wavefront 32 of them;
-// keys and values come in tiles of 64 (32 for dim above 128) by way of registers, the next tile's on their way while this one is multiplied.
+// One pass over the keys with the running maximum and sum of each query.  A wavefront has 64 queries of a head (32 for dim above 128), a workgroup four
+// wavefronts: four heads of a kv head with the same queries where the group allows, else two, or one with more queries.  Keys and values come through LDS
+// in tiles of 32, written there by the loads themselves, three tiles of each.
 //   scores    K Q^T with keys the first operand, 32 keys x 32 queries: a lane has 16 keys of one query, so that maximum and sum are the lane's own and
 //             one exchange with the lane 32 on
 //   weights   are then where the second product, V^T P^T, wants them: its sum over keys may take them in any order
-//   values    are turned as they enter LDS, four keys of a column next to each other in the order in which the weights stand
-// What is not seen: its score is -infinity, its weight 0.  A value that is infinite or NaN would still enter as 0 times itself, so tiles at the edge of
-// what is seen are looked at as they are loaded, and one that holds such a value is multiplied without it; what it does to those that do see it
-// is added by counting.
+//   values    are turned as they are read from LDS (four keys of a column to a lane)
+// A step multiplies the next tile's keys and the last tile's values while it takes the exponentials of this one, so that matrix cores and vector units work side by
+// side within a wavefront.
+// The maximum that exponentials are taken from is kept while no score passes it by 2^8, and is a whole power of two: so sums are rarely multiplied, and exactly.
+// What is not seen: its score is -infinity, its weight 0.  A value that is infinite or NaN would still enter as 0 times itself, so the values of tiles at the edge
+// of what is seen are looked at, and one that holds such a value is multiplied without it; what it does to those that do see it is added by counting.
 #include "hlq_kv.h"
 
 namespace {
 
-constexpr int WAVES = 4, ROWS = 32 * WAVES;
+constexpr int WAVES = 4, KEYS = 32, STAGES = 3;
 constexpr float NONE = -__builtin_inff();
 
 typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 typedef float float16v __attribute__((ext_vector_type(16)));
+typedef short short4v __attribute__((ext_vector_type(4)));
 
 struct Prompt {
     int B, H, group, D;
+    int abreast;   // heads of a workgroup: 4, 2 or 1
     int Tq, Tk;
     KvRows q, k, v, out;
     const int32_t *q_offsets, *k_offsets;
     int causal, window;
-    float scale;   // times log2(e)
+    float scale, sign;   // the scale's magnitude times log2(e) (1 if it is 0), and its sign
 };
 
 template <int T> struct Fragment { using type = bf8v; using scalar = __bf16; static constexpr uint32_t EXPONENT = 0x7f807f80u, ONE = 0x00800080u; };
@@ -41,14 +46,31 @@ __device__ __forceinline__ float other_half(float v, float &own)
     own = as_float(s[0]);
     return as_float(s[1]);
 }
-__device__ __forceinline__ float base_of(float m) { return m == NONE ? 0.f : m; }
+
+// c + a + b
+__device__ __forceinline__ float add_pair(__bf16 a, __bf16 b, float c)
+{
+    const mx4_bf2 one = {(__bf16)1.f, (__bf16)1.f};
+    return __builtin_amdgcn_fdot2_f32_bf16((mx4_bf2){a, b}, one, c, false);
+}
+__device__ __forceinline__ float add_pair(_Float16 a, _Float16 b, float c)
+{
+    const mx4_half2 one = {(_Float16)1.f, (_Float16)1.f};
+    return __builtin_amdgcn_fdot2((mx4_half2){a, b}, one, c, false);
+}
+
+// 16 bytes a lane from an offset of a descriptor (zeros past its end) to LDS at `to`, lane after lane
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, int offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(r), "s"(to) : "memory");
+}
 
 // sequence and tile of a workgroup; every lane of the wavefront takes part and gets the same answer
 struct Place {
     int q0, n_q, k0, n_k;   // rows of the sequence
     int first;              // query of the tile's first row; n_q = 0: there are fewer tiles
 };
-__device__ __forceinline__ Place place_of(const Prompt &a, int tile)
+__device__ __forceinline__ Place place_of(const Prompt &a, int tile, int rows)
 {
     const int lane = (int)(threadIdx.x & 63u);
     // offsets are device data: whatever they hold, rows stay inside
@@ -62,7 +84,7 @@ __device__ __forceinline__ Place place_of(const Prompt &a, int tile)
             n = offset(a.q_offsets, b + 1, a.Tq) - lo;
             n = n < 0 ? 0 : n;
         }
-        const int mine = n / ROWS + (n % ROWS > 0);
+        const int mine = n / rows + (n % rows > 0);
         int upto = mine;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -77,7 +99,7 @@ __device__ __forceinline__ Place place_of(const Prompt &a, int tile)
             p.n_q = __builtin_amdgcn_readlane(n, f);
             const int past = __builtin_amdgcn_readlane(upto, f);
             // of a sequence the last tile first: it sees most keys
-            p.first = (past - 1 - (tile - before)) * ROWS;
+            p.first = (past - 1 - (tile - before)) * rows;
             p.k0 = offset(a.k_offsets, at + f, a.Tk);
             const int n_k = offset(a.k_offsets, at + f + 1, a.Tk) - p.k0;
             p.n_k = __builtin_amdgcn_readfirstlane(n_k < 0 ? 0 : n_k);
@@ -89,232 +111,324 @@ __device__ __forceinline__ Place place_of(const Prompt &a, int tile)
     return {0, 0, 0, 0, 0};
 }
 
-template <int T, int DP>
+// DMA: rows of keys and values begin at multiples of 16 bytes
+template <int T, int DP, bool DMA>
 __global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2)
 hlq_attn_prompt_kernel(const Prompt a)
 {
     using F = typename Fragment<T>::type;
     using S = typename Fragment<T>::scalar;
-    constexpr int KEYS = DP > 128 ? 32 : 64, BLOCKS = KEYS / 32;
-    constexpr int KP = DP * 2 + 16, VP = KEYS * 2 + 16;                 // bytes of a row in LDS: of a key, of a column of values
-    constexpr int KEY_LOADS = KEYS * DP / 8 / (64 * WAVES);             // 16 bytes each
-    constexpr int UNITS = KEYS / 4 * (DP / 8);                          // of values: four keys, eight columns
-    constexpr int VALUE_UNITS = (UNITS + 64 * WAVES - 1) / (64 * WAVES);
-    __shared__ __attribute__((aligned(16))) char key_rows[KEYS * KP], value_rows[DP * VP];
-    __shared__ int strange[2];                                          // the tile has values that are no numbers
+    constexpr int KS = DP / 16, DS = DP / 32;
+    constexpr int ROW = DP * 2, PIECES = DP / 8, TILE = KEYS * ROW;     // bytes; 16-byte pieces of a row
+    constexpr int LOADS = TILE / 1024 / WAVES;                          // of a wavefront, 1024 bytes each, of keys and as many of values
+    __shared__ __attribute__((aligned(1024))) char lds[2 * STAGES * TILE];
+    const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
 
     const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int col = lane & 31, half = lane >> 5;
     int id = (int)blockIdx.x;
     const int h = id % a.H;   // kv heads in turn: one each XCD where there are eight
     id /= a.H;
-    const int head = h * a.group + id % a.group;
-    const Place p = place_of(a, id / a.group);
+    const int sets = a.group / a.abreast, set = id % sets;
+    const int rows = 32 * (WAVES / a.abreast);                 // queries of a workgroup
+    const Place p = place_of(a, id / sets, rows);
     if (p.n_q == 0) return;
+    const int head = h * a.group + set * a.abreast + wave % a.abreast;
+    const int row0 = wave / a.abreast * 32;                    // of this wavefront in the tile
 
     const int shift = p.n_k - p.n_q;                                    // place of query 0
-    const int rows = p.n_q - p.first < ROWS ? p.n_q - p.first : ROWS;
-    // keys that some query of the workgroup sees
-    int key_end = p.n_k, key_first = 0;
-    if (a.causal) key_end = shift + p.first + rows < key_end ? shift + p.first + rows : key_end;
-    if (a.window > 0) {
-        const int64_t lowest = (int64_t)shift + p.first - a.window + 1;
-        key_first = lowest > 0 ? (int)lowest & ~(KEYS - 1) : 0;
-    }
+    const int tile_rows = p.n_q - p.first < rows ? p.n_q - p.first : rows;
+    // steps of 32 keys that some query of rows [from, from + n) sees
+    auto steps_of = [&](int from, int n, int &begin, int &end) {
+        int last = p.n_k;
+        if (a.causal) last = shift + p.first + from + n < last ? shift + p.first + from + n : last;
+        int first = 0;
+        if (a.window > 0) {
+            const int64_t lowest = (int64_t)shift + p.first + from - a.window + 1;
+            first = lowest > 0 ? (int)lowest : 0;
+        }
+        begin = first / KEYS;
+        end = n > 0 && last > first ? (last + KEYS - 1) / KEYS : begin;
+    };
+    int all_begin, all_end, begin, end;
+    steps_of(0, tile_rows, all_begin, all_end);
+    const int own_rows = tile_rows - row0 < 0 ? 0 : tile_rows - row0 < 32 ? tile_rows - row0 : 32;
+    steps_of(row0, own_rows, begin, end);
 
-    // queries, the second operand
-    const int row = wave * 32 + col, my_place = shift + p.first + row;
-    F query[DP / 16];
+    // queries, the second operand; of a negative scale they have the sign, so that the largest score has the largest product
+    const int first_place = shift + p.first + row0;                     // of the wavefront's first query
+    F query[KS];
     {
-        const S *q = (const S *)a.q.p + (int64_t)(p.q0 + p.first + (row < rows ? row : 0)) * a.q.ts + head * a.q.hs;
+        const bool there = col < own_rows;
+        const S *q = (const S *)a.q.p + (int64_t)(p.q0 + p.first + (there ? row0 + col : 0)) * a.q.ts + head * a.q.hs;
 #pragma unroll
-        for (int s = 0; s < DP / 16; ++s) {
+        for (int s = 0; s < KS; ++s) {
             S v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = (S)0.f;
-            if (row < rows && 16 * s + 8 * half < a.D) mx4_read8<false>(q + 16 * s + 8 * half, v);
+            if (there && a.sign != 0.f && 16 * s + 8 * half < a.D) mx4_read8<false>(q + 16 * s + 8 * half, v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) query[s][i] = v[i];
+            for (int i = 0; i < 8; ++i) query[s][i] = a.sign < 0.f ? -v[i] : v[i];
         }
     }
 
-    mx4_u4 key_in[KEY_LOADS], value_in[VALUE_UNITS][4];
-    const S *const k = (const S *)a.k.p + (int64_t)p.k0 * a.k.ts + h * a.k.hs, *const v = (const S *)a.v.p + (int64_t)p.k0 * a.v.ts + h * a.v.hs;
-    const mx4_u4 zero = {0u, 0u, 0u, 0u};
-    auto load = [&](int key0) {
+    // Tiles in LDS: row after row, a row's 16-byte pieces in another order, so that reads meet every bank evenly: piece c of key k at c ^ (k & 7), of a
+    // value's row at c ^ 2 (k & 3).  A lane loads what belongs in its place.
+    constexpr int OUTSIDE = 0x7fffffff;
+    const int key_step = (int)(a.k.ts * 2), value_step = (int)(a.v.ts * 2);   // bytes from row to row (DMA)
+    int at_key[LOADS], key_piece[LOADS], value_piece[LOADS], key_at[LOADS], value_at[LOADS];
 #pragma unroll
-        for (int i = 0; i < KEY_LOADS; ++i) {
-            const int at = i * 64 * WAVES + (int)threadIdx.x, key = key0 + at / (DP / 8), d = at % (DP / 8) * 8;
-            key_in[i] = key < p.n_k && d < a.D ? *(const mx4_u4_any *)(k + key * a.k.ts + d) : zero;
-        }
-#pragma unroll
-        for (int i = 0; i < VALUE_UNITS; ++i) {
-            const int at = i * 64 * WAVES + (int)threadIdx.x, key = key0 + at / (DP / 8) * 4, d = at % (DP / 8) * 8;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) value_in[i][e] = at < UNITS && key + e < p.n_k && d < a.D ? *(const mx4_u4_any *)(v + (key + e) * a.v.ts + d) : zero;
-        }
+    for (int i = 0; i < LOADS; ++i) {
+        at_key[i] = (wave * LOADS + i) * (64 / PIECES) + lane / PIECES;
+        key_piece[i] = (lane % PIECES ^ (at_key[i] & 7)) * 8;
+        value_piece[i] = (lane % PIECES ^ (at_key[i] & 3) << 1) * 8;
+        key_at[i] = key_piece[i] < a.D ? at_key[i] * key_step + key_piece[i] * 2 : OUTSIDE;
+        value_at[i] = value_piece[i] < a.D ? at_key[i] * value_step + value_piece[i] * 2 : OUTSIDE;
+    }
+    // what the next requests read: tiles of keys or values one after the other, nothing behind the last key that somebody sees
+    struct Feed {
+        const char *from;
+        int64_t step;
+        int left;
     };
-    auto enter = [&](bool look, int turn) {
+    const int limit = all_end * KEYS < p.n_k ? all_end * KEYS : p.n_k;
+    auto feed = [&](const KvRows &x) {
+        const int first = all_begin * KEYS;
+        return Feed{(const char *)((const S *)x.p + (int64_t)(p.k0 + first) * x.ts + h * x.hs), x.ts * 2 * KEYS, limit - first};
+    };
+    Feed key_feed = feed(a.k), value_feed = feed(a.v);
+    mx4_u4 kept[DMA ? 1 : 2 * LOADS];
+    auto request = [&](bool of_keys, Feed &f, uint32_t slot) {
+        const int n = f.left < 0 ? 0 : f.left < KEYS ? f.left : KEYS;
+        if constexpr (DMA) {
+            const int step = of_keys ? key_step : value_step, bytes = n * step - (step - a.D * 2);   // rows are no nearer than their length
+            const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(f.from), 0, bytes > 0 ? bytes : 0, 0x00020000);
+            const uint32_t to = lds_at + slot + wave * LOADS * 1024;
 #pragma unroll
-        for (int i = 0; i < KEY_LOADS; ++i) {
-            const int at = i * 64 * WAVES + (int)threadIdx.x;
-            *(mx4_u4 *)(key_rows + at / (DP / 8) * KP + at % (DP / 8) * 16) = key_in[i];
-        }
+            for (int i = 0; i < LOADS; ++i) load_to_lds(r, of_keys ? key_at[i] : value_at[i], to + i * 1024);
+        } else {
 #pragma unroll
-        for (int i = 0; i < VALUE_UNITS; ++i) {
-            const int at = i * 64 * WAVES + (int)threadIdx.x, four = at / (DP / 8), d = at % (DP / 8) * 8;
-            const int place = (four & ~3) | (four & 1) << 1 | (four >> 1 & 1);   // of the four keys in the order of the weights
-            if (UNITS % (64 * WAVES) && at >= UNITS) continue;
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                const uint32_t pick = c & 1 ? 0x07060302u : 0x05040100u;
-                *(mx4_u2 *)(value_rows + (d + c) * VP + place * 8) = (mx4_u2){__builtin_amdgcn_perm(value_in[i][1][c >> 1], value_in[i][0][c >> 1], pick),
-                                                                              __builtin_amdgcn_perm(value_in[i][3][c >> 1], value_in[i][2][c >> 1], pick)};
+            for (int i = 0; i < LOADS; ++i) {
+                const int piece = of_keys ? key_piece[i] : value_piece[i];
+                kept[of_keys ? i : LOADS + i] = at_key[i] < n && piece < a.D ? *(const mx4_u4_any *)(f.from + (at_key[i] * (of_keys ? a.k.ts : a.v.ts) + piece) * 2) : (mx4_u4){0u, 0u, 0u, 0u};
             }
         }
-        if (look) {
-            uint32_t found = 0;
+        f.from += f.step;
+        f.left -= KEYS;
+    };
+    auto enter = [&](bool of_keys, uint32_t slot) {
 #pragma unroll
-            for (int i = 0; i < VALUE_UNITS; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) found |= (value_in[i][e][w] & Fragment<T>::EXPONENT) + Fragment<T>::ONE;
-            if (found & 0x80008000u) strange[turn] = 1;
-        }
+        for (int i = 0; i < LOADS; ++i) *(mx4_u4 *)(lds + slot + (wave * LOADS + i) * 1024 + lane * 16) = kept[of_keys ? i : LOADS + i];
     };
 
-    float16v acc[DP / 32];
+    // reads: a key's pieces 2 s + half, and four keys of a column of values
+    int key_read[4], value_read[2];
 #pragma unroll
-    for (int j = 0; j < DP / 32; ++j)
+    for (int s = 0; s < 4; ++s) key_read[s] = col * ROW + ((2 * s + half) ^ (col & 7)) * 16;
+    {
+        const int i = lane & 15, c = ((lane >> 4) & 1) * 2 + ((i & 3) >> 1), turn = (i >> 2) << 1;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) value_read[j] = (4 * half + (i >> 2)) * ROW + ((4 * j + c) ^ turn) * 16 + (i & 1) * 8;
+    }
+    auto key = [&](uint32_t slot, int s) { return *(const F *)(lds + slot + key_read[s & 3] + (s >> 2) * 128); };
+    auto value = [&](uint32_t slot, int j, int u) {
+        typedef __attribute__((address_space(3))) short4v *Four;
+        const char *at = lds + slot + value_read[j & 1] + (j >> 1) * 128 + 16 * u * ROW;
+        struct { short4v v[2]; } two;
+        two.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)at);
+        two.v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(at + 8 * ROW));
+        return __builtin_bit_cast(F, two);
+    };
+
+    float16v acc[DS];
+    float base = 0.f, most = NONE, total = 0.f;   // most: scores up to it need no new base
+#pragma unroll
+    for (int j = 0; j < DS; ++j)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
-    float top = NONE, total = 0.f;
-    // places of the wavefront's first and last query
-    const int wave_first = shift + p.first + wave * 32, wave_last = shift + p.first + (wave * 32 + 31 < rows ? wave * 32 + 31 : rows - 1);
-    // whether some query of the workgroup (or wavefront) does not see all of a tile's keys
-    auto edge = [&](int key0, int first, int last) {
-        return key0 + KEYS > p.n_k || (a.causal && key0 + KEYS - 1 > first) || (a.window > 0 && key0 <= last - a.window);
+    // steps of which every query of the wavefront sees every key
+    const int last_place = first_place + own_rows - 1;
+    int full_end = p.n_k;
+    if (a.causal && first_place + 1 < full_end) full_end = first_place + 1;
+    full_end = full_end < 0 ? 0 : full_end / KEYS;
+    const int full_begin = a.window > 0 && last_place >= a.window ? (last_place - a.window) / KEYS + 1 : 0;
+    auto edge = [&](int step) { return step < full_begin || step >= full_end; };
+    auto seen = [&](int step, int i) {
+        const int key = step * KEYS + 8 * (i >> 2) + 4 * half + (i & 3), place = first_place + col;
+        return key < p.n_k && (!a.causal || key <= place) && (a.window == 0 || key > place - a.window);
     };
 
-    if (threadIdx.x < 2) strange[threadIdx.x] = 0;
-    int turn = 0;
-    if (key_first < key_end) load(key_first);
-    for (int key0 = key_first; key0 < key_end; key0 += KEYS) {
-        __syncthreads();
-        enter(edge(key0, shift + p.first, shift + p.first + rows - 1), turn);
-        __syncthreads();
-        if (key0 + KEYS < key_end) load(key0 + KEYS);
-        const bool odd = strange[turn];
-        if (threadIdx.x == 0) strange[turn ^ 1] = 0;
-        turn ^= 1;
-        if (wave * 32 >= rows || (a.causal && key0 > wave_last) || (a.window > 0 && key0 + KEYS <= wave_first - a.window + 1)) continue;   // nothing to see
-        const bool part = edge(key0, wave_first, wave_last);
-
-        float x[BLOCKS][16];
+    auto multiply_keys = [&](float16v &score, uint32_t slot) {
 #pragma unroll
-        for (int t = 0; t < BLOCKS; ++t) {
-            float16v s;
+        for (int i = 0; i < 16; ++i) score[i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        for (int s = 0; s < KS; ++s) score = multiply(key(slot, s), query[s], score);
+    };
+    auto multiply_values = [&](const F (&weight)[2], uint32_t slot) {
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i) s = multiply(*(const F *)(key_rows + (t * 32 + col) * KP + i * 32 + half * 16), query[i], s);
+        for (int j = 0; j < DS; ++j)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[t][i] = s[i] * a.scale;
-        }
-        auto seen = [&](int t, int i) {
-            const int key = key0 + t * 32 + 8 * (i >> 2) + 4 * half + (i & 3);
-            return key < p.n_k && (!a.causal || key <= my_place) && (a.window == 0 || key > my_place - a.window);
-        };
-        if (part) {
+            for (int u = 0; u < 2; ++u) acc[j] = multiply(value(slot, j, u), weight[u], acc[j]);
+    };
+    // values that are numbers as above; +infinity, and -infinity, and NaN as both, once for each query that sees one
+    auto multiply_odd_values = [&](const F (&weight)[2], int step, uint32_t slot) {
+        F sees[2];
 #pragma unroll
-            for (int t = 0; t < BLOCKS; ++t)
+        for (int i = 0; i < 16; ++i) sees[i >> 3][i & 7] = (S)(seen(step, i) ? 1.f : 0.f);
+#pragma unroll
+        for (int j = 0; j < DS; ++j) {
+#pragma unroll
+            for (int sign = 0; sign < 2; ++sign) {
+                float16v count;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) count[i] = 0.f;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    F c = value(slot, j, u), is;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float f = (float)c[e];
+                        is[e] = (S)((sign ? f > NONE : f < __builtin_inff()) ? 0.f : 1.f);
+                        if (!(fabsf(f) < __builtin_inff())) c[e] = (S)0.f;
+                    }
+                    if (sign == 0) acc[j] = multiply(c, weight[u], acc[j]);
+                    count = multiply(is, sees[u], count);
+                }
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (!seen(t, i)) x[t][i] = NONE;
+                    if (count[i] > 0.f) acc[j][i] += sign ? NONE : __builtin_inff();
+            }
         }
-        float m = x[0][0];
+    };
+    auto odd_values = [&](uint32_t slot) {   // whether the tile has values that are no numbers
+        uint32_t found = 0;
 #pragma unroll
-        for (int t = 0; t < BLOCKS; ++t)
+        for (int j = 0; j < DS; ++j)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) m = fmaxf(m, x[t][i]);
+            for (int u = 0; u < 2; ++u) {
+                const mx4_u4 w = __builtin_bit_cast(mx4_u4, value(slot, j, u));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) found |= (w[i] & Fragment<T>::EXPONENT) + Fragment<T>::ONE;
+            }
+        return __any((found & 0x80008000u) != 0u);
+    };
+    // sees to it that scores are at most 2^8 times what the exponentials are taken from; `weight`, not yet multiplied, goes by that too
+    auto keep_up = [&](const float16v &score, F (&weight)[2]) {
+        float m = score[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) m = fmaxf(m, score[i]);
         float own;
         const float other = other_half(m, own);
-        m = fmaxf(top, fmaxf(own, other));
-        const float base = base_of(m);
-        if (__any(m > top)) {
-            const float keep = __builtin_amdgcn_exp2f(top - base);
+        m = fmaxf(own, other) * a.scale;
+        if (__builtin_expect(__any(m > most), 0)) {
+            const bool now = m > most;
+            const float to = now ? ceilf(m) : base;
+            const float keep = !now ? 1.f : most == NONE ? 0.f : __builtin_amdgcn_exp2f(base - to);
+            base = to;
+            most = now ? to + 8.f : most;
             total *= keep;
 #pragma unroll
-            for (int j = 0; j < DP / 32; ++j)
+            for (int j = 0; j < DS; ++j)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[j][i] *= keep;
-            top = m;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) weight[u][e] = (S)((float)weight[u][e] * keep);
         }
-        F weight[BLOCKS][2];
+    };
+    auto exponentials = [&](const float16v &score, F (&weight)[2]) {
 #pragma unroll
-        for (int t = 0; t < BLOCKS; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float w = __builtin_amdgcn_exp2f(x[t][i] - base);
-                total += w;
-                weight[t][i >> 3][i & 7] = (S)w;
-            }
-        auto value = [&](int j, int t, int u) { return *(const F *)(value_rows + (j * 32 + col) * VP + t * 64 + u * 32 + half * 16); };
-        if (!(part && odd)) {
-#pragma unroll
-            for (int j = 0; j < DP / 32; ++j)
-#pragma unroll
-                for (int t = 0; t < BLOCKS; ++t)
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) acc[j] = multiply(value(j, t, u), weight[t][u], acc[j]);
-        } else {
-            // values that are numbers as above; +infinity, and -infinity, and NaN as both, once for each query that sees one
-            F sees[BLOCKS][2];
-#pragma unroll
-            for (int t = 0; t < BLOCKS; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    sees[t][i >> 3][i & 7] = (S)(seen(t, i) ? 1.f : 0.f);
-                    if (!seen(t, i)) weight[t][i >> 3][i & 7] = (S)0.f;
-                }
-#pragma unroll
-            for (int j = 0; j < DP / 32; ++j) {
-                float16v plus, minus;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) plus[i] = minus[i] = 0.f;
-#pragma unroll
-                for (int t = 0; t < BLOCKS; ++t)
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        F c = value(j, t, u), up, down;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float f = (float)c[e];
-                            up[e] = (S)(f < __builtin_inff() ? 0.f : 1.f);
-                            down[e] = (S)(f > NONE ? 0.f : 1.f);
-                            if (!(fabsf(f) < __builtin_inff())) c[e] = (S)0.f;
-                        }
-                        acc[j] = multiply(c, weight[t][u], acc[j]);
-                        plus = multiply(up, sees[t][u], plus);
-                        minus = multiply(down, sees[t][u], minus);
-                    }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if (plus[i] > 0.f) acc[j][i] += __builtin_inff();
-                    if (minus[i] > 0.f) acc[j][i] -= __builtin_inff();
-                }
-            }
+        for (int i = 0; i < 16; i += 2) {
+            const S w0 = (S)__builtin_amdgcn_exp2f(fmaf(score[i], a.scale, -base)), w1 = (S)__builtin_amdgcn_exp2f(fmaf(score[i + 1], a.scale, -base));
+            weight[i >> 3][i & 7] = w0;
+            weight[i >> 3][(i & 7) + 1] = w1;
+            total = add_pair(w0, w1, total);
         }
+    };
+
+    if (all_begin < all_end) {
+        // Step t multiplies the keys of t + 1 and the values of t - 1, takes the exponentials of t, and requests the keys of t + 3 and the values of t + 1.
+        // Three slots of each: t's is `here`, t + 1's `ahead`, t - 1's `behind`.
+        constexpr uint32_t OF_VALUES = STAGES * TILE;
+        uint32_t here = 2 * TILE, ahead = 0, behind = TILE;
+        float16v score;
+        F weight[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) score[i] = 0.f, weight[i >> 3][i & 7] = (S)0.f;
+        request(true, key_feed, ahead);
+        if constexpr (!DMA) enter(true, ahead);
+        request(true, key_feed, behind);
+        int t = all_begin - 1;
+        auto meet = [&](bool first) {
+            if constexpr (DMA) {
+                // what was requested the step before last is there
+                if (first) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+                else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
+            } else {
+                __syncthreads();
+                enter(true, behind);
+                if (!first) enter(false, OF_VALUES + here);
+            }
+            request(true, key_feed, here);
+            request(false, value_feed, OF_VALUES + ahead);
+        };
+        auto advance = [&]() {
+            const uint32_t was = behind;
+            behind = here;
+            here = ahead;
+            ahead = was;
+            ++t;
+        };
+        // most of a long prompt: nothing to mask, nothing to look at
+        const int hot_begin = begin + 1 > full_begin + 1 ? begin + 1 : full_begin + 1, hot_end = end - 1 < full_end ? end - 1 : full_end;
+        while (t <= all_end) {
+            if (t >= hot_begin && t + 1 < hot_end) {
+                do {
+                    float16v next;
+                    F later[2];
+                    meet(false);
+                    keep_up(score, weight);
+                    multiply_keys(next, ahead);
+                    multiply_values(weight, OF_VALUES + behind);
+                    exponentials(score, later);
+                    advance();
+                    meet(false);
+                    keep_up(next, later);
+                    multiply_keys(score, ahead);
+                    multiply_values(later, OF_VALUES + behind);
+                    exponentials(next, weight);
+                    advance();
+                } while (t + 1 < hot_end);
+                continue;
+            }
+            meet(t < all_begin);
+            const bool ask = t + 1 >= begin && t + 1 < end, weigh = t >= begin && t < end, sum = t - 1 >= begin && t - 1 < end;
+            if (sum) {
+                if (edge(t - 1) && odd_values(OF_VALUES + behind)) multiply_odd_values(weight, t - 1, OF_VALUES + behind);
+                else multiply_values(weight, OF_VALUES + behind);
+            }
+            if (weigh) {
+                if (edge(t)) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (!seen(t, i)) score[i] = NONE;
+                }
+                keep_up(score, weight);
+                exponentials(score, weight);
+            }
+            if (ask) multiply_keys(score, ahead);
+            advance();
+        }
+        if constexpr (DMA) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
     float own;
     const float other = other_half(total, own);
-    total = own + other;
-    if (row >= rows) return;
-    const float by = total == 0.f ? 0.f : 1.f / total;
-    const int64_t at = (int64_t)(p.q0 + p.first + row) * a.out.ts + head * a.out.hs;
+    const float all = own + other, by = all == 0.f ? 0.f : 1.f / all;
+    if (col >= own_rows) return;
+    const int64_t at = (int64_t)(p.q0 + p.first + row0 + col) * a.out.ts + head * a.out.hs;
 #pragma unroll
-    for (int j = 0; j < DP / 32; ++j)
+    for (int j = 0; j < DS; ++j)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const int d = 32 * j + 2 * i + 4 * half;
@@ -323,13 +437,13 @@ hlq_attn_prompt_kernel(const Prompt a)
         }
 }
 
-template <int T>
+template <int T, bool DMA>
 void launch(const Prompt &a, int64_t grid, hipStream_t st)
 {
     const dim3 g((unsigned)grid), block(64 * WAVES);
-    if (a.D <= 64) hlq_attn_prompt_kernel<T, 64><<<g, block, 0, st>>>(a);
-    else if (a.D <= 128) hlq_attn_prompt_kernel<T, 128><<<g, block, 0, st>>>(a);
-    else hlq_attn_prompt_kernel<T, 256><<<g, block, 0, st>>>(a);
+    if (a.D <= 64) hlq_attn_prompt_kernel<T, 64, DMA><<<g, block, 0, st>>>(a);
+    else if (a.D <= 128) hlq_attn_prompt_kernel<T, 128, DMA><<<g, block, 0, st>>>(a);
+    else hlq_attn_prompt_kernel<T, 256, DMA><<<g, block, 0, st>>>(a);
 }
 
 hlq_status check(int64_t Tq, int64_t Tk, int32_t B, int32_t q_heads, int32_t heads, int32_t dim)
@@ -387,14 +501,20 @@ hlq_status hlq_attn_prompt(int32_t B, int32_t q_heads, int32_t heads, int32_t di
     a.k_offsets = k_offsets;
     a.causal = causal != 0;
     a.window = window < 1 << 30 ? window : 0;   // no sequence is longer
-    a.scale = scale * 1.44269504f;
+    a.scale = scale == 0.f ? 1.f : fabsf(scale) * 1.44269504f;
+    a.sign = scale < 0.f ? -1.f : scale == 0.f ? 0.f : 1.f;
+    a.abreast = a.group % 4 == 0 ? 4 : a.group % 2 == 0 ? 2 : 1;
     // never more tiles than the queries can make, whatever the offsets hold
-    const int64_t tiles = Tq / ROWS + (Tq < B ? Tq : B), grid = tiles * q_heads;
+    const int rows = 32 * (WAVES / a.abreast);
+    const int64_t tiles = Tq / rows + (Tq < B ? Tq : B), grid = tiles * (q_heads / a.abreast);
     if (grid > ((int64_t)1 << 24) - 1) return HLQ_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 lanes
+    // loads that go to LDS by themselves: rows at multiples of 16 bytes, no nearer than their length, a tile's offsets in 31 bits
+    const auto whole = [&](const KvRows &x) { return x.ts >= dim && ((uintptr_t)x.p & 15u) == 0 && x.ts % 8 == 0 && x.hs % 8 == 0 && x.ts < 1 << 23; };
+    const bool dma = whole(a.k) && whole(a.v);
     const hipStream_t st = (hipStream_t)stream;
     hlq_clear_stale_error();
-    if (type == HLQ_F16) launch<HLQ_F16>(a, grid, st);
-    else launch<HLQ_BF16>(a, grid, st);
+    if (type == HLQ_F16) dma ? launch<HLQ_F16, true>(a, grid, st) : launch<HLQ_F16, false>(a, grid, st);
+    else dma ? launch<HLQ_BF16, true>(a, grid, st) : launch<HLQ_BF16, false>(a, grid, st);
     return hlq_hip_status(hipGetLastError());
 }
 

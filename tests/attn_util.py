@@ -3,7 +3,8 @@
 Bounds.  A score is a sum of dim exact products in fp32: with an addition off by 2^-23 of what is summed (the matrix core may cut off instead of
 rounding) it is off by at most (dim + 4) 2^-23 S, S the sum of its products' magnitudes; the two factors it is multiplied by, the difference and the
 exponential add 2^-21 (1 + |score|) <= 2^-21 (1 + S) more.  A weight is off by that relative to itself, twice (numerator and sum), and by what it is
-rounded by: `weight`.  With A the weighted sum of the values' magnitudes a result is off by at most
+rounded by, h: once if the sum is of the weights before (`weight` = h), and if the sum is of the rounded ones twice (`weight` = 2 h), since then
+sum p~ v / sum p~ - y = sum (p~ - p) (v - y) / sum p~ for the result y = sum p v / sum p, at most h (A + |y|) <= 2 h A.  With A the weighted sum of the values' magnitudes a result is off by at most
     A (2 (dim + 4) 2^-23 S + 2^-20 (1 + S) + weight + n 2^-23) + n 2^-25 max|v|,
 the last two for n additions and, in f16, for weights below its smallest normal number, and then by its own rounding."""
 import numpy as np

@@ -52,7 +52,7 @@ class Packed:
             for h in range(Hq) if heads is None else heads:
                 v = self.v[keys, h // (Hq // H)]
                 y, size, products = O.attend(self.q[rows, h], self.k[keys, h // (Hq // H)], v, s, scale)
-                e = bound(size, products[:, None], n, D, np.abs(v).max() if n_k else 0, HALF_STEP[self.dtype], self.dtype, y)
+                e = bound(size, products[:, None], n, D, np.abs(v).max() if n_k else 0, 2 * HALF_STEP[self.dtype], self.dtype, y)
                 bad = ~(np.abs(got[rows, h] - y) <= e)
                 assert not bad.any(), f"sequence {b} ({n_q}, {n_k}), head {h}: worst {np.nanmax(np.abs(got[rows, h] - y) / e):.3g} times the bound, rows {np.nonzero(bad.any(1))[0][:5]}"
                 assert (got[rows, h][~s.any(1)] == 0).all()

@@ -110,7 +110,7 @@ def test_tokens_one_by_one_are_the_prompts_rows(dtype):
         for h in range(HQ):
             s = np.tril(np.ones((layer.total[b],) * 2, bool))[n:]
             y, size, products = O.attend(host(q[n:, h]), host(k[:, h // 4]), host(v[:, h // 4]), s, np.float32(D**-0.5))
-            e = bound(size, products[:, None], layer.total[b], D, 6.0, HALF_STEP[dtype], dtype, y)
+            e = bound(size, products[:, None], layer.total[b], D, 6.0, 2 * HALF_STEP[dtype], dtype, y)
             assert (np.abs(host(whole[n:, h]) - host(got[:, h])) <= 2 * e).all()
 
 
@@ -131,7 +131,7 @@ def test_a_prompt_in_pieces_over_what_is_read_back(kind):
     keys, values = (host(x) for x in B.hlq_kv_read(layer.kv, torch.from_numpy(layer.slots(0, np.arange(n))).cuda()))
     for h in range(HQ):
         y, size, products = O.attend(host(q[:, h]), keys[:, h // 4], values[:, h // 4], np.tril(np.ones((n, n), bool)), np.float32(D**-0.5))
-        assert (np.abs(got[:, h] - y) <= bound(size, products[:, None], n, D, 8.0, HALF_STEP["bf16"], "bf16", y)).all()
+        assert (np.abs(got[:, h] - y) <= bound(size, products[:, None], n, D, 8.0, 2 * HALF_STEP["bf16"], "bf16", y)).all()
 
 
 @pytest.mark.parametrize("kind", ["bf16", "mx4"])
