@@ -17,6 +17,8 @@
 namespace {
 
 constexpr int WAVES = 4, KEYS = 32, STAGES = 3;
+constexpr int LEAST_STEPS = 8;   // of a cut
+constexpr int64_t SLOTS = 512;    // workgroups that a cut launch makes at most: two a compute unit
 constexpr float NONE = -__builtin_inff();
 
 typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
@@ -27,6 +29,9 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 struct Prompt {
     int B, H, group, D;
     int abreast;   // heads of a workgroup: 4, 2 or 1
+    int cuts;      // workgroups that a tile's keys may be cut over
+    int *arrived;
+    uint64_t *partial;
     int Tq, Tk;
     KvRows q, k, v, out;
     const int32_t *q_offsets, *k_offsets;
@@ -129,6 +134,8 @@ hlq_attn_prompt_kernel(const Prompt a)
     int id = (int)blockIdx.x;
     const int h = id % a.H;   // kv heads in turn: one each XCD where there are eight
     id /= a.H;
+    const int cut = id % a.cuts;
+    id /= a.cuts;
     const int sets = a.group / a.abreast, set = id % sets;
     const int rows = 32 * (WAVES / a.abreast);                 // queries of a workgroup
     const Place p = place_of(a, id / sets, rows);
@@ -152,8 +159,21 @@ hlq_attn_prompt_kernel(const Prompt a)
     };
     int all_begin, all_end, begin, end;
     steps_of(0, tile_rows, all_begin, all_end);
+    // this workgroup's share of them; one at least has one, which writes zeros where nothing is seen
+    int active = 1;
+    if (a.cuts > 1) {
+        const int steps = all_end - all_begin;
+        int share = (steps + a.cuts - 1) / a.cuts;
+        share = share < LEAST_STEPS ? LEAST_STEPS : share;
+        active = steps > share ? (steps + share - 1) / share : 1;
+        if (cut >= active) return;
+        all_begin += cut * share;
+        all_end = all_begin + share < all_end ? all_begin + share : all_end;
+    }
     const int own_rows = tile_rows - row0 < 0 ? 0 : tile_rows - row0 < 32 ? tile_rows - row0 : 32;
     steps_of(row0, own_rows, begin, end);
+    begin = begin < all_begin ? all_begin : begin;
+    end = end > all_end ? all_end : end;
 
     // queries, the second operand; of a negative scale they have the sign, so that the largest score has the largest product
     const int first_place = shift + p.first + row0;                     // of the wavefront's first query
@@ -422,6 +442,50 @@ hlq_attn_prompt_kernel(const Prompt a)
         }
         if constexpr (DMA) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
+    if (active > 1) {
+        // Cut: sums, and the base and total, past the XCD's own L2 (device-scope stores, complete before the arrival is counted); whoever is last adds the
+        // cuts in their order.  Bases are whole powers of two: so the sums are brought to the largest exactly.
+        constexpr int PAIRS = DS * 8 + 1;
+        const int64_t who = blockIdx.x / (a.cuts * a.H) * a.H + h;
+        uint64_t *const every = a.partial + (who * a.cuts * WAVES + wave) * (PAIRS * 64) + lane;
+        uint64_t *const mine = every + (int64_t)cut * WAVES * (PAIRS * 64);
+        const auto pair = [](float x, float y) { return as_bits(x) | (uint64_t)as_bits(y) << 32; };
+#pragma unroll
+        for (int j = 0; j < DS; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) __hip_atomic_store(mine + (j * 8 + i) * 64, pair(acc[j][2 * i], acc[j][2 * i + 1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(mine + DS * 8 * 64, pair(most == NONE ? NONE : base, total), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        int *const last = (int *)lds;
+        if (threadIdx.x == 0) *last = __hip_atomic_fetch_add(a.arrived + who, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == active - 1;
+        __syncthreads();
+        if (!*last) return;
+        if (threadIdx.x == 0) __hip_atomic_store(a.arrived + who, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const auto from = [&](int c, int i) { return __hip_atomic_load(every + ((int64_t)c * WAVES * PAIRS + i) * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+        float highest = NONE;
+        for (int c = 0; c < active; ++c) highest = fmaxf(highest, as_float((uint32_t)from(c, DS * 8)));
+        highest = highest == NONE ? 0.f : highest;
+        total = 0.f;
+#pragma unroll
+        for (int j = 0; j < DS; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
+        for (int c = 0; c < active; ++c) {
+            uint64_t in[PAIRS];
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) in[i] = from(c, i);
+            const float weight = __builtin_amdgcn_exp2f(as_float((uint32_t)in[PAIRS - 1]) - highest);
+            total = fmaf(weight, as_float((uint32_t)(in[PAIRS - 1] >> 32)), total);
+#pragma unroll
+            for (int j = 0; j < DS; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    acc[j][2 * i] = fmaf(weight, as_float((uint32_t)in[j * 8 + i]), acc[j][2 * i]);
+                    acc[j][2 * i + 1] = fmaf(weight, as_float((uint32_t)(in[j * 8 + i] >> 32)), acc[j][2 * i + 1]);
+                }
+        }
+    }
     float own;
     const float other = other_half(total, own);
     const float all = own + other, by = all == 0.f ? 0.f : 1.f / all;
@@ -446,11 +510,30 @@ void launch(const Prompt &a, int64_t grid, hipStream_t st)
     else hlq_attn_prompt_kernel<T, 256, DMA><<<g, block, 0, st>>>(a);
 }
 
-hlq_status check(int64_t Tq, int64_t Tk, int32_t B, int32_t q_heads, int32_t heads, int32_t dim)
+struct Shape {
+    int abreast, cuts;
+    int64_t workgroups;   // of a launch that is not cut
+    size_t bytes;         // of the workspace, enough for fewer rows and sequences too
+};
+hlq_status shape_of(int64_t Tq, int64_t Tk, int32_t B, int32_t q_heads, int32_t heads, int32_t dim, Shape *out)
 {
     if (Tq < 0 || Tk < 0 || B < 0 || heads < 1 || q_heads < 1 || q_heads % heads || dim < 8 || dim % 8) return HLQ_ERR_BAD_DESC;
     constexpr int64_t MOST = (int64_t)1 << 30;
-    return Tq > MOST || Tk > MOST || B > MOST || q_heads > KV_MOST_HEADS || dim > KV_MOST_DIM ? HLQ_ERR_UNSUPPORTED : HLQ_OK;
+    if (Tq > MOST || Tk > MOST || B > MOST || q_heads > KV_MOST_HEADS || dim > KV_MOST_DIM) return HLQ_ERR_UNSUPPORTED;
+    Shape s{};
+    const int group = q_heads / heads;
+    s.abreast = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
+    // never more tiles than the queries can make, whatever the offsets hold
+    const int rows = 32 * (WAVES / s.abreast);
+    s.workgroups = (Tq / rows + (Tq < B ? Tq : B)) * (q_heads / s.abreast);
+    if (s.workgroups > ((int64_t)1 << 24) - 1) return HLQ_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 lanes
+    // few queries over many keys: the keys are cut so that the card is full
+    const int64_t most = (Tk + KEYS * LEAST_STEPS - 1) / (KEYS * LEAST_STEPS), want = s.workgroups > 0 ? SLOTS / s.workgroups : 1;
+    s.cuts = (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
+    const int DP = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
+    s.bytes = HLQ_WS_COUNTER_BYTES + (most > 1 ? (size_t)SLOTS * WAVES * 64 * (DP / 4 + 1) * 8u : 0u);
+    *out = s;
+    return HLQ_OK;
 }
 
 }  // namespace
@@ -459,10 +542,11 @@ extern "C" {
 
 hlq_status hlq_attn_prompt_workspace_bytes(int64_t Tq, int64_t Tk, int32_t B, int32_t q_heads, int32_t heads, int32_t dim, size_t *bytes)
 {
-    const hlq_status s = check(Tq, Tk, B, q_heads, heads, dim);
+    Shape shape;
+    const hlq_status s = shape_of(Tq, Tk, B, q_heads, heads, dim, &shape);
     if (s != HLQ_OK) return s;
     if (!bytes) return HLQ_ERR_NULL;
-    *bytes = HLQ_WS_COUNTER_BYTES;
+    *bytes = shape.bytes;
     return HLQ_OK;
 }
 
@@ -471,7 +555,8 @@ hlq_status hlq_attn_prompt(int32_t B, int32_t q_heads, int32_t heads, int32_t di
                            const int32_t *k_offsets, int32_t causal, int32_t window, float scale, void *out, int64_t o_ts, int64_t o_hs, void *ws,
                            size_t ws_bytes, void *stream)
 {
-    hlq_status s = check(Tq, Tk, B, q_heads, heads, dim);
+    Shape shape;
+    hlq_status s = shape_of(Tq, Tk, B, q_heads, heads, dim, &shape);
     if (s != HLQ_OK) return s;
     if (type != HLQ_F16 && type != HLQ_BF16) return HLQ_ERR_UNSUPPORTED;
     if (window < 0) return HLQ_ERR_BAD_DESC;
@@ -484,8 +569,11 @@ hlq_status hlq_attn_prompt(int32_t B, int32_t q_heads, int32_t heads, int32_t di
         if ((s = hlq_check_rows(k, Tk, heads, dim, k_ts, k_hs, type, false)) != HLQ_OK) return s;
         if ((s = hlq_check_rows(v, Tk, heads, dim, v_ts, v_hs, type, false)) != HLQ_OK) return s;
     }
-    (void)ws;
-    (void)ws_bytes;
+    if (shape.cuts > 1) {
+        if (!ws) return HLQ_ERR_NULL;
+        if ((uintptr_t)ws & 15u) return HLQ_ERR_BAD_STRIDE;
+        if (ws_bytes < shape.bytes) return HLQ_ERR_BUFFER_TOO_SMALL;
+    }
     Prompt a{};
     a.B = B;
     a.H = heads;
@@ -503,11 +591,11 @@ hlq_status hlq_attn_prompt(int32_t B, int32_t q_heads, int32_t heads, int32_t di
     a.window = window < 1 << 30 ? window : 0;   // no sequence is longer
     a.scale = scale == 0.f ? 1.f : fabsf(scale) * 1.44269504f;
     a.sign = scale < 0.f ? -1.f : scale == 0.f ? 0.f : 1.f;
-    a.abreast = a.group % 4 == 0 ? 4 : a.group % 2 == 0 ? 2 : 1;
-    // never more tiles than the queries can make, whatever the offsets hold
-    const int rows = 32 * (WAVES / a.abreast);
-    const int64_t tiles = Tq / rows + (Tq < B ? Tq : B), grid = tiles * (q_heads / a.abreast);
-    if (grid > ((int64_t)1 << 24) - 1) return HLQ_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 lanes
+    a.abreast = shape.abreast;
+    a.cuts = shape.cuts;
+    a.arrived = (int *)ws;
+    a.partial = ws ? (uint64_t *)((char *)ws + HLQ_WS_COUNTER_BYTES) : nullptr;
+    const int64_t grid = shape.workgroups * shape.cuts;
     // loads that go to LDS by themselves: rows at multiples of 16 bytes, no nearer than their length, a tile's offsets in 31 bits
     const auto whole = [&](const KvRows &x) { return x.ts >= dim && ((uintptr_t)x.p & 15u) == 0 && x.ts % 8 == 0 && x.hs % 8 == 0 && x.ts < 1 << 23; };
     const bool dma = whole(a.k) && whole(a.v);
