@@ -1,6 +1,7 @@
 // Attention of one new token over the paged cache:  out = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q . k_j - m),  m the largest score.
 //
-// One pass over keys and values with the running maximum and sum (Milakov and Gimelshein's online softmax).  A wavefront has the query heads of one
+// One pass over keys and values with the running maximum and sum (Milakov and Gimelshein's online softmax); the maximum that exponentials are taken from is
+// kept while no score passes it by 2^8, and is a whole power of two: so sums are rarely multiplied, and exactly.  A wavefront has the query heads of one
 // kv head (16 of them at most) and goes through tiles of 32 tokens, all in registers:
 //   scores    two products 16 tokens x 16 heads, keys the first operand.  A lane has tokens 4 g .. 4 g + 3 of each for one head (g = lane / 16).
 //   weights   are then where the second product wants them: its sum over tokens may take them in any order, so place 8 g + e of the sum is
@@ -33,7 +34,7 @@ struct Decode {
     int width;
     const int32_t *lengths;
     int window;
-    float scale;                  // times log2(e)
+    float scale, sign;            // the scale's magnitude times log2(e) (1 if it is 0), and its sign
     KvRows out;
     int otype;
     int *arrived;
@@ -46,6 +47,14 @@ template <> struct Fragment<HLQ_F16> { using type = half8v; using scalar = _Floa
 
 __device__ __forceinline__ float4v multiply(bf8v a, bf8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ float4v multiply(half8v a, half8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// lanes 8..15 of sixteen get of b what lanes 0..7 have, and these of a what lanes 8..15 had: a of the first eight lanes and b of the last stay
+__device__ __forceinline__ void change_places(uint32_t &a, uint32_t &b)
+{
+    const uint32_t was = a;
+    a = (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)b, 0x128, 0xf, 0xc, false);
+    b = (uint32_t)__builtin_amdgcn_update_dpp((int)b, (int)was, 0x128, 0xf, 0x3, false);
+}
 
 // over the four lanes of a head
 __device__ __forceinline__ float over_lanes_max(float v)
@@ -62,6 +71,7 @@ __device__ __forceinline__ float over_lanes_sum(float v)
     s = __builtin_amdgcn_permlane16_swap(as_bits(v), as_bits(v), false, false);
     return as_float(s[0]) + as_float(s[1]);
 }
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 // what a maximum is subtracted as: where nothing was seen, or only -infinity, 0, so that no difference is NaN
 __device__ __forceinline__ float base_of(float m) { return m == NONE ? 0.f : m; }
 
@@ -69,18 +79,18 @@ constexpr int OUTSIDE = 0x7fffffff;   // an offset that every descriptor ends be
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const void *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00020000); }
 
-// N dwords (or 2 bytes: N = 0) through a descriptor.  (No scalar offset: only what is added in the lane counts in the comparison with the end.)
+// N dwords (or 2 bytes: N = 0) through a descriptor, not to be kept in the caches.  (No scalar offset: only what is added in the lane counts in the comparison with the end.)
 template <int N>
 __device__ __forceinline__ void fetch(uint32_t *to, __amdgpu_buffer_rsrc_t r, int offset)
 {
-    if constexpr (N == 0) to[0] = __builtin_amdgcn_raw_buffer_load_b16(r, offset, 0, 0);
-    else if constexpr (N == 1) to[0] = __builtin_amdgcn_raw_buffer_load_b32(r, offset, 0, 0);
+    if constexpr (N == 0) to[0] = __builtin_amdgcn_raw_buffer_load_b16(r, offset, 0, 2);
+    else if constexpr (N == 1) to[0] = __builtin_amdgcn_raw_buffer_load_b32(r, offset, 0, 2);
     else if constexpr (N == 2) {
-        const mx4_u2 v = __builtin_bit_cast(mx4_u2, __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, 0));
+        const mx4_u2 v = __builtin_bit_cast(mx4_u2, __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, 2));
         to[0] = v.x, to[1] = v.y;
     } else {
         static_assert(N == 4, "");
-        const mx4_u4 v = __builtin_bit_cast(mx4_u4, __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, 0));
+        const mx4_u4 v = __builtin_bit_cast(mx4_u4, __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, 2));
         to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w;
     }
 }
@@ -95,7 +105,7 @@ __device__ __forceinline__ uint32_t widen(uint32_t c, float scale)
 
 // C: the cache's type, T: the queries', DP: dim up to 64, 128 or 256
 template <int C, int T, int DP>
-__global__ void __launch_bounds__(64 * WAVES)
+__global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 3)
 hlq_attn_decode_kernel(const Decode a)
 {
     using F = typename Fragment<C>::type;
@@ -105,11 +115,19 @@ hlq_attn_decode_kernel(const Decode a)
     constexpr int KS = DP / 32, E = DP / 16;                       // products over dim; columns of a lane
     constexpr int TERMS = MX && T == HLQ_F16 ? 2 : 1;              // of the queries
     constexpr int PITCH = DP + 4;                                  // of a row in LDS
+    // a lane's pieces of a key (16 bytes or a quarter of a row), and their values; products of a piece; pieces of a value's row (VALUE_DWORDS 0: two bytes)
+    constexpr int KEY_DWORDS = KS * 8 / PER, KEY_PIECE = KEY_DWORDS < 4 ? KEY_DWORDS : 4, KEY_PIECES = KEY_DWORDS / KEY_PIECE, PIECE_VALUES = KEY_PIECE * PER;
+    constexpr int PRODUCTS = PIECE_VALUES / 8;
+    constexpr bool PAIRED = KEY_PIECES > 1, TWO_ROWS = C == HLQ_MX4 && DP == 128;
+    constexpr int VALUE_DWORDS = TWO_ROWS ? 2 : E / PER, VALUE_PIECE = VALUE_DWORDS < 4 ? VALUE_DWORDS : 4, VALUE_PIECES = VALUE_DWORDS ? VALUE_DWORDS / VALUE_PIECE : 1;
+    constexpr int VALUE_LOADS = TWO_ROWS ? 2 : 4;                  // of 16 tokens
+    constexpr int UNIT = 1, STEP = UNIT * TILE;           // tiles of a step: their loads are on their way together; tokens
     __shared__ __attribute__((aligned(16))) float sums[WAVES * 16 * PITCH];
     __shared__ float tops[WAVES][16], totals[WAVES][16];
 
     const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int col = lane & 15, g = lane >> 4;
+    const auto column_of = [](int lane) { return TWO_ROWS ? 16 * (lane & 7) + 8 * (lane >> 3) : E * lane; };   // the first of a lane's E columns
     int id = (int)blockIdx.x;
     const int h = id % a.kv.H;
     id /= a.kv.H;
@@ -122,13 +140,13 @@ hlq_attn_decode_kernel(const Decode a)
     int n = a.lengths[b];
     n = n < 0 ? 0 : n > room ? (int)room : n;
     const int start = a.window > 0 && n > a.window ? n - a.window : 0, first = start & ~(TILE - 1);
-    const int tiles = (n - first + TILE - 1) / TILE;
+    const int steps = (n - first + STEP - 1) / STEP;
     // workgroups that have a share, at least one, which writes the zeros of an empty sequence
-    int share = (tiles + a.cuts - 1) / a.cuts;
+    int share = (steps + a.cuts - 1) / a.cuts;
     share = (share + WAVES - 1) / WAVES * WAVES;
-    const int active = tiles > 0 ? (tiles + share - 1) / share : 1;
+    const int active = steps > 0 ? (steps + share - 1) / share : 1;
     if (cut >= active) return;
-    const int tile_end = (cut + 1) * share < tiles ? (cut + 1) * share : tiles;
+    const int step_end = (cut + 1) * share < steps ? (cut + 1) * share : steps;
 
     const int head0 = block * 16, heads = a.group - head0 < 16 ? a.group - head0 : 16;   // of this workgroup
     const int first_head = h * a.group + head0;
@@ -139,11 +157,13 @@ hlq_attn_decode_kernel(const Decode a)
         const V *q = (const V *)a.q.p + b * a.q.ts + (int64_t)(first_head + (col < heads ? col : 0)) * a.q.hs;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            const int d = MX ? KS * 8 * g + 8 * s : 32 * s + 8 * g;
+            const int d = (4 * (s / PRODUCTS) + g) * PIECE_VALUES + s % PRODUCTS * 8;
             V v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = (V)0.f;
-            if (col < heads && d < a.D) mx4_read8<false>(q + d, v);
+            if (col < heads && d < a.D && a.sign != 0.f) mx4_read8<false>(q + d, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = a.sign < 0.f ? -v[i] : v[i];   // so that the largest score has the largest product
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const S hi = (S)(float)v[i];
@@ -153,105 +173,114 @@ hlq_attn_decode_kernel(const Decode a)
         }
     }
 
-    // offsets of this lane: of a key's pieces in its row, of a value's
-    constexpr int KEY_DWORDS = KS * 8 / PER, KEY_PIECE = KEY_DWORDS < 4 ? KEY_DWORDS : 4, KEY_PIECES = KEY_DWORDS / KEY_PIECE;
-    constexpr int VALUE_DWORDS = E / PER, VALUE_PIECE = VALUE_DWORDS < 4 ? VALUE_DWORDS : 4;   // 0: two bytes
-    constexpr int VALUE_PIECES = VALUE_DWORDS ? VALUE_DWORDS / VALUE_PIECE : 1;
+    // Offsets of this lane.  Keys' rows come in eights, 128 bytes of each at a time where they are that long, so that lines are asked for whole: lanes
+    // 0..7 of sixteen have the first four pieces of rows 0..7, lanes 8..15 the next four, a second load rows 8..15; then they change places.
+    // Values: a lane's eight tokens row by row; rows of 64 bytes two at a time (TWO_ROWS), then lanes change places too.
     const int row_bytes = a.kv.row_bytes;
-    int key_at[KEY_PIECES], value_at[4][VALUE_PIECES];
+    int key_at[KEY_PIECES], value_at[VALUE_LOADS][VALUE_PIECES];
 #pragma unroll
     for (int i = 0; i < KEY_PIECES; ++i) {
-        const int d = MX ? KS * 8 * g + i * KEY_PIECE * PER : 32 * i + 8 * g;
-        key_at[i] = d < a.D ? col * row_bytes + d * 4 / PER : OUTSIDE;
+        const int row = PAIRED ? (i & 1) * 8 + (col & 7) : col, d = (PAIRED ? 8 * (i >> 1) + 4 * (col >> 3) + g : 4 * i + g) * PIECE_VALUES;
+        key_at[i] = d < a.D ? row * row_bytes + d * 4 / PER : OUTSIDE;
     }
 #pragma unroll
     for (int i = 0; i < VALUE_PIECES; ++i) {
-        const int d = E * col + i * VALUE_PIECE * PER;
+        const int d = TWO_ROWS ? 16 * (col & 7) : E * col + i * VALUE_PIECE * PER;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) value_at[e][i] = d < a.D ? (4 * g + e) * row_bytes + d * 4 / PER : OUTSIDE;
+        for (int e = 0; e < VALUE_LOADS; ++e) value_at[e][i] = d < a.D ? (4 * g + (TWO_ROWS ? 2 * e + (col >> 3) : e)) * row_bytes + d * 4 / PER : OUTSIDE;
     }
-    constexpr int KEY_SCALES = KS == 8 ? 2 : 1;
-    int key_scale_at[KEY_SCALES], value_scale_at = 0;
+    int key_scale_at[KEY_PIECES], value_scale_at = 0;
     if constexpr (MX) {
 #pragma unroll
-        for (int i = 0; i < KEY_SCALES; ++i) {
-            const int blk = KS * 8 * g / 32 + i;
+        for (int i = 0; i < KEY_PIECES; ++i) {
+            const int blk = (4 * i + g) * PIECE_VALUES / 32;
             key_scale_at[i] = blk < a.kv.blocks ? (blk << log_page) + col : OUTSIDE;
         }
-        const int blk = E * col / 32;
+        const int blk = column_of(col) / 32;
         value_scale_at = blk < a.kv.blocks ? (blk << log_page) + 4 * g : OUTSIDE;
     }
 
     // what is loaded of a tile: its two halves of 16 tokens lie in a page each
-    struct Keys { uint32_t v[2][KEY_DWORDS], scale[2][KEY_SCALES]; };
-    struct Values { uint32_t v[8][VALUE_DWORDS ? VALUE_DWORDS : 1], scale[2]; };
+    struct Keys { uint32_t v[2][KEY_DWORDS], scale[2][KEY_PIECES]; };
+    struct Values { uint32_t v[2 * VALUE_LOADS][VALUE_DWORDS ? VALUE_DWORDS : 1], scale[2]; };
+    struct Half { int page, at, bytes; };   // where its tokens begin in which page, the bytes of those up to the sequence's end
     const int32_t *const table = a.table + b * a.ld_table;
-    auto page_of = [&](int tile, int half) {
-        int tok = first + tile * TILE + 16 * half;
-        tok = tok < n ? tok : n - 1;
-        int64_t page = table[tok >> log_page];
-        page = page < 0 ? 0 : page >= a.kv.pages ? a.kv.pages - 1 : page;
-        return __builtin_amdgcn_readfirstlane((int)page);
+    auto half_of = [&](int tok, int half) {
+        tok += 16 * half;
+        const int left = n - tok;
+        int page = table[(left > 0 ? tok : n - 1) >> log_page];
+        page = page < 0 ? 0 : page >= (int)a.kv.pages ? (int)a.kv.pages - 1 : page;   // (fewer than 2^31)
+        return Half{uniform(page), uniform(tok & ((1 << log_page) - 1)), uniform((left < 0 ? 0 : left < 16 ? left : 16) * row_bytes)};
     };
-    // tokens of the half up to the sequence's end, and where the half begins in its page
-    auto inside = [&](int tile, int half) {
-        const int left = n - (first + tile * TILE + 16 * half);
-        return left <= 0 ? 0 : left < 16 ? left : 16;
-    };
-    auto begins = [&](int tile, int half) { return (first + tile * TILE + 16 * half) & ((1 << log_page) - 1); };
-    auto load_keys = [&](Keys &k, int tile, const int (&pages)[2]) {
+    // of this kv head: the keys' rows of page 0, bytes from page to page, from keys to values; the same of scale bytes
+    const uint32_t piece = (uint32_t)row_bytes << log_page, scale_piece = (uint32_t)a.kv.blocks << log_page;
+    const uint8_t *const rows0 = a.kv.codes + (uint64_t)piece * h, *const scales0 = a.kv.scales + (uint64_t)scale_piece * h;
+    const uint32_t to_values = piece * a.kv.H, page_bytes = 2 * to_values, scale_to_values = scale_piece * a.kv.H, scale_page_bytes = 2 * scale_to_values;
+    auto load_keys = [&](Keys &k, const Half (&where)[2]) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int at = begins(tile, half);
-            const auto r = descriptor(a.kv.rows(pages[half], 0, h) + at * row_bytes, inside(tile, half) * row_bytes);
+            const Half &w = where[half];
+            const auto r = descriptor(rows0 + (uint64_t)page_bytes * (uint32_t)w.page + (uint32_t)(w.at * row_bytes), w.bytes);
 #pragma unroll
             for (int i = 0; i < KEY_PIECES; ++i) fetch<KEY_PIECE>(k.v[half] + i * KEY_PIECE, r, key_at[i]);
             if constexpr (MX) {
-                const auto rs = descriptor(a.kv.bytes(pages[half], 0, h) + at, (a.kv.blocks << log_page) - at);
+                const auto rs = descriptor(scales0 + (uint64_t)scale_page_bytes * (uint32_t)w.page + (uint32_t)w.at, uniform((int)scale_piece - w.at));
 #pragma unroll
-                for (int i = 0; i < KEY_SCALES; ++i) k.scale[half][i] = __builtin_amdgcn_raw_buffer_load_b8(rs, key_scale_at[i], 0, 0);
+                for (int i = 0; i < KEY_PIECES; ++i) k.scale[half][i] = __builtin_amdgcn_raw_buffer_load_b8(rs, key_scale_at[i], 0, 0);
             }
         }
     };
-    auto load_values = [&](Values &v, int tile, const int (&pages)[2]) {
+    auto load_values = [&](Values &v, const Half (&where)[2]) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int at = begins(tile, half);
-            const auto r = descriptor(a.kv.rows(pages[half], 1, h) + at * row_bytes, inside(tile, half) * row_bytes);
+            const Half &w = where[half];
+            const auto r = descriptor(rows0 + (uint64_t)page_bytes * (uint32_t)w.page + (to_values + (uint32_t)(w.at * row_bytes)), w.bytes);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < VALUE_LOADS; ++e)
 #pragma unroll
-                for (int i = 0; i < VALUE_PIECES; ++i) fetch<VALUE_PIECE>(v.v[4 * half + e] + i * VALUE_PIECE, r, value_at[e][i]);
+                for (int i = 0; i < VALUE_PIECES; ++i) fetch<VALUE_PIECE>(v.v[VALUE_LOADS * half + e] + i * VALUE_PIECE, r, value_at[e][i]);
             if constexpr (MX) {
-                const auto rs = descriptor(a.kv.bytes(pages[half], 1, h) + at, (a.kv.blocks << log_page) - at);
+                const auto rs = descriptor(scales0 + (uint64_t)scale_page_bytes * (uint32_t)w.page + (scale_to_values + (uint32_t)w.at), uniform((int)scale_piece - w.at));
                 v.scale[half] = __builtin_amdgcn_raw_buffer_load_b32(rs, value_scale_at, 0, 0);
             }
         }
     };
 
     float4v acc[E];
-    float top = NONE, total = 0.f;
-    // lane (head, g) has columns E (4 g + i) .. of row 4 g + i
-    auto own_sums = [&](int i, int j) { return (float4v *)(sums + (wave * 16 + col) * PITCH + E * (4 * g + i) + j); };
-    auto pass = [&](bool two) {
+    float base = 0.f, most = NONE, total = 0.f;   // most: scores up to it need no new base
+    // lane (head, g) has the columns of lane 4 g + i in its row i
+    auto own_sums = [&](int i, int j) { return (float4v *)(sums + (wave * 16 + col) * PITCH + column_of(4 * g + i) + j); };
+    bool two = true, again = false;
+    for (;;) {
 #pragma unroll
         for (int j = 0; j < E; ++j) acc[j] = (float4v){0.f, 0.f, 0.f, 0.f};
-        top = NONE, total = 0.f;
-        int tile = cut * share + wave;
-        if (tile < tile_end) {
-            Keys keys;
-            Values values;
-            int pages[2] = {page_of(tile, 0), page_of(tile, 1)};
-            load_keys(keys, tile, pages);
-            load_values(values, tile, pages);
+        base = 0.f, most = NONE, total = 0.f;
+        int step = cut * share + wave;
+        if (step < step_end) {
+            Keys loaded_keys[UNIT];
+            Values loaded_values[UNIT];
+            Half where[UNIT][2];
+            auto look_up = [&](int step) {
+#pragma unroll
+                for (int u = 0; u < UNIT; ++u)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) where[u][half] = half_of(first + step * STEP + u * TILE, half);
+            };
+            look_up(step);
+#pragma unroll
+            for (int u = 0; u < UNIT; ++u) {
+                load_keys(loaded_keys[u], where[u]);
+                load_values(loaded_values[u], where[u]);
+            }
             for (;;) {
-                const int next = tile + WAVES;
-                const bool more = next < tile_end;
-                if (more) {
-                    pages[0] = page_of(next, 0);
-                    pages[1] = page_of(next, 1);
-                }
-                const int tok0 = first + tile * TILE;
+                const int next = step + WAVES;
+                const bool more = next < step_end;
+                if (more) look_up(next);
+#pragma unroll
+                for (int u = 0; u < UNIT; ++u) {
+                Keys &keys = loaded_keys[u];
+                Values &values = loaded_values[u];
+                const int tok0 = first + step * STEP + u * TILE;
                 const bool part = tok0 < start || tok0 + TILE > n;   // some tokens are not to be seen
 
                 // scores
@@ -259,15 +288,20 @@ hlq_attn_decode_kernel(const Decode a)
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     float4v s = {0.f, 0.f, 0.f, 0.f};
+                    if constexpr (PAIRED)
+#pragma unroll
+                        for (int i = 0; i < KEY_DWORDS; i += 8)
+#pragma unroll
+                            for (int w = i; w < i + 4; ++w) change_places(keys.v[half][w], keys.v[half][w + 4]);
 #pragma unroll
                     for (int i = 0; i < KS; ++i) {
                         mx4_u4 w;
                         if constexpr (C == HLQ_MX4) {
-                            const float scale = as_float(keys.scale[half][i * KEY_SCALES / KS] << 23);
+                            const float scale = as_float(keys.scale[half][i / PRODUCTS] << 23);
                             const uint32_t c = keys.v[half][i];
                             w = (mx4_u4){widen<C, 0>(c, scale), widen<C, 1>(c, scale), widen<C, 2>(c, scale), widen<C, 3>(c, scale)};
                         } else if constexpr (C == HLQ_MX8) {
-                            const float scale = as_float(keys.scale[half][i * KEY_SCALES / KS] << 23);
+                            const float scale = as_float(keys.scale[half][i / PRODUCTS] << 23);
                             const uint32_t c = keys.v[half][2 * i], d = keys.v[half][2 * i + 1];
                             w = (mx4_u4){widen<C, 0>(c, scale), widen<C, 1>(c, scale), widen<C, 0>(d, scale), widen<C, 1>(d, scale)};
                         } else
@@ -277,9 +311,9 @@ hlq_attn_decode_kernel(const Decode a)
                         for (int t = 0; t < TERMS; ++t) s = multiply(k, query[t][i], s);
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[4 * half + e] = s[e] * a.scale;
+                    for (int e = 0; e < 4; ++e) x[4 * half + e] = s[e];
                 }
-                if (more) load_keys(keys, next, pages);
+                if (more) load_keys(keys, where[u]);
                 if (part) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -287,22 +321,26 @@ hlq_attn_decode_kernel(const Decode a)
                         if (tok < start || tok >= n) x[e] = NONE;
                     }
                 }
-                float m = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-                m = fmaxf(top, over_lanes_max(m));
-                const float base = base_of(m);
-                if (__any(m > top)) {
-                    const float keep = __builtin_amdgcn_exp2f(top - base);
+                float m = x[0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) m = fmaxf(m, x[e]);
+                m = over_lanes_max(m) * a.scale;
+                if (__builtin_expect(__any(m > most), 0)) {
+                    const bool now = m > most;
+                    const float to = now ? ceilf(m) : base;
+                    const float keep = !now ? 1.f : most == NONE ? 0.f : __builtin_amdgcn_exp2f(base - to);
+                    base = to;
+                    most = now ? to + 8.f : most;
                     total *= keep;
 #pragma unroll
                     for (int j = 0; j < E; ++j)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) acc[j][i] *= keep;
-                    top = m;
                 }
                 F p, rest;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float w = __builtin_amdgcn_exp2f(x[e] - base);
+                    const float w = __builtin_amdgcn_exp2f(fmaf(x[e], a.scale, -base));
                     total += w;
                     p[e] = (S)w;
                     rest[e] = (S)(w - (float)p[e]);
@@ -310,6 +348,9 @@ hlq_attn_decode_kernel(const Decode a)
 
                 // values, two tokens' of one column in a register
                 uint32_t rows[8][E / 2];
+                if constexpr (TWO_ROWS)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) change_places(values.v[e][0], values.v[e][1]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     if constexpr (MX) {
@@ -318,7 +359,7 @@ hlq_attn_decode_kernel(const Decode a)
                         const float scale = as_float((e & 3) == 3 ? four >> 1 : four << (23 - 8 * (e & 3)));
 #pragma unroll
                         for (int i = 0; i < E / 2; ++i) {
-                            const uint32_t c = values.v[e][i * 2 / PER];
+                            const uint32_t c = TWO_ROWS ? values.v[e >> 1][e & 1] : values.v[e][i * 2 / PER];
                             if constexpr (C == HLQ_MX4) rows[e][i] = i % 4 == 0 ? widen<C, 0>(c, scale) : i % 4 == 1 ? widen<C, 1>(c, scale) : i % 4 == 2 ? widen<C, 2>(c, scale) : widen<C, 3>(c, scale);
                             else rows[e][i] = i % 2 == 0 ? widen<C, 0>(c, scale) : widen<C, 1>(c, scale);
                         }
@@ -340,39 +381,34 @@ hlq_attn_decode_kernel(const Decode a)
                         }
                     }
                 }
-                F turned[E];
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
                     const uint32_t pick = j & 1 ? 0x07060302u : 0x05040100u;
                     const mx4_u4 w = {__builtin_amdgcn_perm(rows[1][j >> 1], rows[0][j >> 1], pick), __builtin_amdgcn_perm(rows[3][j >> 1], rows[2][j >> 1], pick),
                                       __builtin_amdgcn_perm(rows[5][j >> 1], rows[4][j >> 1], pick), __builtin_amdgcn_perm(rows[7][j >> 1], rows[6][j >> 1], pick)};
-                    turned[j] = __builtin_bit_cast(F, w);
+                    const F turned = __builtin_bit_cast(F, w);
+                    acc[j] = multiply(turned, p, acc[j]);
+                    if (two) acc[j] = multiply(turned, rest, acc[j]);
                 }
-                if (more) load_values(values, next, pages);
-#pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    acc[j] = multiply(turned[j], p, acc[j]);
-                    if (two) acc[j] = multiply(turned[j], rest, acc[j]);
+                if (more) load_values(values, where[u]);
                 }
                 if (!more) break;
-                tile = next;
+                step = next;
             }
         }
-    };
-    pass(true);
-    // An infinite value times a second term, which may be 0 or below it, is NaN: where a sum is NaN, the first terms alone are its result.
-    bool nan = false;
+        // An infinite value times a second term, which may be 0 or below it, is NaN: where a sum is NaN, the first terms alone are its result.
+        bool nan = false;
 #pragma unroll
-    for (int j = 0; j < E; ++j)
+        for (int j = 0; j < E; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) nan = nan || acc[j][i] != acc[j][i];
-    const bool again = __any(nan);
-    if (again) {
+            for (int i = 0; i < 4; ++i) nan = nan || acc[j][i] != acc[j][i];
+        if (!two || !__any(nan)) break;
+        again = true;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < E; j += 4) *own_sums(i, j) = (float4v){acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]};
-        pass(false);
+        two = false;
     }
     total = over_lanes_sum(total);
 
@@ -390,7 +426,7 @@ hlq_attn_decode_kernel(const Decode a)
             *own_sums(i, j) = v;
         }
     if (g == 0) {
-        tops[wave][col] = top;
+        tops[wave][col] = most == NONE ? NONE : base;
         totals[wave][col] = total;
     }
     __syncthreads();
@@ -500,22 +536,24 @@ hlq_attn_decode_kernel(const Decode a)
     }
 }
 
-// How a launch is cut.  Workgroups of up to 1024 tokens each, so that long sequences do not end alone, where that is not more than 16384 workgroups;
-// and 2048 of them if there are tokens for that, 128 each at least; 128 cuts at most, and none where the counters do not suffice.
-constexpr int64_t WANTED = 2048, MOST_WORKGROUPS = 16384, MOST_TOKENS = 1024, LEAST_TOKENS = 128, MOST_CUTS = 128;
+// How a launch is cut.  One round of the card, three workgroups a compute unit, if there are tokens for that, 128 a workgroup at least; and workgroups of 512 KB of
+// keys and values at most (1024 tokens at least), so that long sequences do not end alone, where that is not more than 16384 of them.  128 cuts at most, and none
+// where the counters do not suffice.  (Two sequences of 131072 tokens in 4 bits: 2048 workgroups 79 us, 768 58; 64 of 0 .. 8191 in 16 bits: workgroups
+// of 512, 1024, 2048 tokens 223, 215, 217.)
+constexpr int64_t WANTED = 768, MOST_WORKGROUPS = 16384, MOST_BYTES = 512 << 10, LEAST_TOKENS = 128, MOST_CUTS = 128;
 struct Cuts {
     int cuts;
     size_t room;   // partial results in the workspace, enough for fewer sequences and narrower tables too
 };
-Cuts cuts_of(int64_t workgroups, int64_t tokens)
+Cuts cuts_of(int64_t workgroups, int64_t tokens, int row_bytes)
 {
     if (workgroups < 1 || workgroups > HLQ_WS_ARRIVAL_COUNTERS || tokens <= LEAST_TOKENS) return {1, 0};
     const auto up = [](int64_t n, int64_t by) { return (n + by - 1) / by; };
     const auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
     const auto most = [](int64_t a, int64_t b) { return a < b ? b : a; };
-    const int64_t cuts = least(most(up(WANTED, workgroups), least(up(tokens, MOST_TOKENS), MOST_WORKGROUPS / workgroups)), least(up(tokens, LEAST_TOKENS), MOST_CUTS));
-    const int64_t room = least(most(WANTED + workgroups, least(workgroups * up(tokens, MOST_TOKENS), MOST_WORKGROUPS + workgroups)),
-                               workgroups * least(up(tokens, LEAST_TOKENS), MOST_CUTS));
+    const int64_t share = most(1024, MOST_BYTES / (2 * row_bytes)), possible = least(up(tokens, LEAST_TOKENS), MOST_CUTS);
+    const int64_t cuts = least(most(most(WANTED / workgroups, 1), least(up(tokens, share), MOST_WORKGROUPS / workgroups)), possible);
+    const int64_t room = least(most(WANTED + workgroups, least(workgroups * up(tokens, share), MOST_WORKGROUPS + workgroups)), workgroups * possible);
     return {(int)cuts, (size_t)room};
 }
 int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
@@ -538,7 +576,7 @@ hlq_status shape_of(const hlq_kv_desc *c, int32_t q_heads, int64_t B, int32_t wi
     const int64_t tokens = (int64_t)width << s.d.log_page;
     if (B > ((int64_t)1 << 24) / (s.d.H * s.blocks) || tokens > 0x7fffffe0) return HLQ_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 lanes
     s.workgroups = B * s.d.H * s.blocks;
-    const Cuts k = cuts_of(s.workgroups, tokens);
+    const Cuts k = cuts_of(s.workgroups, tokens, s.d.row_bytes);
     s.cuts = k.cuts;
     s.bytes = HLQ_WS_COUNTER_BYTES + k.room * (size_t)((s.group < 16 ? s.group : 16) * (padded(s.d.D) + 2)) * sizeof(float);
     s.bytes = (s.bytes + 255u) & ~(size_t)255u;
@@ -605,7 +643,8 @@ hlq_status hlq_attn_decode(const hlq_kv_desc *c, const void *cache, size_t cache
     a.width = table_width;
     a.lengths = lengths;
     a.window = window;
-    a.scale = scale * 1.44269504f;
+    a.scale = scale == 0.f ? 1.f : fabsf(scale) * 1.44269504f;
+    a.sign = scale < 0.f ? -1.f : scale == 0.f ? 0.f : 1.f;
     a.out = KvRows{out, o_ts, o_hs};
     a.otype = otype;
     a.arrived = (int *)ws;
