@@ -825,7 +825,7 @@ class KvCache:
     """A paged cache of keys and values in the library's layout: `pages` pages of `page` tokens for each of `heads` heads of `dim` values, as torch.float16,
     torch.bfloat16, HLQ_MX8 or HLQ_MX4.  A token's slot is page number * page + its place in the page."""
 
-    __slots__ = ("blob", "pages", "page", "heads", "dim", "type", "_desc", "_need", "_device")
+    __slots__ = ("blob", "pages", "page", "heads", "dim", "type", "_desc", "_need", "_device", "_rows")
 
     def __init__(self, blob, pages: int, page: int, heads: int, dim: int, dtype=None):
         desc = HlqKvDesc(int(pages), int(page), int(heads), int(dim), _kv_type(torch.float16 if dtype is None else dtype))
@@ -833,7 +833,7 @@ class KvCache:
         if blob.dtype != torch.uint8 or blob.numel() < need or not blob.is_contiguous():
             raise ValueError(f"a contiguous blob of {need} bytes is needed, got {blob.dtype} {tuple(blob.shape)}")
         for name, value in (("blob", blob), ("pages", desc.pages), ("page", desc.page_tokens), ("heads", desc.heads), ("dim", desc.dim), ("type", desc.type),
-                            ("_desc", desc), ("_need", need), ("_device", blob.get_device())):
+                            ("_desc", desc), ("_need", need), ("_device", blob.get_device()), ("_rows", None)):
             object.__setattr__(self, name, value)
 
     def __setattr__(self, name, value):
@@ -846,8 +846,10 @@ class KvCache:
         """A 16-bit cache as an array [pages, 2 (keys, values), heads, tokens of a page, dim] over the same memory."""
         if self.type not in (HLQ_F16, HLQ_BF16):
             raise ValueError("the values of an 8- or 4-bit cache are read by hlq_kv_read")
-        kept = self.blob.reshape(-1)[:self._need].view(torch.float16 if self.type == HLQ_F16 else torch.bfloat16)
-        return kept.view(self.pages, 2, self.heads, self.page, self.dim)
+        if self._rows is None or self._rows.data_ptr() != self.blob.data_ptr():   # the blob's memory may have been replaced
+            kept = self.blob.reshape(-1)[:self._need].view(torch.float16 if self.type == HLQ_F16 else torch.bfloat16)
+            object.__setattr__(self, "_rows", kept.view(self.pages, 2, self.heads, self.page, self.dim))
+        return self._rows
 
     def __reduce__(self):
         return _kv_cache_of, (self.blob, self.pages, self.page, self.heads, self.dim, self.type)

@@ -479,6 +479,19 @@ hlq_attn_decode_kernel(const Decode a)
     __syncthreads();
     if (!*last) return;
     if (threadIdx.x == 0) __hip_atomic_store(a.arrived + who, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // the sums of eight cuts at a time; the first of them are on their way while the weights are made
+    uint64_t pair[8][2];
+    auto fetch_sums = [&](int it, int c0) {
+        const uint64_t *from = (const uint64_t *)(partial + it / (DP / 4) * DP + it % (DP / 4) * 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = c0 + i < active ? c0 + i : c0;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) pair[i][e] = __hip_atomic_load(from + c * (size / 2) + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    };
+    const int items = heads * (DP / 4);
+    if ((int)threadIdx.x < items) fetch_sums((int)threadIdx.x, 0);
     float *const weights = sums, *const shares = sums + 16 * 128;   // [head][cut], then 1 / total of each head
     for (int head = wave; head < heads; head += WAVES) {
         float m[2], all[2];
@@ -507,18 +520,11 @@ hlq_attn_decode_kernel(const Decode a)
         if (lane == 0) shares[head] = sum == 0.f ? 0.f : 1.f / sum;
     }
     __syncthreads();
-    for (int it = (int)threadIdx.x; it < heads * (DP / 4); it += 64 * WAVES) {
+    for (int it = (int)threadIdx.x; it < items; it += 64 * WAVES) {
         const int head = it / (DP / 4), d = it % (DP / 4) * 4;
-        const uint64_t *from = (const uint64_t *)(partial + head * DP + d);
         float4v sum = {0.f, 0.f, 0.f, 0.f};
         for (int c0 = 0; c0 < active; c0 += 8) {
-            uint64_t pair[8][2];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int c = c0 + i < active ? c0 + i : c0;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) pair[i][e] = __hip_atomic_load(from + c * (size / 2) + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
+            if (c0 > 0 || it != (int)threadIdx.x) fetch_sums(it, c0);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (c0 + i < active) {

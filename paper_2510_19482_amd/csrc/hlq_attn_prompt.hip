@@ -80,14 +80,22 @@ __device__ __forceinline__ Place place_of(const Prompt &a, int tile, int rows)
     const int lane = (int)(threadIdx.x & 63u);
     // offsets are device data: whatever they hold, rows stay inside
     auto offset = [](const int32_t *o, int i, int most) { const int v = o[i]; return v < 0 ? 0 : v > most ? most : v; };
+    if (a.B == 1) {
+        const int lo = offset(a.q_offsets, 0, a.Tq), n = offset(a.q_offsets, 1, a.Tq) - lo, k0 = offset(a.k_offsets, 0, a.Tk), n_k = offset(a.k_offsets, 1, a.Tk) - k0;
+        const int first = ((n < 0 ? 0 : n) - 1) / rows * rows - tile * rows;
+        return {lo, n > 0 && first >= 0 ? n : 0, k0, n_k < 0 ? 0 : n_k, first};
+    }
     int before = 0;
     for (int at = 0; at < a.B; at += 64) {
         const int b = at + lane;
-        int lo = 0, n = 0;
+        int lo = 0, n = 0, k0 = 0, n_k = 0;
         if (b < a.B) {
             lo = offset(a.q_offsets, b, a.Tq);
             n = offset(a.q_offsets, b + 1, a.Tq) - lo;
+            k0 = offset(a.k_offsets, b, a.Tk);
+            n_k = offset(a.k_offsets, b + 1, a.Tk) - k0;
             n = n < 0 ? 0 : n;
+            n_k = n_k < 0 ? 0 : n_k;
         }
         const int mine = n / rows + (n % rows > 0);
         int upto = mine;
@@ -99,17 +107,9 @@ __device__ __forceinline__ Place place_of(const Prompt &a, int tile, int rows)
         const int all = __builtin_amdgcn_readlane(upto, 63);
         if (tile - before < all) {
             const int f = (int)__builtin_ctzll(__ballot(upto > tile - before));
-            Place p;
-            p.q0 = __builtin_amdgcn_readlane(lo, f);
-            p.n_q = __builtin_amdgcn_readlane(n, f);
-            const int past = __builtin_amdgcn_readlane(upto, f);
             // of a sequence the last tile first: it sees most keys
-            p.first = (past - 1 - (tile - before)) * rows;
-            p.k0 = offset(a.k_offsets, at + f, a.Tk);
-            const int n_k = offset(a.k_offsets, at + f + 1, a.Tk) - p.k0;
-            p.n_k = __builtin_amdgcn_readfirstlane(n_k < 0 ? 0 : n_k);
-            p.k0 = __builtin_amdgcn_readfirstlane(p.k0);
-            return p;
+            return {__builtin_amdgcn_readlane(lo, f), __builtin_amdgcn_readlane(n, f), __builtin_amdgcn_readlane(k0, f), __builtin_amdgcn_readlane(n_k, f),
+                    (__builtin_amdgcn_readlane(upto, f) - 1 - (tile - before)) * rows};
         }
         before += all;
     }
@@ -118,7 +118,7 @@ __device__ __forceinline__ Place place_of(const Prompt &a, int tile, int rows)
 
 // DMA: rows of keys and values begin at multiples of 16 bytes
 template <int T, int DP, bool DMA>
-__global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2)
+__global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : DP > 64 ? 2 : 3)
 hlq_attn_prompt_kernel(const Prompt a)
 {
     using F = typename Fragment<T>::type;
@@ -179,16 +179,17 @@ hlq_attn_prompt_kernel(const Prompt a)
     const int first_place = shift + p.first + row0;                     // of the wavefront's first query
     F query[KS];
     {
-        const bool there = col < own_rows;
-        const S *q = (const S *)a.q.p + (int64_t)(p.q0 + p.first + (there ? row0 + col : 0)) * a.q.ts + head * a.q.hs;
+        const S *q = (const S *)a.q.p + (int64_t)(p.q0 + p.first + row0 + (col < own_rows ? col : 0)) * a.q.ts + head * a.q.hs + 8 * half;
+        if (col < own_rows && a.sign != 0.f && a.D == DP) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            S v[8];
+            for (int s = 0; s < KS; ++s) query[s] = __builtin_bit_cast(F, *(const mx4_u4_any *)(q + 16 * s));
+        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = (S)0.f;
-            if (there && a.sign != 0.f && 16 * s + 8 * half < a.D) mx4_read8<false>(q + 16 * s + 8 * half, v);
+            for (int s = 0; s < KS; ++s) query[s] = __builtin_bit_cast(F, col < own_rows && a.sign != 0.f && 16 * s + 8 * half < a.D ? *(const mx4_u4_any *)(q + 16 * s) : (mx4_u4){0u, 0u, 0u, 0u});
+        }
+        if (a.sign < 0.f) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) query[s][i] = a.sign < 0.f ? -v[i] : v[i];
+            for (int s = 0; s < KS; ++s) query[s] = __builtin_bit_cast(F, __builtin_bit_cast(mx4_u4, query[s]) ^ 0x80008000u);
         }
     }
 
@@ -273,10 +274,14 @@ hlq_attn_prompt_kernel(const Prompt a)
     full_end = full_end < 0 ? 0 : full_end / KEYS;
     const int full_begin = a.window > 0 && last_place >= a.window ? (last_place - a.window) / KEYS + 1 : 0;
     auto edge = [&](int step) { return step < full_begin || step >= full_end; };
-    auto seen = [&](int step, int i) {
-        const int key = step * KEYS + 8 * (i >> 2) + 4 * half + (i & 3), place = first_place + col;
-        return key < p.n_k && (!a.causal || key <= place) && (a.window == 0 || key > place - a.window);
+    // the keys that this lane's query sees; of a step the lane's keys are 4 half + offset_of(i)
+    const int place = first_place + col, last_seen = a.causal && place < p.n_k ? place : p.n_k - 1, first_seen = a.window > 0 ? place - a.window + 1 : 0;
+    const auto offset_of = [](int i) { return 8 * (i >> 2) + (i & 3); };
+    struct Seen {
+        int first, last;   // offsets
+        __device__ __forceinline__ bool operator()(int offset) const { return offset <= last && offset >= first; }
     };
+    auto seen_of = [&](int step) { return Seen{first_seen - step * KEYS - 4 * half, last_seen - step * KEYS - 4 * half}; };
 
     auto multiply_keys = [&](float16v &score, uint32_t slot) {
 #pragma unroll
@@ -293,8 +298,9 @@ hlq_attn_prompt_kernel(const Prompt a)
     // values that are numbers as above; +infinity, and -infinity, and NaN as both, once for each query that sees one
     auto multiply_odd_values = [&](const F (&weight)[2], int step, uint32_t slot) {
         F sees[2];
+        const Seen seen = seen_of(step);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sees[i >> 3][i & 7] = (S)(seen(step, i) ? 1.f : 0.f);
+        for (int i = 0; i < 16; ++i) sees[i >> 3][i & 7] = (S)(seen(offset_of(i)) ? 1.f : 0.f);
 #pragma unroll
         for (int j = 0; j < DS; ++j) {
 #pragma unroll
@@ -430,9 +436,10 @@ hlq_attn_prompt_kernel(const Prompt a)
             }
             if (weigh) {
                 if (edge(t)) {
+                    const Seen seen = seen_of(t);
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (!seen(t, i)) score[i] = NONE;
+                        if (!seen(offset_of(i))) score[i] = NONE;
                 }
                 keep_up(score, weight);
                 exponentials(score, weight);
@@ -472,33 +479,41 @@ hlq_attn_prompt_kernel(const Prompt a)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
         for (int c = 0; c < active; ++c) {
-            uint64_t in[PAIRS];
+            const uint64_t of = from(c, PAIRS - 1);
+            const float weight = __builtin_amdgcn_exp2f(as_float((uint32_t)of) - highest);
+            total = fmaf(weight, as_float((uint32_t)(of >> 32)), total);
+            constexpr int AT_ONCE = DS < 4 ? DS : 4;   // of 32 columns, on their way together
 #pragma unroll
-            for (int i = 0; i < PAIRS; ++i) in[i] = from(c, i);
-            const float weight = __builtin_amdgcn_exp2f(as_float((uint32_t)in[PAIRS - 1]) - highest);
-            total = fmaf(weight, as_float((uint32_t)(in[PAIRS - 1] >> 32)), total);
+            for (int j0 = 0; j0 < DS; j0 += AT_ONCE) {
+                uint64_t in[AT_ONCE * 8];
 #pragma unroll
-            for (int j = 0; j < DS; ++j)
+                for (int i = 0; i < AT_ONCE * 8; ++i) in[i] = from(c, j0 * 8 + i);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    acc[j][2 * i] = fmaf(weight, as_float((uint32_t)in[j * 8 + i]), acc[j][2 * i]);
-                    acc[j][2 * i + 1] = fmaf(weight, as_float((uint32_t)(in[j * 8 + i] >> 32)), acc[j][2 * i + 1]);
+                for (int i = 0; i < AT_ONCE * 8; ++i) {
+                    float16v &sum = acc[j0 + i / 8];
+                    sum[2 * (i % 8)] = fmaf(weight, as_float((uint32_t)in[i]), sum[2 * (i % 8)]);
+                    sum[2 * (i % 8) + 1] = fmaf(weight, as_float((uint32_t)(in[i] >> 32)), sum[2 * (i % 8) + 1]);
                 }
+            }
         }
     }
     float own;
     const float other = other_half(total, own);
     const float all = own + other, by = all == 0.f ? 0.f : 1.f / all;
     if (col >= own_rows) return;
-    const int64_t at = (int64_t)(p.q0 + p.first + row0 + col) * a.out.ts + head * a.out.hs;
+    S *const out = (S *)a.out.p + (int64_t)(p.q0 + p.first + row0 + col) * a.out.ts + head * a.out.hs + 4 * half;
+    auto leave = [&](auto Whole) {
 #pragma unroll
-    for (int j = 0; j < DS; ++j)
+        for (int j = 0; j < DS; ++j)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const int d = 32 * j + 2 * i + 4 * half;
-            const float v4[4] = {acc[j][i] * by, acc[j][i + 1] * by, acc[j][i + 2] * by, acc[j][i + 3] * by};
-            if (d < a.D) mx4_store4(a.out.p, T, at + d, v4, 4);
-        }
+            for (int i = 0; i < 16; i += 4) {
+                const int d = 32 * j + 2 * i;
+                const float v4[4] = {acc[j][i] * by, acc[j][i + 1] * by, acc[j][i + 2] * by, acc[j][i + 3] * by};
+                if (decltype(Whole)::value || d + 4 * half < a.D) mx4_store4(out, T, d, v4, 4);
+            }
+    };
+    if (a.D == DP) leave(std::true_type{});
+    else leave(std::false_type{});
 }
 
 template <int T, bool DMA>
