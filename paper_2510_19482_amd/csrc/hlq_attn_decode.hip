@@ -543,10 +543,11 @@ hlq_attn_decode_kernel(const Decode a)
 }
 
 // How a launch is cut.  One round of the card, three workgroups a compute unit, if there are tokens for that, 128 a workgroup at least; and workgroups of 512 KB of
-// keys and values at most (1024 tokens at least), so that long sequences do not end alone, where that is not more than 16384 of them.  128 cuts at most, and none
-// where the counters do not suffice.  (Two sequences of 131072 tokens in 4 bits: 2048 workgroups 79 us, 768 58; 64 of 0 .. 8191 in 16 bits: workgroups
-// of 512, 1024, 2048 tokens 223, 215, 217.)
-constexpr int64_t WANTED = 768, MOST_WORKGROUPS = 16384, MOST_BYTES = 512 << 10, LEAST_TOKENS = 128, MOST_CUTS = 128;
+// keys and values at most (1024 tokens at least), so that long sequences do not end alone, where that is not more than 16384 of them.  (Two sequences of
+// 131072 tokens in 4 bits: 2048 workgroups 79 us, 768 58; 64 of 0 .. 8191 in 16 bits: workgroups of 512, 1024, 2048 tokens 223, 215, 217.)  As the last workgroup of a
+// sequence adds its cuts, they are no more than the root of a sixteenth of the tokens unless a quarter of the card would be empty (one sequence, 8 heads: 1000 tokens 8,
+// 4, 2 cuts 8.7, 9.5, 11.7 us; 4000 tokens 32, 16, 8 cuts 12.9, 11.6, 12.8; 16000 tokens 63, 32 cuts 22.0, 18.2).  128 cuts at most, none where the counters do not suffice.
+constexpr int64_t WANTED = 768, FILLED = 192, MOST_WORKGROUPS = 16384, MOST_BYTES = 512 << 10, LEAST_TOKENS = 128, MOST_CUTS = 128;
 struct Cuts {
     int cuts;
     size_t room;   // partial results in the workspace, enough for fewer sequences and narrower tables too
@@ -557,8 +558,11 @@ Cuts cuts_of(int64_t workgroups, int64_t tokens, int row_bytes)
     const auto up = [](int64_t n, int64_t by) { return (n + by - 1) / by; };
     const auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
     const auto most = [](int64_t a, int64_t b) { return a < b ? b : a; };
+    int64_t root = 8;
+    while (root < MOST_CUTS && root * root * 16 < tokens) ++root;
     const int64_t share = most(1024, MOST_BYTES / (2 * row_bytes)), possible = least(up(tokens, LEAST_TOKENS), MOST_CUTS);
-    const int64_t cuts = least(most(most(WANTED / workgroups, 1), least(up(tokens, share), MOST_WORKGROUPS / workgroups)), possible);
+    const int64_t round = least(most(WANTED / workgroups, 1), most(root, FILLED / workgroups));
+    const int64_t cuts = least(most(round, least(up(tokens, share), MOST_WORKGROUPS / workgroups)), possible);
     const int64_t room = least(most(WANTED + workgroups, least(workgroups * up(tokens, share), MOST_WORKGROUPS + workgroups)), workgroups * possible);
     return {(int)cuts, (size_t)room};
 }
