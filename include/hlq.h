@@ -379,7 +379,7 @@ HLQ_API hlq_status hlq_expert_combine(int64_t T, int32_t k, int32_t D, int64_t R
  * Rows of heads: an array [T, heads, dim] whose last axis is contiguous; the other two have strides in elements, `ts` (from token to
  * token) and `hs` (from head to head), so that q, k and v may be parts of one projection's rows, or stand head by head.  Strides are 0 or
  * more, any alignment of the type; an output's rows may not overlap each other.  Types f16, bf16 and f32 (attention: f16 and bf16).
- * Limits: dim a multiple of 8 up to 256, heads <= 1024, T < 2^31.  The conventions at the top of this file hold. */
+ * Limits: dim a multiple of 8 up to 256, heads <= 1024, T < 2^31 (prompts: < 2^30).  The conventions at the top of this file hold. */
 
 /* Rotary positions: of each head's first `dims` values (even, at most dim) pairs are turned by position * frequency,
  *     (a, b) -> magnitude * (a cos - b sin, b cos + a sin),

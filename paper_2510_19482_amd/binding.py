@@ -773,6 +773,13 @@ def rotary_frequencies(dims: int, base: float = 10000.0, factor: float = 1.0, tr
     return [f * (r + (1 - r) / factor) for f, r in zip(out, as_is)]
 
 
+def _i32s(**numbers) -> None:
+    """Refuses what the library's 32-bit arguments would cut."""
+    for name, n in numbers.items():
+        if not -(1 << 31) <= n < 1 << 31:
+            raise ValueError(f"{name} {n} does not fit 32 bits")
+
+
 class Rotary:
     """Rotary positions: frequencies (radians a position) of the pairs among each head's first 2 * len(frequencies) values, halves or (interleaved)
     neighbours; `magnitude` multiplies what is turned.  On one device."""
@@ -817,8 +824,10 @@ def hlq_rotary(x, positions, rotary: Rotary, out=None, stream=None):
     return out
 
 
-def _kv_type(dtype) -> int:
-    return dtype if type(dtype) is int else _DTYPES.get(dtype, -1)
+def _kv_desc(pages: int, page: int, heads: int, dim: int, dtype) -> HlqKvDesc:
+    kept = dtype if type(dtype) is int else _DTYPES.get(dtype, -1)
+    _i32s(page=page, heads=heads, dim=dim, dtype=kept)
+    return HlqKvDesc(int(pages), int(page), int(heads), int(dim), kept)
 
 
 class KvCache:
@@ -828,7 +837,7 @@ class KvCache:
     __slots__ = ("blob", "pages", "page", "heads", "dim", "type", "_desc", "_need", "_device", "_rows")
 
     def __init__(self, blob, pages: int, page: int, heads: int, dim: int, dtype=None):
-        desc = HlqKvDesc(int(pages), int(page), int(heads), int(dim), _kv_type(torch.float16 if dtype is None else dtype))
+        desc = _kv_desc(pages, page, heads, dim, torch.float16 if dtype is None else dtype)
         need = _kv_bytes(desc)
         if blob.dtype != torch.uint8 or blob.numel() < need or not blob.is_contiguous():
             raise ValueError(f"a contiguous blob of {need} bytes is needed, got {blob.dtype} {tuple(blob.shape)}")
@@ -866,7 +875,7 @@ def _kv_bytes(desc: HlqKvDesc) -> int:
 
 
 def kv_bytes(pages: int, page: int, heads: int, dim: int, dtype) -> int:
-    return _kv_bytes(HlqKvDesc(pages, page, heads, dim, _kv_type(dtype)))
+    return _kv_bytes(_kv_desc(pages, page, heads, dim, dtype))
 
 
 def alloc_kv_cache(pages: int, page: int, heads: int, dim: int, dtype=None, device="cuda", stream=None) -> KvCache:
@@ -948,12 +957,14 @@ def hlq_kv_read(cache: KvCache, slots, k=None, v=None, dtype=None, stream=None):
 
 
 def decode_workspace_bytes(cache: KvCache, q_heads: int, batch: int, table_width: int) -> int:
+    _i32s(q_heads=q_heads, table_width=table_width)
     n = ctypes.c_size_t()
     _check("hlq_attn_decode_workspace_bytes", lib.hlq_attn_decode_workspace_bytes(cache._desc, q_heads, batch, table_width, ctypes.byref(n)))
     return n.value
 
 
 def prompt_workspace_bytes(q_rows: int, k_rows: int, batch: int, q_heads: int, heads: int, dim: int) -> int:
+    _i32s(batch=batch, q_heads=q_heads, heads=heads, dim=dim)
     n = ctypes.c_size_t()
     _check("hlq_attn_prompt_workspace_bytes", lib.hlq_attn_prompt_workspace_bytes(q_rows, k_rows, batch, q_heads, heads, dim, ctypes.byref(n)))
     return n.value
@@ -991,6 +1002,7 @@ def hlq_attn_decode(cache: KvCache, q, table, lengths, out=None, scale: float | 
         raise ValueError(f"q is {tuple(q.shape)}, out {tuple(out.shape)}, the cache has heads of {cache.dim}")
     if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != B or (table.shape[1] > 1 and table.stride(1) != 1):
         raise ValueError(f"table: expected int32 [{B}, pages], rows contiguous, got {table.dtype} {tuple(table.shape)}")
+    _i32s(window=window)
     width = table.shape[1]
     counts = _numbers("lengths", lengths, torch.int32, B)
     device = cache._device
@@ -1023,6 +1035,7 @@ def hlq_attn_prompt(q, k, v, q_offsets, k_offsets=None, out=None, causal: bool =
     if k_offsets is None:
         k_offsets = q_offsets
     n = q_offsets.numel()
+    _i32s(window=window)
     if n < 1:
         raise ValueError("q_offsets: one more than sequences")
     q_at, k_at = _numbers("q_offsets", q_offsets, torch.int32, n), _numbers("k_offsets", k_offsets, torch.int32, n)

@@ -1,6 +1,6 @@
 // Attention of one new token over the paged cache:  out = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q . k_j - m),  m the largest score.
 //
-// One pass over keys and values with the running maximum and sum (Milakov and Gimelshein's online softmax); the maximum that exponentials are taken from is
+// One pass over keys and values with the running maximum and sum; the maximum that exponentials are taken from is
 // kept while no score passes it by 2^8, and is a whole power of two: so sums are rarely multiplied, and exactly.  A wavefront has the query heads of one
 // kv head (16 of them at most) and goes through tiles of 32 tokens, all in registers:
 //   scores    two products 16 tokens x 16 heads, keys the first operand.  A lane has tokens 4 g .. 4 g + 3 of each for one head (g = lane / 16).
@@ -121,7 +121,6 @@ hlq_attn_decode_kernel(const Decode a)
     constexpr bool PAIRED = KEY_PIECES > 1, TWO_ROWS = C == HLQ_MX4 && DP == 128;
     constexpr int VALUE_DWORDS = TWO_ROWS ? 2 : E / PER, VALUE_PIECE = VALUE_DWORDS < 4 ? VALUE_DWORDS : 4, VALUE_PIECES = VALUE_DWORDS ? VALUE_DWORDS / VALUE_PIECE : 1;
     constexpr int VALUE_LOADS = TWO_ROWS ? 2 : 4;                  // of 16 tokens
-    constexpr int UNIT = 1, STEP = UNIT * TILE;           // tiles of a step: their loads are on their way together; tokens
     __shared__ __attribute__((aligned(16))) float sums[WAVES * 16 * PITCH];
     __shared__ float tops[WAVES][16], totals[WAVES][16];
 
@@ -140,7 +139,7 @@ hlq_attn_decode_kernel(const Decode a)
     int n = a.lengths[b];
     n = n < 0 ? 0 : n > room ? (int)room : n;
     const int start = a.window > 0 && n > a.window ? n - a.window : 0, first = start & ~(TILE - 1);
-    const int steps = (n - first + STEP - 1) / STEP;
+    const int steps = (n - first + TILE - 1) / TILE;
     // workgroups that have a share, at least one, which writes the zeros of an empty sequence
     int share = (steps + a.cuts - 1) / a.cuts;
     share = (share + WAVES - 1) / WAVES * WAVES;
@@ -168,7 +167,7 @@ hlq_attn_decode_kernel(const Decode a)
             for (int i = 0; i < 8; ++i) {
                 const S hi = (S)(float)v[i];
                 query[0][s][i] = hi;
-                if constexpr (TERMS == 2) query[1][s][i] = (S)((float)v[i] - (float)hi);
+                if constexpr (TERMS == 2) query[1][s][i] = (S)((float)v[i] == (float)hi ? 0.f : (float)v[i] - (float)hi);   // (infinities have no rest)
             }
         }
     }
@@ -257,30 +256,21 @@ hlq_attn_decode_kernel(const Decode a)
         base = 0.f, most = NONE, total = 0.f;
         int step = cut * share + wave;
         if (step < step_end) {
-            Keys loaded_keys[UNIT];
-            Values loaded_values[UNIT];
-            Half where[UNIT][2];
+            Keys keys;
+            Values values;
+            Half where[2];
             auto look_up = [&](int step) {
 #pragma unroll
-                for (int u = 0; u < UNIT; ++u)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) where[u][half] = half_of(first + step * STEP + u * TILE, half);
+                for (int half = 0; half < 2; ++half) where[half] = half_of(first + step * TILE, half);
             };
             look_up(step);
-#pragma unroll
-            for (int u = 0; u < UNIT; ++u) {
-                load_keys(loaded_keys[u], where[u]);
-                load_values(loaded_values[u], where[u]);
-            }
+            load_keys(keys, where);
+            load_values(values, where);
             for (;;) {
                 const int next = step + WAVES;
                 const bool more = next < step_end;
                 if (more) look_up(next);
-#pragma unroll
-                for (int u = 0; u < UNIT; ++u) {
-                Keys &keys = loaded_keys[u];
-                Values &values = loaded_values[u];
-                const int tok0 = first + step * STEP + u * TILE;
+                const int tok0 = first + step * TILE;
                 const bool part = tok0 < start || tok0 + TILE > n;   // some tokens are not to be seen
 
                 // scores
@@ -313,7 +303,7 @@ hlq_attn_decode_kernel(const Decode a)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[4 * half + e] = s[e];
                 }
-                if (more) load_keys(keys, where[u]);
+                if (more) load_keys(keys, where);
                 if (part) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -390,8 +380,7 @@ hlq_attn_decode_kernel(const Decode a)
                     acc[j] = multiply(turned, p, acc[j]);
                     if (two) acc[j] = multiply(turned, rest, acc[j]);
                 }
-                if (more) load_values(values, where[u]);
-                }
+                if (more) load_values(values, where);
                 if (!more) break;
                 step = next;
             }
@@ -554,7 +543,9 @@ struct Cuts {
 };
 Cuts cuts_of(int64_t workgroups, int64_t tokens, int row_bytes)
 {
-    if (workgroups < 1 || workgroups > HLQ_WS_ARRIVAL_COUNTERS || tokens <= LEAST_TOKENS) return {1, 0};
+    if (workgroups < 1 || tokens <= LEAST_TOKENS) return {1, 0};
+    const bool whole = workgroups > HLQ_WS_ARRIVAL_COUNTERS;
+    if (whole) workgroups = HLQ_WS_ARRIVAL_COUNTERS;
     const auto up = [](int64_t n, int64_t by) { return (n + by - 1) / by; };
     const auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
     const auto most = [](int64_t a, int64_t b) { return a < b ? b : a; };
@@ -564,7 +555,7 @@ Cuts cuts_of(int64_t workgroups, int64_t tokens, int row_bytes)
     const int64_t round = least(most(WANTED / workgroups, 1), most(root, FILLED / workgroups));
     const int64_t cuts = least(most(round, least(up(tokens, share), MOST_WORKGROUPS / workgroups)), possible);
     const int64_t room = least(most(WANTED + workgroups, least(workgroups * up(tokens, share), MOST_WORKGROUPS + workgroups)), workgroups * possible);
-    return {(int)cuts, (size_t)room};
+    return {whole ? 1 : (int)cuts, (size_t)room};
 }
 int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 

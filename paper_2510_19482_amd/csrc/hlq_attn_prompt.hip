@@ -534,7 +534,7 @@ hlq_status shape_of(int64_t Tq, int64_t Tk, int32_t B, int32_t q_heads, int32_t 
 {
     if (Tq < 0 || Tk < 0 || B < 0 || heads < 1 || q_heads < 1 || q_heads % heads || dim < 8 || dim % 8) return HLQ_ERR_BAD_DESC;
     constexpr int64_t MOST = (int64_t)1 << 30;
-    if (Tq > MOST || Tk > MOST || B > MOST || q_heads > KV_MOST_HEADS || dim > KV_MOST_DIM) return HLQ_ERR_UNSUPPORTED;
+    if (Tq >= MOST || Tk >= MOST || B >= MOST || q_heads > KV_MOST_HEADS || dim > KV_MOST_DIM) return HLQ_ERR_UNSUPPORTED;
     Shape s{};
     const int group = q_heads / heads;
     s.abreast = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
@@ -603,7 +603,7 @@ hlq_status hlq_attn_prompt(int32_t B, int32_t q_heads, int32_t heads, int32_t di
     a.q_offsets = q_offsets;
     a.k_offsets = k_offsets;
     a.causal = causal != 0;
-    a.window = window < 1 << 30 ? window : 0;   // no sequence is longer
+    a.window = window < Tk ? window : 0;   // no sequence is longer
     a.scale = scale == 0.f ? 1.f : fabsf(scale) * 1.44269504f;
     a.sign = scale < 0.f ? -1.f : scale == 0.f ? 0.f : 1.f;
     a.abreast = shape.abreast;

@@ -149,6 +149,9 @@ hlq_kv_rows_kernel(const Rows a)
             sine_of(at * a.turns[pair], a.magnitude, x.s, x.c);
             mine[place(pair)] = x;
         }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");   // the lanes of a wavefront read what others of it wrote
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int d = d0 + i;

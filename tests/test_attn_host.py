@@ -217,3 +217,36 @@ BF = torch.bfloat16
 def test_tensors_that_do_not_fit_are_refused(name, change, error):
     with pytest.raises(error):
         CALLS[name](tensors(**change))
+
+
+def test_a_workspace_for_many_sequences_serves_a_few():
+    # more than there are counters for: those calls are not cut, calls of fewer sequences on the same workspace are
+    n = ctypes.c_size_t()
+    d = desc(10, 64, 8, 128)
+    assert B.lib.hlq_attn_decode_workspace_bytes(d, 8, 5000, 40, ctypes.byref(n)) == 0
+    many = n.value
+    for batch in (1, 7, 100, 1000, 4095, 4096):
+        assert B.lib.hlq_attn_decode_workspace_bytes(d, 8, batch, 40, ctypes.byref(n)) == 0
+        assert n.value <= many
+
+
+@pytest.mark.parametrize("rows", [dict(Tq=2**30), dict(Tk=2**30), dict(B=2**30)])
+def test_prompts_past_the_limit_are_refused(rows):
+    assert B.lib.hlq_attn_prompt(*{**PROMPT, **rows}.values(), None) == UNSUPPORTED
+
+
+def test_numbers_past_32_bits_are_refused():
+    with pytest.raises(ValueError, match="32 bits"):
+        B.alloc_kv_cache(3, 16 + 2**32, 2, 32, torch.bfloat16, device="cpu")
+    with pytest.raises(ValueError, match="32 bits"):
+        B.kv_bytes(3, 16, 2 + 2**32, 32, torch.bfloat16)
+    a = tensors()
+    for window in (2**31, 2**32 + 5):
+        with pytest.raises(ValueError, match="window"):
+            B.hlq_attn_decode(a["cache"], a["q"], a["table"], a["lengths"], window=window, ws=a["ws"])
+        with pytest.raises(ValueError, match="window"):
+            B.hlq_attn_prompt(a["q"], a["k"], a["v"], a["q_offsets"], a["k_offsets"], window=window, ws=a["ws"])
+    with pytest.raises(ValueError, match="32 bits"):
+        B.decode_workspace_bytes(a["cache"], 4, 1, 2**32)
+    with pytest.raises(ValueError, match="32 bits"):
+        B.prompt_workspace_bytes(5, 5, 2**32, 4, 2, 32)
