@@ -175,23 +175,7 @@ hlq_attn_prompt_kernel(const Prompt a)
     begin = begin < all_begin ? all_begin : begin;
     end = end > all_end ? all_end : end;
 
-    // queries, the second operand; of a negative scale they have the sign, so that the largest score has the largest product
     const int first_place = shift + p.first + row0;                     // of the wavefront's first query
-    F query[KS];
-    {
-        const S *q = (const S *)a.q.p + (int64_t)(p.q0 + p.first + row0 + (col < own_rows ? col : 0)) * a.q.ts + head * a.q.hs + 8 * half;
-        if (col < own_rows && a.sign != 0.f && a.D == DP) {
-#pragma unroll
-            for (int s = 0; s < KS; ++s) query[s] = __builtin_bit_cast(F, *(const mx4_u4_any *)(q + 16 * s));
-        } else {
-#pragma unroll
-            for (int s = 0; s < KS; ++s) query[s] = __builtin_bit_cast(F, col < own_rows && a.sign != 0.f && 16 * s + 8 * half < a.D ? *(const mx4_u4_any *)(q + 16 * s) : (mx4_u4){0u, 0u, 0u, 0u});
-        }
-        if (a.sign < 0.f) {
-#pragma unroll
-            for (int s = 0; s < KS; ++s) query[s] = __builtin_bit_cast(F, __builtin_bit_cast(mx4_u4, query[s]) ^ 0x80008000u);
-        }
-    }
 
     // Tiles in LDS: row after row, a row's 16-byte pieces in another order, so that reads meet every bank evenly: piece c of key k at c ^ (k & 7), of a
     // value's row at c ^ 2 (k & 3).  A lane loads what belongs in its place.
@@ -283,12 +267,6 @@ hlq_attn_prompt_kernel(const Prompt a)
     };
     auto seen_of = [&](int step) { return Seen{first_seen - step * KEYS - 4 * half, last_seen - step * KEYS - 4 * half}; };
 
-    auto multiply_keys = [&](float16v &score, uint32_t slot) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) score[i] = 0.f;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) score = multiply(key(slot, s), query[s], score);
-    };
     auto multiply_values = [&](const F (&weight)[2], uint32_t slot) {
 #pragma unroll
         for (int j = 0; j < DS; ++j)
@@ -382,9 +360,40 @@ hlq_attn_prompt_kernel(const Prompt a)
         F weight[2];
 #pragma unroll
         for (int i = 0; i < 16; ++i) score[i] = 0.f, weight[i >> 3][i & 7] = (S)0.f;
+        // queries, the second operand: whole rows by way of the slots that nothing is in yet, with their pieces as a key's
+        F query[KS];
+        const S *const q = (const S *)a.q.p + (int64_t)(p.q0 + p.first + row0) * a.q.ts + head * a.q.hs;
+        if constexpr (DMA) {
+            const int step = (int)(a.q.ts * 2), bytes = own_rows > 0 && a.sign != 0.f ? (own_rows - 1) * step + a.D * 2 : 0;
+            const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<S *>(q), 0, bytes, 0x00020000);
+#pragma unroll
+            for (int i = 0; i < 32 * PIECES / 64; ++i) {
+                const int at = i * (64 / PIECES) + lane / PIECES, piece = (lane % PIECES ^ (at & 7)) * 8;
+                load_to_lds(r, piece < a.D ? at * step + piece * 2 : OUTSIDE, lds_at + here + wave * 32 * ROW + i * 1024);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) query[s] = __builtin_bit_cast(F, col < own_rows && a.sign != 0.f && 16 * s + 8 * half < a.D ? *(const mx4_u4_any *)(q + col * a.q.ts + 16 * s + 8 * half) : (mx4_u4){0u, 0u, 0u, 0u});
+        }
         request(true, key_feed, ahead);
         if constexpr (!DMA) enter(true, ahead);
         request(true, key_feed, behind);
+        if constexpr (DMA) {
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
+#pragma unroll
+            for (int s = 0; s < KS; ++s) query[s] = key(here + wave * 32 * ROW, s);
+        }
+        // of a negative scale they have the sign, so that the largest score has the largest product
+        if (a.sign < 0.f) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) query[s] = __builtin_bit_cast(F, __builtin_bit_cast(mx4_u4, query[s]) ^ 0x80008000u);
+        }
+        auto multiply_keys = [&](float16v &score, uint32_t slot) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) score[i] = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) score = multiply(key(slot, s), query[s], score);
+        };
         int t = all_begin - 1;
         auto meet = [&](bool first) {
             if constexpr (DMA) {
@@ -500,20 +509,26 @@ hlq_attn_prompt_kernel(const Prompt a)
     float own;
     const float other = other_half(total, own);
     const float all = own + other, by = all == 0.f ? 0.f : 1.f / all;
-    if (col >= own_rows) return;
-    S *const out = (S *)a.out.p + (int64_t)(p.q0 + p.first + row0 + col) * a.out.ts + head * a.out.hs + 4 * half;
-    auto leave = [&](auto Whole) {
+    // by way of LDS, so that whole rows leave
+    constexpr int TURN = PIECES < 16 ? PIECES - 1 : 15;
+    char *const mine = lds + wave * 32 * ROW;
+    __syncthreads();
 #pragma unroll
-        for (int j = 0; j < DS; ++j)
+    for (int j = 0; j < DS; ++j)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const int d = 32 * j + 2 * i;
-                const float v4[4] = {acc[j][i] * by, acc[j][i + 1] * by, acc[j][i + 2] * by, acc[j][i + 3] * by};
-                if (decltype(Whole)::value || d + 4 * half < a.D) mx4_store4(out, T, d, v4, 4);
-            }
-    };
-    if (a.D == DP) leave(std::true_type{});
-    else leave(std::false_type{});
+        for (int i = 0; i < 16; i += 4) {
+            typedef S four __attribute__((ext_vector_type(4)));
+            *(four *)(mine + col * ROW + ((4 * j + i / 4) ^ (col & TURN)) * 16 + 8 * half) = (four){(S)(acc[j][i] * by), (S)(acc[j][i + 1] * by), (S)(acc[j][i + 2] * by), (S)(acc[j][i + 3] * by)};
+        }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");   // the lanes of a wavefront read what others of it wrote
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    S *const out = (S *)a.out.p + (int64_t)(p.q0 + p.first + row0) * a.out.ts + head * a.out.hs;
+#pragma unroll
+    for (int i = 0; i < 32 * PIECES / 64; ++i) {
+        const int row = i * (64 / PIECES) + lane / PIECES, piece = lane % PIECES;
+        if (row < own_rows && piece * 8 < a.D) *(mx4_u4_any *)(out + row * a.out.ts + piece * 8) = *(const mx4_u4 *)(mine + row * ROW + (piece ^ (row & TURN)) * 16);
+    }
 }
 
 template <int T, bool DMA>
@@ -613,7 +628,7 @@ hlq_status hlq_attn_prompt(int32_t B, int32_t q_heads, int32_t heads, int32_t di
     const int64_t grid = shape.workgroups * shape.cuts;
     // loads that go to LDS by themselves: rows at multiples of 16 bytes, no nearer than their length, a tile's offsets in 31 bits
     const auto whole = [&](const KvRows &x) { return x.ts >= dim && ((uintptr_t)x.p & 15u) == 0 && x.ts % 8 == 0 && x.hs % 8 == 0 && x.ts < 1 << 23; };
-    const bool dma = whole(a.k) && whole(a.v);
+    const bool dma = whole(a.q) && whole(a.k) && whole(a.v);
     const hipStream_t st = (hipStream_t)stream;
     hlq_clear_stale_error();
     if (type == HLQ_F16) dma ? launch<HLQ_F16, true>(a, grid, st) : launch<HLQ_F16, false>(a, grid, st);
