@@ -17,8 +17,8 @@
 namespace {
 
 constexpr int WAVES = 4, KEYS = 32, STAGES = 3;
-constexpr int LEAST_STEPS = 8;   // of a cut
-constexpr int64_t SLOTS = 512;    // workgroups that a cut launch makes at most: two a compute unit
+constexpr int LEAST_STEPS = 8;                  // of a cut
+constexpr int64_t UNITS = 256, MOST_PARTIALS = 4 * UNITS, MOST_CUTS = 128;   // compute units; workgroups that a cut launch makes at most; cuts
 constexpr float NONE = -__builtin_inff();
 
 typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
@@ -555,13 +555,23 @@ hlq_status shape_of(int64_t Tq, int64_t Tk, int32_t B, int32_t q_heads, int32_t 
     s.abreast = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
     // never more tiles than the queries can make, whatever the offsets hold
     const int rows = 32 * (WAVES / s.abreast);
-    s.workgroups = (Tq / rows + (Tq < B ? Tq : B)) * (q_heads / s.abreast);
+    s.workgroups = (Tq + (Tq < B ? Tq : B) * (rows - 1)) / rows * (q_heads / s.abreast);
     if (s.workgroups > ((int64_t)1 << 24) - 1) return HLQ_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 lanes
-    // few queries over many keys: the keys are cut so that the card is full
-    const int64_t most = (Tk + KEYS * LEAST_STEPS - 1) / (KEYS * LEAST_STEPS), want = s.workgroups > 0 ? SLOTS / s.workgroups : 1;
-    s.cuts = (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
+    // Few queries over many keys: the keys are cut as many times as the compute unit with most to do then has least (sequences taken as of one length).  In
+    // tenths of a step of one of two workgroups of a unit: alone it takes 13 (dim above 128 always), it begins and ends in five steps, a joined tile takes eight and five a cut.
+    // (32 heads of 128, 8 of keys: 512 queries over 8192 keys whole 158 us, in 2, 3, 4, 6, 8 cuts 95, 94, 83, 104, 109; 32 over 4096: 77, in 4, 8, 16 cuts 33, 30, 38; over 512: 16, in two 16.5.)
     const int DP = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
-    s.bytes = HLQ_WS_COUNTER_BYTES + (most > 1 ? (size_t)SLOTS * WAVES * 64 * (DP / 4 + 1) * 8u : 0u);
+    const int64_t most = (Tk + KEYS * LEAST_STEPS - 1) / (KEYS * LEAST_STEPS), some = Tq < B ? Tq : B;
+    const int64_t steps = some > 0 ? (Tk / some + KEYS - 1) / KEYS : 0, likely = some > 0 ? some * ((Tq / some + rows - 1) / rows) * (q_heads / s.abreast) : 0;
+    int64_t best = 0;
+    s.cuts = 1;
+    for (int64_t cuts = 1; cuts <= MOST_CUTS && (cuts == 1 || (cuts <= most && s.workgroups * cuts <= MOST_PARTIALS)); ++cuts) {
+        const int64_t each = (likely * cuts + UNITS - 1) / UNITS, pace = DP > 128 ? 13 * each : 10 * each + (each & 1) * 3;
+        const int64_t cost = ((steps + cuts - 1) / cuts + 5) * pace + (cuts > 1 ? 80 + 50 * cuts : 0);
+        if (cuts == 1 || cost < best) best = cost, s.cuts = (int)cuts;
+    }
+    const int64_t partials = most < 2 ? 0 : s.workgroups * most < MOST_PARTIALS ? s.workgroups * most : MOST_PARTIALS;
+    s.bytes = HLQ_WS_COUNTER_BYTES + (size_t)partials * WAVES * 64 * (DP / 4 + 1) * 8u;
     *out = s;
     return HLQ_OK;
 }
