@@ -1,17 +1,25 @@
 // Attention of packed prompts:  out_i = sum_j p_ij v_j / sum_j p_ij over the keys j that query i sees,  p_ij = exp(scale q_i . k_j - m_i).
 //
-// One pass over the keys with the running maximum and sum of each query.  A wavefront has 64 queries of a head (32 for dim above 128), a workgroup four
-// wavefronts: four heads of a kv head with the same queries where the group allows, else two, or one with more queries.  Keys and values come through LDS
+// One pass over the keys with the running maximum and sum of each query.  A wavefront has 32 queries of a head, a workgroup four wavefronts: four heads of a
+// kv head with the same queries where the group allows, else two, or one with more queries.  Keys and values come through LDS
 // in tiles of 32, written there by the loads themselves, three tiles of each.
 //   scores    K Q^T with keys the first operand, 32 keys x 32 queries: a lane has 16 keys of one query, so that maximum and sum are the lane's own and
 //             one exchange with the lane 32 on
 //   weights   are then where the second product, V^T P^T, wants them: its sum over keys may take them in any order
 //   values    are turned as they are read from LDS (four keys of a column to a lane)
 // A step multiplies the next tile's keys and the last tile's values while it takes the exponentials of this one, so that matrix cores and vector units work side by
-// side within a wavefront.
+// side within a wavefront.  Most steps mask nothing and look at nothing; they have a loop of their own.
 // The maximum that exponentials are taken from is kept while no score passes it by 2^8, and is a whole power of two: so sums are rarely multiplied, and exactly.
+// Weights are rounded once, to the inputs' type, for the second product; their sum is of the rounded ones, so that a result is a true mean of values.
 // What is not seen: its score is -infinity, its weight 0.  A value that is infinite or NaN would still enter as 0 times itself, so the values of tiles at the edge
 // of what is seen are looked at, and one that holds such a value is multiplied without it; what it does to those that do see it is added by counting.
+// Rows that do not begin at multiples of 16 bytes go to LDS by way of registers (8192 tokens 610 -> 870 us, dim 256,
+// where that spills, three times as long).
+//
+// What bounds it: 8192 bf16 tokens, causal, 32 heads of 128 over 8 take 530 us, 1040 TFLOP/s (a library product reaches 1250 on this card).  Of the cycles the matrix
+// cores are busy 58 %, vector instructions issue in 55 % (105 a step and wavefront, 16 of them exponentials of 16 cycles each), at 1.7 GHz, the clock that power holds; LDS without its
+// bank conflicts (28 % of its time) made 1 % of difference, raised priority none.  Dims of 64 and 256: 840 and 820 TFLOP/s.  Short sequences (16 x 512: 75 us, 460 TFLOP/s) are bound by
+// what a workgroup does before its first product and after its last: where it is 0.7 us, queries and first keys 1.9, results 1.2, and the steps at the edge.
 #include "hlq_kv.h"
 
 namespace {
@@ -341,14 +349,15 @@ hlq_attn_prompt_kernel(const Prompt a)
                 for (int e = 0; e < 8; ++e) weight[u][e] = (S)((float)weight[u][e] * keep);
         }
     };
+    auto two_exponentials = [&](const float16v &score, F (&weight)[2], int i) {
+        const S w0 = (S)__builtin_amdgcn_exp2f(fmaf(score[i], a.scale, -base)), w1 = (S)__builtin_amdgcn_exp2f(fmaf(score[i + 1], a.scale, -base));
+        weight[i >> 3][i & 7] = w0;
+        weight[i >> 3][(i & 7) + 1] = w1;
+        total = add_pair(w0, w1, total);
+    };
     auto exponentials = [&](const float16v &score, F (&weight)[2]) {
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            const S w0 = (S)__builtin_amdgcn_exp2f(fmaf(score[i], a.scale, -base)), w1 = (S)__builtin_amdgcn_exp2f(fmaf(score[i + 1], a.scale, -base));
-            weight[i >> 3][i & 7] = w0;
-            weight[i >> 3][(i & 7) + 1] = w1;
-            total = add_pair(w0, w1, total);
-        }
+        for (int i = 0; i < 16; i += 2) two_exponentials(score, weight, i);
     };
 
     if (all_begin < all_end) {
@@ -415,6 +424,41 @@ hlq_attn_prompt_kernel(const Prompt a)
             ahead = was;
             ++t;
         };
+        // The step between two barriers: `score` becomes `later`, the keys ahead `next`, and the values behind are added by `weight`.  Dim above 128 has one wavefront a
+        // SIMD, so there its order is laid down: reads from LDS stand four products before their use, two exponentials behind each four (4096 tokens of dim 256 354 -> 337 us).
+        auto multiply_both = [&](const float16v &score, float16v &next, const F (&weight)[2], F (&later)[2]) {
+            if constexpr (DP <= 128) {
+                multiply_keys(next, ahead);
+                multiply_values(weight, OF_VALUES + behind);
+                exponentials(score, later);
+            } else {
+                constexpr int FOURS = KS / 4, PAIRS = 4 / FOURS;   // pairs of exponentials for each four products
+                F read[2][4];
+                auto fetch = [&](int n) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) read[n & 1][e] = n < FOURS ? key(ahead, 4 * n + e) : value(OF_VALUES + behind, 2 * (n - FOURS) + e / 2, e & 1);
+                };
+                fetch(0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) next[i] = 0.f;
+#pragma unroll
+                for (int n = 0; n < 2 * FOURS; ++n) {
+                    if (n + 1 < 2 * FOURS) fetch(n + 1);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (n < FOURS) next = multiply(read[n & 1][e], query[4 * n + e], next);
+                        else {
+                            float16v &sum = acc[2 * (n - FOURS) + e / 2];
+                            sum = multiply(read[n & 1][e], weight[e & 1], sum);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < PAIRS; ++e) two_exponentials(score, later, 2 * (PAIRS * n + e));
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        };
         // most of a long prompt: nothing to mask, nothing to look at
         const int hot_begin = begin + 1 > full_begin + 1 ? begin + 1 : full_begin + 1, hot_end = end - 1 < full_end ? end - 1 : full_end;
         while (t <= all_end) {
@@ -424,20 +468,20 @@ hlq_attn_prompt_kernel(const Prompt a)
                     F later[2];
                     meet(false);
                     keep_up(score, weight);
-                    multiply_keys(next, ahead);
-                    multiply_values(weight, OF_VALUES + behind);
-                    exponentials(score, later);
+                    multiply_both(score, next, weight, later);
                     advance();
                     meet(false);
                     keep_up(next, later);
-                    multiply_keys(score, ahead);
-                    multiply_values(later, OF_VALUES + behind);
-                    exponentials(next, weight);
+                    multiply_both(next, score, later, weight);
                     advance();
                 } while (t + 1 < hot_end);
                 continue;
             }
             meet(t < all_begin);
+            if (DP > 128 && (t + 1 < begin || t > end)) {   // (below, such registers are spilled that a wavefront without queries would wait for every load)
+                advance();
+                continue;
+            }
             const bool ask = t + 1 >= begin && t + 1 < end, weigh = t >= begin && t < end, sum = t - 1 >= begin && t - 1 < end;
             if (sum) {
                 if (edge(t - 1) && odd_values(OF_VALUES + behind)) multiply_odd_values(weight, t - 1, OF_VALUES + behind);
