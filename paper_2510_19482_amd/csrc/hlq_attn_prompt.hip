@@ -432,7 +432,7 @@ hlq_attn_prompt_kernel(const Prompt a)
                 multiply_values(weight, OF_VALUES + behind);
                 exponentials(score, later);
             } else {
-                constexpr int FOURS = KS / 4, PAIRS = 4 / FOURS;   // pairs of exponentials for each four products
+                constexpr int FOURS = KS / 4;
                 F read[2][4];
                 auto fetch = [&](int n) {
 #pragma unroll
@@ -453,8 +453,7 @@ hlq_attn_prompt_kernel(const Prompt a)
                             sum = multiply(read[n & 1][e], weight[e & 1], sum);
                         }
                     }
-#pragma unroll
-                    for (int e = 0; e < PAIRS; ++e) two_exponentials(score, later, 2 * (PAIRS * n + e));
+                    two_exponentials(score, later, 2 * n);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
