@@ -454,10 +454,10 @@ hlq_attn_decode_kernel(const Decode a)
             for (int i = 0; i < 4; ++i) sum[i] *= by;
             if (d < a.D) put(head, d, sum);
         } else {
-            uint64_t *to = (uint64_t *)(partial + cut * size + head * DP + d);
+            uint64_t *to = (uint64_t *)(partial + cut * size) + it;   // the first two of each four, then the others, so that a store's lanes stand side by side
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                __hip_atomic_store(to + i, as_bits(sum[2 * i]) | (uint64_t)as_bits(sum[2 * i + 1]) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __hip_atomic_store(to + i * (a.rows * (DP / 4)), as_bits(sum[2 * i]) | (uint64_t)as_bits(sum[2 * i + 1]) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             if (d == 0)
                 __hip_atomic_store((uint64_t *)(partial + cut * size + a.rows * DP) + head, as_bits(m) | (uint64_t)as_bits(all) << 32,
                                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -476,12 +476,12 @@ hlq_attn_decode_kernel(const Decode a)
     // the sums of eight cuts at a time; the first of them are on their way while the weights are made
     uint64_t pair[8][2];
     auto fetch_sums = [&](int it, int c0) {
-        const uint64_t *from = (const uint64_t *)(partial + it / (DP / 4) * DP + it % (DP / 4) * 4);
+        const uint64_t *from = (const uint64_t *)partial + it;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int c = c0 + i < active ? c0 + i : c0;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) pair[i][e] = __hip_atomic_load(from + c * (size / 2) + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            for (int e = 0; e < 2; ++e) pair[i][e] = __hip_atomic_load(from + c * (size / 2) + e * (a.rows * (DP / 4)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     };
     const int items = heads * (DP / 4);
