@@ -17,7 +17,7 @@
 // where that spills, three times as long).
 //
 // What bounds it: 8192 bf16 tokens, causal, 32 heads of 128 over 8 take 530 us, 1040 TFLOP/s (a library product reaches 1250 on this card).  Of the cycles the matrix
-// cores are busy 58 %, vector instructions issue in 55 % (105 a step and wavefront, 16 of them exponentials of 16 cycles each), at 1.7 GHz, the clock that power holds; LDS without its
+// cores are busy 50 to 58 %, vector instructions issue in 45 to 55 % (105 a step and wavefront, 16 of them exponentials of 16 cycles each), at 1.7 GHz, the clock that power holds; LDS without its
 // bank conflicts (28 % of its time) made 1 % of difference, raised priority none.  Dims of 64 and 256: 840 and 820 TFLOP/s.  Short sequences (16 x 512: 75 us, 460 TFLOP/s) are bound by
 // what a workgroup does before its first product and after its last: where it is 0.7 us, queries and first keys 1.9, results 1.2, and the steps at the edge.
 #include "hlq_kv.h"
