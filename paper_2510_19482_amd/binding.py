@@ -749,7 +749,7 @@ def _heads(t):
         ts, hs, one = t.stride()
     except ValueError:
         raise ValueError(f"expected [tokens, heads, dim], got shape {tuple(t.shape)}") from None
-    if one != 1 and D > 1:
+    if one != 1 and D > 1 and T and H:   # (an array of nothing has any strides)
         raise ValueError(f"expected a contiguous last axis, got shape {tuple(t.shape)} with strides {t.stride()}")
     return T, H, D, t.data_ptr(), dtype, ts, hs
 

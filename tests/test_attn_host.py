@@ -250,3 +250,11 @@ def test_numbers_past_32_bits_are_refused():
         B.decode_workspace_bytes(a["cache"], 4, 1, 2**32)
     with pytest.raises(ValueError, match="32 bits"):
         B.prompt_workspace_bytes(5, 5, 2**32, 4, 2, 32)
+
+
+def test_an_array_of_nothing_may_have_any_strides():
+    # as one made of an empty numpy array has
+    nothing = torch.from_numpy(np.zeros((0, 2, 32))).to(torch.bfloat16)
+    empty = nothing.as_strided((0, 2, 32), (0, 0, 0))
+    with pytest.raises(ValueError, match="one GPU"):
+        CALLS["prompt"](tensors(k=empty, v=empty))
