@@ -447,7 +447,8 @@ HLQ_API hlq_status hlq_attn_decode(const hlq_kv_desc *c, const void *cache, size
  * i of n_q stands at place n_k - n_q + i, and sees key j if
  *     j < n_k,   j <= its place if causal,   j > its place - window if window > 0;
  * a query that sees no key (or none whose score is above -infinity) has 0.  out [Tq, q_heads, dim]; rows of no sequence stay as they were.  Offsets count
- * as the nearest number in 0 .. Tq, or Tk; a sequence that ends before it begins is empty.  Products are exact, sums fp32, p is rounded to the inputs' type (f16, bf16), which is out's too.
+ * as the nearest number in 0 .. Tq, or Tk; a sequence that ends before it begins is empty.  Products are exact, sums fp32, p is rounded to the inputs' type (f16, bf16), which is out's too,
+ * and summed as rounded.
  * ws: as for hlq_attn_decode. */
 HLQ_API hlq_status hlq_attn_prompt_workspace_bytes(int64_t Tq, int64_t Tk, int32_t B, int32_t q_heads, int32_t heads, int32_t dim, size_t *bytes);
 HLQ_API hlq_status hlq_attn_prompt(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, hlq_dtype type, int64_t Tq, const void *q, int64_t q_ts, int64_t q_hs,

@@ -292,7 +292,8 @@ hlq_kv_read_kernel(const Read a)
     }
 }
 
-// A token's heads on one wavefront, so that its angles are made once, unless that leaves the card half empty: then on several.
+// A token's heads on one wavefront, so that its angles are made once, unless that leaves the card half empty: then on several.  (1024 tokens of 48 heads into 16 bits and back:
+// 2048 wavefronts 11.6 us, 4096 10.0, 16384 15.0; 8192 tokens of 40 heads turned: one a token 31, two 35, four 45.)
 void cut_heads(int64_t T, int all, int fit, int &parts, int &per_part)
 {
     const int rounds = (all + fit - 1) / fit;
