@@ -433,7 +433,8 @@ HLQ_API hlq_status hlq_kv_read(const hlq_kv_desc *c, const void *cache, size_t c
  * the newest token's key and value are in the cache already.  table [B, >= pages of a sequence] (int32, leading dimension ld_table): the page of
  * tokens i * page_tokens ..; lengths [B] int32.  A length counts as at most table_width * page_tokens and as at least 0, a page as the
  * nearest one inside the cache.  Length 0, or no score above -infinity: 0.  q_heads is a multiple of heads.  q has the type of a 16-bit cache, f16 or
- * bf16 with MX8 and MX4; out f16, bf16 or f32.  Products are exact, sums fp32; p is held to 2^-16 of itself (f16: 2^-22, absolutely 2^-25).  Results do not
+ * bf16 with MX8 and MX4; out f16, bf16 or f32.  Products are exact (8- and 4-bit values below
+ * 2^-126 may count as 0), sums fp32; p is held to 2^-16 of itself (f16: 2^-22, absolutely 2^-25).  Results do not
  * depend on the order in which workgroups end.
  * ws: of hlq_attn_decode_workspace_bytes() (host-only; enough for smaller B and table_width too), seen by hlq_workspace_init once; calls that may run at
  * the same time need one each. */

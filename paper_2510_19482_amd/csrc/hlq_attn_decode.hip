@@ -11,7 +11,7 @@
 // The four wavefronts of a workgroup take tiles in turn and meet in LDS.  A sequence is cut over up to `cuts` workgroups by its length; the last one to
 // end adds their sums in order (hand-over by device-scope stores and a counter), so results do not depend on which is last.
 // Weights are two terms of 16 bits (the second product runs twice: it waits for memory anyway), so that p is not rounded to 8 bits.  8- and 4-bit
-// values become bf16, which holds them and their scale exactly; f16 queries are two bf16 terms then.
+// values become bf16, which holds them and their scale exactly (from 2^-126 up); f16 queries are two bf16 terms then.
 // Keys' rows are asked for in lines of 128 bytes, and rows are not kept in the caches: by 64 bytes of each of 16 rows, and kept, 64 x 4096 tokens took 204 us for 184.
 // What bounds it: memory.  64 sequences of 4096 tokens, 8 heads of 128 with 64 queries: 16 bits 184 to 188 us = 5.7 to 5.8 TB/s (a plain read reaches 6.9), 8 bits 112 to 117 = 4.8, 4 bits
 // 65 to 68 = 4.3; the fewer bits a tile has, the less of it is on its way (a wavefront has one tile, 17, 8.5 or 4.4 KB; two tiles a wavefront, or fewer registers and four
