@@ -75,7 +75,7 @@ __device__ __forceinline__ float add_pair(_Float16 a, _Float16 b, float c)
 // 16 bytes a lane from an offset of a descriptor (zeros past its end) to LDS at `to`, lane after lane
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, int offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(r), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(r), "s"(to) : "memory", "m0");
 }
 
 // sequence and tile of a workgroup; every lane of the wavefront takes part and gets the same answer
