@@ -449,9 +449,9 @@ hlq_attn_decode_kernel(const Decode a)
             for (int i = 0; i < 4; ++i) sum[i] = fmaf(weight, v[i], sum[i]);
         }
         if (alone) {
-            const float by = all == 0.f ? 0.f : 1.f / all;
+            const float by = 1.f / all;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] *= by;
+            for (int i = 0; i < 4; ++i) sum[i] = all == 0.f ? 0.f : sum[i] * by;   // nothing seen is 0, whatever the values are
             if (d < a.D) put(head, d, sum);
         } else {
             uint64_t *to = (uint64_t *)(partial + cut * size) + it;   // the first two of each four, then the others, so that a store's lanes stand side by side
@@ -511,7 +511,7 @@ hlq_attn_decode_kernel(const Decode a)
         }
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-        if (lane == 0) shares[head] = sum == 0.f ? 0.f : 1.f / sum;
+        if (lane == 0) shares[head] = sum == 0.f ? 0.f : 1.f / sum;   // (0: nothing seen)
     }
     __syncthreads();
     for (int it = (int)threadIdx.x; it < items; it += 64 * WAVES) {
@@ -531,7 +531,7 @@ hlq_attn_decode_kernel(const Decode a)
                 }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] *= shares[head];
+        for (int i = 0; i < 4; ++i) sum[i] = shares[head] == 0.f ? 0.f : sum[i] * shares[head];
         if (d < a.D) put(head, d, sum);
     }
 }

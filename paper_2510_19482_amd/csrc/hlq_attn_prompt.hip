@@ -552,6 +552,12 @@ hlq_attn_prompt_kernel(const Prompt a)
     float own;
     const float other = other_half(total, own);
     const float all = own + other, by = all == 0.f ? 0.f : 1.f / all;
+    if (__any(all == 0.f)) {   // a query that has seen nothing: 0, whatever the values are
+#pragma unroll
+        for (int j = 0; j < DS; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[j][i] = all == 0.f ? 0.f : acc[j][i];
+    }
     // by way of LDS, so that whole rows leave
     constexpr int TURN = PIECES < 16 ? PIECES - 1 : 15;
     char *const mine = lds + wave * 32 * ROW;
