@@ -434,8 +434,8 @@ HLQ_API hlq_status hlq_kv_read(const hlq_kv_desc *c, const void *cache, size_t c
  * tokens i * page_tokens ..; lengths [B] int32.  A length counts as at most table_width * page_tokens and as at least 0, a page as the
  * nearest one inside the cache.  Length 0, or no score above -infinity: 0.  q_heads is a multiple of heads.  q has the type of a 16-bit cache, f16 or
  * bf16 with MX8 and MX4; out f16, bf16 or f32.  Products are exact (8- and 4-bit values below
- * 2^-126 may count as 0), sums fp32; p is held to 2^-16 of itself (f16: 2^-22, absolutely 2^-25).  Results do not
- * depend on the order in which workgroups end.
+ * 2^-126 may count as 0), sums fp32; p is held to 2^-16 of itself (f16 caches: 2^-22, and 2^-42 of the largest).
+ * Results do not depend on the order in which workgroups end.
  * ws: of hlq_attn_decode_workspace_bytes() (host-only; enough for smaller B and table_width too), seen by hlq_workspace_init once; calls that may run at
  * the same time need one each. */
 HLQ_API hlq_status hlq_attn_decode_workspace_bytes(const hlq_kv_desc *c, int32_t q_heads, int64_t B, int32_t table_width, size_t *bytes);
@@ -449,7 +449,7 @@ HLQ_API hlq_status hlq_attn_decode(const hlq_kv_desc *c, const void *cache, size
  *     j < n_k,   j <= its place if causal,   j > its place - window if window > 0;
  * a query that sees no key (or none whose score is above -infinity) has 0.  out [Tq, q_heads, dim]; rows of no sequence stay as they were.  Offsets count
  * as the nearest number in 0 .. Tq, or Tk; a sequence that ends before it begins is empty.  Products are exact, sums fp32, p is rounded to the inputs' type (f16, bf16), which is out's too,
- * and summed as rounded.
+ * and summed as rounded (f16: also to 2^-31 of the largest).
  * ws: as for hlq_attn_decode. */
 HLQ_API hlq_status hlq_attn_prompt_workspace_bytes(int64_t Tq, int64_t Tk, int32_t B, int32_t q_heads, int32_t heads, int32_t dim, size_t *bytes);
 HLQ_API hlq_status hlq_attn_prompt(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, hlq_dtype type, int64_t Tq, const void *q, int64_t q_ts, int64_t q_hs,

@@ -47,8 +47,12 @@ struct Decode {
     int rows;                     // of a partial result: min(16, group)
 };
 
-template <int C> struct Fragment { using type = bf8v; using scalar = __bf16; };
-template <> struct Fragment<HLQ_F16> { using type = half8v; using scalar = _Float16; };
+// LIFT: what the largest weight is brought to is 2^(LIFT - 1) to 2^LIFT (2^8 times that while the base is kept); REST: what a weight's second term is multiplied by.
+// f16 ends at 2^16 and has steps of 2^-24 at its lower end, so that small weights beside a large one would be lost (8192 tokens of which 128 have a score that is 17 higher: a tenth
+// of the others' share): they stand as high as they can, and their second terms are 2^11 times as large, with a product that is brought back before it is added.
+// bf16 has fp32's exponents and needs neither.
+template <int C> struct Fragment { using type = bf8v; using scalar = __bf16; static constexpr float LIFT = 0.f, REST = 1.f; };
+template <> struct Fragment<HLQ_F16> { using type = half8v; using scalar = _Float16; static constexpr float LIFT = 7.f, REST = 2048.f; };
 
 __device__ __forceinline__ float4v multiply(bf8v a, bf8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ float4v multiply(half8v a, half8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -115,6 +119,7 @@ hlq_attn_decode_kernel(const Decode a)
 {
     using F = typename Fragment<C>::type;
     using S = typename Fragment<C>::scalar;
+    constexpr float LIFT = Fragment<C>::LIFT, REST = Fragment<C>::REST;
     constexpr bool MX = C == HLQ_MX8 || C == HLQ_MX4;
     constexpr int PER = C == HLQ_MX4 ? 8 : C == HLQ_MX8 ? 4 : 2;   // values of a dword
     constexpr int KS = DP / 32, E = DP / 16;                       // products over dim; columns of a lane
@@ -322,10 +327,10 @@ hlq_attn_decode_kernel(const Decode a)
                 m = over_lanes_max(m) * a.scale;
                 if (__builtin_expect(__any(m > most), 0)) {
                     const bool now = m > most;
-                    const float to = now ? ceilf(m) : base;
+                    const float to = now ? ceilf(m) - LIFT : base;
                     const float keep = !now ? 1.f : most == NONE ? 0.f : __builtin_amdgcn_exp2f(base - to);
                     base = to;
-                    most = now ? to + 8.f : most;
+                    most = now ? to + (LIFT + 8.f) : most;
                     total *= keep;
 #pragma unroll
                     for (int j = 0; j < E; ++j)
@@ -338,7 +343,7 @@ hlq_attn_decode_kernel(const Decode a)
                     const float w = __builtin_amdgcn_exp2f(fmaf(x[e], a.scale, -base));
                     total += w;
                     p[e] = (S)w;
-                    rest[e] = (S)(w - (float)p[e]);
+                    rest[e] = (S)((w - (float)p[e]) * REST);
                 }
 
                 // values, two tokens' of one column in a register
@@ -376,14 +381,28 @@ hlq_attn_decode_kernel(const Decode a)
                         }
                     }
                 }
+                // four columns at a time, so that nothing waits for a second term's product (f16, 32 x 4096 tokens of dim 256: one by one 214 us, so 205; without products of their own 197)
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    const uint32_t pick = j & 1 ? 0x07060302u : 0x05040100u;
-                    const mx4_u4 w = {__builtin_amdgcn_perm(rows[1][j >> 1], rows[0][j >> 1], pick), __builtin_amdgcn_perm(rows[3][j >> 1], rows[2][j >> 1], pick),
-                                      __builtin_amdgcn_perm(rows[5][j >> 1], rows[4][j >> 1], pick), __builtin_amdgcn_perm(rows[7][j >> 1], rows[6][j >> 1], pick)};
-                    const F turned = __builtin_bit_cast(F, w);
-                    acc[j] = multiply(turned, p, acc[j]);
-                    if (two) acc[j] = multiply(turned, rest, acc[j]);
+                for (int j0 = 0; j0 < E; j0 += 4) {
+                    float4v low[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = j0 + i;
+                        const uint32_t pick = j & 1 ? 0x07060302u : 0x05040100u;
+                        const mx4_u4 w = {__builtin_amdgcn_perm(rows[1][j >> 1], rows[0][j >> 1], pick), __builtin_amdgcn_perm(rows[3][j >> 1], rows[2][j >> 1], pick),
+                                          __builtin_amdgcn_perm(rows[5][j >> 1], rows[4][j >> 1], pick), __builtin_amdgcn_perm(rows[7][j >> 1], rows[6][j >> 1], pick)};
+                        const F turned = __builtin_bit_cast(F, w);
+                        acc[j] = multiply(turned, p, acc[j]);
+                        if constexpr (REST == 1.f) {
+                            if (two) acc[j] = multiply(turned, rest, acc[j]);
+                        } else
+                            low[i] = multiply(turned, rest, (float4v){0.f, 0.f, 0.f, 0.f});
+                    }
+                    if constexpr (REST != 1.f) {
+                        if (two)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) acc[j0 + i / 4][i % 4] = fmaf(low[i / 4][i % 4], 1.f / REST, acc[j0 + i / 4][i % 4]);
+                    }
                 }
                 if (more) load_values(values, where);
                 if (!more) break;
