@@ -432,7 +432,8 @@ HLQ_API hlq_status hlq_kv_read(const hlq_kv_desc *c, const void *cache, size_t c
  *     out[b, h] = sum_j p_j v_j,   p = softmax over j of scale * q[b, h] . k_j,   j < lengths[b], and j >= lengths[b] - window if window > 0;
  * the newest token's key and value are in the cache already.  table [B, >= pages of a sequence] (int32, leading dimension ld_table): the page of
  * tokens i * page_tokens ..; lengths [B] int32.  A length counts as at most table_width * page_tokens and as at least 0, a page as the
- * nearest one inside the cache.  Length 0, or no score above -infinity: 0.  q_heads is a multiple of heads.  q has the type of a 16-bit cache, f16 or
+ * nearest one inside the cache.  Length 0, or no score above -infinity: 0.  A key whose score is -infinity counts as one that is not seen; a value that is
+ * infinite or NaN is its column's result for every head that sees its key, however small p (both infinities: NaN).  q_heads is a multiple of heads.  q has the type of a 16-bit cache, f16 or
  * bf16 with MX8 and MX4; out f16, bf16 or f32.  Products are exact (8- and 4-bit values below
  * 2^-126 may count as 0), sums fp32; p is held to 2^-16 of itself (f16 caches: 2^-22, and 2^-42 of the largest).
  * Results do not depend on the order in which workgroups end.
@@ -447,7 +448,7 @@ HLQ_API hlq_status hlq_attn_decode(const hlq_kv_desc *c, const void *cache, size
  * values in rows k_offsets[b] .. of k and v [Tk, heads, dim] (offsets int32 [B + 1], ascending).  The last query and the last key are the same token: query
  * i of n_q stands at place n_k - n_q + i, and sees key j if
  *     j < n_k,   j <= its place if causal,   j > its place - window if window > 0;
- * a query that sees no key (or none whose score is above -infinity) has 0.  out [Tq, q_heads, dim]; rows of no sequence stay as they were.  Offsets count
+ * a query that sees no key (or none whose score is above -infinity) has 0, and values that are infinite or NaN are as for hlq_attn_decode.  out [Tq, q_heads, dim]; rows of no sequence stay as they were.  Offsets count
  * as the nearest number in 0 .. Tq, or Tk; a sequence that ends before it begins is empty.  Products are exact, sums fp32, p is rounded to the inputs' type (f16, bf16), which is out's too,
  * and summed as rounded (f16: also to 2^-31 of the largest).
  * ws: as for hlq_attn_decode. */

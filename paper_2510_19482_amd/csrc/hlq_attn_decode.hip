@@ -12,6 +12,7 @@
 // end adds their sums in order (hand-over by device-scope stores and a counter), so results do not depend on which is last.
 // Weights are two terms of 16 bits (the second product runs twice: it waits for memory anyway), so that p is not rounded to 8 bits.  8- and 4-bit
 // values become bf16, which holds them and their scale exactly (from 2^-126 up); f16 queries are two bf16 terms then.
+// A wavefront that ends with a NaN goes through its tiles once more, multiplies without the values that are infinite or NaN, and adds what they do to those that see them by counting.
 // Keys' rows are asked for in lines of 128 bytes, and rows are not kept in the caches: by 64 bytes of each of 16 rows, and kept, 64 x 4096 tokens took 204 us for 184.
 // What bounds it: memory.  64 sequences of 4096 tokens, 8 heads of 128 with 64 queries: 16 bits 184 to 188 us = 5.7 to 5.8 TB/s (a plain read reaches 6.9), 8 bits 112 to 117 = 4.8, 4 bits
 // 65 to 68 = 4.3; the fewer bits a tile has, the less of it is on its way (a wavefront has one tile, 17, 8.5 or 4.4 KB; two tiles a wavefront, or fewer registers and four
@@ -84,6 +85,37 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 // what a maximum is subtracted as: where nothing was seen, or only -infinity, 0, so that no difference is NaN
 __device__ __forceinline__ float base_of(float m) { return m == NONE ? 0.f : m; }
 
+// what sums are multiplied by: not 0, so that an infinite sum stays one; what 2^-126 leaves of a finite one is far below a rounding
+__device__ __forceinline__ float exp2_above_0(float v) { return fmaxf(__builtin_amdgcn_exp2f(v), 0x1p-126f); }
+
+// adds +infinity, -infinity, or for a NaN both to the sums of the heads that have its token in `present`
+template <class F>
+__device__ __forceinline__ void count_odd(F v, uint32_t present, float4v &sum)
+{
+    const float4v none = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int sign = 0; sign < 2; ++sign) {
+        F sees, is;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            sees[e] = present >> e & 1u ? 1.f : 0.f;
+            is[e] = (sign ? (float)v[e] > NONE : (float)v[e] < __builtin_inff()) ? 0.f : 1.f;
+        }
+        const float4v count = multiply(is, sees, none);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (count[i] > 0.f) sum[i] += sign ? NONE : __builtin_inff();
+    }
+}
+// two values, 0 where they are infinite or NaN
+template <class F>
+__device__ __forceinline__ uint32_t without_odd(uint32_t two)
+{
+    constexpr uint32_t most = __is_same(F, half8v) ? 0x7c00u : 0x7f80u;
+    const uint32_t low = (two & most) == most ? 0u : two & 0xffffu, high = (two >> 16 & most) == most ? 0u : two & 0xffff0000u;
+    return low | high;
+}
+
 constexpr int OUTSIDE = 0x7fffffff;   // an offset that every descriptor ends before
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const void *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00020000); }
@@ -112,9 +144,10 @@ __device__ __forceinline__ uint32_t widen(uint32_t c, float scale)
     else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, I));
 }
 
-// C: the cache's type, T: the queries', DP: dim up to 64, 128 or 256
+// C: the cache's type, T: the queries', DP: dim up to 64, 128 or 256.  Dims above 128 have one wavefront a SIMD, but two where 8- or 4-bit rows and queries of one term leave the
+// registers for it (32 x 4096 tokens of dim 256, 8 bits 115 -> 104 us, 4 bits 91 -> 72; queries of two terms 118 -> 146 and 93 -> 100).
 template <int C, int T, int DP>
-__global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 3)
+__global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 3 : (C == HLQ_MX8 || C == HLQ_MX4) && T == HLQ_BF16 ? 2 : 1)
 hlq_attn_decode_kernel(const Decode a)
 {
     using F = typename Fragment<C>::type;
@@ -259,8 +292,10 @@ hlq_attn_decode_kernel(const Decode a)
     float base = 0.f, most = NONE, total = 0.f;   // most: scores up to it need no new base
     // lane (head, g) has the columns of lane 4 g + i in its row i
     auto own_sums = [&](int i, int j) { return (float4v *)(sums + (wave * 16 + col) * PITCH + column_of(4 * g + i) + j); };
-    bool two = true, again = false;
-    for (;;) {
+    // The first pass looks at nothing.  What an infinite or NaN value makes of other heads' or tokens' weights, 0 times itself, shows as NaN; then comes a careful one, which multiplies
+    // the values that are numbers and adds +infinity, -infinity, or both for a NaN, where a head sees one: with a score above -infinity, however small the weight.
+    const auto pass = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
 #pragma unroll
         for (int j = 0; j < E; ++j) acc[j] = (float4v){0.f, 0.f, 0.f, 0.f};
         base = 0.f, most = NONE, total = 0.f;
@@ -279,7 +314,7 @@ hlq_attn_decode_kernel(const Decode a)
             for (;;) {
                 const int next = step + WAVES;
                 const bool more = next < step_end;
-                if (more) look_up(next);
+                if (!CAREFUL && more) look_up(next);   // (a careful pass has no registers for the next tile)
                 const int tok0 = first + step * TILE;
                 const bool part = tok0 < start || tok0 + TILE > n;   // some tokens are not to be seen
 
@@ -313,7 +348,7 @@ hlq_attn_decode_kernel(const Decode a)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[4 * half + e] = s[e];
                 }
-                if (more) load_keys(keys, where);
+                if (!CAREFUL && more) load_keys(keys, where);
                 if (part) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -328,7 +363,7 @@ hlq_attn_decode_kernel(const Decode a)
                 if (__builtin_expect(__any(m > most), 0)) {
                     const bool now = m > most;
                     const float to = now ? ceilf(m) - LIFT : base;
-                    const float keep = !now ? 1.f : most == NONE ? 0.f : __builtin_amdgcn_exp2f(base - to);
+                    const float keep = !now || most == NONE ? 1.f : exp2_above_0(base - to);
                     base = to;
                     most = now ? to + (LIFT + 8.f) : most;
                     total *= keep;
@@ -337,6 +372,10 @@ hlq_attn_decode_kernel(const Decode a)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) acc[j][i] *= keep;
                 }
+                uint32_t present = 0;   // tokens that this lane's head sees
+                if constexpr (CAREFUL)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) present |= (uint32_t)(x[e] > NONE) << e;
                 F p, rest;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -381,63 +420,69 @@ hlq_attn_decode_kernel(const Decode a)
                         }
                     }
                 }
-                // four columns at a time, so that nothing waits for a second term's product (f16, 32 x 4096 tokens of dim 256: one by one 214 us, so 205; without products of their own 197)
+                const auto turned = [&](int j) {
+                    const uint32_t pick = j & 1 ? 0x07060302u : 0x05040100u;
+                    const mx4_u4 w = {__builtin_amdgcn_perm(rows[1][j >> 1], rows[0][j >> 1], pick), __builtin_amdgcn_perm(rows[3][j >> 1], rows[2][j >> 1], pick),
+                                      __builtin_amdgcn_perm(rows[5][j >> 1], rows[4][j >> 1], pick), __builtin_amdgcn_perm(rows[7][j >> 1], rows[6][j >> 1], pick)};
+                    return __builtin_bit_cast(F, w);
+                };
+                if constexpr (CAREFUL) {
 #pragma unroll
-                for (int j0 = 0; j0 < E; j0 += 4) {
-                    float4v low[4];
+                    for (int j = 0; j < E; ++j) count_odd(turned(j), present, acc[j]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int j = j0 + i;
-                        const uint32_t pick = j & 1 ? 0x07060302u : 0x05040100u;
-                        const mx4_u4 w = {__builtin_amdgcn_perm(rows[1][j >> 1], rows[0][j >> 1], pick), __builtin_amdgcn_perm(rows[3][j >> 1], rows[2][j >> 1], pick),
-                                          __builtin_amdgcn_perm(rows[5][j >> 1], rows[4][j >> 1], pick), __builtin_amdgcn_perm(rows[7][j >> 1], rows[6][j >> 1], pick)};
-                        const F turned = __builtin_bit_cast(F, w);
-                        acc[j] = multiply(turned, p, acc[j]);
-                        if constexpr (REST == 1.f) {
-                            if (two) acc[j] = multiply(turned, rest, acc[j]);
-                        } else
-                            low[i] = multiply(turned, rest, (float4v){0.f, 0.f, 0.f, 0.f});
+                    for (int e = 0; e < 8; ++e)
+#pragma unroll
+                        for (int i = 0; i < E / 2; ++i) rows[e][i] = without_odd<F>(rows[e][i]);
+                }
+                if constexpr (REST == 1.f) {
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        const F v = turned(j);
+                        acc[j] = multiply(v, p, acc[j]);
+                        acc[j] = multiply(v, rest, acc[j]);
                     }
-                    if constexpr (REST != 1.f) {
+                } else {
+                    // Several columns at a time, so that nothing waits for a second term's product (32 x 4096 tokens of dim 256: one by one 214 us, so 198).  Dim 128: the branch,
+                    // which is hardly ever passed by, keeps the compiler from having more on its way than there are registers (64 x 4096 tokens 205 us, so 183).
+                    constexpr int AT_ONCE = DP > 128 ? 4 : 2;
+                    const mx4_u4 second = __builtin_bit_cast(mx4_u4, rest);
+                    const bool two = DP != 128 || __any(((second.x | second.y | second.z | second.w) & 0x7fff7fffu) != 0u);
+#pragma unroll
+                    for (int j0 = 0; j0 < E; j0 += AT_ONCE) {
+                        float4v low[AT_ONCE];
+#pragma unroll
+                        for (int i = 0; i < AT_ONCE; ++i) {
+                            const F v = turned(j0 + i);
+                            acc[j0 + i] = multiply(v, p, acc[j0 + i]);
+                            low[i] = multiply(v, rest, (float4v){0.f, 0.f, 0.f, 0.f});
+                        }
                         if (two)
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) acc[j0 + i / 4][i % 4] = fmaf(low[i / 4][i % 4], 1.f / REST, acc[j0 + i / 4][i % 4]);
+                            for (int i = 0; i < 4 * AT_ONCE; ++i) acc[j0 + i / 4][i % 4] = fmaf(low[i / 4][i % 4], 1.f / REST, acc[j0 + i / 4][i % 4]);
                     }
+                }
+                if (CAREFUL && more) {
+                    look_up(next);
+                    load_keys(keys, where);
                 }
                 if (more) load_values(values, where);
                 if (!more) break;
                 step = next;
             }
         }
-        // An infinite value times a second term, which may be 0 or below it, is NaN: where a sum is NaN, the first terms alone are its result.
-        bool nan = false;
+    };
+    pass(std::false_type());
+    bool odd = !(total < __builtin_inff());
 #pragma unroll
-        for (int j = 0; j < E; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) nan = nan || acc[j][i] != acc[j][i];
-        if (!two || !__any(nan)) break;
-        again = true;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < E; j += 4) *own_sums(i, j) = (float4v){acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]};
-        two = false;
-    }
+    for (int j = 0; j < E; ++j) odd = odd || __builtin_isunordered(acc[j][0], acc[j][1]) || __builtin_isunordered(acc[j][2], acc[j][3]);
+    if (__builtin_expect(__any(odd), 0)) pass(std::true_type());
     total = over_lanes_sum(total);
 
     // the wavefronts' sums meet in LDS
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < E; j += 4) {
-            float4v v = {acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]};
-            if (again) {
-                const float4v before = *own_sums(i, j);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] = before[c] == before[c] ? before[c] : v[c];
-            }
-            *own_sums(i, j) = v;
-        }
+        for (int j = 0; j < E; j += 4) *own_sums(i, j) = (float4v){acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]};
     if (g == 0) {
         tops[wave][col] = most == NONE ? NONE : base;
         totals[wave][col] = total;
@@ -461,7 +506,7 @@ hlq_attn_decode_kernel(const Decode a)
         float all = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float weight = __builtin_amdgcn_exp2f(tops[w][head] - base);
+            const float weight = exp2_above_0(tops[w][head] - base);
             const float4v v = *(const float4v *)(sums + (w * 16 + head) * PITCH + d);
             all = fmaf(weight, totals[w][head], all);
 #pragma unroll
@@ -524,7 +569,7 @@ hlq_attn_decode_kernel(const Decode a)
         const float base = base_of(most);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float w = __builtin_amdgcn_exp2f(m[i] - base);
+            const float w = exp2_above_0(m[i] - base);
             sum = fmaf(w, all[i], sum);
             weights[head * 128 + lane + 64 * i] = w;
         }

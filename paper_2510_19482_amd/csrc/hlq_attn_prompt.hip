@@ -11,8 +11,8 @@
 // side within a wavefront.  Most steps mask nothing and look at nothing; they have a loop of their own.
 // The maximum that exponentials are taken from is kept while no score passes it by 2^8, and is a whole power of two: so sums are rarely multiplied, and exactly.
 // Weights are rounded once, to the inputs' type, for the second product; their sum is of the rounded ones, so that a result is a true mean of values.
-// What is not seen: its score is -infinity, its weight 0.  A value that is infinite or NaN would still enter as 0 times itself, so the values of tiles at the edge
-// of what is seen are looked at, and one that holds such a value is multiplied without it; what it does to those that do see it is added by counting.
+// What is not seen: its score is -infinity, its weight 0.  A value that is infinite or NaN would still enter as 0 times itself: a workgroup that ends with a NaN goes
+// through its tiles once more, multiplies without such values, and adds what they do to those that see them by counting.
 // Rows that do not begin at multiples of 16 bytes go to LDS by way of registers (8192 tokens 610 -> 870 us, dim 256,
 // where that spills, three times as long).
 //
@@ -34,6 +34,9 @@ typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 
+// what sums are multiplied by: not 0, so that an infinite sum stays one; what 2^-126 leaves of a finite one is far below a rounding
+__device__ __forceinline__ float exp2_above_0(float v) { return fmaxf(__builtin_amdgcn_exp2f(v), 0x1p-126f); }
+
 struct Prompt {
     int B, H, group, D;
     int abreast;   // heads of a workgroup: 4, 2 or 1
@@ -49,8 +52,8 @@ struct Prompt {
 
 // LIFT: what the largest weight is brought to is 2^(LIFT - 1) to 2^LIFT (2^8 times that while the base is kept).  f16 ends at 2^16 and has steps of 2^-24 at its lower end: there weights
 // stand as high as they can, so that small ones beside a large one count (16384 keys of which 8 have a score that is 17 higher: without it their share, 8.5e-5, is off by 22 to 44 %).
-template <int T> struct Fragment { using type = bf8v; using scalar = __bf16; static constexpr uint32_t EXPONENT = 0x7f807f80u, ONE = 0x00800080u; static constexpr float LIFT = 0.f; };
-template <> struct Fragment<HLQ_F16> { using type = half8v; using scalar = _Float16; static constexpr uint32_t EXPONENT = 0x7c007c00u, ONE = 0x04000400u; static constexpr float LIFT = 7.f; };
+template <int T> struct Fragment { using type = bf8v; using scalar = __bf16; static constexpr float LIFT = 0.f; };
+template <> struct Fragment<HLQ_F16> { using type = half8v; using scalar = _Float16; static constexpr float LIFT = 7.f; };
 
 __device__ __forceinline__ float16v multiply(bf8v a, bf8v b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ float16v multiply(half8v a, half8v b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
@@ -77,7 +80,7 @@ __device__ __forceinline__ float add_pair(_Float16 a, _Float16 b, float c)
 // 16 bytes a lane from an offset of a descriptor (zeros past its end) to LDS at `to`, lane after lane
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, int offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(r), "s"(to) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(r), "s"(__builtin_amdgcn_readfirstlane(to)) : "memory", "m0");
 }
 
 // sequence and tile of a workgroup; every lane of the wavefront takes part and gets the same answer
@@ -211,7 +214,6 @@ hlq_attn_prompt_kernel(const Prompt a)
         const int first = all_begin * KEYS;
         return Feed{(const char *)((const S *)x.p + (int64_t)(p.k0 + first) * x.ts + h * x.hs), x.ts * 2 * KEYS, limit - first};
     };
-    Feed key_feed = feed(a.k), value_feed = feed(a.v);
     mx4_u4 kept[DMA ? 1 : 2 * LOADS];
     auto request = [&](bool of_keys, Feed &f, uint32_t slot) {
         const int n = f.left < 0 ? 0 : f.left < KEYS ? f.left : KEYS;
@@ -256,11 +258,15 @@ hlq_attn_prompt_kernel(const Prompt a)
     };
 
     float16v acc[DS];
-    float base = 0.f, most = NONE, total = 0.f;   // most: scores up to it need no new base
+    float base, most, total;   // most: scores up to it need no new base
+    const auto clear = [&]() {
+        base = 0.f, most = NONE, total = 0.f;
 #pragma unroll
-    for (int j = 0; j < DS; ++j)
+        for (int j = 0; j < DS; ++j)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
+            for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
+    };
+    clear();
     // steps of which every query of the wavefront sees every key
     const int last_place = first_place + own_rows - 1;
     int full_end = p.n_k;
@@ -283,12 +289,11 @@ hlq_attn_prompt_kernel(const Prompt a)
 #pragma unroll
             for (int u = 0; u < 2; ++u) acc[j] = multiply(value(slot, j, u), weight[u], acc[j]);
     };
-    // values that are numbers as above; +infinity, and -infinity, and NaN as both, once for each query that sees one
-    auto multiply_odd_values = [&](const F (&weight)[2], int step, uint32_t slot) {
+    // values that are numbers as above; +infinity, and -infinity, and NaN as both, once for each query that sees one (`present`: the lane's keys that do)
+    auto multiply_odd_values = [&](const F (&weight)[2], uint32_t present, uint32_t slot) {
         F sees[2];
-        const Seen seen = seen_of(step);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sees[i >> 3][i & 7] = (S)(seen(offset_of(i)) ? 1.f : 0.f);
+        for (int i = 0; i < 16; ++i) sees[i >> 3][i & 7] = (S)(present >> i & 1u ? 1.f : 0.f);
 #pragma unroll
         for (int j = 0; j < DS; ++j) {
 #pragma unroll
@@ -314,18 +319,6 @@ hlq_attn_prompt_kernel(const Prompt a)
             }
         }
     };
-    auto odd_values = [&](uint32_t slot) {   // whether the tile has values that are no numbers
-        uint32_t found = 0;
-#pragma unroll
-        for (int j = 0; j < DS; ++j)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const mx4_u4 w = __builtin_bit_cast(mx4_u4, value(slot, j, u));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) found |= (w[i] & Fragment<T>::EXPONENT) + Fragment<T>::ONE;
-            }
-        return __any((found & 0x80008000u) != 0u);
-    };
     // sees to it that scores are at most 2^8 times what the exponentials are taken from; `weight`, not yet multiplied, goes by that too
     auto keep_up = [&](const float16v &score, F (&weight)[2]) {
         float m = score[0];
@@ -337,7 +330,7 @@ hlq_attn_prompt_kernel(const Prompt a)
         if (__builtin_expect(__any(m > most), 0)) {
             const bool now = m > most;
             const float to = now ? ceilf(m) - Fragment<T>::LIFT : base;
-            const float keep = !now ? 1.f : most == NONE ? 0.f : __builtin_amdgcn_exp2f(base - to);
+            const float keep = !now || most == NONE ? 1.f : exp2_above_0(base - to);
             base = to;
             most = now ? to + (Fragment<T>::LIFT + 8.f) : most;
             total *= keep;
@@ -362,13 +355,18 @@ hlq_attn_prompt_kernel(const Prompt a)
         for (int i = 0; i < 16; i += 2) two_exponentials(score, weight, i);
     };
 
-    if (all_begin < all_end) {
+    // The first pass looks at no value.  What an infinite or NaN value makes of the weights of those that do not see it, 0 times itself, shows as NaN; then the workgroup takes a
+    // careful one, which looks at each tile, and adds infinities by counting for who sees them: with a score above -infinity, however small the weight.
+    const auto pass = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
         // Step t multiplies the keys of t + 1 and the values of t - 1, takes the exponentials of t, and requests the keys of t + 3 and the values of t + 1.
         // Three slots of each: t's is `here`, t + 1's `ahead`, t - 1's `behind`.
         constexpr uint32_t OF_VALUES = STAGES * TILE;
+        Feed key_feed = feed(a.k), value_feed = feed(a.v);
         uint32_t here = 2 * TILE, ahead = 0, behind = TILE;
         float16v score;
         F weight[2];
+        uint32_t present = 0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) score[i] = 0.f, weight[i >> 3][i & 7] = (S)0.f;
         // queries, the second operand: whole rows by way of the slots that nothing is in yet, with their pieces as a key's
@@ -463,7 +461,7 @@ hlq_attn_prompt_kernel(const Prompt a)
         // most of a long prompt: nothing to mask, nothing to look at
         const int hot_begin = begin + 1 > full_begin + 1 ? begin + 1 : full_begin + 1, hot_end = end - 1 < full_end ? end - 1 : full_end;
         while (t <= all_end) {
-            if (t >= hot_begin && t + 1 < hot_end) {
+            if (!CAREFUL && t >= hot_begin && t + 1 < hot_end) {
                 do {
                     float16v next;
                     F later[2];
@@ -484,8 +482,11 @@ hlq_attn_prompt_kernel(const Prompt a)
                 continue;
             }
             const bool ask = t + 1 >= begin && t + 1 < end, weigh = t >= begin && t < end, sum = t - 1 >= begin && t - 1 < end;
+            // a careful pass scales and adds in the order of the first, so that results are the same bits
+            const bool was_hot = CAREFUL && t >= hot_begin && t - ((t - hot_begin) & 1) + 1 < hot_end;
+            if (CAREFUL && was_hot) keep_up(score, weight);
             if (sum) {
-                if (edge(t - 1) && odd_values(OF_VALUES + behind)) multiply_odd_values(weight, t - 1, OF_VALUES + behind);
+                if constexpr (CAREFUL) multiply_odd_values(weight, present, OF_VALUES + behind);
                 else multiply_values(weight, OF_VALUES + behind);
             }
             if (weigh) {
@@ -495,13 +496,35 @@ hlq_attn_prompt_kernel(const Prompt a)
                     for (int i = 0; i < 16; ++i)
                         if (!seen(offset_of(i))) score[i] = NONE;
                 }
-                keep_up(score, weight);
+                if (!CAREFUL || !was_hot) keep_up(score, weight);
+                if constexpr (CAREFUL) {
+                    present = 0;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) present |= (uint32_t)(score[i] > NONE) << i;
+                }
                 exponentials(score, weight);
             }
             if (ask) multiply_keys(score, ahead);
             advance();
         }
         if constexpr (DMA) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
+    if (all_begin < all_end) {
+        __shared__ int found[WAVES];
+        pass(std::false_type());
+        bool odd = !(total < __builtin_inff());
+#pragma unroll
+        for (int j = 0; j < DS; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) odd = odd || __builtin_isunordered(acc[j][i], acc[j][i + 1]);
+        const bool any = __any(odd && col < own_rows);
+        if (lane == 0) found[wave] = any;
+        __syncthreads();
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(found[0] | found[1] | found[2] | found[3]), 0)) {
+            clear();
+            pass(std::true_type());
+            __syncthreads();
+        }
     }
     if (active > 1) {
         // Cut: sums, and the base and total, past the XCD's own L2 (device-scope stores, complete before the arrival is counted); whoever is last adds the
@@ -534,7 +557,7 @@ hlq_attn_prompt_kernel(const Prompt a)
             for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
         for (int c = 0; c < active; ++c) {
             const uint64_t of = from(c, PAIRS - 1);
-            const float weight = __builtin_amdgcn_exp2f(as_float((uint32_t)of) - highest);
+            const float weight = exp2_above_0(as_float((uint32_t)of) - highest);
             total = fmaf(weight, as_float((uint32_t)(of >> 32)), total);
             constexpr int AT_ONCE = DS < 4 ? DS : 4;   // of 32 columns, on their way together
 #pragma unroll
@@ -560,10 +583,10 @@ hlq_attn_prompt_kernel(const Prompt a)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[j][i] = all == 0.f ? 0.f : acc[j][i];
     }
-    // by way of LDS, so that whole rows leave
+    // by way of LDS, so that whole rows leave (nothing of the tiles is read any more)
     constexpr int TURN = PIECES < 16 ? PIECES - 1 : 15;
     char *const mine = lds + wave * 32 * ROW;
-    __syncthreads();
+    if (active > 1) __syncthreads();   // (else one stands behind the last tile)
 #pragma unroll
     for (int j = 0; j < DS; ++j)
 #pragma unroll
