@@ -12,7 +12,7 @@
 // end adds their sums in order (hand-over by device-scope stores and a counter), so results do not depend on which is last.
 // Weights are two terms of 16 bits (the second product runs twice: it waits for memory anyway), so that p is not rounded to 8 bits.  8- and 4-bit
 // values become bf16, which holds them and their scale exactly (from 2^-126 up); f16 queries are two bf16 terms then.
-// A wavefront that ends with a NaN goes through its tiles once more, multiplies without the values that are infinite or NaN, and adds what they do to those that see them by counting.
+// A wavefront that ends with a NaN, or with scores so large that their rounding is felt, goes through its tiles once more, multiplies without the values that are infinite or NaN, and adds what they do to those that see them by counting.
 // Keys' rows are asked for in lines of 128 bytes, and rows are not kept in the caches: by 64 bytes of each of 16 rows, and kept, 64 x 4096 tokens took 204 us for 184.
 // What bounds it: memory.  64 sequences of 4096 tokens, 8 heads of 128 with 64 queries: 16 bits 184 to 188 us = 5.7 to 5.8 TB/s (a plain read reaches 6.9), 8 bits 112 to 117 = 4.8, 4 bits
 // 65 to 68 = 4.3; the fewer bits a tile has, the less of it is on its way (a wavefront has one tile, 17, 8.5 or 4.4 KB; two tiles a wavefront, or fewer registers and four
@@ -84,9 +84,6 @@ __device__ __forceinline__ float over_lanes_sum(float v)
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 // what a maximum is subtracted as: where nothing was seen, or only -infinity, 0, so that no difference is NaN
 __device__ __forceinline__ float base_of(float m) { return m == NONE ? 0.f : m; }
-
-// what sums are multiplied by: not 0, so that an infinite sum stays one; what 2^-126 leaves of a finite one is far below a rounding
-__device__ __forceinline__ float exp2_above_0(float v) { return fmaxf(__builtin_amdgcn_exp2f(v), 0x1p-126f); }
 
 // adds +infinity, -infinity, or for a NaN both to the sums of the heads that have its token in `present`
 template <class F>
@@ -379,7 +376,7 @@ hlq_attn_decode_kernel(const Decode a)
                 F p, rest;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float w = __builtin_amdgcn_exp2f(fmaf(x[e], a.scale, -base));
+                    const float w = __builtin_amdgcn_exp2f(CAREFUL ? above_base(x[e], a.scale, base) : fmaf(x[e], a.scale, -base));
                     total += w;
                     p[e] = (S)w;
                     rest[e] = (S)((w - (float)p[e]) * REST);
@@ -472,7 +469,7 @@ hlq_attn_decode_kernel(const Decode a)
         }
     };
     pass(std::false_type());
-    bool odd = !(total < __builtin_inff());
+    bool odd = !(total < __builtin_inff()) || fabsf(base) >= LARGE;
 #pragma unroll
     for (int j = 0; j < E; ++j) odd = odd || __builtin_isunordered(acc[j][0], acc[j][1]) || __builtin_isunordered(acc[j][2], acc[j][3]);
     if (__builtin_expect(__any(odd), 0)) pass(std::true_type());

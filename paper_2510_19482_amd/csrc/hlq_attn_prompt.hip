@@ -11,8 +11,8 @@
 // side within a wavefront.  Most steps mask nothing and look at nothing; they have a loop of their own.
 // The maximum that exponentials are taken from is kept while no score passes it by 2^8, and is a whole power of two: so sums are rarely multiplied, and exactly.
 // Weights are rounded once, to the inputs' type, for the second product; their sum is of the rounded ones, so that a result is a true mean of values.
-// What is not seen: its score is -infinity, its weight 0.  A value that is infinite or NaN would still enter as 0 times itself: a workgroup that ends with a NaN goes
-// through its tiles once more, multiplies without such values, and adds what they do to those that see them by counting.
+// What is not seen: its score is -infinity, its weight 0.  A value that is infinite or NaN would still enter as 0 times itself: a workgroup that ends with a NaN (or with scores
+// so large that their rounding is felt) goes through its tiles once more, multiplies without such values, and adds what they do to those that see them by counting.
 // Rows that do not begin at multiples of 16 bytes go to LDS by way of registers (8192 tokens 610 -> 870 us, dim 256,
 // where that spills, three times as long).
 //
@@ -33,9 +33,6 @@ typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef short short4v __attribute__((ext_vector_type(4)));
-
-// what sums are multiplied by: not 0, so that an infinite sum stays one; what 2^-126 leaves of a finite one is far below a rounding
-__device__ __forceinline__ float exp2_above_0(float v) { return fmaxf(__builtin_amdgcn_exp2f(v), 0x1p-126f); }
 
 struct Prompt {
     int B, H, group, D;
@@ -344,15 +341,16 @@ hlq_attn_prompt_kernel(const Prompt a)
                 for (int e = 0; e < 8; ++e) weight[u][e] = (S)((float)weight[u][e] * keep);
         }
     };
-    auto two_exponentials = [&](const float16v &score, F (&weight)[2], int i) {
-        const S w0 = (S)__builtin_amdgcn_exp2f(fmaf(score[i], a.scale, -base)), w1 = (S)__builtin_amdgcn_exp2f(fmaf(score[i + 1], a.scale, -base));
+    auto two_exponentials = [&](const float16v &score, F (&weight)[2], int i, auto careful) {
+        const auto of = [&](float x) { return (S)__builtin_amdgcn_exp2f(decltype(careful)::value ? above_base(x, a.scale, base) : fmaf(x, a.scale, -base)); };
+        const S w0 = of(score[i]), w1 = of(score[i + 1]);
         weight[i >> 3][i & 7] = w0;
         weight[i >> 3][(i & 7) + 1] = w1;
         total = add_pair(w0, w1, total);
     };
-    auto exponentials = [&](const float16v &score, F (&weight)[2]) {
+    auto exponentials = [&](const float16v &score, F (&weight)[2], auto careful) {
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) two_exponentials(score, weight, i);
+        for (int i = 0; i < 16; i += 2) two_exponentials(score, weight, i, careful);
     };
 
     // The first pass looks at no value.  What an infinite or NaN value makes of the weights of those that do not see it, 0 times itself, shows as NaN; then the workgroup takes a
@@ -430,7 +428,7 @@ hlq_attn_prompt_kernel(const Prompt a)
             if constexpr (DP <= 128) {
                 multiply_keys(next, ahead);
                 multiply_values(weight, OF_VALUES + behind);
-                exponentials(score, later);
+                exponentials(score, later, careful);
             } else {
                 constexpr int FOURS = KS / 4;
                 F read[2][4];
@@ -453,7 +451,7 @@ hlq_attn_prompt_kernel(const Prompt a)
                             sum = multiply(read[n & 1][e], weight[e & 1], sum);
                         }
                     }
-                    two_exponentials(score, later, 2 * n);
+                    two_exponentials(score, later, 2 * n, careful);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -502,7 +500,7 @@ hlq_attn_prompt_kernel(const Prompt a)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) present |= (uint32_t)(score[i] > NONE) << i;
                 }
-                exponentials(score, weight);
+                exponentials(score, weight, careful);
             }
             if (ask) multiply_keys(score, ahead);
             advance();
@@ -512,7 +510,7 @@ hlq_attn_prompt_kernel(const Prompt a)
     if (all_begin < all_end) {
         __shared__ int found[WAVES];
         pass(std::false_type());
-        bool odd = !(total < __builtin_inff());
+        bool odd = !(total < __builtin_inff()) || fabsf(base) >= LARGE;
 #pragma unroll
         for (int j = 0; j < DS; ++j)
 #pragma unroll

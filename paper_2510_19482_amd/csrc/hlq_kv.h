@@ -53,6 +53,18 @@ static inline hlq_status hlq_check_rows(const void *p, int64_t T, int heads, int
 __device__ __forceinline__ float as_float(uint32_t v) { return __builtin_bit_cast(float, v); }
 __device__ __forceinline__ uint32_t as_bits(float v) { return __builtin_bit_cast(uint32_t, v); }
 
+// Softmax of both attention kernels.  What sums are multiplied by: not 0, so that an infinite sum stays one; what 2^-126 leaves of a finite one is far below a rounding
+__device__ __forceinline__ float exp2_above_0(float v) { return fmaxf(__builtin_amdgcn_exp2f(v), 0x1p-126f); }
+// A base is the largest product with the scale, rounded.  From 2^22 on that rounding is felt, later it is more than an exponential holds: there the other products are rounded
+// likewise before the base is taken away, so that the largest has its weight.  (At most 2^15.9, which f16 holds: the allowance of 2^8 is itself rounded there.)
+constexpr float LARGE = 0x1p22f;
+__device__ __forceinline__ float above_base(float x, float scale, float base)
+{
+#pragma clang fp contract(off)
+    const float product = x * scale, far = product - base, v = fabsf(base) < LARGE ? __builtin_fmaf(x, scale, -base) : far;
+    return v > 15.9f ? 15.9f : v;   // (a NaN stays)
+}
+
 // storage type of a cache's values
 template <int T> struct KvType { using type = uint8_t; };
 template <> struct KvType<HLQ_F16> { using type = _Float16; };
