@@ -378,7 +378,8 @@ HLQ_API hlq_status hlq_expert_combine(int64_t T, int32_t k, int32_t D, int64_t R
  *
  * Rows of heads: an array [T, heads, dim] whose last axis is contiguous; the other two have strides in elements, `ts` (from token to
  * token) and `hs` (from head to head), so that q, k and v may be parts of one projection's rows, or stand head by head.  Strides are 0 or
- * more, any alignment of the type; an output's rows may not overlap each other.  Types f16, bf16 and f32 (attention: f16 and bf16).
+ * more, any alignment of the type; an output's rows may not overlap each other, nor an input's (HLQ_ERR_BAD_STRIDE: exact for arrays of one token
+ * stride, such as parts of one projection's rows), unless output and input are one array, of the same strides: y and x, k_out and k, q_out and q, out and q of attention.  Types f16, bf16 and f32 (attention: f16 and bf16).
  * Limits: dim a multiple of 8 up to 256, heads <= 1024, T < 2^31 (prompts: < 2^30).  The conventions at the top of this file hold. */
 
 /* Rotary positions: of each head's first `dims` values (even, at most dim) pairs are turned by position * frequency,
@@ -395,7 +396,7 @@ typedef struct {
 } hlq_rotary_desc;
 HLQ_API hlq_status hlq_rotary_turns(int32_t pairs, const double *frequencies, uint64_t *turns);
 
-/* y = x turned by positions [T] (int32); y = x, with the same strides, is allowed. */
+/* y = x turned by positions [T] (int32). */
 HLQ_API hlq_status hlq_rotary(const hlq_rotary_desc *r, int64_t T, int32_t heads, int32_t dim, hlq_dtype type, const int32_t *positions, const void *x,
                               int64_t x_ts, int64_t x_hs, void *y, int64_t y_ts, int64_t y_hs, void *stream);
 

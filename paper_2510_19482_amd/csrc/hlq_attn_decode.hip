@@ -698,6 +698,7 @@ hlq_status hlq_attn_decode(const hlq_kv_desc *c, const void *cache, size_t cache
         if ((uintptr_t)ws & 15u) return HLQ_ERR_BAD_STRIDE;
         if (ws_bytes < s.bytes) return HLQ_ERR_BUFFER_TOO_SMALL;
     }
+    if (hlq_rows_in_the_way(hlq_span(q, B, q_heads, q_ts, q_hs, type), hlq_span(out, B, q_heads, o_ts, o_hs, otype), s.d.D)) return HLQ_ERR_BAD_STRIDE;
     Decode a{};
     a.kv = hlq_kv_view(s.d, cache);
     a.D = s.d.D;

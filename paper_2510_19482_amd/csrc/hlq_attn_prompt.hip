@@ -686,6 +686,10 @@ hlq_status hlq_attn_prompt(int32_t B, int32_t q_heads, int32_t heads, int32_t di
         if ((uintptr_t)ws & 15u) return HLQ_ERR_BAD_STRIDE;
         if (ws_bytes < shape.bytes) return HLQ_ERR_BUFFER_TOO_SMALL;
     }
+    const KvSpan to = hlq_span(out, Tq, q_heads, o_ts, o_hs, type);
+    if (hlq_rows_in_the_way(hlq_span(q, Tq, q_heads, q_ts, q_hs, type), to, dim) || hlq_rows_overlap(hlq_span(k, Tk, heads, k_ts, k_hs, type), to, dim) ||
+        hlq_rows_overlap(hlq_span(v, Tk, heads, v_ts, v_hs, type), to, dim))
+        return HLQ_ERR_BAD_STRIDE;
     Prompt a{};
     a.B = B;
     a.H = heads;

@@ -49,6 +49,55 @@ static inline hlq_status hlq_check_rows(const void *p, int64_t T, int heads, int
     return (uintptr_t)p % (unsigned)hlq_dtype_bytes(type) ? HLQ_ERR_BAD_STRIDE : HLQ_OK;
 }
 
+// An array [T, heads, dim] whose elements have `bytes`.
+struct KvSpan {
+    KvRows x;
+    int64_t T;
+    int heads, bytes;
+};
+static inline KvSpan hlq_span(const void *p, int64_t T, int heads, int64_t ts, int64_t hs, hlq_dtype type)
+{
+    return KvSpan{KvRows{const_cast<void *>(p), ts, hs}, T, heads, hlq_dtype_bytes(type)};
+}
+// Whether two of them share memory.  Exact where strides from token to token are the same, so that parts of one projection's rows stand apart; else a head's rows are taken as one
+// piece if strides from head to head are the same, or all of an array.
+static inline bool hlq_rows_overlap(const KvSpan &a, const KvSpan &b, int dim)
+{
+    if (a.T < 1 || b.T < 1 || !a.x.p || !b.x.p) return false;
+    const int64_t far = (int64_t)((uintptr_t)b.x.p - (uintptr_t)a.x.p);
+    const int64_t ats = a.x.ts * a.bytes, bts = b.x.ts * b.bytes, ahs = a.x.hs * a.bytes, bhs = b.x.hs * b.bytes, arow = (int64_t)dim * a.bytes, brow = (int64_t)dim * b.bytes;
+    // [at, at + n), moved by some of low .. high periods, and [bt, bt + m)
+    const auto meet = [](int64_t at, int64_t n, int64_t bt, int64_t m, int64_t period, int64_t low, int64_t high) {
+        int64_t k = 0;
+        if (period > 0) {
+            const int64_t room = bt + m - 1 - at;   // the furthest that it begins before [bt, bt + m) ends
+            k = room / period - (room % period < 0);
+            k = k > high ? high : k;
+            if (k < low) return false;
+        }
+        return at + k * period < bt + m && bt < at + k * period + n;
+    };
+    typedef __int128 Wide;
+    const Wide aend = (Wide)(a.T - 1) * ats + (a.heads - 1) * ahs + arow, bend = (Wide)(b.T - 1) * bts + (b.heads - 1) * bhs + brow;
+    if (far >= aend || -(Wide)far >= bend) return false;
+    const int64_t period = a.T > 1 ? ats : bts;
+    if (a.T == 1 || b.T == 1 || ats == bts) {
+        const auto rows = [&](int64_t at, int64_t n, int64_t bt, int64_t m) { return meet(at, n, bt, m, period, 1 - b.T, a.T - 1); };
+        if (!rows(0, (a.heads - 1) * ahs + arow, far, (b.heads - 1) * bhs + brow)) return false;
+        for (int i = 0; i < a.heads; ++i)
+            for (int j = 0; j < b.heads; ++j)
+                if (rows(i * ahs, arow, far + j * bhs, brow)) return true;
+        return false;
+    }
+    return ahs != bhs || meet(0, (a.T - 1) * ats + arow, far, (b.T - 1) * bts + brow, ahs, 1 - b.heads, a.heads - 1);
+}
+// An output may be where the input is that it is made of, row for row, or where nothing of it is.
+static inline bool hlq_rows_in_the_way(const KvSpan &in, const KvSpan &out, int dim)
+{
+    const bool same = in.x.p == out.x.p && in.T == out.T && in.heads == out.heads && in.bytes == out.bytes && (in.T == 1 || in.x.ts == out.x.ts) && (in.heads == 1 || in.x.hs == out.x.hs);
+    return !same && hlq_rows_overlap(in, out, dim);
+}
+
 // By value: a bit cast of a vector's element reads the vector's first.
 __device__ __forceinline__ float as_float(uint32_t v) { return __builtin_bit_cast(float, v); }
 __device__ __forceinline__ uint32_t as_bits(float v) { return __builtin_bit_cast(uint32_t, v); }

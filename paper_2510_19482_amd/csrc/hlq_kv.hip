@@ -442,6 +442,7 @@ hlq_status hlq_rotary(const hlq_rotary_desc *r, int64_t T, int32_t heads, int32_
     if (T == 0) return HLQ_OK;
     if ((s = hlq_check_rows(x, T, heads, dim, x_ts, x_hs, type, false)) != HLQ_OK) return s;
     if ((s = hlq_check_rows(y, T, heads, dim, y_ts, y_hs, type, true)) != HLQ_OK) return s;
+    if (hlq_rows_in_the_way(hlq_span(x, T, heads, x_ts, x_hs, type), hlq_span(y, T, heads, y_ts, y_hs, type), dim)) return HLQ_ERR_BAD_STRIDE;
     Rows a{};
     a.T = T;
     a.D = dim;
@@ -474,6 +475,11 @@ hlq_status hlq_kv_write(const hlq_kv_desc *c, void *cache, size_t cache_bytes, i
         if ((s = hlq_check_rows(q, T, q_heads, d.D, q_ts, q_hs, type, false)) != HLQ_OK) return s;
         if ((s = hlq_check_rows(q_out, T, q_heads, d.D, qo_ts, qo_hs, type, true)) != HLQ_OK) return s;
     }
+    const KvSpan ki = hlq_span(k, T, d.H, k_ts, k_hs, type), vi = hlq_span(v, T, d.H, v_ts, v_hs, type), ko = hlq_span(k_out, T, d.H, ko_ts, ko_hs, type);
+    const KvSpan qi = hlq_span(q_heads > 0 ? q : nullptr, T, q_heads, q_ts, q_hs, type), qo = hlq_span(q_heads > 0 ? q_out : nullptr, T, q_heads, qo_ts, qo_hs, type);
+    if (hlq_rows_in_the_way(ki, ko, d.D) || hlq_rows_in_the_way(qi, qo, d.D) || hlq_rows_overlap(vi, ko, d.D) || hlq_rows_overlap(qi, ko, d.D) || hlq_rows_overlap(ki, qo, d.D) ||
+        hlq_rows_overlap(vi, qo, d.D) || hlq_rows_overlap(ko, qo, d.D))
+        return HLQ_ERR_BAD_STRIDE;
     Rows a{};
     a.T = T;
     a.D = d.D;
@@ -503,6 +509,7 @@ hlq_status hlq_kv_read(const hlq_kv_desc *c, const void *cache, size_t cache_byt
     if ((uintptr_t)slots & 7u) return HLQ_ERR_BAD_STRIDE;
     if (k && (s = hlq_check_rows(k, T, d.H, d.D, k_ts, k_hs, type, true)) != HLQ_OK) return s;
     if (v && (s = hlq_check_rows(v, T, d.H, d.D, v_ts, v_hs, type, true)) != HLQ_OK) return s;
+    if (hlq_rows_overlap(hlq_span(k, T, d.H, k_ts, k_hs, type), hlq_span(v, T, d.H, v_ts, v_hs, type), d.D)) return HLQ_ERR_BAD_STRIDE;
     Read a{};
     a.T = T;
     a.H = d.H;
