@@ -37,7 +37,7 @@ __device__ __forceinline__ void sine_of(uint64_t turn, double m, double &s, doub
 {
     const uint32_t quarter = (uint32_t)((turn + ((uint64_t)1 << 61)) >> 62);
     const int64_t rest = (int64_t)(turn - ((uint64_t)quarter << 62));       // an eighth of a turn to either side
-    const double x = (double)rest * 3.4061215800304444e-19, z = x * x;      // 2 pi / 2^64
+    const double x = (double)rest * 3.4061215800865545e-19, z = x * x;      // 2 pi / 2^64
     // z^n / (2 n + 1)! and z^n / (2 n)!, signs in turn; what is left out is below 5e-17 and 2e-18 at pi / 4
     double a = -1. / 1307674368000.;
     a = fma(a, z, 1. / 6227020800.);
