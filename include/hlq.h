@@ -391,7 +391,7 @@ HLQ_API hlq_status hlq_expert_combine(int64_t T, int32_t k, int32_t D, int64_t R
  * A frequency that is not finite or of 2^32 and more: HLQ_ERR_BAD_DESC. */
 typedef struct {
     int32_t dims, interleaved;
-    float magnitude;
+    double magnitude;
     const uint64_t *turns;
 } hlq_rotary_desc;
 HLQ_API hlq_status hlq_rotary_turns(int32_t pairs, const double *frequencies, uint64_t *turns);

@@ -35,7 +35,7 @@ class HlqKvDesc(ctypes.Structure):
 
 
 class HlqRotaryDesc(ctypes.Structure):
-    _fields_ = [("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float), ("turns", ctypes.c_void_p)]
+    _fields_ = [("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_double), ("turns", ctypes.c_void_p)]
 
 
 class HlqError(RuntimeError):
