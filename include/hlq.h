@@ -439,7 +439,7 @@ HLQ_API hlq_status hlq_kv_read(const hlq_kv_desc *c, const void *cache, size_t c
  * 2^-126 may count as 0), sums fp32, scores fp32 numbers of any size; p is held to 2^-16 of itself (f16 caches: 2^-22, and 2^-42 of the largest).
  * Results do not depend on the order in which workgroups end.
  * ws: of hlq_attn_decode_workspace_bytes() (host-only; enough for smaller B and table_width too), seen by hlq_workspace_init once; calls that may run at
- * the same time need one each. */
+ * the same time need one each.  NULL is enough where the launch is not cut over the tokens, else HLQ_ERR_NULL. */
 HLQ_API hlq_status hlq_attn_decode_workspace_bytes(const hlq_kv_desc *c, int32_t q_heads, int64_t B, int32_t table_width, size_t *bytes);
 HLQ_API hlq_status hlq_attn_decode(const hlq_kv_desc *c, const void *cache, size_t cache_bytes, int32_t q_heads, int64_t B, hlq_dtype type, const void *q,
                                    int64_t q_ts, int64_t q_hs, const int32_t *table, int64_t ld_table, int32_t table_width, const int32_t *lengths,

@@ -12,6 +12,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("HLQ_LIB", os.path.join(_PKG, "libhlq.so"))
 
 HLQ_OK = 0
+HLQ_ERR_NULL = 1
 HLQ_OUT_F16 = 0
 HLQ_OUT_F32 = 1
 
@@ -978,6 +979,11 @@ def _workspace_on(device: int, nbytes: int, stream):
     return ws
 
 
+def _given(ws) -> tuple:
+    """Address and size of a workspace, or of none."""
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
+
+
 def alloc_decode_workspace(cache: KvCache, q_heads: int, batch: int, table_width: int, stream=None):
     """Workspace of hlq_attn_decode for up to `batch` sequences of up to `table_width` pages."""
     if cache._device < 0:
@@ -1006,16 +1012,16 @@ def hlq_attn_decode(cache: KvCache, q, table, lengths, out=None, scale: float | 
     width = table.shape[1]
     counts = _numbers("lengths", lengths, torch.int32, B)
     device = cache._device
-    if ws is None:
-        ws = alloc_decode_workspace(cache, Hq, B, width, stream)
     if (device < 0 or q.get_device() != device or out.get_device() != device or table.get_device() != device or lengths.get_device() != device
-            or ws.get_device() != device):
-        raise _not_on_gpu(cache, q, out, table, lengths, ws)
+            or (ws is not None and ws.get_device() != device)):
+        raise _not_on_gpu(*(t for t in (cache, q, out, table, lengths, ws) if t is not None))
     if device != _current_device():
         return _there(device, hlq_attn_decode, cache, q, table, lengths, out, scale, window, None, ws, stream)
     blob = cache.blob
     status = lib.hlq_attn_decode(cache._desc, blob.data_ptr(), blob.numel(), Hq, B, qtype, qp, qt, qh, table.data_ptr(), table.stride(0) if B > 1 else width, width, counts,
-                                 window, D ** -0.5 if scale is None else scale, op, otype, ot, oh, ws.data_ptr(), ws.numel(), _stream_of(stream, device))
+                                 window, D ** -0.5 if scale is None else scale, op, otype, ot, oh, *_given(ws), _stream_of(stream, device))
+    if status == HLQ_ERR_NULL and ws is None:   # cut over the tokens: its parts meet in a workspace
+        return hlq_attn_decode(cache, q, table, lengths, out, scale, window, None, alloc_decode_workspace(cache, Hq, B, width, stream), stream)
     if status != HLQ_OK:
         raise HlqError("hlq_attn_decode", status)
     return out
@@ -1040,15 +1046,16 @@ def hlq_attn_prompt(q, k, v, q_offsets, k_offsets=None, out=None, causal: bool =
         raise ValueError("q_offsets: one more than sequences")
     q_at, k_at = _numbers("q_offsets", q_offsets, torch.int32, n), _numbers("k_offsets", k_offsets, torch.int32, n)
     device = q.get_device()
-    if ws is None and device >= 0:
-        ws = _workspace_on(device, prompt_workspace_bytes(Tq, Tk, n - 1, Hq, H, D), stream)
     if (device < 0 or k.get_device() != device or v.get_device() != device or q_offsets.get_device() != device or k_offsets.get_device() != device
-            or out.get_device() != device or ws.get_device() != device):
+            or out.get_device() != device or (ws is not None and ws.get_device() != device)):
         raise _not_on_gpu(*(t for t in (q, k, v, q_offsets, k_offsets, out, ws) if t is not None))
     if device != _current_device():
         return _there(device, hlq_attn_prompt, q, k, v, q_offsets, k_offsets, out, causal, window, scale, ws, stream)
     status = lib.hlq_attn_prompt(n - 1, Hq, H, D, dtype, Tq, qp, qt, qh, Tk, kp, kt, kh, vp, vt, vh, q_at, k_at, 1 if causal else 0, window,
-                                 D ** -0.5 if scale is None else scale, op, ot, oh, ws.data_ptr(), ws.numel(), _stream_of(stream, device))
+                                 D ** -0.5 if scale is None else scale, op, ot, oh, *_given(ws), _stream_of(stream, device))
+    if status == HLQ_ERR_NULL and ws is None:   # cut over the keys: its parts meet in a workspace
+        ws = _workspace_on(device, prompt_workspace_bytes(Tq, Tk, n - 1, Hq, H, D), stream)
+        return hlq_attn_prompt(q, k, v, q_offsets, k_offsets, out, causal, window, scale, ws, stream)
     if status != HLQ_OK:
         raise HlqError("hlq_attn_prompt", status)
     return out
