@@ -929,29 +929,31 @@ def hlq_kv_write(cache: KvCache, k, v, slots, rotary: Rotary | None = None, posi
     return q_out
 
 
-def hlq_kv_read(cache: KvCache, slots, k=None, v=None, dtype=None, stream=None):
+def hlq_kv_read(cache: KvCache, slots, k=None, v=None, dtype=None, stream=None, only: str | None = None):
     """(k, v) [T, heads, dim] from slots [T] (int64) of the cache, in the tensors given or new ones of `dtype` (f32 by default); a row whose slot is outside the
-    cache stays as it was."""
+    cache stays as it was.  only="k" or "v": keys or values alone, the other is None."""
     T = slots.numel()
     at = _numbers("slots", slots, torch.int64, T)
     shape = (T, cache.heads, cache.dim)
+    if only not in (None, "k", "v") or (only == "k" and v is not None) or (only == "v" and k is not None):
+        raise ValueError(f'only {only!r}: "k" without v, or "v" without k')
     if dtype is None:
         dtype = k.dtype if k is not None else v.dtype if v is not None else torch.float32
-    if k is None:
+    if k is None and only != "v":
         k = _empty(shape, dtype, cache.blob.device, stream)
-    if v is None:
+    if v is None and only != "k":
         v = _empty(shape, dtype, cache.blob.device, stream)
-    kT, kH, kD, kp, ktype, kt, kh = _heads(k)
-    vT, vH, vD, vp, vtype, vt, vh = _heads(v)
+    kT, kH, kD, kp, ktype, kt, kh = _heads(k if k is not None else v)
+    vT, vH, vD, vp, vtype, vt, vh = _heads(v if v is not None else k)
     if (kT, kH, kD) != shape or (vT, vH, vD) != shape or ktype != vtype:
-        raise ValueError(f"k is {k.dtype} {tuple(k.shape)}, v {v.dtype} {tuple(v.shape)}, the rows are {shape}")
+        raise ValueError(f"k and v are {[(t.dtype, tuple(t.shape)) for t in (k, v) if t is not None]}, the rows are {shape}")
     device = cache._device
-    if device < 0 or slots.get_device() != device or k.get_device() != device or v.get_device() != device:
-        raise _not_on_gpu(cache, slots, k, v)
+    if device < 0 or slots.get_device() != device or (k is not None and k.get_device() != device) or (v is not None and v.get_device() != device):
+        raise _not_on_gpu(*(t for t in (cache, slots, k, v) if t is not None))
     if device != _current_device():
-        return _there(device, hlq_kv_read, cache, slots, k, v, None, stream)
+        return _there(device, hlq_kv_read, cache, slots, k, v, None, stream, only)
     blob = cache.blob
-    status = lib.hlq_kv_read(cache._desc, blob.data_ptr(), blob.numel(), T, at, ktype, kp, kt, kh, vp, vt, vh, _stream_of(stream, device))
+    status = lib.hlq_kv_read(cache._desc, blob.data_ptr(), blob.numel(), T, at, ktype, None if k is None else kp, kt, kh, None if v is None else vp, vt, vh, _stream_of(stream, device))
     if status != HLQ_OK:
         raise HlqError("hlq_kv_read", status)
     return k, v

@@ -51,6 +51,6 @@ def test_a_call_without_one():
     out = torch.empty_like(q)
     assert taken(lambda: B.hlq_attn_decode(kv, q, table, lengths, out=out)) == 0
     assert (out == 0).all()
-    one = table.view(1, -1).contiguous()
-    assert taken(lambda: B.hlq_attn_decode(kv, q[:1], one, lengths[:1] * 512, out=out[:1])) > 0
+    one, n = table.view(1, -1).contiguous(), lengths[:1] * 512
+    assert taken(lambda: B.hlq_attn_decode(kv, q[:1], one, n, out=out[:1])) > 0
     assert (out == 0).all()
