@@ -303,13 +303,11 @@ void cut_heads(int64_t T, int all, int fit, int &parts, int &per_part)
     parts = (all + per_part - 1) / per_part;
 }
 
-bool grid_of(int64_t T, int parts, dim3 &grid)
-{
-    const int64_t blocks = (T * parts + WAVES - 1) / WAVES;
-    if (blocks > ((int64_t)1 << 31) - 1 || blocks * 64 * WAVES >= (int64_t)1 << 32) return false;   // a launch has fewer than 2^32 lanes
-    grid = dim3((unsigned)blocks);
-    return true;
-}
+// A launch has fewer than 2^32 lanes: the tokens of one, and its grid.
+int64_t tokens_of_launch(int parts) { return (((int64_t)1 << 32) / (64 * WAVES) - 1) * WAVES / parts; }
+dim3 grid_of(int64_t T, int parts) { return dim3((unsigned)((T * parts + WAVES - 1) / WAVES)); }
+
+KvRows behind(const KvRows &x, int64_t tokens, int bytes) { return KvRows{x.p ? (char *)x.p + tokens * x.ts * bytes : nullptr, x.ts, x.hs}; }
 
 template <int T>
 void launch_rows(const Rows &a, int cache, dim3 grid, hipStream_t st)
@@ -370,13 +368,21 @@ hlq_status go(Rows &a, int all, int type, int cache, void *stream)
     a.lanes = a.D / 8;
     a.fit = 64 / a.lanes;
     cut_heads(a.T, all, a.fit, a.parts, a.per_part);
-    dim3 grid;
-    if (!grid_of(a.T, a.parts, grid)) return HLQ_ERR_UNSUPPORTED;
+    const int64_t each = tokens_of_launch(a.parts);
+    const int bytes = hlq_dtype_bytes((hlq_dtype)type);
     const hipStream_t st = (hipStream_t)stream;
     hlq_clear_stale_error();
-    if (type == HLQ_F16) launch_rows<HLQ_F16>(a, cache, grid, st);
-    else if (type == HLQ_BF16) launch_rows<HLQ_BF16>(a, cache, grid, st);
-    else launch_rows<HLQ_F32>(a, cache, grid, st);
+    for (int64_t t = 0; t < a.T; t += each) {
+        Rows b = a;
+        b.T = a.T - t < each ? a.T - t : each;
+        b.q = behind(a.q, t, bytes), b.q_out = behind(a.q_out, t, bytes), b.k = behind(a.k, t, bytes), b.k_out = behind(a.k_out, t, bytes), b.v = behind(a.v, t, bytes);
+        if (a.positions) b.positions = a.positions + t;
+        if (a.slots) b.slots = a.slots + t;
+        const dim3 grid = grid_of(b.T, b.parts);
+        if (type == HLQ_F16) launch_rows<HLQ_F16>(b, cache, grid, st);
+        else if (type == HLQ_BF16) launch_rows<HLQ_BF16>(b, cache, grid, st);
+        else launch_rows<HLQ_F32>(b, cache, grid, st);
+    }
     return hlq_hip_status(hipGetLastError());
 }
 
@@ -521,13 +527,20 @@ hlq_status hlq_kv_read(const hlq_kv_desc *c, const void *cache, size_t cache_byt
     a.lanes = d.D / 8;
     a.fit = 64 / a.lanes;
     cut_heads(T, (k && v ? 2 : 1) * d.H, a.fit, a.parts, a.per_part);
-    dim3 grid;
-    if (!grid_of(T, a.parts, grid)) return HLQ_ERR_UNSUPPORTED;
+    const int64_t each = tokens_of_launch(a.parts);
+    const int bytes = hlq_dtype_bytes(type);
     const hipStream_t st = (hipStream_t)stream;
     hlq_clear_stale_error();
-    if (type == HLQ_F16) launch_read<HLQ_F16>(a, d.type, grid, st);
-    else if (type == HLQ_BF16) launch_read<HLQ_BF16>(a, d.type, grid, st);
-    else launch_read<HLQ_F32>(a, d.type, grid, st);
+    for (int64_t t = 0; t < T; t += each) {
+        Read b = a;
+        b.T = T - t < each ? T - t : each;
+        b.slots = slots + t;
+        b.k = behind(a.k, t, bytes), b.v = behind(a.v, t, bytes);
+        const dim3 grid = grid_of(b.T, b.parts);
+        if (type == HLQ_F16) launch_read<HLQ_F16>(b, d.type, grid, st);
+        else if (type == HLQ_BF16) launch_read<HLQ_BF16>(b, d.type, grid, st);
+        else launch_read<HLQ_F32>(b, d.type, grid, st);
+    }
     return hlq_hip_status(hipGetLastError());
 }
 
