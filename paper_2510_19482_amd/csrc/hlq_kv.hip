@@ -187,50 +187,50 @@ hlq_kv_rows_kernel(const Rows a)
             if (h0 + n * a.fit < end) mx4_read8<false>(row_of(h0 + n * a.fit) + d0, every[n]);
 #pragma unroll
         for (int n = 0; n < BATCH; ++n) {
-        const int h = h0 + n * a.fit;
-        if (h >= end) break;
-        V (&v)[8] = every[n];
-        const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + a.kv_heads;
-        const int own_h = is_q ? h : is_v ? h - a.q_heads - a.kv_heads : h - a.q_heads;
-        if (turn && !is_v) {
-            V other[8];
-            if (a.interleaved) {
+            const int h = h0 + n * a.fit;
+            if (h >= end) break;
+            V (&v)[8] = every[n];
+            const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + a.kv_heads;
+            const int own_h = is_q ? h : is_v ? h - a.q_heads - a.kv_heads : h - a.q_heads;
+            if (turn && !is_v) {
+                V other[8];
+                if (a.interleaved) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) other[i] = v[i ^ 1];
-            } else if (a.whole) {
-                using E = Mx4Eight<V>;
-                typename E::Values e;
+                    for (int i = 0; i < 8; ++i) other[i] = v[i ^ 1];
+                } else if (a.whole) {
+                    using E = Mx4Eight<V>;
+                    typename E::Values e;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) e.v[i] = v[i];
-                typename E::Raw raw = __builtin_bit_cast(typename E::Raw, e);
+                    for (int i = 0; i < 8; ++i) e.v[i] = v[i];
+                    typename E::Raw raw = __builtin_bit_cast(typename E::Raw, e);
 #pragma unroll
-                for (int i = 0; i < E::N; ++i)
+                    for (int i = 0; i < E::N; ++i)
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) raw.r[i][w] = (uint32_t)__builtin_amdgcn_ds_bpermute(partner, (int)raw.r[i][w]);
-                e = __builtin_bit_cast(typename E::Values, raw);
+                        for (int w = 0; w < 4; ++w) raw.r[i][w] = (uint32_t)__builtin_amdgcn_ds_bpermute(partner, (int)raw.r[i][w]);
+                    e = __builtin_bit_cast(typename E::Values, raw);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) other[i] = e.v[i];
-            } else {
+                    for (int i = 0; i < 8; ++i) other[i] = e.v[i];
+                } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int d = d0 + i;
-                    other[i] = d >= a.dims ? v[i] : row_of(h)[d < a.half ? d + a.half : d - a.half];
+                    for (int i = 0; i < 8; ++i) {
+                        const int d = d0 + i;
+                        other[i] = d >= a.dims ? v[i] : row_of(h)[d < a.half ? d + a.half : d - a.half];
+                    }
                 }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (d0 + i < a.dims) {
+                        float y = (float)fma((double)(float)other[i], sine[i], (double)(float)v[i] * cosine[i]);
+                        asm("" : "+v"(y));   // by way of f32: from 64 to 16 bits in one step the compiler has ten instructions
+                        v[i] = (V)y;
+                    }
             }
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (d0 + i < a.dims) {
-                    float y = (float)fma((double)(float)other[i], sine[i], (double)(float)v[i] * cosine[i]);
-                    asm("" : "+v"(y));   // by way of f32: from 64 to 16 bits in one step the compiler has ten instructions
-                    v[i] = (V)y;
-                }
-        }
-        if (is_q || (!is_v && a.k_out.p)) {
-            const KvRows &to = is_q ? a.q_out : a.k_out;
-            store_eight(v, (V *)to.p + t * to.ts + own_h * to.hs + d0);
-        }
-        if constexpr (C != NO_CACHE)
-            if (!is_q && slot >= 0) put<C>(a.kv, slot, is_v ? 1 : 0, own_h, chunk, v);
+            if (is_q || (!is_v && a.k_out.p)) {
+                const KvRows &to = is_q ? a.q_out : a.k_out;
+                store_eight(v, (V *)to.p + t * to.ts + own_h * to.hs + d0);
+            }
+            if constexpr (C != NO_CACHE)
+                if (!is_q && slot >= 0) put<C>(a.kv, slot, is_v ? 1 : 0, own_h, chunk, v);
         }
     }
 }
