@@ -996,6 +996,8 @@ def alloc_decode_workspace(cache: KvCache, q_heads: int, batch: int, table_width
 def alloc_prompt_workspace(q_rows: int, k_rows: int, batch: int, q_heads: int, heads: int, dim: int, device="cuda", stream=None):
     """Workspace of hlq_attn_prompt for up to these numbers of rows and sequences."""
     device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError(f"workspaces are on a GPU, not on {device}")
     return _workspace_on(_current_device() if device.index is None else device.index, prompt_workspace_bytes(q_rows, k_rows, batch, q_heads, heads, dim), stream)
 
 

@@ -68,3 +68,8 @@ def test_a_prompts_workspace_serves_smaller_calls():
                     less[i] = below[-1]
                     if tuple(less) in table:
                         assert table[tuple(less)] <= most
+
+
+def test_a_workspace_is_on_a_gpu():
+    with pytest.raises(ValueError, match="on a GPU"):
+        B.alloc_prompt_workspace(5, 5, 1, 4, 2, 64, device="cpu")
