@@ -49,8 +49,8 @@ struct Prompt {
 
 // LIFT: what the largest weight is brought to is 2^(LIFT - 1) to 2^LIFT (2^8 times that while the base is kept).  f16 ends at 2^16 and has steps of 2^-24 at its lower end: there weights
 // stand as high as they can, so that small ones beside a large one count (16384 keys of which 8 have a score that is 17 higher: without it their share, 8.5e-5, is off by 22 to 44 %).
-template <int T> struct Fragment { using type = bf8v; using scalar = __bf16; static constexpr float LIFT = 0.f; };
-template <> struct Fragment<HLQ_F16> { using type = half8v; using scalar = _Float16; static constexpr float LIFT = 7.f; };
+template <int T> struct Fragment { using type = bf8v; using scalar = __bf16; static constexpr uint32_t EXPONENT = 0x7f807f80u, ONE = 0x00800080u; static constexpr float LIFT = 0.f; };
+template <> struct Fragment<HLQ_F16> { using type = half8v; using scalar = _Float16; static constexpr uint32_t EXPONENT = 0x7c007c00u, ONE = 0x04000400u; static constexpr float LIFT = 7.f; };
 
 __device__ __forceinline__ float16v multiply(bf8v a, bf8v b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ float16v multiply(half8v a, half8v b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
@@ -288,32 +288,46 @@ hlq_attn_prompt_kernel(const Prompt a)
     };
     // values that are numbers as above; +infinity, and -infinity, and NaN as both, once for each query that sees one (`present`: the lane's keys that do)
     auto multiply_odd_values = [&](const F (&weight)[2], uint32_t present, uint32_t slot) {
-        F sees[2];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sees[i >> 3][i & 7] = (S)(present >> i & 1u ? 1.f : 0.f);
 #pragma unroll
         for (int j = 0; j < DS; ++j) {
+            F c[2];
+            uint32_t found = 0;
 #pragma unroll
-            for (int sign = 0; sign < 2; ++sign) {
-                float16v count;
+            for (int u = 0; u < 2; ++u) {
+                c[u] = value(slot, j, u);
+                const mx4_u4 w = __builtin_bit_cast(mx4_u4, c[u]);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) count[i] = 0.f;
+                for (int i = 0; i < 4; ++i) found |= (w[i] & Fragment<T>::EXPONENT) + Fragment<T>::ONE;
+            }
+            if (__any((found & 0x80008000u) != 0u)) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    F c = value(slot, j, u), is;
+                for (int sign = 0; sign < 2; ++sign) {
+                    float16v count;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float f = (float)c[e];
-                        is[e] = (S)((sign ? f > NONE : f < __builtin_inff()) ? 0.f : 1.f);
-                        if (!(fabsf(f) < __builtin_inff())) c[e] = (S)0.f;
+                    for (int i = 0; i < 16; ++i) count[i] = 0.f;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        F is, sees;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float f = (float)c[u][e];
+                            is[e] = (S)((sign ? f > NONE : f < __builtin_inff()) ? 0.f : 1.f);
+                            sees[e] = (S)(present >> (8 * u + e) & 1u ? 1.f : 0.f);
+                        }
+                        count = multiply(is, sees, count);
                     }
-                    if (sign == 0) acc[j] = multiply(c, weight[u], acc[j]);
-                    count = multiply(is, sees[u], count);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (count[i] > 0.f) acc[j][i] += sign ? NONE : __builtin_inff();
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (count[i] > 0.f) acc[j][i] += sign ? NONE : __builtin_inff();
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (!(fabsf((float)c[u][e]) < __builtin_inff())) c[u][e] = (S)0.f;
             }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) acc[j] = multiply(c[u], weight[u], acc[j]);
         }
     };
     // sees to it that scores are at most 2^8 times what the exponentials are taken from; `weight`, not yet multiplied, goes by that too
@@ -385,6 +399,7 @@ hlq_attn_prompt_kernel(const Prompt a)
         request(true, key_feed, ahead);
         if constexpr (!DMA) enter(true, ahead);
         request(true, key_feed, behind);
+        if constexpr (!DMA && CAREFUL) enter(true, behind);
         if constexpr (DMA) {
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
 #pragma unroll
@@ -409,11 +424,15 @@ hlq_attn_prompt_kernel(const Prompt a)
                 else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
             } else {
                 __syncthreads();
-                enter(true, behind);
-                if (!first) enter(false, OF_VALUES + here);
+                if constexpr (!CAREFUL) {
+                    enter(true, behind);
+                    if (!first) enter(false, OF_VALUES + here);
+                }
             }
             request(true, key_feed, here);
+            if constexpr (!DMA && CAREFUL) enter(true, here);   // (a careful pass keeps nothing on its way: registers)
             request(false, value_feed, OF_VALUES + ahead);
+            if constexpr (!DMA && CAREFUL) enter(false, OF_VALUES + ahead);
         };
         auto advance = [&]() {
             const uint32_t was = behind;

@@ -7,6 +7,7 @@ import torch
 
 from attn_util import KINDS, TYPES, rng, rounded
 from paper_2510_19482_amd import binding as B
+from test_gpu_attn_corners import shifted
 
 pytestmark = pytest.mark.gpu
 
@@ -78,6 +79,20 @@ def test_prompt(before, Hq, low, D, dtype):
     clean = B.hlq_attn_prompt(q, k, clear(v, odd), q_at, k_at, window=90)
     got = B.hlq_attn_prompt(q, k, put(v, odd), q_at, k_at, window=90)
     same(got, expected(clean, lambda row: (i >= row - before) & (i < row - before + 90), odd))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 72, 128, 256])
+@pytest.mark.parametrize("before,causal", [(0, True), (0, False), (2600, True)])
+def test_prompt_of_rows_at_any_alignment(before, causal, D, dtype):
+    n = 200
+    q, k, v = inputs(rng("infinite, any", before, causal, D, dtype), n, before + n, 2, D, dtype, -25.0)
+    odd = {row + before: x for row, x in ODD.items()}
+    q_at, k_at = (torch.tensor([0, x], dtype=torch.int32, device="cuda") for x in (n, before + n))
+    want = B.hlq_attn_prompt(q, k, put(v, odd), q_at, k_at, causal=causal)
+    clean = B.hlq_attn_prompt(q, k, clear(v, odd), q_at, k_at, causal=causal)
+    same(want, expected(clean, lambda row: torch.arange(n, device="cuda") >= (row - before if causal else 0), odd))
+    same(B.hlq_attn_prompt(shifted(q), shifted(k, 3), shifted(put(v, odd)), q_at, k_at, causal=causal), want)
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])

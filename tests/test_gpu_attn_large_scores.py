@@ -6,6 +6,7 @@ import torch
 
 from attn_util import HALF_STEP, TYPES, rng, rounded
 from paper_2510_19482_amd import binding as B
+from test_gpu_attn_corners import shifted
 
 pytestmark = pytest.mark.gpu
 
@@ -47,6 +48,7 @@ def test_prompt(D, sign, scale, dtype, a, b):
         got = B.hlq_attn_prompt(q.cuda(), k.cuda(), v.cuda(), q_at, k_at, causal=causal, scale=scale)
         j = torch.arange(n_k)
         check(got, q, k, v, lambda i: (j <= n_k - n_q + i) if causal else j >= 0, scale, dtype)
+        assert torch.equal(B.hlq_attn_prompt(shifted(q.cuda()), shifted(k.cuda()), shifted(v.cuda()), q_at, k_at, causal=causal, scale=scale), got)
 
 
 @pytest.mark.parametrize("kind,dtype,a,b", [(t, t, a, b) for t, a, b in CASES] + [("mx8", "bf16", 20, 25), ("mx8", "f16", 15, 15), ("mx4", "bf16", 30, 40), ("mx4", "f16", 13, 14)])
