@@ -386,7 +386,7 @@ HLQ_API hlq_status hlq_expert_combine(int64_t T, int32_t k, int32_t D, int64_t R
  *     (a, b) -> magnitude * (a cos - b sin, b cos + a sin),
  * pair i being values i and i + dims / 2, or (interleaved != 0) 2 i and 2 i + 1.  The other values stay as they are.
  * `turns` (device, dims / 2 numbers, 8-byte aligned) are the pairs' frequencies as hlq_rotary_turns (host-only) makes them of radians a position:
- * the part of a turn that a position adds, times 2^64, so that an angle is exact to 2^-33 turns wherever in int32 the position is.  Turned in
+ * the part of a turn that a position adds, times 2^64, so that an angle is exact to 2^-33 turns wherever in int32 the position is (frequencies above 1: in proportion).  Turned in
  * 64 bits and rounded once (16-bit types: by way of f32).  Any scheme of stretched positions is a choice of frequencies and magnitude.
  * A frequency that is not finite or of 2^32 and more: HLQ_ERR_BAD_DESC. */
 typedef struct {
@@ -437,7 +437,8 @@ HLQ_API hlq_status hlq_kv_read(const hlq_kv_desc *c, const void *cache, size_t c
  * infinite or NaN is its column's result for every head that sees its key, however small p (both infinities: NaN).  q_heads is a multiple of heads.  q has the type of a 16-bit cache, f16 or
  * bf16 with MX8 and MX4; out f16, bf16 or f32.  Products are exact (8- and 4-bit values below
  * 2^-126 may count as 0), sums fp32, scores fp32 numbers of any size; p is held to 2^-16 of itself (f16 caches: 2^-22, and 2^-42 of the largest).
- * Results do not depend on the order in which workgroups end.
+ * Results do not depend on the order in which workgroups end; B and the table's width go into how sums are cut, and so into their last bits.  B times kv heads times (q_heads / heads
+ * in sixteens) is below 2^24, else HLQ_ERR_UNSUPPORTED.
  * ws: of hlq_attn_decode_workspace_bytes() (host-only; enough for smaller B and table_width too), seen by hlq_workspace_init once; calls that may run at
  * the same time need one each.  NULL is enough where the launch is not cut over the tokens, else HLQ_ERR_NULL. */
 HLQ_API hlq_status hlq_attn_decode_workspace_bytes(const hlq_kv_desc *c, int32_t q_heads, int64_t B, int32_t table_width, size_t *bytes);
@@ -452,6 +453,8 @@ HLQ_API hlq_status hlq_attn_decode(const hlq_kv_desc *c, const void *cache, size
  * a query that sees no key (or none whose score is above -infinity) has 0, and values that are infinite or NaN are as for hlq_attn_decode.  out [Tq, q_heads, dim]; rows of no sequence stay as they were.  Offsets count
  * as the nearest number in 0 .. Tq, or Tk; a sequence that ends before it begins is empty.  Products are exact, sums fp32, p is rounded to the inputs' type (f16, bf16), which is out's too,
  * and summed as rounded (f16: also to 2^-31 of the largest).
+ * Tq and Tk and B go into how sums are cut.  Below 2^24 workgroups (of 32, 64 or 128 queries of 4, 2 or 1 heads as q_heads / heads divides by them, and one more of each sequence),
+ * else HLQ_ERR_UNSUPPORTED.
  * ws: as for hlq_attn_decode. */
 HLQ_API hlq_status hlq_attn_prompt_workspace_bytes(int64_t Tq, int64_t Tk, int32_t B, int32_t q_heads, int32_t heads, int32_t dim, size_t *bytes);
 HLQ_API hlq_status hlq_attn_prompt(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, hlq_dtype type, int64_t Tq, const void *q, int64_t q_ts, int64_t q_hs,

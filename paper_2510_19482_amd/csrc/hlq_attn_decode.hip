@@ -14,9 +14,9 @@
 // values become bf16, which holds them and their scale exactly (from 2^-126 up); f16 queries are two bf16 terms then.
 // A wavefront that ends with a NaN, or with scores so large that their rounding is felt, goes through its tiles once more, multiplies without the values that are infinite or NaN, and adds what they do to those that see them by counting.
 // Keys' rows are asked for in lines of 128 bytes, and rows are not kept in the caches: by 64 bytes of each of 16 rows, and kept, 64 x 4096 tokens took 204 us for 184.
-// What bounds it: memory.  64 sequences of 4096 tokens, 8 heads of 128 with 64 queries: 16 bits 184 to 188 us = 5.7 to 5.8 TB/s (a plain read reaches 6.9), 8 bits 112 to 117 = 4.8, 4 bits
+// What bounds it: memory.  64 sequences of 4096 tokens, 8 heads of 128 with 64 queries: 16 bits 182 to 185 us = 5.8 to 5.9 TB/s (a plain read reaches 6.9), 8 bits 111 to 118 = 4.7 to 5.0, 4 bits
 // 65 to 68 = 4.3; the fewer bits a tile has, the less of it is on its way (a wavefront has one tile, 17, 8.5 or 4.4 KB; two tiles a wavefront, or fewer registers and four
-// workgroups a unit, brought nothing), and vector instructions take 42 % of the cycles at 4 bits (18 % at 16).  Pages of 16 tokens 5.1 TB/s.  A single sequence of 1000 tokens takes 8.6 us, one token 5.3: of dependent steps,
+// workgroups a unit, brought nothing), and vector instructions take 44 % of the cycles at 4 bits (19 % at 16).  Pages of 16 tokens 5.1 TB/s.  A single sequence of 1000 tokens takes 8.6 us, one token 5.3: of dependent steps,
 // the length, the table, keys, and the cuts' hand-over.
 // Pages' pieces are read through buffer descriptors that end with the sequence's last token: what lies behind, and columns past dim, is 0 without a
 // comparison.

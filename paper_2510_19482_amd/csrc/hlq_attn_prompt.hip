@@ -13,12 +13,12 @@
 // Weights are rounded once, to the inputs' type, for the second product; their sum is of the rounded ones, so that a result is a true mean of values.
 // What is not seen: its score is -infinity, its weight 0.  A value that is infinite or NaN would still enter as 0 times itself: a workgroup that ends with a NaN (or with scores
 // so large that their rounding is felt) goes through its tiles once more, multiplies without such values, and adds what they do to those that see them by counting.
-// Rows that do not begin at multiples of 16 bytes go to LDS by way of registers (8192 tokens 610 -> 870 us, dim 256,
-// where that spills, three times as long).
+// Rows that do not begin at multiples of 16 bytes go to LDS by way of registers (8192 tokens 534 -> 840 us, of dim 64 310 -> 424; 4096 of dim 256, where that spills, 331 -> 615).
+// The look for a NaN, and the barrier that joins it, take 0.4 us of a workgroup; 8192 tokens of which all see a NaN 1390 us.
 //
 // What bounds it: 8192 bf16 tokens, causal, 32 heads of 128 over 8 take 530 us, 1040 TFLOP/s (a library product reaches 1250 on this card).  Of the cycles the matrix
 // cores are busy 50 to 58 %, vector instructions issue in 45 to 55 % (105 a step and wavefront, 16 of them exponentials of 16 cycles each), at 1.7 GHz, the clock that power holds; LDS without its
-// bank conflicts (28 % of its time) made 1 % of difference, raised priority none.  Dims of 64 and 256: 840 and 820 TFLOP/s.  Short sequences (16 x 512: 75 us, 460 TFLOP/s) are bound by
+// bank conflicts (28 % of its time) made 1 % of difference, raised priority none.  Dims of 64 and 256: 890 and 815 TFLOP/s.  Short sequences (16 x 512: 73 us, 470 TFLOP/s) are bound by
 // what a workgroup does before its first product and after its last: where it is 0.7 us, queries and first keys 1.9, results 1.2, and the steps at the edge.
 #include "hlq_kv.h"
 

@@ -11,7 +11,7 @@
 // token and goes through heads of it, queries, keys, then values; the angles of its lanes stay in registers.
 //
 // What bounds them: memory.  8192 tokens of 40 f16 heads turned 29 us (168 MB, 5.8 TB/s); the same with 8 heads of values into 4 bits 42 us (200 MB, 4.8 TB/s); 65536 tokens
-// read from 4 bits 54 us (340 MB, 6.2 TB/s), from 16 bits 90.  A step of 32 tokens takes 4.5 us, of which a launch and three dependent loads are most; 77 tokens read 2.8.
+// read from 4 bits 54 us (340 MB, 6.2 TB/s), from 16 bits 90.  A step of 32 tokens takes 4.5 to 4.8 us, of which a launch and three dependent loads are most; 77 tokens read 2.8.
 #include "hlq_kv.h"
 
 namespace {
