@@ -436,7 +436,8 @@ HLQ_API hlq_status hlq_kv_read(const hlq_kv_desc *c, const void *cache, size_t c
  * nearest one inside the cache.  Length 0, or no score above -infinity: 0.  A key whose score is -infinity counts as one that is not seen; a value that is
  * infinite or NaN is its column's result for every head that sees its key, however small p (both infinities: NaN).  q_heads is a multiple of heads.  q has the type of a 16-bit cache, f16 or
  * bf16 with MX8 and MX4; out f16, bf16 or f32.  Products are exact (8- and 4-bit values below
- * 2^-126 may count as 0), sums fp32, scores fp32 numbers of any size; p is held to 2^-16 of itself (f16 caches: 2^-22, and 2^-42 of the largest).
+ * 2^-126 may count as 0), sums fp32, scores fp32 numbers up to 2^127; p is held to 2^-16 of itself (f16 caches: 2^-22, and 2^-42 of the largest),
+ * and counts as 0 below 2^-126 of the largest.
  * Results do not depend on the order in which workgroups end; B and the table's width go into how sums are cut, and so into their last bits.  B times kv heads times (q_heads / heads
  * in sixteens) is below 2^24, else HLQ_ERR_UNSUPPORTED.
  * ws: of hlq_attn_decode_workspace_bytes() (host-only; enough for smaller B and table_width too), seen by hlq_workspace_init once; calls that may run at

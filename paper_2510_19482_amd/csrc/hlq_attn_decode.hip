@@ -472,7 +472,7 @@ hlq_attn_decode_kernel(const Decode a)
     bool odd = !(total < __builtin_inff()) || fabsf(base) >= LARGE;
 #pragma unroll
     for (int j = 0; j < E; ++j) odd = odd || __builtin_isunordered(acc[j][0], acc[j][1]) || __builtin_isunordered(acc[j][2], acc[j][3]);
-    if (__builtin_expect(__any(odd), 0)) pass(std::true_type());
+    if (__builtin_expect(__any(odd && col < heads), 0)) pass(std::true_type());   // (lanes past the heads have queries of 0, which an infinite key makes NaN)
     total = over_lanes_sum(total);
 
     // the wavefronts' sums meet in LDS
